@@ -529,6 +529,145 @@ lookme_status_t lookme_inject_text(int32_t dtype, const void* table, int64_t voc
                                    int64_t n, int32_t d_h, void* stream);
 
 /*
+ * lookme_residual_norm -- what follows a layer's additions (Eq. 2): the
+ * residual sum of `parts` weighted rows a token, the root-mean-square norm of
+ * the sum for the next block, and that norm in 8 bits for products on
+ * quantised rows (lookme_grouped_product_quant).  For every row t < n:
+ *   s     = round(hidden[t, :] + sum_j part_w[t, j] add[t, j, :])
+ *   y     = s / sqrt(mean(s^2) + eps) * weight
+ *   hidden_out[t, :] = s,  out[t, :] = round(y)
+ *   scale_out[t] = max(max|y| / 448, 2^-126),  out_quant[t, :] = e4m3(y / scale_out[t])
+ * float32 throughout (part j into partial sum j mod 4, these one after another,
+ * then hidden), one rounding (ties to even) into each output.  A part of
+ * weight 0 is left out whatever its row holds.
+ * A row with a NaN or an infinity gives what IEEE arithmetic gives (NaN in
+ * out and scale_out).
+ *   dtype      lookme_dtype_t of hidden, add, weight, hidden_out and out (no
+ *              handle)
+ *   hidden     [n, d]
+ *   add        [n, parts, d]; NULL exactly when parts = 0
+ *   part_w     [n, parts] float32 or NULL (every weight 1)
+ *   weight     [d] or NULL (1)
+ *   hidden_out [n, d] or NULL; may be hidden itself
+ *   out        [n, d] or NULL
+ *   out_quant  [n, d] e4m3 (OCP: 4 exponent bits, 3 of the significand, no
+ *              infinity, largest value 448), one byte each, with
+ *   scale_out  [n] float32; both or neither
+ * At least one output; the outputs overlap neither each other nor an input
+ * (but hidden_out).  d * elem_size a multiple of 16 bytes, eps >= 0.  n = 0
+ * does nothing.  Needs no workspace.
+ */
+lookme_status_t lookme_residual_norm(int32_t dtype, int64_t n, int32_t d, const void* hidden,
+                                     int32_t parts, const void* add, const float* part_w,
+                                     const void* weight, float eps, void* hidden_out, void* out,
+                                     void* out_quant, float* scale_out, void* stream);
+
+/* Most groups of lookme_group_rows and the grouped products. */
+#define LOOKME_MAX_GROUPS 16384
+
+/*
+ * lookme_group_rows -- the entries of every group, for the grouped products: a
+ * stable counting sort of the ids that a router picked (scene_out of
+ * lookme_route, or the prim_out of a lookup, whose k picks of token t are
+ * entries k t .. k t + k - 1).
+ *   pick        [n] int32; an id outside [0, groups) (-1 for a masked token)
+ *               belongs to no group and is left out
+ *   rows_out    [n] int32: the entries of group 0 in ascending order, then
+ *               those of group 1, ...; what lies behind the last group's
+ *               entries is left as it was
+ *   offsets_out [groups + 1] int32: group g's entries are rows_out[offsets[g]
+ *               .. offsets[g + 1]); offsets[groups] is the number of entries
+ * 1 <= groups <= LOOKME_MAX_GROUPS, n <= 2^30.  n = 0 writes zero offsets.
+ * Needs no handle and no workspace.
+ */
+lookme_status_t lookme_group_rows(int32_t groups, int64_t n, const int32_t* pick,
+                                  int32_t* rows_out, int32_t* offsets_out, void* stream);
+
+/*
+ * lookme_grouped_product -- products of rows that come in groups, each group
+ * with a matrix of its own (a scene's or an expert's).  For group g and
+ * offsets[g] <= i < offsets[g + 1], with src = rows[i] / picks (picks >= 1) or
+ * i (picks = 0), and dst = rows[i] (scatter) or i:
+ *   out[dst, :] = round(w[g] x[src, :]), or with w_up
+ *   out[dst, :] = round(silu(w[g] x[src, :]) * (w_up[g] x[src, :]))
+ * float32 accumulation, one rounding.  With the outputs of lookme_group_rows,
+ * picks = k reads each token's row for its k entries, and scatter gives the
+ * outputs in the entries' order [token, k], as lookme_residual_norm adds them.
+ *   dtype   lookme_dtype_t of x, w, w_up and out (no handle)
+ *   offsets [groups + 1] int32 on the device, ascending, within [0, m]; the
+ *           groups' sizes are not known to the host
+ *   m       rows of out, and entries of rows
+ *   x       [x_rows, d_in]; x_rows >= m where entry i reads row i
+ *   rows    [m] int32; NULL needs picks = 0 and scatter = 0
+ *   w, w_up [groups, d_out, d_in] (output-row-major); w_up may be NULL
+ *   out     [m, d_out]; rows of no group are left as they were, and so are the
+ *           outputs of an entry whose src or dst is out of range (or whose
+ *           rows[i] is negative).  An index that scatter names twice races.
+ * d_in and d_out times elem_size multiples of 16 bytes.  m = 0 does nothing.
+ * Needs no workspace.
+ */
+lookme_status_t lookme_grouped_product(int32_t dtype, int32_t groups, int64_t m, int32_t d_in,
+                                       int32_t d_out, const void* x, int64_t x_rows,
+                                       const int32_t* rows, int32_t picks, const int32_t* offsets,
+                                       const void* w, const void* w_up, void* out,
+                                       int32_t scatter, void* stream);
+
+/*
+ * lookme_grouped_product_quant -- lookme_grouped_product on e4m3 operands with
+ * a float32 scale a row, out in bf16:
+ *   out[dst, c] = round(x_scale[src] w_scale[g, c] sum_k w[g, c, k] x[src, k])
+ * (with w_up: both sums scaled, then silu(.) * .).
+ *   x [x_rows, d_in] e4m3, x_scale [x_rows] (out_quant and scale_out of
+ *   lookme_residual_norm); w, w_up [groups, d_out, d_in] e4m3, w_scale,
+ *   up_scale [groups, d_out]; w_up and up_scale both or neither
+ * The products are exact.  The matrix cores add those of 16 neighbouring k
+ * aligned to the largest one, to 13 bits behind its leading bit; these sums
+ * are added in float32.
+ * d_in a multiple of 16, d_out of 8.  The other arguments as above.
+ */
+lookme_status_t lookme_grouped_product_quant(int32_t groups, int64_t m, int32_t d_in,
+                                             int32_t d_out, const void* x, const float* x_scale,
+                                             int64_t x_rows, const int32_t* rows, int32_t picks,
+                                             const int32_t* offsets, const void* w,
+                                             const float* w_scale, const void* w_up,
+                                             const float* up_scale, void* out, int32_t scatter,
+                                             void* stream);
+
+/*
+ * lookme_quant_product -- a product of few rows (decoded tokens) with weights
+ * of 4 bits, in groups along d_in that share a scale and a zero point:
+ *   out[t, c] = round(add[t, c] + sum_G scale[c, G] sum_{k in G} (q[c, k] - zero[c, G]) x[t, k])
+ * The products are exact, the sums float32, no weight is rounded.  Every 16
+ * rows (32 from 17 on) read the weights again: for many rows unpack them once.
+ * A row of x with an infinity or a NaN gives NaN.
+ *   dtype  lookme_dtype_t of x, scale, add and out (no handle)
+ *   group  32, 64 or a multiple of 128; d_in a multiple of it
+ *   w      [d_out, d_in / 2] bytes: byte j of a row holds q[2 j] in its low
+ *          half and q[2 j + 1] in its high half
+ *   scale  [d_out, d_in / group];  zero [d_out, d_in / group] bytes in
+ *          [0, 15], or NULL (8)
+ *   add    [n, d_out], or NULL (0); out may be add itself
+ * d_in * elem_size (by its group) and d_out * elem_size multiples of 16 bytes,
+ * n at most 2^20 - 16.  n = 0 does nothing.  Needs no workspace.
+ */
+lookme_status_t lookme_quant_product(int32_t dtype, int64_t n, int32_t d_in, int32_t d_out,
+                                     int32_t group, const void* x, const void* w,
+                                     const void* scale, const uint8_t* zero, const void* add,
+                                     void* out, void* stream);
+
+/*
+ * lookme_quant_swiglu -- the gate and up half of the SwiGLU fusion of Eq. 10
+ * (lookme_set_fusion) on such weights: out[t, :] = round(silu(W_gate x[t, :])
+ * * (W_up x[t, :])).  lookme_quant_product with add is the other half:
+ * hidden + W_down u.  Arguments as above, out [n, d_ff].
+ */
+lookme_status_t lookme_quant_swiglu(int32_t dtype, int64_t n, int32_t d_in, int32_t d_ff,
+                                    int32_t group, const void* x, const void* w_gate,
+                                    const void* scale_gate, const uint8_t* zero_gate,
+                                    const void* w_up, const void* scale_up,
+                                    const uint8_t* zero_up, void* out, void* stream);
+
+/*
  * Measurement support (not part of the method).  When enabled, each kernel
  * group that route/lookup/inject launches is bracketed by a pair of HIP timing
  * events recorded on the call's stream; the Level-2 scoring launch of the

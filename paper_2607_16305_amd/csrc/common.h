@@ -15,12 +15,14 @@
 
 namespace lookme {
 
-enum : int { DT_F32 = 0, DT_BF16 = 1 };
+// DT_E4M3: operands of the grouped products only (8 bits, scales beside them)
+enum : int { DT_F32 = 0, DT_BF16 = 1, DT_E4M3 = 2 };
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int WAVE = 64;
 
@@ -54,6 +56,26 @@ __device__ __forceinline__ f32x4_t mfma_chunk<DT_F32>(u32x4_t a, u32x4_t b, f32x
   c = __builtin_amdgcn_mfma_f32_16x16x4f32(af[2], bf[2], c, 0, 0, 0);
   c = __builtin_amdgcn_mfma_f32_16x16x4f32(af[3], bf[3], c, 0, 0, 0);
   return c;
+}
+
+// e4m3: a 64-byte step holds 64 values, eight of a lane's sixteen per product.
+template <>
+__device__ __forceinline__ f32x4_t mfma_chunk<DT_E4M3>(u32x4_t a, u32x4_t b, f32x4_t c) {
+  typedef long i64x2_t __attribute__((ext_vector_type(2)));
+  const i64x2_t af = __builtin_bit_cast(i64x2_t, a);
+  const i64x2_t bf = __builtin_bit_cast(i64x2_t, b);
+  c = __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(af[0], bf[0], c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(af[1], bf[1], c, 0, 0, 0);
+}
+// Two steps of it in one instruction of twice the rate (block scales of 1).
+__device__ __forceinline__ f32x4_t mfma_stage_e4m3(u32x4_t a0, u32x4_t a1, u32x4_t b0, u32x4_t b1,
+                                                   f32x4_t c) {
+  const i32x8_t a = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3],
+                     (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
+  const i32x8_t b = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3],
+                     (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0x7F7F7F7F, 0,
+                                                          0x7F7F7F7F);
 }
 
 // Scalar reinterpretation.  Always pass a scalar value (never a vector

@@ -289,4 +289,50 @@ hipError_t launch_text_inject(int dt, int64_t n_text, const int32_t* kept, const
                               int64_t vocab, int d_t, void* hidden, int64_t n, int d_h,
                               hipStream_t st);
 
+// ---- residual sum and root-mean-square norm (norm.hip) --------------------
+hipError_t launch_residual_norm(int dt, int64_t n, int d, const void* hidden, int parts,
+                                const void* add, const float* part_w, const void* weight,
+                                float eps, void* hidden_out, void* out, void* out_quant,
+                                float* scale_out, hipStream_t st);
+
+// ---- entries grouped by id (group_rows.hip) --------------------------------
+hipError_t launch_group_rows(int groups, int64_t n, const int32_t* pick, int32_t* rows,
+                             int32_t* offsets, hipStream_t st);
+
+// ---- products of grouped rows (grouped.hip) --------------------------------
+struct GroupedParams {
+  const char* x;             // [x_rows, K]
+  const char* w;             // [groups, cols, K]
+  const char* w_up;          // the same, or null
+  const float* x_scale;      // [x_rows]            (DT_E4M3)
+  const float* w_scale;      // [groups, cols]      (DT_E4M3)
+  const float* up_scale;     // [groups, cols]      (DT_E4M3 with w_up)
+  const int32_t* rows;       // [m] or null
+  const int32_t* offsets;    // [groups + 1]
+  char* out;                 // [m, cols]
+  int64_t x_rows, m, k_bytes;
+  int groups, cols;
+  int picks;                 // entry i reads row rows[i] / picks; 0: row i
+  bool scatter;              // its output goes to row rows[i]; else to row i
+};
+constexpr int GROUPED_E4M3 = 2;   // dt of e4m3 operands (out in bf16)
+hipError_t launch_grouped(int dt, const GroupedParams& p, hipStream_t st);
+
+// ---- products with 4-bit weights (quant.hip) -------------------------------
+struct QuantMatrix {
+  const char* w;             // [cols, K / 2]
+  const char* scale;         // [cols, K / group] of the dtype
+  const uint8_t* zero;       // [cols, K / group] or null (8)
+};
+struct QuantParams {
+  const char* x;             // [n, K]
+  QuantMatrix m[2];          // the matrix; gate and up
+  const char* add;           // [n, cols] or null
+  char* out;                 // [n, cols]
+  int64_t n;
+  int k, cols, group;
+  bool up;
+};
+hipError_t launch_quant(int dt, const QuantParams& p, hipStream_t st);
+
 }  // namespace lookme

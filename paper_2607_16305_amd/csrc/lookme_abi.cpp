@@ -277,6 +277,97 @@ class Stamped {
     if (st_ != LOOKME_OK) return st_;       \
   } while (0)
 
+// ---- the entry points without a handle ------------------------------------
+lookme_status_t check_optional(const void* p, const char* name) {
+  return p == nullptr ? LOOKME_OK : check_ptr(p, name);
+}
+
+lookme_status_t check_dtype(int32_t dtype) {
+  if (dtype != LOOKME_F32 && dtype != LOOKME_BF16)
+    return fail(LOOKME_ERR_INVALID, "unknown dtype %d", dtype);
+  return LOOKME_OK;
+}
+
+lookme_status_t check_rows(int64_t n) {
+  if (n < 0) return fail(LOOKME_ERR_INVALID, "n must be >= 0 (got %lld)", (long long)n);
+  if (n > (int64_t)1 << 30)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%lld rows exceed 2^30", (long long)n);
+  return LOOKME_OK;
+}
+
+// a row of `width` elements: whole 16-byte chunks
+lookme_status_t check_width(int32_t width, int es, const char* name) {
+  if (width < 1) return fail(LOOKME_ERR_INVALID, "%s must be positive", name);
+  if (((int64_t)width * es) % 16 != 0)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%s times the element size must be a multiple of 16",
+                name);
+  if ((int64_t)width * es > (int64_t)1 << 24)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%s: a row exceeds 16 MiB", name);
+  return LOOKME_OK;
+}
+
+lookme_status_t check_groups(int32_t groups) {
+  if (groups < 1) return fail(LOOKME_ERR_INVALID, "groups must be >= 1 (got %d)", groups);
+  if (groups > LOOKME_MAX_GROUPS)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%d groups, at most %d", groups, LOOKME_MAX_GROUPS);
+  return LOOKME_OK;
+}
+
+lookme_status_t grouped_params(int32_t groups, int64_t m, int32_t d_in, int32_t d_out, int es,
+                               int out_es, const void* x, int64_t x_rows, const int32_t* rows,
+                               int32_t picks, const int32_t* offsets, const void* w,
+                               const void* w_up, void* out, int32_t scatter,
+                               lookme::GroupedParams* p) {
+  LOOKME_TRY(check_groups(groups));
+  LOOKME_TRY(check_rows(m));
+  LOOKME_TRY(check_width(d_in, es, "d_in"));
+  LOOKME_TRY(check_width(d_out, out_es, "d_out"));
+  if (picks < 0) return fail(LOOKME_ERR_INVALID, "picks must be >= 0 (got %d)", picks);
+  if (x_rows < 0 || x_rows > (int64_t)INT32_MAX)
+    return fail(LOOKME_ERR_INVALID, "x_rows %lld outside [0, 2^31)", (long long)x_rows);
+  if (m == 0) return LOOKME_OK;
+  if (rows == nullptr && (picks != 0 || scatter != 0))
+    return fail(LOOKME_ERR_INVALID, "picks or scatter given without rows");
+  if (x_rows < (picks == 0 ? m : 1))
+    return fail(LOOKME_ERR_INVALID, "x has %lld rows for %lld entries", (long long)x_rows,
+                (long long)m);
+  LOOKME_TRY(check_ptr(x, "x"));
+  LOOKME_TRY(check_optional(rows, "rows"));
+  LOOKME_TRY(check_ptr(offsets, "offsets"));
+  LOOKME_TRY(check_ptr(w, "w"));
+  LOOKME_TRY(check_optional(w_up, "w_up"));
+  LOOKME_TRY(check_ptr(out, "out"));
+  p->x = static_cast<const char*>(x);
+  p->w = static_cast<const char*>(w);
+  p->w_up = static_cast<const char*>(w_up);
+  p->rows = rows;
+  p->offsets = offsets;
+  p->out = static_cast<char*>(out);
+  p->x_rows = x_rows;
+  p->m = m;
+  p->k_bytes = (int64_t)d_in * es;
+  p->groups = groups;
+  p->cols = d_out;
+  p->picks = picks;
+  p->scatter = scatter != 0;
+  return LOOKME_OK;
+}
+
+lookme_status_t check_quant(int32_t dtype, int64_t n, int32_t d_in, int32_t d_out, int32_t group) {
+  LOOKME_TRY(check_dtype(dtype));
+  if (n < 0) return fail(LOOKME_ERR_INVALID, "n must be >= 0 (got %lld)", (long long)n);
+  if (n > (1 << 20) - 16)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%lld rows: a product of few rows", (long long)n);
+  if (group < 1 || d_in < 1)
+    return fail(LOOKME_ERR_INVALID, "group and d_in must be positive");
+  if (group != 32 && group != 64 && group % 128 != 0)
+    return fail(LOOKME_ERR_UNSUPPORTED, "group %d is neither 32, 64 nor a multiple of 128", group);
+  if (d_in % group != 0)
+    return fail(LOOKME_ERR_INVALID, "d_in %d is no multiple of the group, %d", d_in, group);
+  LOOKME_TRY(check_width(d_in, elem_size(dtype), "d_in"));
+  return check_width(d_out, elem_size(dtype), "d_out");
+}
+
 // criticality norms and, when n_keep > 0, the top-n_keep select (Eq. 9)
 lookme_status_t run_select(lookme_t h, const Layout& L, int32_t layers, int64_t n,
                            int64_t n_keep, const void* crit, int32_t d_c, int32_t* kept,
@@ -1150,6 +1241,143 @@ lookme_status_t lookme_inject_multiscale_gated(lookme_t h, int64_t n, const int3
                                               d.value_dim, d.top_k, h->ms_w, d_h, hidden,
                                               ws + L.ms_r, ws + L.ms_q, st, count),
                     "multi-scale injection launch");
+}
+
+lookme_status_t lookme_residual_norm(int32_t dtype, int64_t n, int32_t d, const void* hidden,
+                                     int32_t parts, const void* add, const float* part_w,
+                                     const void* weight, float eps, void* hidden_out, void* out,
+                                     void* out_quant, float* scale_out, void* stream) {
+  LOOKME_TRY(check_dtype(dtype));
+  LOOKME_TRY(check_rows(n));
+  if (d < 1) return fail(LOOKME_ERR_INVALID, "d must be positive");
+  LOOKME_TRY(check_width(d, elem_size(dtype), "d"));
+  if (parts < 0) return fail(LOOKME_ERR_INVALID, "parts must be >= 0 (got %d)", parts);
+  if (parts == 0 && (add != nullptr || part_w != nullptr))
+    return fail(LOOKME_ERR_INVALID, "add or part_w given for parts = 0");
+  if (!(eps >= 0.f)) return fail(LOOKME_ERR_INVALID, "eps must be >= 0");
+  if (n == 0) return LOOKME_OK;
+  if (hidden_out == nullptr && out == nullptr && out_quant == nullptr)
+    return fail(LOOKME_ERR_INVALID, "no output given");
+  if ((out_quant == nullptr) != (scale_out == nullptr))
+    return fail(LOOKME_ERR_INVALID, "out_quant and scale_out go together");
+  LOOKME_TRY(check_ptr(hidden, "hidden"));
+  if (parts > 0) LOOKME_TRY(check_ptr(add, "add"));
+  LOOKME_TRY(check_optional(part_w, "part_w"));
+  LOOKME_TRY(check_optional(weight, "weight"));
+  LOOKME_TRY(check_optional(hidden_out, "hidden_out"));
+  LOOKME_TRY(check_optional(out, "out"));
+  LOOKME_TRY(check_optional(out_quant, "out_quant"));
+  LOOKME_TRY(check_optional(scale_out, "scale_out"));
+  return hip_status(lookme::launch_residual_norm(dtype, n, d, hidden, parts, add, part_w, weight,
+                                                 eps, hidden_out, out, out_quant, scale_out,
+                                                 static_cast<hipStream_t>(stream)),
+                    "residual norm launch");
+}
+
+lookme_status_t lookme_group_rows(int32_t groups, int64_t n, const int32_t* pick,
+                                  int32_t* rows_out, int32_t* offsets_out, void* stream) {
+  LOOKME_TRY(check_groups(groups));
+  LOOKME_TRY(check_rows(n));
+  if (n > 0) {
+    LOOKME_TRY(check_ptr(pick, "pick"));
+    LOOKME_TRY(check_ptr(rows_out, "rows_out"));
+  }
+  LOOKME_TRY(check_ptr(offsets_out, "offsets_out"));
+  return hip_status(lookme::launch_group_rows(groups, n, pick, rows_out, offsets_out,
+                                              static_cast<hipStream_t>(stream)),
+                    "group rows launch");
+}
+
+lookme_status_t lookme_grouped_product(int32_t dtype, int32_t groups, int64_t m, int32_t d_in,
+                                       int32_t d_out, const void* x, int64_t x_rows,
+                                       const int32_t* rows, int32_t picks, const int32_t* offsets,
+                                       const void* w, const void* w_up, void* out,
+                                       int32_t scatter, void* stream) {
+  LOOKME_TRY(check_dtype(dtype));
+  lookme::GroupedParams p{};
+  LOOKME_TRY(grouped_params(groups, m, d_in, d_out, elem_size(dtype), elem_size(dtype), x, x_rows,
+                            rows, picks, offsets, w, w_up, out, scatter, &p));
+  if (m == 0) return LOOKME_OK;
+  return hip_status(lookme::launch_grouped(dtype, p, static_cast<hipStream_t>(stream)),
+                    "grouped product launch");
+}
+
+lookme_status_t lookme_grouped_product_quant(int32_t groups, int64_t m, int32_t d_in,
+                                             int32_t d_out, const void* x, const float* x_scale,
+                                             int64_t x_rows, const int32_t* rows, int32_t picks,
+                                             const int32_t* offsets, const void* w,
+                                             const float* w_scale, const void* w_up,
+                                             const float* up_scale, void* out, int32_t scatter,
+                                             void* stream) {
+  lookme::GroupedParams p{};
+  LOOKME_TRY(grouped_params(groups, m, d_in, d_out, 1, 2, x, x_rows, rows, picks, offsets, w,
+                            w_up, out, scatter, &p));
+  if ((w_up == nullptr) != (up_scale == nullptr))
+    return fail(LOOKME_ERR_INVALID, "w_up and up_scale go together");
+  if (m == 0) return LOOKME_OK;
+  LOOKME_TRY(check_ptr(x_scale, "x_scale"));
+  LOOKME_TRY(check_ptr(w_scale, "w_scale"));
+  LOOKME_TRY(check_optional(up_scale, "up_scale"));
+  p.x_scale = x_scale;
+  p.w_scale = w_scale;
+  p.up_scale = up_scale;
+  return hip_status(lookme::launch_grouped(lookme::GROUPED_E4M3, p,
+                                           static_cast<hipStream_t>(stream)),
+                    "grouped product launch");
+}
+
+lookme_status_t lookme_quant_product(int32_t dtype, int64_t n, int32_t d_in, int32_t d_out,
+                                     int32_t group, const void* x, const void* w,
+                                     const void* scale, const uint8_t* zero, const void* add,
+                                     void* out, void* stream) {
+  LOOKME_TRY(check_quant(dtype, n, d_in, d_out, group));
+  if (n == 0) return LOOKME_OK;
+  LOOKME_TRY(check_ptr(x, "x"));
+  LOOKME_TRY(check_ptr(w, "w"));
+  LOOKME_TRY(check_ptr(scale, "scale"));
+  LOOKME_TRY(check_optional(zero, "zero"));
+  LOOKME_TRY(check_optional(add, "add"));
+  LOOKME_TRY(check_ptr(out, "out"));
+  lookme::QuantParams p{};
+  p.x = static_cast<const char*>(x);
+  p.m[0] = {static_cast<const char*>(w), static_cast<const char*>(scale), zero};
+  p.add = static_cast<const char*>(add);
+  p.out = static_cast<char*>(out);
+  p.n = n;
+  p.k = d_in;
+  p.cols = d_out;
+  p.group = group;
+  return hip_status(lookme::launch_quant(dtype, p, static_cast<hipStream_t>(stream)),
+                    "quant product launch");
+}
+
+lookme_status_t lookme_quant_swiglu(int32_t dtype, int64_t n, int32_t d_in, int32_t d_ff,
+                                    int32_t group, const void* x, const void* w_gate,
+                                    const void* scale_gate, const uint8_t* zero_gate,
+                                    const void* w_up, const void* scale_up,
+                                    const uint8_t* zero_up, void* out, void* stream) {
+  LOOKME_TRY(check_quant(dtype, n, d_in, d_ff, group));
+  if (n == 0) return LOOKME_OK;
+  LOOKME_TRY(check_ptr(x, "x"));
+  LOOKME_TRY(check_ptr(w_gate, "w_gate"));
+  LOOKME_TRY(check_ptr(scale_gate, "scale_gate"));
+  LOOKME_TRY(check_optional(zero_gate, "zero_gate"));
+  LOOKME_TRY(check_ptr(w_up, "w_up"));
+  LOOKME_TRY(check_ptr(scale_up, "scale_up"));
+  LOOKME_TRY(check_optional(zero_up, "zero_up"));
+  LOOKME_TRY(check_ptr(out, "out"));
+  lookme::QuantParams p{};
+  p.x = static_cast<const char*>(x);
+  p.m[0] = {static_cast<const char*>(w_gate), static_cast<const char*>(scale_gate), zero_gate};
+  p.m[1] = {static_cast<const char*>(w_up), static_cast<const char*>(scale_up), zero_up};
+  p.out = static_cast<char*>(out);
+  p.n = n;
+  p.k = d_in;
+  p.cols = d_ff;
+  p.group = group;
+  p.up = true;
+  return hip_status(lookme::launch_quant(dtype, p, static_cast<hipStream_t>(stream)),
+                    "quant swiglu launch");
 }
 
 }  // extern "C"

@@ -107,12 +107,20 @@ struct PgLoop {
                                              const u32x4_t (&fb)[2][NJ],
                                              f32x4_t (&acc)[MI][NJ]) {
     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    if constexpr (DT == DT_E4M3) {   // a stage's 128 values are one step
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] = mfma_chunk<DT>(fb[ks][j], fa[ks][i], acc[i][j]);
+        for (int j = 0; j < NJ; ++j)
+          acc[i][j] = mfma_stage_e4m3(fb[0][j], fb[1][j], fa[0][i], fa[1][i], acc[i][j]);
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] = mfma_chunk<DT>(fb[ks][j], fa[ks][i], acc[i][j]);
+    }
   }
   // ends a phase: this wave's LDS reads have returned and all but the V
   // youngest of its loads have landed; then the barrier (a plain s_barrier:

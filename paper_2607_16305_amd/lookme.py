@@ -23,6 +23,7 @@ LOOKME_F32, LOOKME_BF16 = 0, 1
 LOOKME_SCORE_DOT, LOOKME_SCORE_COS = 0, 1
 LOOKME_KMAX = 32
 LOOKME_NOALLOC_MAX_ROWS = 131072
+LOOKME_MAX_GROUPS = 16384
 
 STATUS_NAMES = {0: "OK", 1: "INVALID", 2: "UNSUPPORTED", 3: "WORKSPACE", 4: "HIP"}
 
@@ -36,7 +37,9 @@ EXPORTED = ("lookme_create", "lookme_workspace_size", "lookme_set_workspace", "l
             "lookme_inject_text", "lookme_lookup_select", "lookme_lookup_gate",
             "lookme_scene_keys", "lookme_index_errors",
             "lookme_destroy", "lookme_last_error",
-            "lookme_profile_enable", "lookme_profile_read", "lookme_inject_noalloc")
+            "lookme_profile_enable", "lookme_profile_read", "lookme_inject_noalloc",
+            "lookme_residual_norm", "lookme_group_rows", "lookme_grouped_product",
+            "lookme_grouped_product_quant", "lookme_quant_product", "lookme_quant_swiglu")
 
 GROUPS = ("project", "route", "bucket", "score", "norm", "select", "inject")
 
@@ -115,6 +118,21 @@ def load():
                                  ctypes.c_int64, _vp, ctypes.c_int32, _vp, _vp],
         "lookme_lookup_gate": [_vp, ctypes.c_int32, ctypes.c_int64, _vp, _vp, _vp, _vp, _vp,
                                ctypes.c_int32, _vp, _vp, _vp, _vp],
+        "lookme_residual_norm": [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, _vp,
+                                 ctypes.c_int32, _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp,
+                                 _vp, _vp],
+        "lookme_group_rows": [ctypes.c_int32, ctypes.c_int64, _vp, _vp, _vp, _vp],
+        "lookme_grouped_product": [ctypes.c_int32, ctypes.c_int32, ctypes.c_int64,
+                                   ctypes.c_int32, ctypes.c_int32, _vp, ctypes.c_int64, _vp,
+                                   ctypes.c_int32, _vp, _vp, _vp, _vp, ctypes.c_int32, _vp],
+        "lookme_grouped_product_quant": [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                         ctypes.c_int32, _vp, _vp, ctypes.c_int64, _vp,
+                                         ctypes.c_int32, _vp, _vp, _vp, _vp, _vp, _vp,
+                                         ctypes.c_int32, _vp],
+        "lookme_quant_product": [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                 ctypes.c_int32, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
+        "lookme_quant_swiglu": [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                ctypes.c_int32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
         "lookme_destroy": [_vp],
         "lookme_profile_enable": [_vp, ctypes.c_int32],
         "lookme_profile_read": [_vp, ctypes.c_int32, ctypes.POINTER(ctypes.c_int64),
@@ -326,6 +344,208 @@ def inject_text(table, pos, ids, hidden, kept=None, count=None, stream=None):
     lookme_inject_text(DTYPE_CODE[table.dtype], table, table.shape[0], table.shape[1],
                        pos.numel(), pos, ids, kept, count, hidden, hidden.shape[0],
                        hidden.shape[1], stream)
+
+
+def lookme_residual_norm(dtype, n, d, hidden, parts, add, part_w, weight, eps, hidden_out, out,
+                         out_quant, scale_out, stream=None):
+    _check(load().lookme_residual_norm(dtype, n, d, _ptr(hidden), parts, _ptr(add), _ptr(part_w),
+                                       _ptr(weight), eps, _ptr(hidden_out), _ptr(out),
+                                       _ptr(out_quant), _ptr(scale_out), _stream(stream)))
+
+
+def lookme_group_rows(groups, n, pick, rows_out, offsets_out, stream=None):
+    _check(load().lookme_group_rows(groups, n, _ptr(pick), _ptr(rows_out), _ptr(offsets_out),
+                                    _stream(stream)))
+
+
+def lookme_grouped_product(dtype, groups, m, d_in, d_out, x, x_rows, rows, picks, offsets, w,
+                           w_up, out, scatter, stream=None):
+    _check(load().lookme_grouped_product(dtype, groups, m, d_in, d_out, _ptr(x), x_rows,
+                                         _ptr(rows), picks, _ptr(offsets), _ptr(w), _ptr(w_up),
+                                         _ptr(out), scatter, _stream(stream)))
+
+
+def lookme_grouped_product_quant(groups, m, d_in, d_out, x, x_scale, x_rows, rows, picks,
+                                 offsets, w, w_scale, w_up, up_scale, out, scatter, stream=None):
+    _check(load().lookme_grouped_product_quant(groups, m, d_in, d_out, _ptr(x), _ptr(x_scale),
+                                               x_rows, _ptr(rows), picks, _ptr(offsets), _ptr(w),
+                                               _ptr(w_scale), _ptr(w_up), _ptr(up_scale),
+                                               _ptr(out), scatter, _stream(stream)))
+
+
+def lookme_quant_product(dtype, n, d_in, d_out, group, x, w, scale, zero, add, out, stream=None):
+    _check(load().lookme_quant_product(dtype, n, d_in, d_out, group, _ptr(x), _ptr(w),
+                                       _ptr(scale), _ptr(zero), _ptr(add), _ptr(out),
+                                       _stream(stream)))
+
+
+def lookme_quant_swiglu(dtype, n, d_in, d_ff, group, x, w_gate, scale_gate, zero_gate, w_up,
+                        scale_up, zero_up, out, stream=None):
+    _check(load().lookme_quant_swiglu(dtype, n, d_in, d_ff, group, _ptr(x), _ptr(w_gate),
+                                      _ptr(scale_gate), _ptr(zero_gate), _ptr(w_up),
+                                      _ptr(scale_up), _ptr(zero_up), _ptr(out),
+                                      _stream(stream)))
+
+
+# The same on torch tensors: sizes come from the shapes, which are checked (the
+# C side sees pointers only), and the call runs on the tensors' device.
+
+def _refuse(msg):
+    raise LookmeError(LOOKME_ERR_INVALID, msg)
+
+
+def _tensor(name, t, dtype, shape, device):
+    if t.dtype is not dtype:
+        _refuse(f"{name} is {t.dtype}, not {dtype}")
+    if t.shape != shape:
+        _refuse(f"{name} has the shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.device != device:
+        _refuse(f"{name} is on {t.device}, not on {device}")
+    if not t.is_contiguous():
+        _refuse(f"{name} is not contiguous")
+
+
+def _dtype_code(name, t):
+    code = DTYPE_CODE.get(t.dtype)
+    if code is None:
+        _refuse(f"{name} is {t.dtype}: float32 or bfloat16")
+    return code
+
+
+def _on(device, call, *args):
+    """call(*args) with the tensors' device current; their device is a GPU."""
+    if device.type != "cuda":
+        _refuse(f"tensors on {device}: device memory is needed")
+    if device.index == torch.cuda.current_device():
+        return call(*args)
+    with torch.cuda.device(device):
+        return call(*args)
+
+
+def residual_norm(hidden, weight=None, eps=1e-6, add=None, part_w=None, hidden_out=None,
+                  out=None, out_quant=None, scale_out=None, stream=None):
+    """lookme_residual_norm on torch tensors: hidden [n, d]; add [n, d] or
+    [n, parts, d]; part_w [n, parts] float32; weight [d]; the outputs
+    hidden_out (may be hidden), out [n, d], out_quant [n, d] float8_e4m3fn
+    with scale_out [n] float32."""
+    code, dev, dt = _dtype_code("hidden", hidden), hidden.device, hidden.dtype
+    if hidden.dim() != 2:
+        _refuse(f"hidden has {hidden.dim()} dimensions, not 2")
+    _tensor("hidden", hidden, dt, hidden.shape, dev)
+    n, d = hidden.shape
+    parts = 0
+    if add is not None:
+        parts = 1 if add.dim() == 2 else add.shape[1] if add.dim() == 3 else 0
+        _tensor("add", add, dt, (n, d) if add.dim() == 2 else (n, parts, d), dev)
+        if parts == 0:
+            add = None
+    if part_w is not None:
+        _tensor("part_w", part_w, torch.float32, (n, parts), dev)
+        if parts == 0:
+            part_w = None
+    for name, t, want, shape in (("weight", weight, dt, (d,)),
+                                 ("hidden_out", hidden_out, dt, (n, d)),
+                                 ("out", out, dt, (n, d)),
+                                 ("out_quant", out_quant, torch.float8_e4m3fn, (n, d)),
+                                 ("scale_out", scale_out, torch.float32, (n,))):
+        if t is not None:
+            _tensor(name, t, want, shape, dev)
+    _on(dev, lookme_residual_norm, code, n, d, hidden, parts, add, part_w, weight, eps,
+        hidden_out, out, out_quant, scale_out, stream)
+
+
+def group_rows(pick, groups, rows_out, offsets_out, stream=None):
+    """lookme_group_rows on torch tensors: pick (any shape, n entries) and
+    rows_out (as many) int32, offsets_out [groups + 1] int32."""
+    dev, n = pick.device, pick.numel()
+    _tensor("pick", pick, torch.int32, pick.shape, dev)
+    if rows_out.numel() != n:
+        _refuse(f"rows_out has {rows_out.numel()} entries, not {n}")
+    _tensor("rows_out", rows_out, torch.int32, rows_out.shape, dev)
+    _tensor("offsets_out", offsets_out, torch.int32, (groups + 1,), dev)
+    _on(dev, lookme_group_rows, groups, n, pick, rows_out, offsets_out, stream)
+
+
+def grouped_product(x, w, offsets, out, rows=None, picks=1, w_up=None, scatter=False,
+                    x_scale=None, w_scale=None, w_up_scale=None, stream=None):
+    """lookme_grouped_product on torch tensors, or lookme_grouped_product_quant
+    for float8_e4m3fn: x [x_rows, d_in], w and w_up [groups, d_out, d_in],
+    offsets [groups + 1] int32, out [m, d_out], rows [m] int32.  With rows,
+    entry i reads x[rows[i] // picks] (picks = 0: x[i]); without, x[i]."""
+    dev, quant = x.device, x.dtype is torch.float8_e4m3fn
+    code = 0 if quant else _dtype_code("x", x)
+    if x.dim() != 2 or w.dim() != 3 or out.dim() != 2:
+        _refuse("x and out have 2 dimensions, w has 3")
+    x_rows, d_in = x.shape
+    groups, d_out = w.shape[0], w.shape[1]
+    m = out.shape[0]
+    _tensor("x", x, x.dtype, x.shape, dev)
+    _tensor("w", w, x.dtype, (groups, d_out, d_in), dev)
+    if w_up is not None:
+        _tensor("w_up", w_up, x.dtype, w.shape, dev)
+    _tensor("offsets", offsets, torch.int32, (groups + 1,), dev)
+    _tensor("out", out, torch.bfloat16 if quant else x.dtype, (m, d_out), dev)
+    if rows is None:
+        picks = 0
+    else:
+        _tensor("rows", rows, torch.int32, (m,), dev)
+    if not quant:
+        if x_scale is not None or w_scale is not None or w_up_scale is not None:
+            _refuse(f"scales given for {x.dtype}")
+        return _on(dev, lookme_grouped_product, code, groups, m, d_in, d_out, x, x_rows, rows,
+                   picks, offsets, w, w_up, out, int(scatter), stream)
+    if x_scale is None or w_scale is None:
+        _refuse("float8_e4m3fn needs x_scale and w_scale")
+    _tensor("x_scale", x_scale, torch.float32, (x_rows,), dev)
+    _tensor("w_scale", w_scale, torch.float32, (groups, d_out), dev)
+    if w_up_scale is not None:
+        _tensor("w_up_scale", w_up_scale, torch.float32, (groups, d_out), dev)
+    _on(dev, lookme_grouped_product_quant, groups, m, d_in, d_out, x, x_scale, x_rows, rows,
+        picks, offsets, w, w_scale, w_up, w_up_scale, out, int(scatter), stream)
+
+
+def _quant_matrix(name, x, w, scale, zero):
+    d_in, (d_out, groups) = x.shape[1], scale.shape
+    if groups < 1 or d_in % groups != 0:
+        _refuse(f"scale has {groups} groups for {d_in} columns")
+    _tensor(name, w, torch.uint8, (d_out, d_in // 2), x.device)
+    _tensor(name + " scale", scale, x.dtype, (d_out, groups), x.device)
+    if zero is not None:
+        _tensor(name + " zero", zero, torch.uint8, (d_out, groups), x.device)
+    return d_out, d_in // groups
+
+
+def quant_product(x, w, scale, out, zero=None, add=None, stream=None):
+    """lookme_quant_product on torch tensors: x [n, d_in], w [d_out, d_in / 2]
+    uint8, scale [d_out, groups], zero [d_out, groups] uint8, add and out
+    [n, d_out] (out may be add)."""
+    code = _dtype_code("x", x)
+    if x.dim() != 2 or scale.dim() != 2:
+        _refuse("x and scale have 2 dimensions")
+    n, d_in = x.shape
+    _tensor("x", x, x.dtype, x.shape, x.device)
+    d_out, group = _quant_matrix("w", x, w, scale, zero)
+    _tensor("out", out, x.dtype, (n, d_out), x.device)
+    if add is not None:
+        _tensor("add", add, x.dtype, (n, d_out), x.device)
+    _on(x.device, lookme_quant_product, code, n, d_in, d_out, group, x, w, scale, zero, add, out,
+        stream)
+
+
+def quant_swiglu(x, w_gate, s_gate, w_up, s_up, out, z_gate=None, z_up=None, stream=None):
+    """lookme_quant_swiglu on torch tensors, each matrix as for quant_product;
+    out [n, d_ff]."""
+    code = _dtype_code("x", x)
+    if x.dim() != 2 or s_gate.dim() != 2 or s_up.dim() != 2:
+        _refuse("x and the scales have 2 dimensions")
+    n, d_in = x.shape
+    _tensor("x", x, x.dtype, x.shape, x.device)
+    d_ff, group = _quant_matrix("w_gate", x, w_gate, s_gate, z_gate)
+    if _quant_matrix("w_up", x, w_up, s_up, z_up) != (d_ff, group):
+        _refuse("w_gate and w_up differ in size or group")
+    _tensor("out", out, x.dtype, (n, d_ff), x.device)
+    _on(x.device, lookme_quant_swiglu, code, n, d_in, d_ff, group, x, w_gate, s_gate, z_gate,
+        w_up, s_up, z_up, out, stream)
 
 
 def lookme_destroy(h):

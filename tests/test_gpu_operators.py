@@ -1,0 +1,363 @@
+"""GPU parity of the operators around a LookME layer (residual sum and norm,
+grouping, grouped products, 4-bit products) with their plain float64 forms,
+through the bindings on torch tensors."""
+
+import pytest
+import torch
+
+from tests import operators as R
+
+pytestmark = pytest.mark.gpu
+
+BF, F32, E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+DT = {"bf16": BF, "f32": F32}
+
+
+@pytest.fixture(scope="module")
+def lk():
+    from paper_2607_16305_amd import lookme
+    assert torch.cuda.is_available(), "no GPU visible"
+    lookme.load()
+    return lookme
+
+
+def _say(*a):
+    print("[gpu-operators]", *a, flush=True)
+
+
+def _rand(seed, *shape, std=1.0, dtype=F32):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std).to(dtype)
+
+
+def _close(got, want, bound, what):
+    err = (got.double().cpu() - want).abs() - bound
+    bad = ~(err <= 0)
+    assert not bad.any(), (f"{what}: {int(bad.sum())} of {bad.numel()} values, the worst "
+                           f"{float(err[bad].max()) if bad.any() else 0}")
+
+
+# ---------------------------------------------------------------------------
+# residual sum and norm
+# ---------------------------------------------------------------------------
+
+def _norm_case(lk, dtype, n, d, parts, weighted, weight=True, hidden_out="own", out=True,
+               quant=True, eps=1e-6, edit=None):
+    _say("norm", dtype, n, d, parts, weighted, hidden_out, out, quant)
+    dt = DT[dtype]
+    h = _rand(1, n, d, std=2.0, dtype=dt)
+    add = _rand(2, n, parts, d, dtype=dt) if parts else None
+    pw = torch.softmax(_rand(3, n, parts), 1) if weighted else None
+    g = _rand(4, d, dtype=dt) if weight else None
+    if edit is not None:
+        edit(h, add, pw)
+    cu = lambda t: None if t is None else t.cuda()  # noqa: E731
+    hd = h.cuda()
+    ho = hd if hidden_out == "hidden" else torch.empty_like(hd) if hidden_out else None
+    o = torch.full_like(hd, 7.0) if out else None
+    q = torch.zeros((n, d), dtype=E4M3, device="cuda") if quant else None
+    sc = torch.zeros((n,), device="cuda") if quant else None
+    a = cu(add)
+    lk.residual_norm(hd, weight=cu(g), eps=eps, add=a if parts != 1 else a[:, 0].contiguous(),
+                     part_w=cu(pw), hidden_out=ho, out=o, out_quant=q, scale_out=sc)
+    torch.cuda.synchronize()
+    return h, add, pw, g, ho, o, q, sc
+
+
+def _check_norm(h, add, pw, g, ho, o, q, sc, eps=1e-6):
+    s, bound = R.residual_sum(h, add, pw)
+    if ho is not None:
+        _close(ho, s, bound, "hidden_out")
+        stored = ho.cpu()
+    else:
+        stored = s.to(h.dtype)
+        if h.dtype is BF and add is not None:
+            return   # a sum next to a rounding border may be stored either way
+    y, e = R.norm(stored, g, eps)
+    if ho is None and add is not None:
+        e = e + bound.amax(1, keepdim=True) * 4
+    if o is not None:
+        _close(o, y, e + R.HALF[h.dtype] * y.abs() * (1 + 2 ** -7), "out")
+    if q is not None:
+        rel = ((e / y.abs().clamp_min(1e-300)).max() + 4 * R.U32).item()
+        scale = (y.abs().amax(1) / 448).clamp_min(R.TINY)
+        _close(sc, scale, rel * scale, "scale")
+        v = y / sc.double().cpu()[:, None]
+        _close(q.float(), v, (2.0 ** -4 + 2 * rel) * v.abs() + 2.0 ** -10, "quant")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,d,parts,weighted", [
+    (1, 8, 0, False), (1, 2048, 1, False), (3, 520, 2, True), (5, 1160, 8, True),
+    (17, 4096, 1, True), (2, 8200, 3, False), (257, 256, 1, False), (2, 40000, 2, True),
+    (70, 64, 5, True)])
+def test_norm_parity(lk, dtype, n, d, parts, weighted):
+    _check_norm(*_norm_case(lk, dtype, n, d, parts, weighted))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [512, 40000])
+@pytest.mark.parametrize("kw", [
+    dict(hidden_out=None, out=True, quant=False), dict(hidden_out=None, out=False, quant=True),
+    dict(hidden_out="own", out=False, quant=False), dict(hidden_out="hidden", out=True, quant=True),
+    dict(weight=False)])
+def test_norm_outputs(lk, dtype, d, kw):
+    _check_norm(*_norm_case(lk, dtype, 6, d, 0 if kw.get("hidden_out", 1) is None else 2,
+                            False, **kw))
+
+
+@pytest.mark.parametrize("d", [512, 40000])
+def test_norm_leaves_out_parts_of_weight_zero(lk, d):
+    """the rows of such parts may hold anything; all of them left out is H"""
+    def edit(h, add, pw):
+        pw[0, 1] = 0
+        add[0, 1] = float("nan")
+        add[1] = float("inf")
+        pw[1] = 0
+    case = _norm_case(lk, "bf16", 4, d, 3, True, edit=edit)
+    _check_norm(*case)
+    assert torch.equal(case[4][1].cpu(), case[0][1])
+
+
+@pytest.mark.parametrize("d", [256, 2048, 40000])
+def test_norm_rows_of_zeros_and_of_special_values(lk, d):
+    def edit(h, add, pw):
+        h[0] = 0
+        h[1, 3] = float("nan")
+        h[2, 5] = float("inf")
+        h[3] = 1e-30
+    h, _, _, g, ho, o, q, sc = _norm_case(lk, "bf16", 6, d, 0, False, edit=edit)
+    assert torch.equal(ho.view(torch.int16).cpu(), h.view(torch.int16))
+    assert (o[0] == 0).all() and (q[0].float() == 0).all() and sc[0] == R.TINY
+    assert o[1].isnan().all() and sc[1].isnan() and q[1].float().isnan().all()
+    assert o[2, 5].isnan() and sc[2].isnan()
+    y, e = R.norm(h[3:], g, 1e-6)
+    _close(o[3:], y, e + R.HALF[BF] * y.abs() * (1 + 2 ** -7) + 2.0 ** -126, "rows beside them")
+
+
+# ---------------------------------------------------------------------------
+# grouping
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n,groups,low,high", [
+    (0, 5, 0, 5), (1, 1, 0, 1), (1, 300, 299, 300), (64, 128, 0, 128), (257, 3, -1, 4),
+    (5000, 257, -3, 260), (4096, 1000, 17, 18), (20000, 16384, 0, 16384), (9000, 7, -9, 0),
+    (100003, 64, 0, 64)])
+def test_group_rows(lk, n, groups, low, high):
+    _say("group", n, groups, low, high)
+    pick = torch.randint(low, high, (n,), generator=torch.Generator().manual_seed(n + groups),
+                         dtype=torch.int32)
+    rows = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    offsets = torch.full((groups + 1,), -7, dtype=torch.int32, device="cuda")
+    lk.group_rows(pick.cuda(), groups, rows, offsets)
+    want, off = R.group_rows(pick, groups)
+    assert offsets.tolist() == off
+    assert rows.tolist() == want + [-7] * (n - len(want))
+
+
+# ---------------------------------------------------------------------------
+# grouped products
+# ---------------------------------------------------------------------------
+
+def _offsets(sizes):
+    return torch.tensor([0] + sizes).cumsum(0).to(torch.int32)
+
+
+def _grouped_case(lk, dtype, sizes, d_in, d_out, up=False, picks=0, scatter=False, m=None,
+                  rows=None, x_rows=None, seed=5):
+    _say("grouped", dtype, sizes[:8], d_in, d_out, up, picks, scatter)
+    quant = dtype == "e4m3"
+    dt = BF if quant else DT[dtype]
+    G, total = len(sizes), sum(sizes)
+    m = total if m is None else m
+    g = torch.Generator().manual_seed(seed)
+    if rows is None and (picks or scatter):
+        rows = torch.randperm(m, generator=g).to(torch.int32)
+    if x_rows is None:
+        x_rows = -(-m // picks) if picks else m
+    x = _rand(seed + 1, x_rows, d_in, dtype=dt)
+    w = _rand(seed + 2, G, d_out, d_in, std=d_in ** -0.5, dtype=dt)
+    wu = _rand(seed + 3, G, d_out, d_in, std=d_in ** -0.5, dtype=dt) if up else None
+    kw = {}
+    if quant:
+        (x, kw["x_scale"]), (w, kw["w_scale"]) = R.quantize_rows(x), R.quantize_rows(w)
+        if up:
+            wu, kw["w_up_scale"] = R.quantize_rows(wu)
+    off = _offsets(sizes)
+    out = torch.full((m, d_out), -7.0, dtype=dt, device="cuda")
+    cu = lambda t: None if t is None else t.cuda()  # noqa: E731
+    lk.grouped_product(cu(x), cu(w), off.cuda(), out, rows=cu(rows), picks=picks,
+                       w_up=cu(wu), scatter=scatter, **{k: v.cuda() for k, v in kw.items()})
+    want, bound = R.grouped(x, w, off, m, rows, picks, wu, scatter, kw.get("x_scale"),
+                            kw.get("w_scale"), kw.get("w_up_scale"), dt)
+    got = out.cpu()
+    written = ~want.isnan().all(1)
+    assert (got[~written] == -7).all(), "rows of no group were written"
+    _close(got[written], want[written], bound[written], "out")
+    return out
+
+
+DTYPES = ["bf16", "f32", "e4m3"]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("up", [False, True])
+@pytest.mark.parametrize("sizes,d_in,d_out", [
+    ([1], 16, 8), ([0, 1, 0, 0, 2], 128, 64), ([16, 17, 0, 3], 272, 72), ([1] * 40, 336, 24),
+    ([5, 0, 33, 20, 64, 1], 144, 136), ([0, 0, 0], 64, 8)])
+def test_grouped_few_rows(lk, dtype, up, sizes, d_in, d_out):
+    _grouped_case(lk, dtype, sizes, d_in, d_out, up)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("up", [False, True])
+@pytest.mark.parametrize("sizes,d_in,d_out", [
+    ([300], 128, 264), ([256, 0, 129, 128], 272, 72), ([0, 513, 1, 70, 0], 400, 320),
+    ([40, 41, 200], 16, 8), ([37, 90], 1040, 520)])
+def test_grouped_many_rows(lk, dtype, up, sizes, d_in, d_out):
+    _grouped_case(lk, dtype, sizes, d_in, d_out, up)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("picks,scatter", [(1, False), (4, False), (0, True), (3, True)])
+@pytest.mark.parametrize("sizes", [[3, 0, 9, 1], [100, 156, 0, 300]])
+def test_grouped_gather_and_scatter(lk, dtype, picks, scatter, sizes):
+    _grouped_case(lk, dtype, sizes, 144, 72, False, picks, scatter)
+    # rows behind the last group, which no entry names
+    _grouped_case(lk, dtype, sizes, 144, 72, True, picks, scatter, m=sum(sizes) + 40)
+
+
+@pytest.mark.parametrize("sizes", [[4, 0, 5], [120, 300]])
+def test_grouped_entries_out_of_range_are_left_out(lk, sizes):
+    m = sum(sizes)
+    rows = torch.randperm(m, generator=torch.Generator().manual_seed(3)).to(torch.int32)
+    rows[1] = -1
+    rows[2] = 2 ** 31 - 1
+    rows[m - 1] = -(2 ** 31)
+    for picks, scatter in ((1, False), (1, True), (0, True), (2, False)):
+        _grouped_case(lk, "bf16", sizes, 144, 72, False, picks, scatter, rows=rows, x_rows=m)
+
+
+@pytest.mark.parametrize("dtype,d_in", [("bf16", 2048), ("e4m3", 2048), ("f32", 1024)])
+@pytest.mark.parametrize("sizes", [[2, 1, 0, 3], [130, 100, 5]])
+def test_grouped_long_sums(lk, dtype, d_in, sizes):
+    _grouped_case(lk, dtype, sizes, d_in, 64)
+
+
+def test_grouped_bad_offsets_stay_in_bounds(lk):
+    """offsets that are not ascending, or past m, name some rows twice or
+    none; no row outside [0, m) is touched"""
+    x, w = _rand(1, 40, 64, dtype=BF).cuda(), _rand(2, 3, 64, 64, dtype=BF).cuda()
+    buf = torch.full((60, 64), -7.0, dtype=BF, device="cuda")
+    for off in ([0, 90, 5, 20], [-4, 10, 30, 2 ** 31 - 1], [60, 50, 45, 41]):
+        lk.grouped_product(x, w, torch.tensor(off, dtype=torch.int32, device="cuda"), buf[:40])
+        torch.cuda.synchronize()
+    assert (buf[40:] == -7).all()
+
+
+def test_grouped_weights_past_32_bits(lk):
+    """the last of groups whose matrices lie past 4 GiB"""
+    G, d_out, d_in = 70, 4096, 8192
+    w = torch.zeros((G, d_out, d_in), dtype=BF, device="cuda")
+    last = _rand(1, d_out, d_in, std=0.01, dtype=BF)
+    w[G - 1] = last.cuda()
+    for rows in (2, 40 * G):   # the small and the tiled kernel
+        x = _rand(2, rows, d_in, dtype=BF)
+        off = torch.zeros(G + 1, dtype=torch.int32)
+        off[G] = rows
+        out = torch.empty((rows, d_out), dtype=BF, device="cuda")
+        lk.grouped_product(x.cuda(), w, off.cuda(), out)
+        want = x[:2].double() @ last.double().T
+        bound = (d_in + 4) * R.U32 * (x[:2].double().abs() @ last.double().abs().T)
+        _close(out[:2], want, bound + R.HALF[BF] * 1.01 * want.abs(), "out")
+
+
+# ---------------------------------------------------------------------------
+# 4-bit products
+# ---------------------------------------------------------------------------
+
+def _matrix(seed, d_out, d_in, group, dtype, zero):
+    g = torch.Generator().manual_seed(seed)
+    w = torch.randint(0, 256, (d_out, d_in // 2), generator=g, dtype=torch.uint8)
+    s = ((torch.rand((d_out, d_in // group), generator=g) + 0.5) * d_in ** -0.5).to(dtype)
+    z = torch.randint(0, 16, s.shape, generator=g, dtype=torch.uint8) if zero else None
+    return w, s, z
+
+
+QUANT = [(1, 32, 8, 32), (1, 64, 24, 64), (1, 2048, 40, 128), (3, 384, 72, 128),
+         (16, 1120, 16, 32), (17, 192, 136, 64), (33, 768, 8, 384), (64, 256, 200, 256),
+         (2, 9600, 16, 32), (100, 128, 8, 32)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("zero", [False, True])
+@pytest.mark.parametrize("n,d_in,d_out,group", QUANT)
+def test_quant_product(lk, dtype, zero, n, d_in, d_out, group):
+    _say("quant", dtype, zero, n, d_in, d_out, group)
+    x = _rand(1, n, d_in, dtype=DT[dtype])
+    w, s, z = _matrix(2, d_out, d_in, group, DT[dtype], zero)
+    add = _rand(3, n, d_out, dtype=DT[dtype])
+    cu = lambda t: None if t is None else t.cuda()  # noqa: E731
+    out = torch.empty((n, d_out), dtype=DT[dtype], device="cuda")
+    lk.quant_product(cu(x), cu(w), cu(s), out, zero=cu(z))
+    _close(out, *R.quant(x, w, s, z), "out")
+    a = add.cuda()
+    lk.quant_product(cu(x), cu(w), cu(s), a, zero=cu(z), add=a)
+    _close(a, *R.quant(x, w, s, z, add), "out on add")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,d_in,d_out,group", QUANT)
+def test_quant_swiglu(lk, dtype, n, d_in, d_out, group):
+    _say("swiglu", dtype, n, d_in, d_out, group)
+    x = _rand(1, n, d_in, dtype=DT[dtype])
+    a = _matrix(2, d_out, d_in, group, DT[dtype], True)
+    b = _matrix(3, d_out, d_in, group, DT[dtype], False)
+    out = torch.empty((n, d_out), dtype=DT[dtype], device="cuda")
+    lk.quant_swiglu(x.cuda(), a[0].cuda(), a[1].cuda(), b[0].cuda(), b[1].cuda(), out,
+                    z_gate=a[2].cuda())
+    _close(out, *R.quant(x, *a, up=b), "out")
+
+
+def test_quant_weights_are_read_as_they_are(lk):
+    """one-hot rows give the weights back exactly: the layout of the bytes,
+    every nibble value and zero point"""
+    for group in (32, 64, 128):
+        d_in, d_out = 256, 16
+        q = (torch.arange(d_out)[:, None] * 7 + torch.arange(d_in)[None] * 3) % 16
+        z = ((torch.arange(d_out)[:, None] + torch.arange(d_in // group)[None]) % 16)
+        s = torch.full((d_out, d_in // group), 0.5)
+        for dt in (BF, F32):
+            out = torch.empty((d_in, d_out), dtype=dt, device="cuda")
+            lk.quant_product(torch.eye(d_in, dtype=dt, device="cuda"),
+                             R.pack(q.to(torch.uint8)).cuda(), s.to(dt).cuda(), out,
+                             zero=z.to(torch.uint8).cuda())
+            want = (q - z.repeat_interleave(group, 1)).T * 0.5
+            assert torch.equal(out.cpu().float(), want.float()), (group, dt)
+
+
+def test_quant_float32_keeps_every_bit_of_a_value(lk):
+    """the three bf16 parts of a float32 value add up to it"""
+    x = torch.zeros((8, 32))
+    x[:, 3] = torch.tensor([1.0000001, 3.1415927, -2.7182817, 1e-30, 6e29, -1 / 3, 2 ** -20 + 1,
+                            123456.79])
+    w = torch.full((8, 16), 0x88, dtype=torch.uint8)
+    w[:, 1] = 0x98                                  # q[3] = 9: weight 1
+    out = torch.empty((8, 8), device="cuda")
+    lk.quant_product(x.cuda(), w.cuda(), torch.ones((8, 1), device="cuda"), out)
+    # (16 + 9) x - (16 + 8) x in float32: a rounding of 25 |x| each
+    want = x[:, 3].double()[:, None].expand(8, 8)
+    _close(out, want, 3 * 25 * R.U32 * want.abs(), "out")
+
+
+def test_quant_special_values_stay_in_their_row(lk):
+    x = _rand(1, 3, 128, dtype=BF)
+    x[1, 7] = float("inf")
+    w, s, _ = _matrix(2, 16, 128, 32, BF, False)
+    for dt in (BF, F32):
+        xd, out = x.to(dt), torch.empty((3, 16), dtype=dt, device="cuda")
+        lk.quant_product(xd.cuda(), w.cuda(), s.to(dt).cuda(), out)
+        assert out[1].isnan().all()
+        v, e = R.quant(xd, w, s.to(dt))
+        _close(out[0], v[0], e[0], "row 0")
+        _close(out[2], v[2], e[2], "row 2")

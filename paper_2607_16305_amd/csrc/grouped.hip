@@ -13,9 +13,9 @@
 //       from global memory (both operands are K-contiguous, a lane's 16 bytes
 //       are its fragment), D steps in flight in registers, K split over the
 //       waves of a workgroup and summed through LDS.
-//   grouped_tiles_kernel  many rows a group: 256 x 256 tiles (a group's last
-//       rows, where at most 128: 128 x 256) on the phased loop of
-//       phase_gemm.h, one workgroup a CU that takes tile after tile.
+//   grouped_tiles_kernel  many rows a group: 256 x 256, 128 x 256 and 128 x 128
+//       tiles on the phased loop of phase_gemm.h, one workgroup a CU that takes
+//       tile after tile.
 //
 // e4m3 operands carry a float32 scale a row, applied once to the float32 sum:
 // out = round(xs ws sum).
@@ -246,35 +246,91 @@ __global__ __launch_bounds__(GS_THREADS) void grouped_rows_kernel(GroupedParams 
 // ---------------------------------------------------------------------------
 // many rows a group
 // ---------------------------------------------------------------------------
-constexpr int GT_THREADS = 512;
+// One launch of GT_GRID workgroups, each a CU's.  The tiles of the launch are
+// numbered, workgroup s takes tiles s, s + GT_GRID, ...; where they lie is
+// found GT_WINDOW at a time, in one pass over the offsets (GtPlan).
+constexpr int GT_THREADS = 512, GT_GRID = 256, GT_WINDOW = 64;
+enum : int { GT_WHOLE = 0, GT_HALF = 1, GT_QUARTER = 2 };   // 256 x 256, 128 x 256, 128 x 128
 
-// One tile: the group's rows from m0, output columns from n0.
+struct GtLds {
+  int4 tile[GT_WINDOW];        // group (-1: none), first row in it, first column, kind
+  int32_t src[256], dst[256];  // a tile's rows: row of x, row of out (-1: not stored)
+  float xs[256];
+  int scan[GT_THREADS / 64];
+  int total[3];
+  // row blocks before each thread's groups (in LDS: nothing but scalars may
+  // live beside a tile's accumulators)
+  int before[3][GT_THREADS];
+};
+
+// The launch's tiles.  In 256 x 256 tiles a group has a row block for every 256
+// rows, a last one of at most 128 rows as a half; when the last round of whole
+// tiles would be at most half full its tiles are cut in halves too.  Where
+// that leaves most CUs idle the launch is all quarters.  A half round takes
+// about 0.55 of a whole one's time, a round of quarters a third.
+struct GtPlan {
+  int64_t whole, halves, cut;   // whole tiles, a group's own halves, whole tiles cut in two
+  int64_t units;
+  bool quarters;
+};
+__device__ __forceinline__ GtPlan gt_plan(int blocks256, int blocks128, int own_halves, int tn,
+                                          int tn_quarter) {
+  GtPlan pl;
+  const int64_t all = (int64_t)blocks256 * tn;
+  const int64_t rem = all % GT_GRID;
+  pl.cut = rem <= GT_GRID / 2 ? rem : 0;
+  pl.whole = all - pl.cut;
+  pl.halves = (int64_t)own_halves * tn;
+  const int64_t quarters = (int64_t)blocks128 * tn_quarter;
+  auto rounds = [](int64_t n) { return (float)((n + GT_GRID - 1) / GT_GRID); };
+  pl.quarters = 0.33f * rounds(quarters) <
+                rounds(pl.whole) + 0.55f * rounds(pl.halves + 2 * pl.cut);
+  pl.units = pl.quarters ? quarters : pl.whole + pl.halves + 2 * pl.cut;
+  return pl;
+}
+
+// One tile of kind (MI, NJ): the group's rows from m0, output columns from n0.
 template <int DT, int MI, int NJ, bool UP>
-__device__ __forceinline__ void grouped_tile(const GroupedParams& p, char* lds, const GpTile& t,
+__device__ __forceinline__ void grouped_tile(const GroupedParams& p, char* lds, GtLds& gl, int grp,
                                              int64_t m0, int n0) {
   using S = PgShape<MI, NJ>;
   constexpr int ODT = DT == DT_E4M3 ? DT_BF16 : DT;
   constexpr int OES = ODT == DT_BF16 ? 2 : 4;
-  PgLoop<DT, MI, NJ> L(lds, threadIdx.x);
+  // opaque, so that nothing of a tile is computed ahead of the loop over the
+  // tiles: kept in registers beside the accumulators it would be spilled, and
+  // a reload inside the stage loop waits for every load in flight
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  int64_t ga, gb;
+  gp_rows(p, grp, ga, gb);
+  __syncthreads();   // the tile before this one is done with its rows and stages
+  if (tid < S::BM) {
+    int64_t i = ga + m0 + tid, src, dst;
+    const bool in = i < gb;
+    i = in ? i : gb - 1;
+    const bool ok = gp_entry(p, i, src, dst) && in;
+    gl.src[tid] = (int32_t)src;
+    gl.dst[tid] = ok ? (int32_t)dst : -1;
+    if constexpr (DT == DT_E4M3) gl.xs[tid] = p.x_scale[src];
+  }
+  __syncthreads();
+
+  PgLoop<DT, MI, NJ> L(lds, tid);
   PgLoads<S> ld;
   const int nst = (int)(p.k_bytes / 128);
   ld.last = nst - 1;
   // gathered rows count from the operand's first row, others from the tile's
-  const bool gather = p.picks != 0;
-  ld.a_base = p.x + (gather ? 0 : (t.a + m0) * p.k_bytes);
+  const int64_t base = p.picks != 0 ? 0 : ga + m0;
+  ld.a_base = p.x + base * p.k_bytes;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int q = 0; q < S::PA; ++q) {
-      int64_t i = t.a + m0 + h * S::HM + L.a_row(q), src, dst;
-      i = i < t.b ? i : t.b - 1;
-      gp_entry(p, i, src, dst);
-      if (!gather) src = i - (t.a + m0);
-      ld.oa[h][q] = (uint32_t)(src * p.k_bytes) + L.a_chunk(q) * 16;
-    }
+    for (int q = 0; q < S::PA; ++q)
+      ld.oa[h][q] = (uint32_t)((gl.src[h * S::HM + L.a_row(q)] - base) * p.k_bytes) +
+                    L.a_chunk(q) * 16;
     const int nh = n0 + (UP ? 0 : h * S::HN);   // first weight row of the half
     const int first = nh < p.cols ? nh : p.cols - 1;
-    ld.b_base[h] = (UP && h == 1 ? p.w_up : p.w) + ((int64_t)t.g * p.cols + first) * p.k_bytes;
+    ld.b_base[h] = (UP && h == 1 ? p.w_up : p.w) + ((int64_t)grp * p.cols + first) * p.k_bytes;
 #pragma unroll
     for (int q = 0; q < S::PB; ++q) {
       int r = nh + L.b_row(q);
@@ -316,72 +372,151 @@ __device__ __forceinline__ void grouped_tile(const GroupedParams& p, char* lds, 
     }
   }
 
-  constexpr int W = S::W, QJ = UP ? 1 : 2, PC = 16 / OES, NP = W * OES / 16;   // 16-byte pieces
-  static_assert(W * OES % 16 == 0, "whole pieces");
+  // a lane holds W neighbouring columns of a row in every quadrant, stored in
+  // pieces of at most 16 bytes (cols is a multiple of a 16-byte piece)
+  constexpr int W = S::W, QJ = UP ? 1 : 2, PC = W * OES < 16 ? W : 16 / OES, NP = W / PC;
+  int col[QJ][NP];
+  float ws[QJ][W], us[W];
+#pragma unroll
+  for (int qj = 0; qj < QJ; ++qj)
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      col[qj][k] = n0 + qj * S::HN + L.wc * 16 * NJ + W * L.g + PC * k;
+#pragma unroll
+      for (int r = 0; r < PC; ++r) {
+        ws[qj][PC * k + r] = us[PC * k + r] = 1.f;
+        if constexpr (DT == DT_E4M3) {
+          const int c = col[qj][k] < p.cols ? col[qj][k] : p.cols - PC;
+          ws[qj][PC * k + r] = p.w_scale[(int64_t)grp * p.cols + c + r];
+          if constexpr (UP) us[PC * k + r] = p.up_scale[(int64_t)grp * p.cols + c + r];
+        }
+      }
+    }
 #pragma unroll
   for (int qi = 0; qi < 2; ++qi)
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      const int64_t e = t.a + m0 + qi * S::HM + L.wr * 16 * MI + 16 * i + L.n16;
-      int64_t src, dst;
-      if (e >= t.b || !gp_entry(p, e, src, dst)) continue;
-      const float xs = DT == DT_E4M3 ? p.x_scale[src] : 1.f;
+      const int row = qi * S::HM + L.wr * 16 * MI + 16 * i + L.n16;
+      const int dst = gl.dst[row];
+      const float xs = DT == DT_E4M3 ? gl.xs[row] : 1.f;
+      if (dst < 0) continue;
 #pragma unroll
       for (int qj = 0; qj < QJ; ++qj)
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
-          const int col = n0 + qj * S::HN + L.wc * 16 * NJ + W * L.g + PC * k;
-          if (col >= p.cols) continue;   // cols is a multiple of a piece
+          if (col[qj][k] >= p.cols) continue;
           float v[PC];
 #pragma unroll
           for (int r = 0; r < PC; ++r) {
             const int x = PC * k + r;
-            float ws = 1.f, us = 1.f;
-            if constexpr (DT == DT_E4M3) {
-              ws = p.w_scale[(int64_t)t.g * p.cols + col + r];
-              if constexpr (UP) us = p.up_scale[(int64_t)t.g * p.cols + col + r];
-            }
             v[r] = gp_value<DT, UP>(acc[qi][qj][i][x >> 2][x & 3], acc[qi][1][i][x >> 2][x & 3],
-                                    xs, ws, us);
+                                    xs, ws[qj][x], us[x]);
           }
-          st_cols<ODT, PC>(p.out + (dst * p.cols + col) * OES, v);
+          st_cols<ODT, PC>(p.out + ((int64_t)dst * p.cols + col[qj][k]) * OES, v);
         }
     }
 }
 
 template <int DT, bool UP>
 __global__ __launch_bounds__(GT_THREADS, 2) void grouped_tiles_kernel(GroupedParams p) {
-  using S = PgShape<4, 2>;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * S::BUF];
-  __shared__ int find_lds[GP_FIND_LDS];
-  constexpr int TCOLS = UP ? S::HN : S::BN;
-  const int tn = (p.cols + TCOLS - 1) / TCOLS;
-  // whole row blocks of a group (a last one of more than 128 rows counts), and
-  // its half row block
-  auto whole = [](int64_t r) { return (int)((r + 127) / 256); };
-  auto half = [](int64_t r) {
-    const int rem = (int)(r % 256);
-    return rem > 0 && rem <= 128 ? 1 : 0;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * PgShape<4, 2>::BUF];
+  __shared__ GtLds gl;
+  constexpr int TC = UP ? 128 : 256, QC = UP ? 64 : 128;   // output columns of a tile
+  const int tn = (p.cols + TC - 1) / TC, tq = (p.cols + QC - 1) / QC;
+  // neighbouring tiles on one XCD
+  const int slot = (blockIdx.x & 7) * (GT_GRID / 8) + (blockIdx.x >> 3);
+
+  // this thread's groups and the numbers of row blocks before them
+  const int per = (p.groups + GT_THREADS - 1) / GT_THREADS;
+  auto blocks = [&](int g, int& b256, int& b128, int& half) {
+    int64_t a, b;
+    gp_rows(p, g, a, b);
+    const int r = (int)(b - a), rem = r & 255;
+    half = rem > 0 && rem <= 128 ? 1 : 0;
+    b256 = (r >> 8) + (rem > 128 ? 1 : 0);
+    b128 = (r + 127) >> 7;
   };
-  GpTile t;
-  int64_t wholes = INT64_MAX;
-  // a workgroup of the launch's rounds: neighbouring tiles on one XCD
-  const int slot = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
-  for (int64_t unit = slot;; unit += gridDim.x) {
-    if (unit < wholes) {
-      const int rb = (int)(unit / tn);
-      wholes = (int64_t)find_tile<GT_THREADS>(p, rb, find_lds, t, whole) * tn;
-      if (t.g >= 0) {
-        grouped_tile<DT, 4, 2, UP>(p, lds, t, (int64_t)t.idx * S::BM,
-                                   (int)(unit - (int64_t)rb * tn) * TCOLS);
-        continue;
-      }
+  {
+    int n[3] = {0, 0, 0};
+    const int g0 = threadIdx.x * per;
+    for (int g = g0; g < g0 + per && g < p.groups; ++g) {
+      int b, q, h;
+      blocks(g, b, q, h);
+      n[0] += b;
+      n[1] += q;
+      n[2] += h;
     }
-    const int rb = (int)((unit - wholes) / tn);
-    find_tile<GT_THREADS>(p, rb, find_lds, t, half);
-    if (t.g < 0) return;
-    grouped_tile<DT, 2, 2, UP>(p, lds, t, (t.b - t.a) / 256 * 256,
-                               (int)(unit - wholes - (int64_t)rb * tn) * TCOLS);
+#pragma unroll
+    for (int c = 0; c < 3; ++c) {
+      const int incl = block_scan_incl<GT_THREADS / 64>(n[c], gl.scan);
+      gl.before[c][threadIdx.x] = incl - n[c];
+      if (threadIdx.x == GT_THREADS - 1) gl.total[c] = incl;
+    }
+  }
+  __syncthreads();
+  const GtPlan pl = gt_plan(__builtin_amdgcn_readfirstlane(gl.total[0]),
+                            __builtin_amdgcn_readfirstlane(gl.total[1]),
+                            __builtin_amdgcn_readfirstlane(gl.total[2]), tn, tq);
+
+  for (int64_t k0 = 0; slot + k0 * GT_GRID < pl.units; k0 += GT_WINDOW) {
+    __syncthreads();
+    if (threadIdx.x < GT_WINDOW) gl.tile[threadIdx.x] = make_int4(-1, 0, 0, 0);
+    __syncthreads();
+    // this workgroup's tiles among [lo, hi) that lie in the window
+    auto mark = [&](int64_t lo, int64_t hi, auto&& where) {
+      int64_t k = lo <= slot ? 0 : (lo - slot + GT_GRID - 1) / GT_GRID;
+      for (k = k < k0 ? k0 : k; k < k0 + GT_WINDOW; ++k) {
+        const int64_t u = slot + k * GT_GRID;
+        if (u >= hi) break;
+        gl.tile[k - k0] = where(u - lo);
+      }
+    };
+    int64_t at256 = gl.before[0][threadIdx.x], at128 = gl.before[1][threadIdx.x];
+    int64_t athalf = gl.before[2][threadIdx.x];
+    const int g0 = threadIdx.x * per;
+    for (int g = g0; g < g0 + per && g < p.groups; ++g) {
+      int b, q, h;
+      blocks(g, b, q, h);
+      if (pl.quarters) {
+        mark(at128 * tq, (at128 + q) * tq, [&](int64_t u) {
+          return make_int4(g, (int)(u / tq) * 128, (int)(u % tq) * QC, GT_QUARTER);
+        });
+      } else {
+        const int64_t lo = at256 * tn, hi = (at256 + b) * tn;
+        auto whole = [&](int64_t u) {
+          return make_int4(g, (int)(u / tn) * 256, (int)(u % tn) * TC, GT_WHOLE);
+        };
+        mark(lo, hi < pl.whole ? hi : pl.whole, whole);
+        if (h != 0)
+          mark(pl.whole + athalf * tn, pl.whole + (athalf + 1) * tn, [&](int64_t u) {
+            return make_int4(g, b * 256, (int)u * TC, GT_HALF);
+          });
+        const int64_t c0 = lo > pl.whole ? lo : pl.whole;   // its tiles that are cut
+        if (c0 < hi)
+          mark(pl.whole + pl.halves + 2 * (c0 - pl.whole),
+               pl.whole + pl.halves + 2 * (hi - pl.whole), [&](int64_t u) {
+                 int4 t = whole(c0 - lo + (u >> 1));
+                 t.y += (int)(u & 1) * 128;
+                 t.w = GT_HALF;
+                 return t;
+               });
+      }
+      at256 += b;
+      at128 += q;
+      athalf += h;
+    }
+    __syncthreads();
+    for (int k = 0; k < GT_WINDOW; ++k) {
+      const int4 t = gl.tile[k];
+      const int g = __builtin_amdgcn_readfirstlane(t.x);
+      if (g < 0) break;
+      const int m0 = __builtin_amdgcn_readfirstlane(t.y);
+      const int n0 = __builtin_amdgcn_readfirstlane(t.z);
+      const int kind = __builtin_amdgcn_readfirstlane(t.w);
+      if (kind == GT_WHOLE) grouped_tile<DT, 4, 2, UP>(p, lds, gl, g, m0, n0);
+      else if (kind == GT_HALF) grouped_tile<DT, 2, 2, UP>(p, lds, gl, g, m0, n0);
+      else grouped_tile<DT, 2, 1, UP>(p, lds, gl, g, m0, n0);
+    }
   }
 }
 
@@ -405,7 +540,8 @@ static hipError_t launch_grouped_dt(const GroupedParams& p, hipStream_t st) {
   const bool near = p.k_bytes < (4 << 20) &&
                     (p.picks == 0 || p.x_rows * p.k_bytes < ((int64_t)1 << 32));
   if (p.m > 32 * (int64_t)p.groups && p.k_bytes >= 128 && near) {
-    hipLaunchKernelGGL((grouped_tiles_kernel<DT, UP>), dim3(256), dim3(GT_THREADS), 0, st, p);
+    hipLaunchKernelGGL((grouped_tiles_kernel<DT, UP>), dim3(GT_GRID),
+                       dim3(GT_THREADS), 0, st, p);
     return hipGetLastError();
   }
   if (p.m > 8 * (int64_t)p.groups) return launch_rows<DT, 2, 4, 4, UP>(p, st);

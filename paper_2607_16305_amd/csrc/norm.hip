@@ -151,8 +151,8 @@ __device__ __forceinline__ void rn_store_quant(char* row, int c, const float (&y
 }
 
 // A row on a team of T threads, at most CH chunks a thread, kept in registers.
-template <int DT, int T, int CH>
-__global__ __launch_bounds__(RN_THREADS) void residual_norm_kernel(NormParams p) {
+template <int DT, int T, int CH, bool ONE>
+__global__ __launch_bounds__(RN_THREADS, CH < 8 || DT == DT_F32 ? 4 : 3) void residual_norm_kernel(NormParams p) {
   constexpr int E = rn_elems<DT>();
   __shared__ float red_s[RN_THREADS / 64];
   __shared__ uint32_t red_m[RN_THREADS / 64];
@@ -164,21 +164,29 @@ __global__ __launch_bounds__(RN_THREADS) void residual_norm_kernel(NormParams p)
   const float* pw = p.part_w != nullptr ? p.part_w + row * p.parts : nullptr;
   float s[CH][E];
   float ss = 0.f;
+  // one part: its row is loaded beside H's
+  u32x4_t hv[CH], av[CH];
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int c = t + T * i;
+    hv[i] = av[i] = u32x4_t{0, 0, 0, 0};
     if (c < p.chunks) {
-      rn_unpack<DT>(ld16(h + (int64_t)c * 16), s[i]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) s[i][e] = 0.f;
+      hv[i] = ld16(h + (int64_t)c * 16);
+      if constexpr (ONE) av[i] = ld16(add + (int64_t)c * 16);
     }
   }
-  if (p.parts > 0) {
+  const float w0 = ONE && pw != nullptr ? pw[0] : 1.f;
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int c = t + T * i;
-      if (c < p.chunks) rn_add<DT>(p, add, pw, c, s[i]);
+  for (int i = 0; i < CH; ++i) {
+    const int c = t + T * i;
+    rn_unpack<DT>(hv[i], s[i]);
+    if constexpr (ONE) {
+      float a[E];
+      rn_unpack<DT>(av[i], a);
+#pragma unroll
+      for (int e = 0; e < E; ++e) s[i][e] += w0 != 0.f ? __fmul_rn(w0, a[e]) : 0.f;
+    } else {
+      if (p.parts > 0 && c < p.chunks) rn_add<DT>(p, add, pw, c, s[i]);
     }
   }
 #pragma unroll
@@ -291,8 +299,11 @@ __global__ __launch_bounds__(RN_THREADS) void residual_norm_wide_kernel(NormPara
 template <int DT, int T, int CH>
 static void launch_norm_t(const NormParams& p, hipStream_t st) {
   const int64_t rows = RN_THREADS / T;
-  hipLaunchKernelGGL((residual_norm_kernel<DT, T, CH>), dim3((unsigned)((p.n + rows - 1) / rows)),
-                     dim3(RN_THREADS), 0, st, p);
+  const dim3 grid((unsigned)((p.n + rows - 1) / rows));
+  if (p.parts == 1)
+    hipLaunchKernelGGL((residual_norm_kernel<DT, T, CH, true>), grid, dim3(RN_THREADS), 0, st, p);
+  else
+    hipLaunchKernelGGL((residual_norm_kernel<DT, T, CH, false>), grid, dim3(RN_THREADS), 0, st, p);
 }
 
 template <int DT>

@@ -5,17 +5,19 @@
 //   out[i] = round(silu(W[g] x[src(i)]) * (W_up[g] x[src(i)]))
 //
 // The groups' sizes are on the device only.  A workgroup finds its tile by a
-// prefix sum over the groups' tile counts (find_tile), so no tile spans two
-// groups, and empty groups cost nothing.  Two kernels:
+// prefix sum over the groups' tile counts, so no tile spans two groups, and
+// empty groups cost nothing.  Three kernels:
 //
-//   grouped_rows_kernel   few rows a group: bound by the stream of the weights
-//       out of HBM.  A wave multiplies 16 weight rows by 16 NT tokens straight
+//   grouped_rows_kernel   a few rows a group: bound by the stream of the weights
+//       out of HBM.  A wave multiplies 16 weight rows by 16 tokens straight
 //       from global memory (both operands are K-contiguous, a lane's 16 bytes
-//       are its fragment), D steps in flight in registers, K split over the
-//       waves of a workgroup and summed through LDS.
-//   grouped_tiles_kernel  many rows a group: 256 x 256, 128 x 256 and 128 x 128
-//       tiles on the phased loop of phase_gemm.h, one workgroup a CU that takes
-//       tile after tile.
+//       are its fragment), K split over the waves of a workgroup and summed
+//       through LDS.
+//   grouped_mid_kernel    some rows a group: 32 x 64 and 64 x 64 tiles, both
+//       operands through a ring of stages in LDS.
+//   grouped_tiles_kernel  many rows a group: 256 x 256 and 128 x 256 tiles on the
+//       phased loop of phase_gemm.h, one workgroup a CU that takes tile after
+//       tile.
 //
 // e4m3 operands carry a float32 scale a row, applied once to the float32 sum:
 // out = round(xs ws sum).
@@ -41,11 +43,11 @@ __device__ __forceinline__ void gp_rows(const GroupedParams& p, int g, int64_t& 
   b = b < a ? a : (b > p.m ? p.m : b);
 }
 
-// Tile number `unit` in the groups' order, count(rows) tiles a group; all
-// threads of the block.  Returns the number of tiles; t.g is -1 past the last.
-template <int THREADS, class Count>
-__device__ __forceinline__ int find_tile(const GroupedParams& p, int unit, int* lds, GpTile& t,
-                                         Count&& count) {
+// Tile number which(total) in the groups' order, count(rows) tiles a group; all
+// threads of the block.  t.g is -1 past the last tile.
+template <int THREADS, class Count, class Which>
+__device__ __forceinline__ void find_tile(const GroupedParams& p, int* lds, GpTile& t,
+                                          Count&& count, Which&& which) {
   const int per = (p.groups + THREADS - 1) / THREADS;
   const int first = threadIdx.x * per;
   const int last = first + per < p.groups ? first + per : p.groups;
@@ -57,6 +59,9 @@ __device__ __forceinline__ int find_tile(const GroupedParams& p, int unit, int* 
   }
   if (threadIdx.x == 0) lds[0] = -1;
   const int incl = block_scan_incl<THREADS / 64>(sum, lds + 3);
+  if (threadIdx.x == THREADS - 1) lds[2] = incl;
+  __syncthreads();
+  const int unit = which(__builtin_amdgcn_readfirstlane(lds[2]));
   int at = incl - sum;
   if (at <= unit && unit < incl) {
     for (int g = first; g < last; ++g) {
@@ -71,16 +76,16 @@ __device__ __forceinline__ int find_tile(const GroupedParams& p, int unit, int* 
       at += c;
     }
   }
-  if (threadIdx.x == THREADS - 1) lds[2] = incl;
   __syncthreads();
   t.g = __builtin_amdgcn_readfirstlane(lds[0]);
   t.idx = __builtin_amdgcn_readfirstlane(lds[1]);
-  const int total = __builtin_amdgcn_readfirstlane(lds[2]);
   __syncthreads();
   if (t.g >= 0) gp_rows(p, t.g, t.a, t.b);
-  return total;
 }
 constexpr int GP_FIND_LDS = 3 + 16;
+// Most workgroups of a launch: the number of tiles is the device's, and a launch
+// is for the most there can be, in passes of this many.
+constexpr int64_t GP_GRID = 65536;
 
 // Entry i: the row of x it reads (clamped) and the row of out it writes; false
 // where either is out of range, which leaves the row as it was.
@@ -113,16 +118,18 @@ __device__ __forceinline__ float gp_value(float c, float u, float xs, float ws, 
 // ---------------------------------------------------------------------------
 constexpr int GS_THREADS = 256, GS_WAVES = 4;
 
-// NT: token tiles of 16.  KS: waves that share the K of 16 weight rows; the
-// workgroup's other waves take other rows.  D: steps (64 bytes of K) in flight.
-template <int DT, int NT, int KS, int D, bool UP>
+// KS: waves that share the K of 16 weight rows; the workgroup's other waves take
+// other rows.  Two steps (64 bytes of K) are in flight a wave: more registers
+// for more of them cost as many waves (1 row in 128 groups of 2 x 1024 x 2048
+// 187 us, 5.7 TB/s of weights, 195 with four).
+template <int DT, int KS, bool UP>
 __global__ __launch_bounds__(GS_THREADS) void grouped_rows_kernel(GroupedParams p) {
   constexpr int ODT = DT == DT_E4M3 ? DT_BF16 : DT;
   constexpr int OES = ODT == DT_BF16 ? 2 : 4;
   constexpr int MATS = UP ? 2 : 1;
-  constexpr int COLS = 16 * (GS_WAVES / KS);
+  constexpr int COLS = 16 * (GS_WAVES / KS), D = 2;
   __shared__ int find_lds[GP_FIND_LDS];
-  __shared__ f32x4_t part[KS > 1 ? GS_WAVES * MATS * NT * 64 : 1];
+  __shared__ f32x4_t part[GS_WAVES * MATS * 64];
   const int tiles_n = (p.cols + COLS - 1) / COLS;
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -137,45 +144,35 @@ __global__ __launch_bounds__(GS_THREADS) void grouped_rows_kernel(GroupedParams 
   for (int64_t unit = blockIdx.x;; unit += gridDim.x) {
     const int row_tile = (int)(unit / tiles_n);
     GpTile t;
-    find_tile<GS_THREADS>(p, row_tile, find_lds, t,
-                          [](int64_t r) { return (int)((r + 16 * NT - 1) / (16 * NT)); });
+    find_tile<GS_THREADS>(
+        p, find_lds, t, [](int64_t r) { return (int)((r + 15) / 16); },
+        [row_tile](int) { return row_tile; });
     if (t.g < 0) return;
     const int c0 = (int)(unit - (int64_t)row_tile * tiles_n) * COLS + 16 * (wv / KS);
 
-    int64_t dst[NT];
-    bool ok[NT];
-    float xs[NT];
-    const char* xp[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      int64_t i = t.a + (int64_t)t.idx * (16 * NT) + 16 * j + n16, src;
-      const bool in = i < t.b;
-      i = in ? i : t.b - 1;
-      ok[j] = gp_entry(p, i, src, dst[j]) && in;
-      xp[j] = p.x + src * p.k_bytes;
-      xs[j] = 1.f;
-      if constexpr (DT == DT_E4M3) xs[j] = p.x_scale[src];
-    }
+    int64_t i = t.a + (int64_t)t.idx * 16 + n16, src, dst;
+    const bool in = i < t.b;
+    i = in ? i : t.b - 1;
+    const bool ok = gp_entry(p, i, src, dst) && in;
+    const char* xp = p.x + src * p.k_bytes;
+    const float xs = DT == DT_E4M3 ? p.x_scale[src] : 1.f;
     const int wc = c0 + n16 < p.cols ? c0 + n16 : p.cols - 1;
     const int64_t wrow = ((int64_t)t.g * p.cols + wc) * p.k_bytes;
     const char* wp[MATS];
     wp[0] = p.w + wrow;
     if constexpr (UP) wp[1] = p.w_up + wrow;
 
-    f32x4_t acc[MATS][NT];
+    f32x4_t acc[MATS];
 #pragma unroll
-    for (int q = 0; q < MATS; ++q)
-#pragma unroll
-      for (int j = 0; j < NT; ++j) acc[q][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    u32x4_t fw[D][MATS], fx[D][NT];
+    for (int q = 0; q < MATS; ++q) acc[q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    u32x4_t fw[D][MATS], fx[D];
     // unconditional loads from clamped addresses; chunks past K count as zero
     auto load = [&](int d, int s) {
       int c = 4 * s + g;
       c = c < chunks ? c : chunks - 1;
 #pragma unroll
-      for (int q = 0; q < MATS; ++q) fw[d][q] = ld16_nt(wp[q] + (int64_t)c * 16);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) fx[d][j] = ld16(xp[j] + (int64_t)c * 16);
+      for (int q = 0; q < MATS; ++q) fw[d][q] = ld16(wp[q] + (int64_t)c * 16);
+      fx[d] = ld16(xp + (int64_t)c * 16);
     };
     if (s0 < s1) {
 #pragma unroll
@@ -186,59 +183,263 @@ __global__ __launch_bounds__(GS_THREADS) void grouped_rows_kernel(GroupedParams 
       for (int s = s0; s < s1; s += D) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
-          const bool in = s + d < s1 && 4 * (s + d) + g < chunks;
-          u32x4_t w[MATS], x[NT];
+          const bool live = s + d < s1 && 4 * (s + d) + g < chunks;
+          const u32x4_t none = {0, 0, 0, 0};
+          u32x4_t w[MATS];
 #pragma unroll
-          for (int q = 0; q < MATS; ++q) w[q] = in ? fw[d][q] : u32x4_t{0, 0, 0, 0};
-#pragma unroll
-          for (int j = 0; j < NT; ++j) x[j] = in ? fx[d][j] : u32x4_t{0, 0, 0, 0};
+          for (int q = 0; q < MATS; ++q) w[q] = live ? fw[d][q] : none;
+          const u32x4_t x = live ? fx[d] : none;
           load(d, s + d + D);
 #pragma unroll
-          for (int q = 0; q < MATS; ++q)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) acc[q][j] = mfma_chunk<DT>(w[q], x[j], acc[q][j]);
+          for (int q = 0; q < MATS; ++q) acc[q] = mfma_chunk<DT>(w[q], x, acc[q]);
         }
       }
     }
-    if constexpr (KS > 1) {
-      f32x4_t* mine = part + wv * (MATS * NT * 64) + lane;
-      if (kp != 0) {
+    f32x4_t* mine = part + wv * (MATS * 64) + lane;
+    if (kp != 0) {
 #pragma unroll
-        for (int q = 0; q < MATS; ++q)
-#pragma unroll
-          for (int j = 0; j < NT; ++j) mine[(q * NT + j) * 64] = acc[q][j];
-      }
-      __syncthreads();   // (the next unit's find_tile keeps its writes behind these reads)
-      if (kp != 0) continue;
-#pragma unroll
-      for (int o = 1; o < KS; ++o)
-#pragma unroll
-        for (int q = 0; q < MATS; ++q)
-#pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            const f32x4_t v = mine[(o * MATS * NT + q * NT + j) * 64];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[q][j][r] += v[r];
-          }
+      for (int q = 0; q < MATS; ++q) mine[q * 64] = acc[q];
     }
-    // the lane holds columns c0 + 4 g + r of its tokens' rows (cols is a
-    // multiple of 4)
+    __syncthreads();   // (the next unit's find_tile keeps its writes behind these reads)
+    if (kp != 0) continue;
+#pragma unroll
+    for (int o = 1; o < KS; ++o)
+#pragma unroll
+      for (int q = 0; q < MATS; ++q) {
+        const f32x4_t v = mine[(o * MATS + q) * 64];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[q][r] += v[r];
+      }
+    // the lane holds columns c0 + 4 g + r of its token's row (cols is a multiple
+    // of 4)
     const int col = c0 + 4 * g;
-    if (col >= p.cols) continue;
+    if (col >= p.cols || !ok) continue;
     f32x4_t ws = {1.f, 1.f, 1.f, 1.f}, us = ws;
     if constexpr (DT == DT_E4M3) {
       const int64_t s = (int64_t)t.g * p.cols + col;
       ws = *reinterpret_cast<const f32x4_t*>(p.w_scale + s);
       if constexpr (UP) us = *reinterpret_cast<const f32x4_t*>(p.up_scale + s);
     }
+    float v[4];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      if (!ok[j]) continue;
-      float v[4];
+    for (int r = 0; r < 4; ++r)
+      v[r] = gp_value<DT, UP>(acc[0][r], UP ? acc[MATS - 1][r] : 0.f, xs, ws[r], us[r]);
+    st_cols<ODT, 4>(p.out + (dst * p.cols + col) * OES, v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// some rows a group
+// ---------------------------------------------------------------------------
+// 64 x 64 tiles (UP: 64 rows x 32 columns of both matrices), four waves in 2 x
+// 2 of 32 rows x 32 weight rows, K in 128-byte stages loaded straight into a
+// ring of NS in LDS (dtl.h).  Bound by the stages' latency over the bytes in
+// flight, so the ring is deep (NS = 8, 128 KiB) where a CU has one tile, and
+// there are several workgroups a CU where it has more.
+template <int TI>
+using GmShape = DtlShape<2, 2, TI, 2, 128>;
+constexpr int GM_THREADS = 256;
+
+template <int DT, int NS, int TI, bool UP>
+__global__ __launch_bounds__(GM_THREADS) void grouped_mid_kernel(GroupedParams p) {
+  using S = GmShape<TI>;
+  constexpr int RT = 32 * TI;
+  constexpr int ODT = DT == DT_E4M3 ? DT_BF16 : DT;
+  constexpr int OES = ODT == DT_BF16 ? 2 : 4;
+  constexpr int COLS = UP ? 32 : 64;
+  __shared__ __attribute__((aligned(1024))) char lds[NS][S::STAGE];
+  __shared__ int find_lds[GP_FIND_LDS];
+  __shared__ int32_t row_src[RT], row_dst[RT];
+  __shared__ float row_xs[RT];
+  const int tn = (p.cols + COLS - 1) / COLS;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n16 = lane & 15, g = lane >> 4;
+  const int wm = (wv >> 1) * 16 * TI, wn = wv & 1;
+  const int nst = (int)(p.k_bytes / 128);
+  const int tail = (int)(p.k_bytes / 16) - 8 * nst;
+
+  for (int64_t base = 0;; base += gridDim.x) {
+    // the tiles of a group run down the row tiles of a column block first (they
+    // share its weights), neighbours on one XCD
+    GpTile t;
+    find_tile<GM_THREADS>(
+        p, find_lds, t, [tn](int64_t r) { return (int)((r + RT - 1) / RT) * tn; },
+        [&](int total) {
+          const int64_t left = total - base;
+          const int n = (int)(left < (int64_t)gridDim.x ? left : (int64_t)gridDim.x);
+          const int u = n > 0 ? xcd_remap(blockIdx.x, n) : -1;
+          return u < 0 ? -1 : (int)(base + u);
+        });
+    if (t.g < 0) return;
+    const int row_tiles = (int)((t.b - t.a + RT - 1) / RT);
+    const int ct = t.idx / row_tiles;
+    const int64_t m0 = (int64_t)(t.idx - ct * row_tiles) * RT;
+    const int n0 = ct * COLS;
+    if (tid < RT) {
+      int64_t i = t.a + m0 + tid, src, dst;
+      const bool in = i < t.b;
+      i = in ? i : t.b - 1;
+      const bool ok = gp_entry(p, i, src, dst) && in;
+      row_src[tid] = (int32_t)src;
+      row_dst[tid] = ok ? (int32_t)dst : -1;
+      if constexpr (DT == DT_E4M3) row_xs[tid] = p.x_scale[src];
+    }
+    __syncthreads();
+
+    // load b of this wave covers stage row trow (RT rows of x, then 64 of the
+    // weights: UP 32 of gate and the same 32 of up), the lane one chunk of it
+    const char* src[S::PER_WAVE];
+    int chunk[S::PER_WAVE];
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        v[r] = gp_value<DT, UP>(acc[0][j][r], UP ? acc[MATS - 1][j][r] : 0.f, xs[j], ws[r], us[r]);
-      st_cols<ODT, 4>(p.out + (dst[j] * p.cols + col) * OES, v);
+    for (int b = 0; b < S::PER_WAVE; ++b) {
+      const int trow = (wv * S::PER_WAVE + b) * S::RPI + lane / S::LPR;
+      chunk[b] = (lane % S::LPR) ^ blk_swz<128>(trow & 15);
+      if (trow < RT) {
+        src[b] = p.x + row_src[trow] * p.k_bytes;
+      } else {
+        int c = trow - RT;
+        const char* w = p.w;
+        if (UP && c >= 32) {
+          w = p.w_up;
+          c -= 32;
+        }
+        c = n0 + c < p.cols ? n0 + c : p.cols - 1;
+        src[b] = w + ((int64_t)t.g * p.cols + c) * p.k_bytes;
+      }
+      src[b] += chunk[b] * 16;
+    }
+    // stages in a circle from one of the column block's own (GtLoads)
+    const int rot = nst > 0 ? (int)((unsigned)(t.g * 8 + ct) % (unsigned)nst) : 0;
+    auto issue = [&](int i) {
+      int s = (i < nst ? i : nst - 1) + rot;   // past the end: a harmless reload
+      s = s < nst ? s : s - nst;
+      char* dst = lds[i % NS];
+#pragma unroll
+      for (int b = 0; b < S::PER_WAVE; ++b)
+        load_lds16(src[b] + (int64_t)s * 128, dst + (wv * S::PER_WAVE + b) * 1024);
+    };
+    f32x4_t acc[TI][2];   // [row tile][weight tile]
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    auto read = [&](const char* buf, u32x4_t (&fa)[2][TI], u32x4_t (&fb)[2][2]) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+        for (int i = 0; i < TI; ++i) fa[ks][i] = read_frag<128>(buf, wm + 16 * i, ks, n16, g);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          fb[ks][j] =
+              read_frag<128>(buf, RT + (UP ? 32 * j + 16 * wn : 32 * wn + 16 * j), ks, n16, g);
+      }
+    };
+    // weights as operand A: a lane ends with four neighbouring columns of a row
+    auto mma = [&](const u32x4_t (&fa)[2][TI], const u32x4_t (&fb)[2][2]) {
+      if constexpr (DT == DT_E4M3) {
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            acc[i][j] = mfma_stage_e4m3(fb[0][j], fb[1][j], fa[0][i], fa[1][i], acc[i][j]);
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[i][j] = mfma_chunk<DT>(fb[ks][j], fa[ks][i], acc[i][j]);
+      }
+    };
+    // this wave's loads of all but the `younger` latest stages have landed; the
+    // barrier makes every wave's visible and ends every read of the buffer
+    // that the next loads fill
+    auto sync = [&](auto younger) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(younger)::value * S::PER_WAVE) : "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    };
+    if (nst > 0) {
+#pragma unroll
+      for (int i = 0; i < NS - 1; ++i) issue(i);
+      if constexpr (NS == 2) {
+        for (int i = 0; i < nst; ++i) {
+          sync(std::integral_constant<int, 0>{});
+          issue(i + 1);
+          u32x4_t fa[2][TI], fb[2][2];
+          read(lds[i % NS], fa, fb);
+          mma(fa, fb);
+        }
+      } else {
+        // one or two waves a SIMD: stage i + 1 is read while i is multiplied
+        auto step = [&](int i, const u32x4_t (&ca)[2][TI], const u32x4_t (&cb)[2][2],
+                        u32x4_t (&na)[2][TI], u32x4_t (&nb)[2][2]) {
+          sync(std::integral_constant<int, NS - 3>{});
+          read(lds[(i + 1) % NS], na, nb);
+          issue(i + NS - 1);
+          __builtin_amdgcn_sched_barrier(0);
+          mma(ca, cb);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        u32x4_t fa0[2][TI], fb0[2][2], fa1[2][TI], fb1[2][2];
+        sync(std::integral_constant<int, NS - 2>{});
+        read(lds[0], fa0, fb0);
+        int i = 0;
+        for (; i + 1 < nst; i += 2) {
+          step(i, fa0, fb0, fa1, fb1);
+          step(i + 1, fa1, fb1, fa0, fb0);
+        }
+        if (i < nst) step(i, fa0, fb0, fa1, fb1);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load into LDS is left
+    }
+    if (tail != 0) {   // the chunks past the last whole stage, zeros behind them
+      __syncthreads();
+#pragma unroll
+      for (int b = 0; b < S::PER_WAVE; ++b) {
+        const bool in = chunk[b] < tail;
+        const u32x4_t v = ld16(src[b] - (in ? 0 : chunk[b] * 16) + (int64_t)nst * 128);
+        st16(lds[0] + (wv * S::PER_WAVE + b) * 1024 + lane * 16, in ? v : u32x4_t{0, 0, 0, 0});
+      }
+      __syncthreads();
+      u32x4_t fa[2][TI], fb[2][2];
+      read(lds[0], fa, fb);
+      mma(fa, fb);
+    }
+
+    constexpr int NJ = UP ? 1 : 2;
+    int col[NJ];
+    f32x4_t ws[NJ], us = {1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      col[j] = n0 + (UP ? 16 * wn : 32 * wn + 16 * j) + 4 * g;
+      ws[j] = us;
+    }
+    if constexpr (DT == DT_E4M3) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int c = col[j] < p.cols ? col[j] : p.cols - 4;
+        const int64_t at = (int64_t)t.g * p.cols + c;
+        ws[j] = *reinterpret_cast<const f32x4_t*>(p.w_scale + at);
+        if constexpr (UP) us = *reinterpret_cast<const f32x4_t*>(p.up_scale + at);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < TI; ++i) {
+      const int row = wm + 16 * i + n16;
+      const int dst = row_dst[row];
+      const float xs = DT == DT_E4M3 ? row_xs[row] : 1.f;
+      if (dst < 0) continue;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        if (col[j] >= p.cols) continue;
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          v[r] = gp_value<DT, UP>(acc[i][j][r], acc[i][1][r], xs, ws[j][r], us[r]);
+        st_cols<ODT, 4>(p.out + ((int64_t)dst * p.cols + col[j]) * OES, v);
+      }
     }
   }
 }
@@ -250,44 +451,57 @@ __global__ __launch_bounds__(GS_THREADS) void grouped_rows_kernel(GroupedParams 
 // numbered, workgroup s takes tiles s, s + GT_GRID, ...; where they lie is
 // found GT_WINDOW at a time, in one pass over the offsets (GtPlan).
 constexpr int GT_THREADS = 512, GT_GRID = 256, GT_WINDOW = 64;
-enum : int { GT_WHOLE = 0, GT_HALF = 1, GT_QUARTER = 2 };   // 256 x 256, 128 x 256, 128 x 128
+enum : int { GT_WHOLE = 0, GT_HALF = 1 };   // 256 x 256, 128 x 256
 
 struct GtLds {
   int4 tile[GT_WINDOW];        // group (-1: none), first row in it, first column, kind
   int32_t src[256], dst[256];  // a tile's rows: row of x, row of out (-1: not stored)
   float xs[256];
   int scan[GT_THREADS / 64];
-  int total[3];
-  // row blocks before each thread's groups (in LDS: nothing but scalars may
-  // live beside a tile's accumulators)
-  int before[3][GT_THREADS];
+  int total[2];
+  // whole and half row blocks before each thread's groups (in LDS: nothing but
+  // scalars may live beside a tile's accumulators)
+  int before[2][GT_THREADS];
 };
 
-// The launch's tiles.  In 256 x 256 tiles a group has a row block for every 256
-// rows, a last one of at most 128 rows as a half; when the last round of whole
-// tiles would be at most half full its tiles are cut in halves too.  Where
-// that leaves most CUs idle the launch is all quarters.  A half round takes
-// about 0.55 of a whole one's time, a round of quarters a third.
+// The launch's tiles: a group has a row block for every 256 rows, a last one of
+// at most 128 rows as a half; when the last round of whole tiles would be at
+// most half full its tiles are cut in halves too (a round of halves takes 0.73
+// of a whole one's time).
 struct GtPlan {
-  int64_t whole, halves, cut;   // whole tiles, a group's own halves, whole tiles cut in two
+  int64_t whole, halves, cut;   // whole tiles, the groups' own halves, whole tiles cut in two
   int64_t units;
-  bool quarters;
 };
-__device__ __forceinline__ GtPlan gt_plan(int blocks256, int blocks128, int own_halves, int tn,
-                                          int tn_quarter) {
+__device__ __forceinline__ GtPlan gt_plan(int blocks, int own_halves, int tn) {
   GtPlan pl;
-  const int64_t all = (int64_t)blocks256 * tn;
+  const int64_t all = (int64_t)blocks * tn;
   const int64_t rem = all % GT_GRID;
   pl.cut = rem <= GT_GRID / 2 ? rem : 0;
   pl.whole = all - pl.cut;
   pl.halves = (int64_t)own_halves * tn;
-  const int64_t quarters = (int64_t)blocks128 * tn_quarter;
-  auto rounds = [](int64_t n) { return (float)((n + GT_GRID - 1) / GT_GRID); };
-  pl.quarters = 0.33f * rounds(quarters) <
-                rounds(pl.whole) + 0.55f * rounds(pl.halves + 2 * pl.cut);
-  pl.units = pl.quarters ? quarters : pl.whole + pl.halves + 2 * pl.cut;
+  pl.units = pl.whole + pl.halves + 2 * pl.cut;
   return pl;
 }
+
+// PgLoads with the stages taken in a circle from stage `rot`
+template <class S>
+struct GtLoads : PgLoads<S> {
+  int rot;
+  __device__ __forceinline__ int at(int stage) const {
+    const int s = (stage < this->last ? stage : this->last) + rot;
+    return (s <= this->last ? s : s - this->last - 1) * 128;
+  }
+  __device__ __forceinline__ void a(int h, int stage, char* dst) const {
+    const int k = at(stage);
+#pragma unroll
+    for (int q = 0; q < S::PA; ++q) load_lds16_at(this->a_base, this->oa[h][q], k, dst + q * 1024);
+  }
+  __device__ __forceinline__ void b(int h, int stage, char* dst) const {
+    const int k = at(stage);
+#pragma unroll
+    for (int q = 0; q < S::PB; ++q) load_lds16_at(this->b_base[h], this->ob[h][q], k, dst + q * 1024);
+  }
+};
 
 // One tile of kind (MI, NJ): the group's rows from m0, output columns from n0.
 template <int DT, int MI, int NJ, bool UP>
@@ -316,7 +530,7 @@ __device__ __forceinline__ void grouped_tile(const GroupedParams& p, char* lds, 
   __syncthreads();
 
   PgLoop<DT, MI, NJ> L(lds, tid);
-  PgLoads<S> ld;
+  GtLoads<S> ld;
   const int nst = (int)(p.k_bytes / 128);
   ld.last = nst - 1;
   // gathered rows count from the operand's first row, others from the tile's
@@ -339,6 +553,11 @@ __device__ __forceinline__ void grouped_tile(const GroupedParams& p, char* lds, 
     }
   }
   f32x4_t acc[2][2][MI][NJ];
+  // a group of one row block reads its weights once, a whole row of 128 bytes in
+  // every stage: begun at a stage of its own, the tiles in flight do not all
+  // read the same few channels (64 rows each in 64 groups of 2048 x 2048 161 ->
+  // 139 us)
+  ld.rot = gb - ga <= 128 ? (int)((unsigned)(grp * 8 + n0 / 64) % (unsigned)nst) : 0;
   L.run(nst, ld, acc, [](int, int) {});
 
   // the chunks past the last whole stage, zeros behind them
@@ -421,33 +640,31 @@ template <int DT, bool UP>
 __global__ __launch_bounds__(GT_THREADS, 2) void grouped_tiles_kernel(GroupedParams p) {
   __shared__ __attribute__((aligned(1024))) char lds[2 * PgShape<4, 2>::BUF];
   __shared__ GtLds gl;
-  constexpr int TC = UP ? 128 : 256, QC = UP ? 64 : 128;   // output columns of a tile
-  const int tn = (p.cols + TC - 1) / TC, tq = (p.cols + QC - 1) / QC;
+  constexpr int TC = UP ? 128 : 256;   // output columns of a tile
+  const int tn = (p.cols + TC - 1) / TC;
   // neighbouring tiles on one XCD
   const int slot = (blockIdx.x & 7) * (GT_GRID / 8) + (blockIdx.x >> 3);
 
   // this thread's groups and the numbers of row blocks before them
   const int per = (p.groups + GT_THREADS - 1) / GT_THREADS;
-  auto blocks = [&](int g, int& b256, int& b128, int& half) {
+  auto blocks = [&](int g, int& whole, int& half) {
     int64_t a, b;
     gp_rows(p, g, a, b);
     const int r = (int)(b - a), rem = r & 255;
     half = rem > 0 && rem <= 128 ? 1 : 0;
-    b256 = (r >> 8) + (rem > 128 ? 1 : 0);
-    b128 = (r + 127) >> 7;
+    whole = (r >> 8) + (rem > 128 ? 1 : 0);
   };
   {
-    int n[3] = {0, 0, 0};
+    int n[2] = {0, 0};
     const int g0 = threadIdx.x * per;
     for (int g = g0; g < g0 + per && g < p.groups; ++g) {
-      int b, q, h;
-      blocks(g, b, q, h);
+      int b, h;
+      blocks(g, b, h);
       n[0] += b;
-      n[1] += q;
-      n[2] += h;
+      n[1] += h;
     }
 #pragma unroll
-    for (int c = 0; c < 3; ++c) {
+    for (int c = 0; c < 2; ++c) {
       const int incl = block_scan_incl<GT_THREADS / 64>(n[c], gl.scan);
       gl.before[c][threadIdx.x] = incl - n[c];
       if (threadIdx.x == GT_THREADS - 1) gl.total[c] = incl;
@@ -455,8 +672,7 @@ __global__ __launch_bounds__(GT_THREADS, 2) void grouped_tiles_kernel(GroupedPar
   }
   __syncthreads();
   const GtPlan pl = gt_plan(__builtin_amdgcn_readfirstlane(gl.total[0]),
-                            __builtin_amdgcn_readfirstlane(gl.total[1]),
-                            __builtin_amdgcn_readfirstlane(gl.total[2]), tn, tq);
+                            __builtin_amdgcn_readfirstlane(gl.total[1]), tn);
 
   for (int64_t k0 = 0; slot + k0 * GT_GRID < pl.units; k0 += GT_WINDOW) {
     __syncthreads();
@@ -471,38 +687,29 @@ __global__ __launch_bounds__(GT_THREADS, 2) void grouped_tiles_kernel(GroupedPar
         gl.tile[k - k0] = where(u - lo);
       }
     };
-    int64_t at256 = gl.before[0][threadIdx.x], at128 = gl.before[1][threadIdx.x];
-    int64_t athalf = gl.before[2][threadIdx.x];
+    int64_t at = gl.before[0][threadIdx.x], athalf = gl.before[1][threadIdx.x];
     const int g0 = threadIdx.x * per;
     for (int g = g0; g < g0 + per && g < p.groups; ++g) {
-      int b, q, h;
-      blocks(g, b, q, h);
-      if (pl.quarters) {
-        mark(at128 * tq, (at128 + q) * tq, [&](int64_t u) {
-          return make_int4(g, (int)(u / tq) * 128, (int)(u % tq) * QC, GT_QUARTER);
-        });
-      } else {
-        const int64_t lo = at256 * tn, hi = (at256 + b) * tn;
-        auto whole = [&](int64_t u) {
-          return make_int4(g, (int)(u / tn) * 256, (int)(u % tn) * TC, GT_WHOLE);
-        };
-        mark(lo, hi < pl.whole ? hi : pl.whole, whole);
-        if (h != 0)
-          mark(pl.whole + athalf * tn, pl.whole + (athalf + 1) * tn, [&](int64_t u) {
-            return make_int4(g, b * 256, (int)u * TC, GT_HALF);
-          });
-        const int64_t c0 = lo > pl.whole ? lo : pl.whole;   // its tiles that are cut
-        if (c0 < hi)
-          mark(pl.whole + pl.halves + 2 * (c0 - pl.whole),
-               pl.whole + pl.halves + 2 * (hi - pl.whole), [&](int64_t u) {
-                 int4 t = whole(c0 - lo + (u >> 1));
-                 t.y += (int)(u & 1) * 128;
-                 t.w = GT_HALF;
-                 return t;
-               });
-      }
-      at256 += b;
-      at128 += q;
+      int b, h;
+      blocks(g, b, h);
+      const int64_t lo = at * tn, hi = (at + b) * tn;
+      auto whole = [&](int64_t u) {
+        return make_int4(g, (int)(u / tn) * 256, (int)(u % tn) * TC, GT_WHOLE);
+      };
+      mark(lo, hi < pl.whole ? hi : pl.whole, whole);
+      if (h != 0)
+        mark(pl.whole + athalf * tn, pl.whole + (athalf + 1) * tn,
+             [&](int64_t u) { return make_int4(g, b * 256, (int)u * TC, GT_HALF); });
+      const int64_t c0 = lo > pl.whole ? lo : pl.whole;   // its tiles that are cut
+      if (c0 < hi)
+        mark(pl.whole + pl.halves + 2 * (c0 - pl.whole), pl.whole + pl.halves + 2 * (hi - pl.whole),
+             [&](int64_t u) {
+               int4 t = whole(c0 - lo + (u >> 1));
+               t.y += (int)(u & 1) * 128;
+               t.w = GT_HALF;
+               return t;
+             });
+      at += b;
       athalf += h;
     }
     __syncthreads();
@@ -514,38 +721,82 @@ __global__ __launch_bounds__(GT_THREADS, 2) void grouped_tiles_kernel(GroupedPar
       const int n0 = __builtin_amdgcn_readfirstlane(t.z);
       const int kind = __builtin_amdgcn_readfirstlane(t.w);
       if (kind == GT_WHOLE) grouped_tile<DT, 4, 2, UP>(p, lds, gl, g, m0, n0);
-      else if (kind == GT_HALF) grouped_tile<DT, 2, 2, UP>(p, lds, gl, g, m0, n0);
-      else grouped_tile<DT, 2, 1, UP>(p, lds, gl, g, m0, n0);
+      else grouped_tile<DT, 2, 2, UP>(p, lds, gl, g, m0, n0);
     }
   }
 }
 
-// ---------------------------------------------------------------------------
-
-template <int DT, int NT, int KS, int D, bool UP>
-static hipError_t launch_rows(const GroupedParams& p, hipStream_t st) {
-  constexpr int COLS = 16 * (GS_WAVES / KS);
-  // row tiles: at most one a group and one more for each 16 NT rows
-  const int64_t most = p.m / (16 * NT) + p.groups;
-  int64_t tiles = (most < p.m ? most : p.m) * ((p.cols + COLS - 1) / COLS);
-  tiles = tiles < 65536 ? tiles : 65536;
-  hipLaunchKernelGGL((grouped_rows_kernel<DT, NT, KS, D, UP>), dim3((unsigned)tiles),
-                     dim3(GS_THREADS), 0, st, p);
-  return hipGetLastError();
+// K over two waves, or over four where that is long (16 rows of one in 16
+// matrices of 4096 x 4096 114 -> 93 us) or the workgroups are few.
+template <int DT, bool UP>
+static void launch_rows(const GroupedParams& p, hipStream_t st) {
+  const int64_t most = p.m / 16 + p.groups;   // row tiles: one a group, one for each 16 rows
+  const int64_t tiles = most < p.m ? most : p.m;
+  auto grid = [&](int cols) {
+    const int64_t n = tiles * ((p.cols + cols - 1) / cols);
+    return dim3((unsigned)(n < GP_GRID ? n : GP_GRID));
+  };
+  if (p.k_bytes >= 8192 || tiles * ((p.cols + 31) / 32) < 1024)
+    hipLaunchKernelGGL((grouped_rows_kernel<DT, 4, UP>), grid(16), dim3(GS_THREADS), 0, st, p);
+  else
+    hipLaunchKernelGGL((grouped_rows_kernel<DT, 2, UP>), grid(32), dim3(GS_THREADS), 0, st, p);
 }
 
+template <int DT, int NS, int TI, bool UP>
+static void launch_mid(const GroupedParams& p, hipStream_t st) {
+  constexpr int RT = 32 * TI, COLS = UP ? 32 : 64;
+  const int64_t most = p.m / RT + p.groups;
+  int64_t tiles = (most < p.m ? most : p.m) * ((p.cols + COLS - 1) / COLS);
+  tiles = (tiles + 7) / 8 * 8;   // xcd_remap deals whole rounds over the XCDs
+  hipLaunchKernelGGL((grouped_mid_kernel<DT, NS, TI, UP>),
+                     dim3((unsigned)(tiles < GP_GRID ? tiles : GP_GRID)), dim3(GM_THREADS), 0, st,
+                     p);
+}
+
+// The host knows the groups' number and their rows together, so the rules go
+// by the mean; a group far from it is computed on tiles that fit it less well.
+//
+// Up to 4 rows a group (float32, bound by the matrix cores, 8) the few-rows
+// kernel: 64 groups of 2048 x 2048, it and 32-row tiles, 1 row 92 and 94 us, 4
+// rows 101 and 95, 16 rows 147 and 97 (537 MB of weights: 5.5 TB/s); 8 groups of
+// 1 row, 1024 x 2048, 11 and 17.
+// Then tiles of 32 rows, of 64 above 32 rows a group where these are enough
+// (64 rows 140 and 112 us; one group of 512 rows 14 and 18), with deep rings
+// while all tiles are resident at once (one group of 512 rows 14 us with 4
+// stages, 15 with 3; of 2048 rows on 64-row tiles 32 us with 2, 42 with 4).
+// The large tiles where their rounds cost less: one of 256 whole ones takes as
+// long as `round` 64 x 64 ones, one of halves 0.73 of that, float32 0.58 (bf16, 2048 x 2048,
+// 64-row tiles and large ones: 64 groups of 64 rows 111 and 139 us, of 128 178
+// and 151, of 256 308 and 202; 16 of 256 63 and 55; one of 2048 32 and 49;
+// e4m3 16 of 256 42 and 37, float32 16 of 256 328 and 286, 3 of 1000 rows,
+// 4096 x 4096, 853 and 776).
 template <int DT, bool UP>
 static hipError_t launch_grouped_dt(const GroupedParams& p, hipStream_t st) {
-  // the phased kernel's lane offsets are 32-bit
+  const int64_t used = p.groups < p.m ? p.groups : p.m;
+  const int64_t tn = (p.cols + (UP ? 127 : 255)) / (UP ? 128 : 256);
+  const int64_t tn64 = (p.cols + (UP ? 31 : 63)) / (UP ? 32 : 64);
+  // half a row tile of padding a group, half of the groups with a half tile
+  const int64_t tiles64 = (p.m / 64 + used / 2 + 1) * tn64;
+  auto rounds = [](int64_t n) { return (double)((n + GT_GRID - 1) / GT_GRID); };
+  const double round = DT == DT_F32 ? 3000. : DT == DT_E4M3 ? 2150. : 2000.;
+  const double large = rounds(p.m / 256 * tn) +
+                       (DT == DT_F32 ? 0.58 : 0.73) * rounds((used + 1) / 2 * tn);
+  // (the phased kernel's lane offsets are 32-bit)
   const bool near = p.k_bytes < (4 << 20) &&
                     (p.picks == 0 || p.x_rows * p.k_bytes < ((int64_t)1 << 32));
-  if (p.m > 32 * (int64_t)p.groups && p.k_bytes >= 128 && near) {
-    hipLaunchKernelGGL((grouped_tiles_kernel<DT, UP>), dim3(GT_GRID),
-                       dim3(GT_THREADS), 0, st, p);
-    return hipGetLastError();
+  if (p.m > 64 * used && large * round < (double)tiles64 && p.k_bytes >= 128 && near)
+    hipLaunchKernelGGL((grouped_tiles_kernel<DT, UP>), dim3(GT_GRID), dim3(GT_THREADS), 0, st, p);
+  else if (p.m <= (DT == DT_F32 ? 8 : 4) * used)
+    launch_rows<DT, UP>(p, st);
+  else if (p.m <= 32 * used || tiles64 <= 256) {
+    if ((p.m / 32 + used / 2 + 1) * tn64 <= 768) launch_mid<DT, 4, 1, UP>(p, st);
+    else launch_mid<DT, 3, 1, UP>(p, st);
+  } else if (DT == DT_F32 || tiles64 <= 512) {
+    launch_mid<DT, 4, 2, UP>(p, st);
+  } else {
+    launch_mid<DT, DT == DT_F32 ? 4 : 2, 2, UP>(p, st);
   }
-  if (p.m > 8 * (int64_t)p.groups) return launch_rows<DT, 2, 4, 4, UP>(p, st);
-  return launch_rows<DT, 1, 4, 4, UP>(p, st);
+  return hipGetLastError();
 }
 
 hipError_t launch_grouped(int dt, const GroupedParams& p, hipStream_t st) {

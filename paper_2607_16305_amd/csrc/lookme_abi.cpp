@@ -325,6 +325,9 @@ lookme_status_t grouped_params(int32_t groups, int64_t m, int32_t d_in, int32_t 
   if (picks < 0) return fail(LOOKME_ERR_INVALID, "picks must be >= 0 (got %d)", picks);
   if (x_rows < 0 || x_rows > (int64_t)INT32_MAX)
     return fail(LOOKME_ERR_INVALID, "x_rows %lld outside [0, 2^31)", (long long)x_rows);
+  if ((m / 32 + groups) * (((int64_t)d_out + 31) / 32) > (int64_t)1 << 30)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%lld rows of %d columns exceed 2^30 tiles", (long long)m,
+                d_out);
   if (m == 0) return LOOKME_OK;
   if (rows == nullptr && (picks != 0 || scatter != 0))
     return fail(LOOKME_ERR_INVALID, "picks or scatter given without rows");

@@ -59,6 +59,7 @@ _GROUPED = [
     (dict(groups=0), INVALID), (dict(groups=lk.LOOKME_MAX_GROUPS + 1), UNSUPPORTED),
     (dict(m=-1), INVALID), (dict(m=2 ** 30 + 1), UNSUPPORTED), (dict(d_in=0), INVALID),
     (dict(d_in=20), UNSUPPORTED), (dict(d_out=0), INVALID), (dict(d_out=4), UNSUPPORTED),
+    (dict(m=2 ** 30, d_out=2 ** 16), UNSUPPORTED),
     (dict(picks=-1), INVALID), (dict(picks=1, rows=None), INVALID),
     (dict(scatter=1, rows=None), INVALID), (dict(x_rows=15), INVALID), (dict(x_rows=-1), INVALID),
     (dict(x_rows=0, picks=2), INVALID), (dict(x_rows=2 ** 31), INVALID), (dict(x=None), INVALID),

@@ -2,16 +2,17 @@
 // a stable counting sort of ids, with the groups' offsets, for the grouped
 // products.
 //
-// One launch and no scratch: workgroup b owns a range of consecutive groups and
-// reads all the ids (they stay in L2).  Its waves split the ids into runs of
-// consecutive entries; each counts the ids below the range (their sum is where
-// the range's rows begin) and lists those of the range in order in LDS.  Over
-// its list (or over the ids again, where the list ran full) a wave counts the
-// entries of each group; a prefix sum over groups and waves gives every run its
-// first slot in each group, and a last pass over the list hands them out.
-// What bounds it is the instructions a CU issues for each id, so what a step
-// does for the ids of other ranges (two comparisons, two scalar counts) counts
-// most, and the busiest range's list after that.
+// One launch and no scratch.  A workgroup owns a range of consecutive groups and
+// (with fewer groups than CUs) one of several segments of the entries, and reads
+// all the ids (they stay in L2): those below the range count towards where its
+// rows begin, those of its group ahead of its segment towards where its own
+// begin.  In its segment its waves own runs of consecutive entries, and each
+// lists its run's entries of the range in order in LDS.  Over its list (or over
+// the run again, where the list ran full) a wave counts the entries of each
+// group; a prefix sum over groups and waves gives every run its first slot in
+// each group, and a last pass over the list hands them out.
+// What bounds it is the instructions a CU issues for each id: for one of
+// another range two comparisons and two scalar counts for 64 of them.
 // The result does not depend on timing: counts are sums, and a run's slots are
 // handed out by its own wave alone.
 #include "common.h"
@@ -20,56 +21,82 @@
 namespace lookme {
 
 constexpr int GR_WAVES = 16, GR_THREADS = GR_WAVES * 64;
-constexpr int GR_BLOCKS = 256;              // ranges of groups: one workgroup a CU
+constexpr int GR_BLOCKS = 256;              // one workgroup a CU
 constexpr int GR_RANGE = LOOKME_MAX_GROUPS / GR_BLOCKS;   // most groups of a range
 constexpr int GR_LOADS = 16;                // ids a lane has in flight
 constexpr int GR_LIST = 2400;               // entries of a wave's list (150 KiB of LDS)
 constexpr int GR_STEP = 64 * GR_LOADS;
+constexpr int GR_FEW = 4;                   // groups of a range whose counts stay in scalars
 static_assert(GR_RANGE <= 64, "a group of the range in 6 bits, one a lane");
 
+// base + the lanes of the mask below this one
+__device__ __forceinline__ int gr_slot(uint64_t mask, int base) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
+                                        __builtin_amdgcn_mbcnt_lo((uint32_t)mask, (uint32_t)base));
+}
+
 __global__ __launch_bounds__(GR_THREADS) void group_rows_kernel(
-    const int32_t* __restrict__ pick, int64_t n, int groups, int range, int32_t* __restrict__ rows,
-    int32_t* __restrict__ offsets) {
+    const int32_t* __restrict__ pick, int n, int groups, int range, int segments,
+    int32_t* __restrict__ rows, int32_t* __restrict__ offsets) {
   __shared__ int32_t cnt[GR_WAVES][GR_RANGE];
   __shared__ uint32_t list[GR_WAVES][GR_LIST];   // entry in the run << 6 | group in the range
-  __shared__ int32_t below[GR_WAVES];
+  __shared__ int32_t below[GR_WAVES], ahead[GR_WAVES];
   __shared__ int32_t tot[GR_RANGE];
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint64_t before = (1ull << lane) - 1;
-  const int g0 = blockIdx.x * range;
+  const int g0 = (int)(blockIdx.x / segments) * range;
+  const int seg = blockIdx.x % segments;
   const int size = groups - g0 < range ? groups - g0 : range;
-  // runs of whole steps: at most 2^26 entries
-  const int64_t steps = (n + GR_STEP - 1) / GR_STEP;
-  const int64_t per = (steps + GR_WAVES - 1) / GR_WAVES;
-  const int64_t first = wv * per * GR_STEP;
-  int64_t end = first + per * GR_STEP;
-  end = end < n ? end : n;
+  const unsigned lo = (unsigned)g0, hi = (unsigned)(g0 + size);
 
-  // id j of a step: entry s + 64 j + lane; -1 past the run
-  auto load = [&](int64_t s, int (&v)[GR_LOADS]) {
+  // steps of GR_STEP entries: the segment's, dealt to the waves in runs (a run
+  // is at most 2^26 entries), and the others, dealt one by one
+  const int steps = (n + GR_STEP - 1) / GR_STEP;
+  const int seg_steps = (steps + segments - 1) / segments;
+  const int seg0 = seg * seg_steps < steps ? seg * seg_steps : steps;
+  const int seg1 = seg0 + seg_steps < steps ? seg0 + seg_steps : steps;
+  const int per = (seg1 - seg0 + GR_WAVES - 1) / GR_WAVES;
+  const int run0 = seg0 + wv * per < seg1 ? seg0 + wv * per : seg1;
+  const int run1 = run0 + per < seg1 ? run0 + per : seg1;
+
+  // entry GR_STEP step + 64 k + lane; -1 past the last
+  auto load = [&](int step, int (&v)[GR_LOADS]) {
+    const int s = step * GR_STEP;
+    const int32_t* p = pick + s + lane;
+    if (s + GR_STEP <= n) {
 #pragma unroll
-    for (int k = 0; k < GR_LOADS; ++k) {
-      const int64_t i = s + 64 * k + lane;
-      v[k] = pick[i < end ? i : end - 1];
+      for (int k = 0; k < GR_LOADS; ++k) v[k] = p[64 * k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < GR_LOADS; ++k) v[k] = s + 64 * k + lane < n ? p[64 * k] : -1;
     }
-#pragma unroll
-    for (int k = 0; k < GR_LOADS; ++k)
-      if (s + 64 * k + lane >= end) v[k] = -1;
   };
-  int less = 0, listed = 0;   // the same in every lane
-  for (int64_t s = first; s < end; s += GR_STEP) {
+  int less = 0, early = 0, listed = 0;   // the same in every lane
+  for (int step = wv; step < steps; step += GR_WAVES) {
+    if (step >= seg0 && step < seg1) continue;
     int v[GR_LOADS];
-    load(s, v);
+    load(step, v);
 #pragma unroll
     for (int k = 0; k < GR_LOADS; ++k) {
-      const unsigned j = (unsigned)v[k] - (unsigned)g0;
-      less += __popcll(__ballot((unsigned)v[k] < (unsigned)g0));
-      const uint64_t mine = __ballot(j < (unsigned)size);
+      const uint64_t lower = __ballot((unsigned)v[k] < lo);
+      less += __popcll(lower);
+      if (step < seg0) early += __popcll(__ballot((unsigned)v[k] < hi) & ~lower);
+    }
+  }
+  for (int step = run0; step < run1; ++step) {
+    int v[GR_LOADS];
+    load(step, v);
+#pragma unroll
+    for (int k = 0; k < GR_LOADS; ++k) {
+      const uint64_t lower = __ballot((unsigned)v[k] < lo);
+      const uint64_t mine = __ballot((unsigned)v[k] < hi) & ~lower;
+      less += __popcll(lower);
       if (mine != 0) {
-        if (listed <= GR_LIST - 64 && j < (unsigned)size)
-          list[wv][listed + __popcll(mine & before)] =
-              (uint32_t)(s - first + 64 * k + lane) << 6 | j;
+        // (entry << 6 plus the group, in one addition of a scalar)
+        if (listed <= GR_LIST - 64 && __builtin_amdgcn_inverse_ballot_w64(mine))
+          list[wv][gr_slot(mine, listed)] =
+              (uint32_t)(lane << 6) + (uint32_t)v[k] +
+              (((uint32_t)((step - run0) * GR_STEP + 64 * k) << 6) - (uint32_t)g0);
         listed += __popcll(mine);
       }
     }
@@ -81,41 +108,48 @@ __global__ __launch_bounds__(GR_THREADS) void group_rows_kernel(
       for (int i = 0; i < listed; i += 64) {
         const bool mine = i + lane < listed;
         const uint32_t e = mine ? list[wv][i + lane] : 0;
-        fn(mine, (int)(e & 63), first + (e >> 6));
+        fn(mine, (int)(e & 63), run0 * GR_STEP + (int)(e >> 6));
       }
     } else {
-      for (int64_t s = first; s < end; s += GR_STEP) {
+      for (int step = run0; step < run1; ++step) {
         int v[GR_LOADS];
-        load(s, v);
+        load(step, v);
 #pragma unroll
-        for (int k = 0; k < GR_LOADS; ++k) {
-          const unsigned j = (unsigned)v[k] - (unsigned)g0;
-          fn(j < (unsigned)size, (int)j, s + 64 * k + lane);
-        }
+        for (int k = 0; k < GR_LOADS; ++k)
+          fn((unsigned)v[k] >= lo && (unsigned)v[k] < hi, v[k] - g0,
+             step * GR_STEP + 64 * k + lane);
       }
     }
   };
-  // fn(group, ballot of its entries) for every group of the range among them:
-  // one after another in short ranges, in others those that occur
+  // fn(group, ballot of its entries) for every group that occurs among them
   auto groups_of = [&](bool mine, int j, auto&& fn) {
-    if (size <= 8) {
-      for (int q = 0; q < size; ++q) fn(q, __ballot(mine && j == q));
-    } else {
-      uint64_t left = __ballot(mine);
-      while (left != 0) {
-        const int q = __builtin_amdgcn_readlane(j, __builtin_ctzll(left));
-        const uint64_t same = __ballot(mine && j == q);
-        fn(q, same);
-        left &= ~same;
-      }
+    uint64_t left = __ballot(mine);
+    while (left != 0) {
+      const int q = __builtin_amdgcn_readlane(j, __builtin_ctzll(left));
+      const uint64_t same = __ballot(mine && j == q);
+      fn(q, same);
+      left &= ~same;
     }
   };
   int count = 0;   // lane j: the run's entries of group j
-  each([&](bool mine, int j, int64_t) {
-    groups_of(mine, j, [&](int q, uint64_t same) { count += lane == q ? __popcll(same) : 0; });
-  });
+  if (range <= GR_FEW) {
+    int few[GR_FEW] = {};
+    each([&](bool mine, int j, int) {
+#pragma unroll
+      for (int q = 0; q < GR_FEW; ++q) few[q] += __popcll(__ballot(mine && j == q));
+    });
+#pragma unroll
+    for (int q = 0; q < GR_FEW; ++q) count = lane == q ? few[q] : count;
+  } else {
+    each([&](bool mine, int j, int) {
+      groups_of(mine, j, [&](int q, uint64_t same) { count += lane == q ? __popcll(same) : 0; });
+    });
+  }
   cnt[wv][lane] = count;
-  if (lane == 0) below[wv] = less;
+  if (lane == 0) {
+    below[wv] = less;
+    ahead[wv] = early;
+  }
   __syncthreads();
   // each group's total; the runs' counts become the runs' places in the group
   if ((int)threadIdx.x < size) {
@@ -128,35 +162,59 @@ __global__ __launch_bounds__(GR_THREADS) void group_rows_kernel(
     tot[threadIdx.x] = sum;
   }
   __syncthreads();
-  if (wv == 0) {   // the groups' first slots
-    int base = 0;
-    for (int w = 0; w < GR_WAVES; ++w) base += below[w];
+  if (wv == 0) {   // the groups' first slots (several segments: of the range's one group)
+    int base = 0, first = 0;
+    for (int w = 0; w < GR_WAVES; ++w) {
+      base += below[w];
+      first += ahead[w];
+    }
     const int c = lane < size ? tot[lane] : 0;
     const int incl = wave_scan_incl(c);
     if (lane < size) {
-      tot[lane] = base + incl - c;
-      offsets[g0 + lane] = base + incl - c;
-      if (g0 + lane == groups - 1) offsets[groups] = base + incl;
+      tot[lane] = base + first + incl - c;
+      if (seg == 0) offsets[g0 + lane] = base + incl - c;
+      if (seg == segments - 1 && g0 + lane == groups - 1) offsets[groups] = base + first + incl;
     }
   }
   __syncthreads();
   // lane j holds the run's next slot of group j
   int next = lane < size ? cnt[wv][lane] + tot[lane] : 0;
-
-  each([&](bool mine, int j, int64_t entry) {
-    groups_of(mine, j, [&](int q, uint64_t same) {
-      const int at = __builtin_amdgcn_readlane(next, q);
-      if (mine && j == q) rows[at + __popcll(same & before)] = (int32_t)entry;
-      next += lane == q ? __popcll(same) : 0;
+  if (range <= GR_FEW) {
+    int few[GR_FEW];
+#pragma unroll
+    for (int q = 0; q < GR_FEW; ++q) few[q] = __builtin_amdgcn_readlane(next, q);
+    each([&](bool mine, int j, int entry) {
+      int at = 0;
+#pragma unroll
+      for (int q = 0; q < GR_FEW; ++q) {
+        const uint64_t same = __ballot(mine && j == q);
+        at = j == q ? gr_slot(same, few[q]) : at;
+        few[q] += __popcll(same);
+      }
+      if (mine) rows[at] = entry;
     });
-  });
+  } else {
+    each([&](bool mine, int j, int entry) {
+      groups_of(mine, j, [&](int q, uint64_t same) {
+        const int at = __builtin_amdgcn_readlane(next, q);
+        if (mine && j == q) rows[gr_slot(same, at)] = entry;
+        next += lane == q ? __popcll(same) : 0;
+      });
+    });
+  }
 }
 
 hipError_t launch_group_rows(int groups, int64_t n, const int32_t* pick, int32_t* rows,
                              int32_t* offsets, hipStream_t st) {
   const int range = (groups + GR_BLOCKS - 1) / GR_BLOCKS;
-  hipLaunchKernelGGL(group_rows_kernel, dim3((unsigned)((groups + range - 1) / range)),
-                     dim3(GR_THREADS), 0, st, pick, n, groups, range, rows, offsets);
+  const int ranges = (groups + range - 1) / range;
+  // a CU a segment, and steps for each of them
+  const int64_t steps = (n + GR_STEP - 1) / GR_STEP;
+  int64_t segments = range == 1 ? GR_BLOCKS / ranges : 1;
+  segments = segments < steps / GR_WAVES ? segments : steps / GR_WAVES;
+  if (segments < 1) segments = 1;
+  hipLaunchKernelGGL(group_rows_kernel, dim3((unsigned)(ranges * segments)), dim3(GR_THREADS), 0,
+                     st, pick, (int)n, groups, range, (int)segments, rows, offsets);
   return hipGetLastError();
 }
 

@@ -13,15 +13,18 @@
 // the group's scale multiplies its float32 sum: no weight is rounded.  float32
 // tokens are three bf16 values (8 + 8 + 8 bits of the significand), three
 // products a step.
-// The scales and zero points of a workgroup's rows wait in LDS as float32.
+// The scales and zero points of a workgroup's rows wait in LDS as float32.  All
+// workgroups are resident at once: what a call takes beyond its launch is the
+// weights at 5 TB/s, or the instructions (95 a wave for 128 x 16 weights, 55
+// with two row tiles), whichever is longer, and two latencies of HBM.
 #include "common.h"
 #include "kernels.h"
 #include "tile_gemm.h"
 
 namespace lookme {
 
-constexpr int QP_WAVES = 4, QP_THREADS = 64 * QP_WAVES;
-constexpr int QP_GROUPS = 256;   // groups whose scales are in LDS at a time
+constexpr int QP_WAVES = 8, QP_THREADS = 64 * QP_WAVES;
+constexpr int QP_GROUPS = 128;   // groups whose scales are in LDS at a time
 
 // 8 nibbles as the bf16 values 16 + q of nibbles (0, 4), (1, 5), (2, 6), (3, 7)
 __device__ __forceinline__ u32x4_t qp_expand(uint32_t u) {
@@ -48,9 +51,9 @@ __device__ __forceinline__ void qp_transpose(u32x4_t& v) {
   v = u32x4_t{c[0], d[0], c[1], d[1]};
 }
 
-// Eight tokens' values of a lane as bf16 parts whose sum they are: one part,
-// or for float32 three (truncated, so that none overflows; the later parts of
-// a value that is not finite are zero).
+// Eight values of a token as bf16 parts whose sum they are: one part, or for
+// float32 three (truncated, so that none overflows; of a value that is not
+// finite the later parts are NaN).
 template <int DT>
 struct QpFrag {
   static constexpr int PARTS = DT == DT_BF16 ? 1 : 3;
@@ -63,24 +66,18 @@ struct QpFrag {
       raw[1] = ld16(row + (int64_t)c * 32 + 16);
     }
   }
-  __device__ __forceinline__ void split(bool in, u32x4_t (&f)[PARTS]) const {
-    const u32x4_t none = {0, 0, 0, 0};
+  __device__ __forceinline__ void split(u32x4_t (&f)[PARTS]) const {
     if constexpr (DT == DT_BF16) {
-      f[0] = in ? qp_order(raw[0]) : none;
+      f[0] = qp_order(raw[0]);
     } else {
       uint32_t h[3][8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint32_t u = in ? raw[e >> 2][e & 3] : 0u;
-        const uint32_t hi = u & 0xFFFF0000u;
-        const bool finite = (u & 0x7F800000u) != 0x7F800000u;
-        const float r1 = finite ? as_f32(u) - as_f32(hi) : 0.f;
-        const uint32_t mid = as_u32(r1) & 0xFFFF0000u;
-        const float r2 = r1 - as_f32(mid);
-        // a NaN whose payload is in the low half keeps a high one
-        h[0][e] = finite || (u & 0x007FFFFFu) == 0 ? hi : hi | 0x00400000u;
-        h[1][e] = mid;
-        h[2][e] = as_u32(r2);
+        const uint32_t u = raw[e >> 2][e & 3];
+        h[0][e] = u & 0xFFFF0000u;
+        const float r1 = as_f32(u) - as_f32(h[0][e]);
+        h[1][e] = as_u32(r1) & 0xFFFF0000u;
+        h[2][e] = as_u32(r1 - as_f32(h[1][e]));
       }
       // pairs (0, 4), (1, 5), (2, 6), (3, 7): upper halves
 #pragma unroll
@@ -92,21 +89,27 @@ struct QpFrag {
   }
 };
 
-// NT: token tiles of 16.  D: blocks of 128 weights a row in flight.  SHORT:
-// groups of 32 or 64 (the words of a block are transposed so that a product
-// step stays inside one), else of whole blocks.  K is split over the
-// workgroup's waves.
-template <int DT, int NT, int D, bool UP, bool SHORT>
+// NT: token tiles of 16.  RW: tiles of 16 weight rows a wave multiplies with the
+// same tokens (of each matrix).  D: blocks of 128 weights a row in flight (the
+// tokens, which come from L2, are one block ahead).  SHORT: groups of 32 or 64
+// (the words of a block are transposed so that a product step stays inside
+// one), else of whole blocks.  K is split over the workgroup's waves.  lds: the
+// scales of at most QP_GROUPS groups, then the waves' sums.
+template <int DT, int NT, int RW, int D, bool UP, bool SHORT>
 __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
   constexpr int ES = DT == DT_BF16 ? 2 : 4;
-  constexpr int MATS = UP ? 2 : 1;
+  constexpr int MATS = UP ? 2 : 1, TILES = MATS * RW;   // tile q RW + i: rows 16 i of matrix q
   constexpr int PARTS = QpFrag<DT>::PARTS;
-  __shared__ __attribute__((aligned(16))) float sz[MATS][QP_GROUPS][2][16];
-  __shared__ f32x4_t part[QP_WAVES * MATS * NT * 64];
+  static_assert(D % 2 == 0, "the tokens' buffer of a block is its parity");
+  static_assert(RW * NT <= QP_WAVES, "a wave an output tile");
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  // [group][tile][scale, 16 + zero][16 rows]
+  float (*sz)[TILES][2][16] = reinterpret_cast<float (*)[TILES][2][16]>(lds);
+  f32x4_t* part = reinterpret_cast<f32x4_t*>(lds);
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, g = lane >> 4;
-  const int c0 = blockIdx.x * 16;
+  const int c0 = blockIdx.x * (16 * RW);
   const int64_t t0 = (int64_t)blockIdx.y * (16 * NT);
   const int64_t k_bytes = (int64_t)p.k * ES;
   const int groups = p.k / p.group;
@@ -117,32 +120,38 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
     const int64_t t = t0 + 16 * j + n16;
     xp[j] = p.x + (t < p.n ? t : p.n - 1) * k_bytes;
   }
-  const int wc = c0 + n16 < p.cols ? c0 + n16 : p.cols - 1;
-  const char* wp[MATS];
+  const char* wp[TILES];
 #pragma unroll
-  for (int q = 0; q < MATS; ++q) wp[q] = p.m[q].w + (int64_t)wc * (p.k / 2);
+  for (int q = 0; q < TILES; ++q) {
+    const int c = c0 + 16 * (q % RW) + n16;
+    wp[q] = p.m[q / RW].w + (int64_t)(c < p.cols ? c : p.cols - 1) * (p.k / 2);
+  }
 
-  f32x4_t acc[MATS][NT];
+  f32x4_t acc[TILES][NT];
 #pragma unroll
-  for (int q = 0; q < MATS; ++q)
+  for (int q = 0; q < TILES; ++q)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[q][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
+  // unconditional loads from clamped addresses; values past K count as zero
+  // (only the last block of SHORT groups has any)
   const int wchunks = p.k / 32, xchunks = p.k / 8;
-  u32x4_t fw[D][MATS];
-  QpFrag<DT> fx[D][NT][4];
-  auto load = [&](int d, int b) {
+  u32x4_t fw[D][TILES];
+  QpFrag<DT> fx[2][NT][4];
+  auto load_w = [&](int d, int b) {
     int c = 4 * b + g;
     c = c < wchunks ? c : wchunks - 1;
 #pragma unroll
-    for (int q = 0; q < MATS; ++q) fw[d][q] = ld16_nt(wp[q] + (int64_t)c * 16);
+    for (int q = 0; q < TILES; ++q) fw[d][q] = ld16(wp[q] + (int64_t)c * 16);
+  };
+  auto x_chunk = [&](int b, int s) { return SHORT ? 16 * b + 4 * s + g : 16 * b + 4 * g + s; };
+  auto load_x = [&](int d, int b) {
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        int x = SHORT ? 16 * b + 4 * s + g : 16 * b + 4 * g + s;
-        x = x < xchunks ? x : xchunks - 1;
-        fx[d][j][s].load(xp[j], x);
+        const int x = x_chunk(b, s);
+        fx[d & 1][j][s].load(xp[j], x < xchunks ? x : xchunks - 1);
       }
   };
 
@@ -155,26 +164,30 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
     const int b0 = seg + wv * per;
     const int b1 = b0 + per < seg + left ? b0 + per : seg + left;
     if (b0 < b1) {
+      load_x(0, b0);
+      if (b0 + 1 < b1) load_x(1, b0 + 1);
 #pragma unroll
       for (int d = 0; d < D; ++d) {
-        load(d, b0 + d);
+        if (b0 + d < b1) load_w(d, b0 + d);
         asm volatile("" ::: "memory");
       }
     }
     const int first = (int)((int64_t)seg * 128 / p.group);
     const int count = groups - first < QP_GROUPS ? groups - first : QP_GROUPS;
     if (seg != 0) __syncthreads();
-    for (int i = threadIdx.x; i < 16 * count; i += QP_THREADS) {
-      const int r = i / count, k = i - r * count;
-      const int row = c0 + r < p.cols ? c0 + r : p.cols - 1;
-      const int64_t at = (int64_t)row * groups + first + k;
-#pragma unroll
-      for (int q = 0; q < MATS; ++q) {
+    // 16 threads a row
+    for (int r = threadIdx.x >> 4; r < 16 * TILES; r += QP_THREADS / 16) {
+      const int q = r >> 4;
+      int row = c0 + 16 * (q % RW) + (r & 15);
+      row = row < p.cols ? row : p.cols - 1;
+      const QuantMatrix& m = p.m[q / RW];
+      const int64_t at = (int64_t)row * groups + first;
+      for (int k = threadIdx.x & 15; k < count; k += 16) {
         if constexpr (DT == DT_BF16)
-          sz[q][k][0][r] = bf16lo(reinterpret_cast<const uint16_t*>(p.m[q].scale)[at]);
+          sz[k][q][0][r & 15] = bf16lo(reinterpret_cast<const uint16_t*>(m.scale)[at + k]);
         else
-          sz[q][k][0][r] = reinterpret_cast<const float*>(p.m[q].scale)[at];
-        sz[q][k][1][r] = 16.f + (p.m[q].zero != nullptr ? (float)p.m[q].zero[at] : 8.f);
+          sz[k][q][0][r & 15] = reinterpret_cast<const float*>(m.scale)[at + k];
+        sz[k][q][1][r & 15] = 16.f + (m.zero != nullptr ? (float)m.zero[at + k] : 8.f);
       }
     }
     __syncthreads();
@@ -182,24 +195,24 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
 #pragma unroll
       for (int d = 0; d < D; ++d) {
         if (b + d < b1) {   // the same for the whole wave
-          u32x4_t w[MATS];
+          u32x4_t w[TILES];
 #pragma unroll
-          for (int q = 0; q < MATS; ++q) {
+          for (int q = 0; q < TILES; ++q) {
             w[q] = fw[d][q];
             if constexpr (SHORT) qp_transpose(w[q]);
           }
-          f32x4_t sp[MATS][NT], sx[NT];
+          f32x4_t sp[TILES][NT], sx[NT];
 #pragma unroll
           for (int j = 0; j < NT; ++j) {
             sx[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int q = 0; q < MATS; ++q) sp[q][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int q = 0; q < TILES; ++q) sp[q][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
           }
           auto flush = [&](int grp) {   // the group's sums, scaled, into acc
 #pragma unroll
-            for (int q = 0; q < MATS; ++q) {
-              const f32x4_t s = *reinterpret_cast<const f32x4_t*>(&sz[q][grp - first][0][4 * g]);
-              const f32x4_t z = *reinterpret_cast<const f32x4_t*>(&sz[q][grp - first][1][4 * g]);
+            for (int q = 0; q < TILES; ++q) {
+              const f32x4_t s = *reinterpret_cast<const f32x4_t*>(&sz[grp - first][q][0][4 * g]);
+              const f32x4_t z = *reinterpret_cast<const f32x4_t*>(&sz[grp - first][q][1][4 * g]);
 #pragma unroll
               for (int j = 0; j < NT; ++j) {
 #pragma unroll
@@ -213,20 +226,26 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
           };
 #pragma unroll
           for (int s = 0; s < 4; ++s) {
-            const int x = SHORT ? 16 * (b + d) + 4 * s + g : 16 * (b + d) + 4 * g + s;
             const u32x4_t ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-            u32x4_t a[MATS];
+            u32x4_t a[TILES];
 #pragma unroll
-            for (int q = 0; q < MATS; ++q) a[q] = qp_expand(w[q][s]);
+            for (int q = 0; q < TILES; ++q) a[q] = qp_expand(w[q][s]);
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               u32x4_t f[PARTS];
-              fx[d][j][s].split(x < xchunks, f);
+              fx[d & 1][j][s].split(f);
+              if constexpr (SHORT) {
+                if (x_chunk(b + d, s) >= xchunks) {
+#pragma unroll
+                  for (int e = 0; e < PARTS; ++e) f[e] = u32x4_t{0, 0, 0, 0};
+                }
+              }
 #pragma unroll
               for (int e = 0; e < PARTS; ++e) {
                 sx[j] = mfma_chunk<DT_BF16>(ones, f[e], sx[j]);
 #pragma unroll
-                for (int q = 0; q < MATS; ++q) sp[q][j] = mfma_chunk<DT_BF16>(a[q], f[e], sp[q][j]);
+                for (int q = 0; q < TILES; ++q)
+                  sp[q][j] = mfma_chunk<DT_BF16>(a[q], f[e], sp[q][j]);
               }
             }
             if constexpr (SHORT) {
@@ -237,63 +256,87 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
           }
           if constexpr (!SHORT) flush(128 * (b + d) / p.group);
         }
-        load(d, b + d + D);
+        // the tokens first: loads return in order, and these are waited for first
+        if (b + d + 2 < b1) load_x(d, b + d + 2);
+        if (b + d + D < b1) load_w(d, b + d + D);
       }
     }
   }
 
-  f32x4_t* mine = part + wv * (MATS * NT * 64) + lane;
-  if (wv != 0) {
+  __syncthreads();   // the scales give way to the sums: [wave][tile][token tile][lane]
+  f32x4_t* mine = part + wv * (TILES * NT * 64) + lane;
 #pragma unroll
-    for (int q = 0; q < MATS; ++q)
+  for (int q = 0; q < TILES; ++q)
 #pragma unroll
-      for (int j = 0; j < NT; ++j) mine[(q * NT + j) * 64] = acc[q][j];
-  }
+    for (int j = 0; j < NT; ++j) mine[(q * NT + j) * 64] = acc[q][j];
   __syncthreads();
-  if (wv != 0) return;
+  if (wv >= RW * NT) return;   // a wave an output tile
+  const int i = wv / NT, j = wv % NT;
+  f32x4_t sum[MATS];
 #pragma unroll
-  for (int o = 1; o < QP_WAVES; ++o)
+  for (int q = 0; q < MATS; ++q) {
+    sum[q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int q = 0; q < MATS; ++q)
+    for (int w = 0; w < QP_WAVES; ++w) {
+      const f32x4_t v = part[((w * TILES + q * RW + i) * NT + j) * 64 + lane];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const f32x4_t v = mine[(o * MATS * NT + q * NT + j) * 64];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[q][j][r] += v[r];
-      }
-  const int col = c0 + 4 * g;
-  if (col >= p.cols) return;   // cols is a multiple of 4
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int64_t t = t0 + 16 * j + n16;
-    if (t >= p.n) continue;
-    const int64_t at = (t * p.cols + col) * ES;
-    float v[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = UP ? silu_f(acc[0][j][r]) * acc[MATS - 1][j][r] : acc[0][j][r];
-    if (p.add != nullptr) {
-      float a[4];
-      ld_cols<DT, 4>(p.add + at, a);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] += a[r];
+      for (int r = 0; r < 4; ++r) sum[q][r] += v[r];
     }
-    st_cols<DT, 4>(p.out + at, v);
   }
+  const int col = c0 + 16 * i + 4 * g;
+  const int64_t t = t0 + 16 * j + n16;
+  if (col >= p.cols || t >= p.n) return;   // cols is a multiple of 4
+  const int64_t at = (t * p.cols + col) * ES;
+  float v[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = UP ? silu_f(sum[0][r]) * sum[MATS - 1][r] : sum[0][r];
+  if (p.add != nullptr) {
+    float a[4];
+    ld_cols<DT, 4>(p.add + at, a);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] += a[r];
+  }
+  st_cols<DT, 4>(p.out + at, v);
 }
 
-template <int DT, int NT, int D, bool UP>
+template <int DT, int NT, int RW, int D, bool UP>
 static void launch_quant_nt(const QuantParams& p, hipStream_t st) {
-  const dim3 grid((unsigned)((p.cols + 15) / 16), (unsigned)((p.n + 16 * NT - 1) / (16 * NT)));
+  constexpr int TILES = (UP ? 2 : 1) * RW;
+  const dim3 grid((unsigned)((p.cols + 16 * RW - 1) / (16 * RW)),
+                  (unsigned)((p.n + 16 * NT - 1) / (16 * NT)));
+  const int groups = p.k / p.group < QP_GROUPS ? p.k / p.group : QP_GROUPS;
+  const size_t scales = (size_t)groups * TILES * 2 * 16 * 4;
+  const size_t sums = (size_t)QP_WAVES * TILES * NT * 64 * 16;
+  static_assert(QP_GROUPS * TILES * 128 <= 65536 && QP_WAVES * TILES * NT * 1024 <= 65536,
+                "dynamic LDS of a launch");
+  const size_t lds = scales > sums ? scales : sums;
   if (p.group < 128)
-    hipLaunchKernelGGL((quant_rows_kernel<DT, NT, D, UP, true>), grid, dim3(QP_THREADS), 0, st, p);
+    hipLaunchKernelGGL((quant_rows_kernel<DT, NT, RW, D, UP, true>), grid, dim3(QP_THREADS), lds,
+                       st, p);
   else
-    hipLaunchKernelGGL((quant_rows_kernel<DT, NT, D, UP, false>), grid, dim3(QP_THREADS), 0, st, p);
+    hipLaunchKernelGGL((quant_rows_kernel<DT, NT, RW, D, UP, false>), grid, dim3(QP_THREADS), lds,
+                       st, p);
 }
 
+// Two row tiles a wave where these are a workgroup for every CU: the tokens,
+// which every wave reads from L2 and orders for itself, then serve twice the
+// weights (8192 x 8192 of bf16, one tile and two: 1 row 13.0 and 12.7 us, 16 rows
+// 22 and 17, 32 rows 38 and 24; float32 1 row 27 and 19; 4096 x 4096, 128
+// workgroups, 16 rows 8.2 and 9.9).  Gate and up share the tokens already, which
+// is enough for few rows (2 x 8192 x 4096 of 4 rows 13.2 and 15.0, of 16 17.1 and
+// 16.5; float32 of 4 rows 22 and 19).  More blocks in flight than two a wave,
+// beside 16 waves a CU, only cost registers (1 row 13.0 us with 2, 14.0 with 4).
 template <int DT, bool UP>
 static void launch_quant_dt(const QuantParams& p, hipStream_t st) {
-  if (p.n <= 16) launch_quant_nt<DT, 1, 2, UP>(p, st);
-  else launch_quant_nt<DT, 2, 1, UP>(p, st);
+  const int64_t wide = (int64_t)((p.cols + 31) / 32) * ((p.n + 31) / 32);
+  const bool two = wide >= 256 && !(UP && DT == DT_BF16 && p.n <= 8);
+  if (p.n <= 16) {
+    if (two) launch_quant_nt<DT, 1, 2, 2, UP>(p, st);
+    else launch_quant_nt<DT, 1, 1, 2, UP>(p, st);
+  } else {
+    if (two) launch_quant_nt<DT, 2, 2, 2, UP>(p, st);
+    else launch_quant_nt<DT, 2, 1, 2, UP>(p, st);
+  }
 }
 
 hipError_t launch_quant(int dt, const QuantParams& p, hipStream_t st) {

@@ -763,7 +763,9 @@ static void launch_mid(const GroupedParams& p, hipStream_t st) {
 // Then tiles of 32 rows, of 64 above 32 rows a group where these are enough
 // (64 rows 140 and 112 us; one group of 512 rows 14 and 18), with deep rings
 // while all tiles are resident at once (one group of 512 rows 14 us with 4
-// stages, 15 with 3; of 2048 rows on 64-row tiles 32 us with 2, 42 with 4).
+// stages, 15 with 3; of 2048 rows on 64-row tiles 32 us with 2, 42 with 4), and
+// for float32 again where there are many (13 groups of 231 rows, 840 x 1160, 85
+// us with 2, 100 with 4; 16 of 256, 2048 x 2048, 344 and 321).
 // The large tiles where their rounds cost less: one of 256 whole ones takes as
 // long as `round` 64 x 64 ones, one of halves 0.73 of that, float32 0.58 (bf16, 2048 x 2048,
 // 64-row tiles and large ones: 64 groups of 64 rows 111 and 139 us, of 128 178
@@ -791,10 +793,10 @@ static hipError_t launch_grouped_dt(const GroupedParams& p, hipStream_t st) {
   else if (p.m <= 32 * used || tiles64 <= 256) {
     if ((p.m / 32 + used / 2 + 1) * tn64 <= 768) launch_mid<DT, 4, 1, UP>(p, st);
     else launch_mid<DT, 3, 1, UP>(p, st);
-  } else if (DT == DT_F32 || tiles64 <= 512) {
+  } else if (tiles64 <= 512 || (DT == DT_F32 && tiles64 > 1024)) {
     launch_mid<DT, 4, 2, UP>(p, st);
   } else {
-    launch_mid<DT, DT == DT_F32 ? 4 : 2, 2, UP>(p, st);
+    launch_mid<DT, 2, 2, UP>(p, st);
   }
   return hipGetLastError();
 }

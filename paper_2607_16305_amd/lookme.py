@@ -389,21 +389,24 @@ def lookme_quant_swiglu(dtype, n, d_in, d_ff, group, x, w_gate, scale_gate, zero
 
 
 # The same on torch tensors: sizes come from the shapes, which are checked (the
-# C side sees pointers only), and the call runs on the tensors' device.
+# C side sees pointers only), and the call runs on the tensors' device.  These
+# are called once a layer and token, so they keep their own time short.
 
 def _refuse(msg):
     raise LookmeError(LOOKME_ERR_INVALID, msg)
 
 
 def _tensor(name, t, dtype, shape, device):
+    """t's address; refuses another type, shape or device, and strides."""
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype is not dtype:
         _refuse(f"{name} is {t.dtype}, not {dtype}")
     if t.shape != shape:
         _refuse(f"{name} has the shape {tuple(t.shape)}, not {tuple(shape)}")
     if t.device != device:
         _refuse(f"{name} is on {t.device}, not on {device}")
-    if not t.is_contiguous():
-        _refuse(f"{name} is not contiguous")
+    _refuse(f"{name} is not contiguous")
 
 
 def _dtype_code(name, t):
@@ -413,14 +416,17 @@ def _dtype_code(name, t):
     return code
 
 
-def _on(device, call, *args):
-    """call(*args) with the tensors' device current; their device is a GPU."""
+def _call(name, device, stream, *args):
+    """The entry point on `stream` (None: the current one) of the tensors'
+    device, which is a GPU."""
     if device.type != "cuda":
         _refuse(f"tensors on {device}: device memory is needed")
-    if device.index == torch.cuda.current_device():
-        return call(*args)
-    with torch.cuda.device(device):
-        return call(*args)
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _call(name, device, stream, *args)
+    status = getattr(_lib or load(), name)(*args, _stream(stream))
+    if status != LOOKME_OK:
+        _check(status)
 
 
 def residual_norm(hidden, weight=None, eps=1e-6, add=None, part_w=None, hidden_out=None,
@@ -429,42 +435,47 @@ def residual_norm(hidden, weight=None, eps=1e-6, add=None, part_w=None, hidden_o
     [n, parts, d]; part_w [n, parts] float32; weight [d]; the outputs
     hidden_out (may be hidden), out [n, d], out_quant [n, d] float8_e4m3fn
     with scale_out [n] float32."""
-    code, dev, dt = _dtype_code("hidden", hidden), hidden.device, hidden.dtype
+    dev, dt = hidden.device, hidden.dtype
+    code = _dtype_code("hidden", hidden)
     if hidden.dim() != 2:
         _refuse(f"hidden has {hidden.dim()} dimensions, not 2")
-    _tensor("hidden", hidden, dt, hidden.shape, dev)
-    n, d = hidden.shape
-    parts = 0
+    rows = hidden.shape
+    n, d = rows
+    p_hidden = _tensor("hidden", hidden, dt, rows, dev)
+    parts, p_add, p_part = 0, None, None
     if add is not None:
-        parts = 1 if add.dim() == 2 else add.shape[1] if add.dim() == 3 else 0
-        _tensor("add", add, dt, (n, d) if add.dim() == 2 else (n, parts, d), dev)
-        if parts == 0:
-            add = None
+        if add.dim() == 2:
+            parts, p_add = 1, _tensor("add", add, dt, rows, dev)
+        else:
+            parts = add.shape[1] if add.dim() == 3 else 0
+            p_add = _tensor("add", add, dt, (n, parts, d), dev)
+            if parts == 0:
+                p_add = None
     if part_w is not None:
-        _tensor("part_w", part_w, torch.float32, (n, parts), dev)
+        p_part = _tensor("part_w", part_w, torch.float32, (n, parts), dev)
         if parts == 0:
-            part_w = None
-    for name, t, want, shape in (("weight", weight, dt, (d,)),
-                                 ("hidden_out", hidden_out, dt, (n, d)),
-                                 ("out", out, dt, (n, d)),
-                                 ("out_quant", out_quant, torch.float8_e4m3fn, (n, d)),
-                                 ("scale_out", scale_out, torch.float32, (n,))):
-        if t is not None:
-            _tensor(name, t, want, shape, dev)
-    _on(dev, lookme_residual_norm, code, n, d, hidden, parts, add, part_w, weight, eps,
-        hidden_out, out, out_quant, scale_out, stream)
+            p_part = None
+    p_weight = None if weight is None else _tensor("weight", weight, dt, (d,), dev)
+    p_sum = None if hidden_out is None else _tensor("hidden_out", hidden_out, dt, rows, dev)
+    p_out = None if out is None else _tensor("out", out, dt, rows, dev)
+    p_quant = p_scale = None
+    if out_quant is not None:
+        p_quant = _tensor("out_quant", out_quant, torch.float8_e4m3fn, rows, dev)
+    if scale_out is not None:
+        p_scale = _tensor("scale_out", scale_out, torch.float32, (n,), dev)
+    _call("lookme_residual_norm", dev, stream, code, n, d, p_hidden, parts, p_add, p_part,
+          p_weight, eps, p_sum, p_out, p_quant, p_scale)
 
 
 def group_rows(pick, groups, rows_out, offsets_out, stream=None):
     """lookme_group_rows on torch tensors: pick (any shape, n entries) and
     rows_out (as many) int32, offsets_out [groups + 1] int32."""
-    dev, n = pick.device, pick.numel()
-    _tensor("pick", pick, torch.int32, pick.shape, dev)
+    dev, n, i32 = pick.device, pick.numel(), torch.int32
     if rows_out.numel() != n:
         _refuse(f"rows_out has {rows_out.numel()} entries, not {n}")
-    _tensor("rows_out", rows_out, torch.int32, rows_out.shape, dev)
-    _tensor("offsets_out", offsets_out, torch.int32, (groups + 1,), dev)
-    _on(dev, lookme_group_rows, groups, n, pick, rows_out, offsets_out, stream)
+    _call("lookme_group_rows", dev, stream, groups, n, _tensor("pick", pick, i32, pick.shape, dev),
+          _tensor("rows_out", rows_out, i32, rows_out.shape, dev),
+          _tensor("offsets_out", offsets_out, i32, (groups + 1,), dev))
 
 
 def grouped_product(x, w, offsets, out, rows=None, picks=1, w_up=None, scatter=False,
@@ -473,80 +484,83 @@ def grouped_product(x, w, offsets, out, rows=None, picks=1, w_up=None, scatter=F
     for float8_e4m3fn: x [x_rows, d_in], w and w_up [groups, d_out, d_in],
     offsets [groups + 1] int32, out [m, d_out], rows [m] int32.  With rows,
     entry i reads x[rows[i] // picks] (picks = 0: x[i]); without, x[i]."""
-    dev, quant = x.device, x.dtype is torch.float8_e4m3fn
+    dev, dt = x.device, x.dtype
+    quant = dt is torch.float8_e4m3fn
     code = 0 if quant else _dtype_code("x", x)
     if x.dim() != 2 or w.dim() != 3 or out.dim() != 2:
         _refuse("x and out have 2 dimensions, w has 3")
     x_rows, d_in = x.shape
-    groups, d_out = w.shape[0], w.shape[1]
+    groups, d_out, _ = shape = w.shape
     m = out.shape[0]
-    _tensor("x", x, x.dtype, x.shape, dev)
-    _tensor("w", w, x.dtype, (groups, d_out, d_in), dev)
-    if w_up is not None:
-        _tensor("w_up", w_up, x.dtype, w.shape, dev)
-    _tensor("offsets", offsets, torch.int32, (groups + 1,), dev)
-    _tensor("out", out, torch.bfloat16 if quant else x.dtype, (m, d_out), dev)
+    p_x = _tensor("x", x, dt, x.shape, dev)
+    p_w = _tensor("w", w, dt, (groups, d_out, d_in), dev)
+    p_up = None if w_up is None else _tensor("w_up", w_up, dt, shape, dev)
+    p_off = _tensor("offsets", offsets, torch.int32, (groups + 1,), dev)
+    p_out = _tensor("out", out, torch.bfloat16 if quant else dt, (m, d_out), dev)
     if rows is None:
-        picks = 0
+        p_rows, picks = None, 0
     else:
-        _tensor("rows", rows, torch.int32, (m,), dev)
+        p_rows = _tensor("rows", rows, torch.int32, (m,), dev)
     if not quant:
         if x_scale is not None or w_scale is not None or w_up_scale is not None:
-            _refuse(f"scales given for {x.dtype}")
-        return _on(dev, lookme_grouped_product, code, groups, m, d_in, d_out, x, x_rows, rows,
-                   picks, offsets, w, w_up, out, int(scatter), stream)
+            _refuse(f"scales given for {dt}")
+        return _call("lookme_grouped_product", dev, stream, code, groups, m, d_in, d_out, p_x,
+                     x_rows, p_rows, picks, p_off, p_w, p_up, p_out, int(scatter))
     if x_scale is None or w_scale is None:
         _refuse("float8_e4m3fn needs x_scale and w_scale")
-    _tensor("x_scale", x_scale, torch.float32, (x_rows,), dev)
-    _tensor("w_scale", w_scale, torch.float32, (groups, d_out), dev)
-    if w_up_scale is not None:
-        _tensor("w_up_scale", w_up_scale, torch.float32, (groups, d_out), dev)
-    _on(dev, lookme_grouped_product_quant, groups, m, d_in, d_out, x, x_scale, x_rows, rows,
-        picks, offsets, w, w_scale, w_up, w_up_scale, out, int(scatter), stream)
+    f32 = torch.float32
+    p_xs = _tensor("x_scale", x_scale, f32, (x_rows,), dev)
+    p_ws = _tensor("w_scale", w_scale, f32, (groups, d_out), dev)
+    p_us = None if w_up_scale is None else _tensor("w_up_scale", w_up_scale, f32, (groups, d_out),
+                                                   dev)
+    _call("lookme_grouped_product_quant", dev, stream, groups, m, d_in, d_out, p_x, p_xs, x_rows,
+          p_rows, picks, p_off, p_w, p_ws, p_up, p_us, p_out, int(scatter))
 
 
 def _quant_matrix(name, x, w, scale, zero):
-    d_in, (d_out, groups) = x.shape[1], scale.shape
+    """(d_out, group, addresses of w, scale and zero)"""
+    dev, d_in = x.device, x.shape[1]
+    shape = scale.shape
+    d_out, groups = shape
     if groups < 1 or d_in % groups != 0:
         _refuse(f"scale has {groups} groups for {d_in} columns")
-    _tensor(name, w, torch.uint8, (d_out, d_in // 2), x.device)
-    _tensor(name + " scale", scale, x.dtype, (d_out, groups), x.device)
-    if zero is not None:
-        _tensor(name + " zero", zero, torch.uint8, (d_out, groups), x.device)
-    return d_out, d_in // groups
+    return (d_out, d_in // groups, _tensor(name, w, torch.uint8, (d_out, d_in // 2), dev),
+            _tensor("its scale", scale, x.dtype, shape, dev),
+            None if zero is None else _tensor("its zero", zero, torch.uint8, shape, dev))
 
 
 def quant_product(x, w, scale, out, zero=None, add=None, stream=None):
     """lookme_quant_product on torch tensors: x [n, d_in], w [d_out, d_in / 2]
     uint8, scale [d_out, groups], zero [d_out, groups] uint8, add and out
     [n, d_out] (out may be add)."""
+    dev, dt = x.device, x.dtype
     code = _dtype_code("x", x)
     if x.dim() != 2 or scale.dim() != 2:
         _refuse("x and scale have 2 dimensions")
     n, d_in = x.shape
-    _tensor("x", x, x.dtype, x.shape, x.device)
-    d_out, group = _quant_matrix("w", x, w, scale, zero)
-    _tensor("out", out, x.dtype, (n, d_out), x.device)
-    if add is not None:
-        _tensor("add", add, x.dtype, (n, d_out), x.device)
-    _on(x.device, lookme_quant_product, code, n, d_in, d_out, group, x, w, scale, zero, add, out,
-        stream)
+    p_x = _tensor("x", x, dt, x.shape, dev)
+    d_out, group, p_w, p_s, p_z = _quant_matrix("w", x, w, scale, zero)
+    p_out = _tensor("out", out, dt, (n, d_out), dev)
+    p_add = None if add is None else _tensor("add", add, dt, (n, d_out), dev)
+    _call("lookme_quant_product", dev, stream, code, n, d_in, d_out, group, p_x, p_w, p_s, p_z,
+          p_add, p_out)
 
 
 def quant_swiglu(x, w_gate, s_gate, w_up, s_up, out, z_gate=None, z_up=None, stream=None):
     """lookme_quant_swiglu on torch tensors, each matrix as for quant_product;
     out [n, d_ff]."""
+    dev, dt = x.device, x.dtype
     code = _dtype_code("x", x)
     if x.dim() != 2 or s_gate.dim() != 2 or s_up.dim() != 2:
         _refuse("x and the scales have 2 dimensions")
     n, d_in = x.shape
-    _tensor("x", x, x.dtype, x.shape, x.device)
-    d_ff, group = _quant_matrix("w_gate", x, w_gate, s_gate, z_gate)
-    if _quant_matrix("w_up", x, w_up, s_up, z_up) != (d_ff, group):
+    p_x = _tensor("x", x, dt, x.shape, dev)
+    d_ff, group, *gate = _quant_matrix("w_gate", x, w_gate, s_gate, z_gate)
+    d_up, group_up, *up = _quant_matrix("w_up", x, w_up, s_up, z_up)
+    if (d_up, group_up) != (d_ff, group):
         _refuse("w_gate and w_up differ in size or group")
-    _tensor("out", out, x.dtype, (n, d_ff), x.device)
-    _on(x.device, lookme_quant_swiglu, code, n, d_in, d_ff, group, x, w_gate, s_gate, z_gate,
-        w_up, s_up, z_up, out, stream)
+    p_out = _tensor("out", out, dt, (n, d_ff), dev)
+    _call("lookme_quant_swiglu", dev, stream, code, n, d_in, d_ff, group, p_x, *gate, *up, p_out)
 
 
 def lookme_destroy(h):

@@ -68,27 +68,29 @@ def grouped(x, w, offsets, m, rows=None, picks=1, w_up=None, scatter=False, x_sc
     bound = torch.zeros((m, d_out), dtype=torch.float64)
     off = offsets.tolist()
     for g in range(w.shape[0]):
-        for i in range(off[g], off[g + 1]):
-            r = int(rows[i]) if rows is not None else i
-            src = r // picks if rows is not None and picks else i
-            dst = r if scatter else i
-            if r < 0 or src >= x.shape[0] or dst >= m:
+        i = torch.arange(off[g], off[g + 1])
+        r = rows[i].long() if rows is not None else i
+        src = torch.div(r, picks, rounding_mode="trunc") if rows is not None and picks else i
+        dst = r if scatter else i
+        ok = (r >= 0) & (src < x.shape[0]) & (dst < m)
+        src, dst = src[ok], dst[ok]
+        if not len(src):
+            continue
+        xr = x[src].double()
+        both = []
+        for mat, sc in ((w, w_scale), (w_up, up_scale)):
+            if mat is None:
                 continue
-            xr = x[src].double()
-            both = []
-            for mat, sc in ((w, w_scale), (w_up, up_scale)):
-                if mat is None:
-                    continue
-                mr = mat[g].double()
-                v, mag = mr @ xr, mr.abs() @ xr.abs()
-                f = torch.ones(d_out, dtype=torch.float64)
-                e = (d_in + 4) * U32 * mag
-                if x_scale is not None:
-                    f = x_scale[src].double() * sc[g].double()
-                    e = e + 2.0 ** -9 * (mr * xr).abs().reshape(d_out, -1, 16).amax(2).sum(1)
-                both.append((v * f, e * f))
-            v, e = both[0] if w_up is None else silu_product(*both[0], *both[1])
-            out[dst], bound[dst] = v, e + HALF[out_dtype or x.dtype] * v.abs() * (1 + 2 ** -7)
+            mr = mat[g].double()
+            v, e = xr @ mr.T, (d_in + 4) * U32 * (xr.abs() @ mr.abs().T)
+            if x_scale is not None:
+                most = lambda t: t.abs().reshape(len(t), -1, 16).amax(2)  # noqa: E731
+                e = e + 2.0 ** -9 * (most(xr) @ most(mr).T)
+                f = x_scale[src].double()[:, None] * sc[g].double()
+                v, e = v * f, e * f + 4 * U32 * (v * f).abs()
+            both.append((v, e))
+        v, e = both[0] if w_up is None else silu_product(*both[0], *both[1])
+        out[dst], bound[dst] = v, e + HALF[out_dtype or x.dtype] * v.abs() * (1 + 2 ** -7)
     return out, bound
 
 

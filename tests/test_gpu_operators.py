@@ -155,6 +155,28 @@ def test_group_rows(lk, n, groups, low, high):
     assert rows.tolist() == want + [-7] * (n - len(want))
 
 
+@pytest.mark.parametrize("n,groups,heavy,share", [
+    (1 << 20, 3, 1, 0.7), (300000, 1000, 5, 0.6), (200000, 5000, 4321, 0.5), (262144, 100, 0, 0.0),
+    (65537, 1, 0, 0.0), (400000, 16384, 16383, 0.9), (50000, 256, 255, 1.0)])
+def test_group_rows_of_uneven_groups(lk, n, groups, heavy, share):
+    """one group with most of the ids: lists that run full, several segments"""
+    _say("group", n, groups, heavy, share)
+    g = torch.Generator().manual_seed(n)
+    pick = torch.randint(-2, groups + 2, (n,), generator=g, dtype=torch.int32)
+    pick[torch.rand((n,), generator=g) < share] = heavy
+    rows = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    offsets = torch.full((groups + 1,), -7, dtype=torch.int32, device="cuda")
+    lk.group_rows(pick.cuda(), groups, rows, offsets)
+    ok = (pick >= 0) & (pick < groups)
+    at = ok.nonzero()[:, 0]
+    order = at[torch.sort(pick[at], stable=True).indices].to(torch.int32)
+    want = torch.full((n,), -7, dtype=torch.int32)
+    want[:len(order)] = order
+    count = torch.bincount(pick[at].long(), minlength=groups)
+    assert torch.equal(offsets.cpu().long(), torch.cat([torch.zeros(1).long(), count.cumsum(0)]))
+    assert torch.equal(rows.cpu(), want)
+
+
 # ---------------------------------------------------------------------------
 # grouped products
 # ---------------------------------------------------------------------------
@@ -238,6 +260,59 @@ def test_grouped_entries_out_of_range_are_left_out(lk, sizes):
         _grouped_case(lk, "bf16", sizes, 144, 72, False, picks, scatter, rows=rows, x_rows=m)
 
 
+# sizes that the launch rules send to each of the kernels: few rows with K over
+# two waves, tiles of 32 rows with three stages and of 64 rows with four and two,
+# and the large tiles (whole, half and cut ones), with K of whole and of part
+# stages
+KERNELS = [([1] * 64, 48, 512), ([20] * 64, 80, 1024), ([70] * 16, 144, 1024),
+           ([70] * 32, 128, 1024), ([1500, 0, 2000] + [46] * 18, 144, 4096),
+           ([300, 1, 2900, 130, 90] + [40] * 18, 256, 4096)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("up", [False, True])
+@pytest.mark.parametrize("sizes,d_in,d_out", KERNELS)
+def test_grouped_kernels(lk, dtype, up, sizes, d_in, d_out):
+    _grouped_case(lk, dtype, sizes, d_in, d_out, up)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("sizes,d_in,d_out", KERNELS)
+def test_grouped_kernels_gather_and_scatter(lk, dtype, sizes, d_in, d_out):
+    _grouped_case(lk, dtype, sizes, d_in, d_out, False, 2, True, m=sum(sizes) + 30)
+
+
+@pytest.mark.parametrize("rows,d_out,d_in", [(1, 160, 16), (5, 320, 16), (40, 320, 16)])
+def test_grouped_more_tiles_than_a_launch_has_workgroups(lk, rows, d_out, d_in):
+    """the few-rows and ring kernels in several passes"""
+    G = lk.LOOKME_MAX_GROUPS
+    x, w = _rand(1, G * rows, d_in, dtype=BF), _rand(2, G, d_out, d_in, std=0.25, dtype=BF)
+    off = (torch.arange(G + 1) * rows).to(torch.int32)
+    out = torch.full((G * rows, d_out), -7.0, dtype=BF, device="cuda")
+    lk.grouped_product(x.cuda(), w.cuda(), off.cuda(), out)
+    for g in list(range(0, G, 997)) + [G - 1]:
+        xs, ws = x[g * rows:(g + 1) * rows].double(), w[g].double()
+        v = xs @ ws.T
+        _close(out[g * rows:(g + 1) * rows], v, (d_in + 4) * R.U32 * (xs.abs() @ ws.abs().T) +
+               R.HALF[BF] * 1.01 * v.abs(), f"group {g}")
+    assert (out != -7).any(1).all()
+
+
+def test_grouped_more_large_tiles_than_a_window(lk):
+    """over 64 tiles a workgroup, so that their places are found twice"""
+    sizes, d_in, d_out = [20000, 100, 20860], 64, 32768
+    x, w = _rand(1, sum(sizes), d_in, dtype=BF), _rand(2, 3, d_out, d_in, std=0.125, dtype=BF)
+    off = _offsets(sizes)
+    out = torch.full((sum(sizes), d_out), -7.0, dtype=BF, device="cuda")
+    lk.grouped_product(x.cuda(), w.cuda(), off.cuda(), out)
+    for g in range(3):
+        for i in list(range(off[g], off[g + 1], 517)) + [int(off[g + 1]) - 1]:
+            xs, ws = x[i].double(), w[g].double()
+            v = ws @ xs
+            _close(out[i], v, (d_in + 4) * R.U32 * (ws.abs() @ xs.abs()) +
+                   R.HALF[BF] * 1.01 * v.abs(), f"row {i}")
+
+
 @pytest.mark.parametrize("dtype,d_in", [("bf16", 2048), ("e4m3", 2048), ("f32", 1024)])
 @pytest.mark.parametrize("sizes", [[2, 1, 0, 3], [130, 100, 5]])
 def test_grouped_long_sums(lk, dtype, d_in, sizes):
@@ -286,7 +361,9 @@ def _matrix(seed, d_out, d_in, group, dtype, zero):
 
 QUANT = [(1, 32, 8, 32), (1, 64, 24, 64), (1, 2048, 40, 128), (3, 384, 72, 128),
          (16, 1120, 16, 32), (17, 192, 136, 64), (33, 768, 8, 384), (64, 256, 200, 256),
-         (2, 9600, 16, 32), (100, 128, 8, 32)]
+         (2, 9600, 16, 32), (100, 128, 8, 32),
+         # two row tiles a wave
+         (1, 96, 8200, 32), (12, 64, 8192, 64), (20, 128, 8216, 128), (150, 256, 2056, 128)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -421,10 +421,12 @@ def _call(name, device, stream, *args):
     device, which is a GPU."""
     if device.type != "cuda":
         _refuse(f"tensors on {device}: device memory is needed")
-    if device.index != torch.cuda.current_device():
+    index = device.index
+    if index != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             return _call(name, device, stream, *args)
-    status = getattr(_lib or load(), name)(*args, _stream(stream))
+    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)
+    status = getattr(_lib or load(), name)(*args, raw)
     if status != LOOKME_OK:
         _check(status)
 

@@ -264,8 +264,8 @@ def test_grouped_entries_out_of_range_are_left_out(lk, sizes):
 # two waves, tiles of 32 rows with three stages and of 64 rows with four and two,
 # and the large tiles (whole, half and cut ones), with K of whole and of part
 # stages
-KERNELS = [([1] * 64, 48, 512), ([20] * 64, 80, 1024), ([70] * 16, 144, 1024),
-           ([70] * 32, 128, 1024), ([1500, 0, 2000] + [46] * 18, 144, 4096),
+KERNELS = [([1] * 64, 48, 512), ([20] * 64, 80, 1024), ([70] * 8, 144, 1024),
+           ([70] * 16, 144, 1024), ([70] * 32, 128, 1024), ([1500, 0, 2000] + [46] * 18, 144, 4096),
            ([300, 1, 2900, 130, 90] + [40] * 18, 256, 4096)]
 
 
@@ -363,7 +363,8 @@ QUANT = [(1, 32, 8, 32), (1, 64, 24, 64), (1, 2048, 40, 128), (3, 384, 72, 128),
          (16, 1120, 16, 32), (17, 192, 136, 64), (33, 768, 8, 384), (64, 256, 200, 256),
          (2, 9600, 16, 32), (100, 128, 8, 32),
          # two row tiles a wave
-         (1, 96, 8200, 32), (12, 64, 8192, 64), (20, 128, 8216, 128), (150, 256, 2056, 128)]
+         (1, 96, 8200, 32), (12, 64, 8192, 64), (12, 256, 8192, 128), (20, 128, 8216, 128),
+         (150, 256, 2056, 128)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -58,13 +58,9 @@ template <int DT>
 struct QpFrag {
   static constexpr int PARTS = DT == DT_BF16 ? 1 : 3;
   u32x4_t raw[DT == DT_BF16 ? 1 : 2];
-  __device__ __forceinline__ void load(const char* row, int c) {   // chunk of 8 values
-    if constexpr (DT == DT_BF16) {
-      raw[0] = ld16(row + (int64_t)c * 16);
-    } else {
-      raw[0] = ld16(row + (int64_t)c * 32);
-      raw[1] = ld16(row + (int64_t)c * 32 + 16);
-    }
+  __device__ __forceinline__ void load(const char* p) {
+    raw[0] = ld16(p);
+    if constexpr (DT == DT_F32) raw[1] = ld16(p + 16);
   }
   __device__ __forceinline__ void split(u32x4_t (&f)[PARTS]) const {
     if constexpr (DT == DT_BF16) {
@@ -90,17 +86,16 @@ struct QpFrag {
 };
 
 // NT: token tiles of 16.  RW: tiles of 16 weight rows a wave multiplies with the
-// same tokens (of each matrix).  D: blocks of 128 weights a row in flight (the
-// tokens, which come from L2, are one block ahead).  SHORT: groups of 32 or 64
-// (the words of a block are transposed so that a product step stays inside
-// one), else of whole blocks.  K is split over the workgroup's waves.  lds: the
-// scales of at most QP_GROUPS groups, then the waves' sums.
-template <int DT, int NT, int RW, int D, bool UP, bool SHORT>
+// same tokens (of each matrix).  SHORT: groups of 32 or 64 (the words of a block
+// are transposed so that a product step stays inside one), else of whole
+// blocks.  K is split over the workgroup's waves, two blocks of 128 weights in
+// flight in each.  lds: the scales of at most QP_GROUPS groups, then the waves'
+// sums.
+template <int DT, int NT, int RW, bool UP, bool SHORT>
 __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
   constexpr int ES = DT == DT_BF16 ? 2 : 4;
   constexpr int MATS = UP ? 2 : 1, TILES = MATS * RW;   // tile q RW + i: rows 16 i of matrix q
   constexpr int PARTS = QpFrag<DT>::PARTS;
-  static_assert(D % 2 == 0, "the tokens' buffer of a block is its parity");
   static_assert(RW * NT <= QP_WAVES, "a wave an output tile");
   extern __shared__ __attribute__((aligned(16))) char lds[];
   // [group][tile][scale, 16 + zero][16 rows]
@@ -133,26 +128,34 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[q][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  // unconditional loads from clamped addresses; values past K count as zero
-  // (only the last block of SHORT groups has any)
+  // K may end inside the last block of SHORT groups: its chunks past the end are
+  // read from clamped addresses, and their sums, whole steps, never used
+  constexpr int XB = 8 * ES;   // bytes of 8 values
   const int wchunks = p.k / 32, xchunks = p.k / 8;
-  u32x4_t fw[D][TILES];
+  u32x4_t fw[2][TILES];
   QpFrag<DT> fx[2][NT][4];
   auto load_w = [&](int d, int b) {
     int c = 4 * b + g;
-    c = c < wchunks ? c : wchunks - 1;
+    if constexpr (SHORT) c = c < wchunks ? c : wchunks - 1;
 #pragma unroll
-    for (int q = 0; q < TILES; ++q) fw[d][q] = ld16(wp[q] + (int64_t)c * 16);
+    for (int q = 0; q < TILES; ++q) fw[d][q] = ld16(wp[q] + c * 16);
   };
-  auto x_chunk = [&](int b, int s) { return SHORT ? 16 * b + 4 * s + g : 16 * b + 4 * g + s; };
   auto load_x = [&](int d, int b) {
+    if (!SHORT || 128 * (b + 1) <= p.k) {
+      const int off = (16 * b + (SHORT ? g : 4 * g)) * XB;
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+      for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int x = x_chunk(b, s);
-        fx[d & 1][j][s].load(xp[j], x < xchunks ? x : xchunks - 1);
-      }
+        for (int s = 0; s < 4; ++s) fx[d][j][s].load(xp[j] + off + (SHORT ? 4 * s : s) * XB);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const int x = 16 * b + 4 * s + g;
+          fx[d][j][s].load(xp[j] + (x < xchunks ? x : xchunks - 1) * XB);
+        }
+    }
   };
 
   // blocks whose groups' scales fit LDS; one pass for all but long K of short groups
@@ -164,11 +167,12 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
     const int b0 = seg + wv * per;
     const int b1 = b0 + per < seg + left ? b0 + per : seg + left;
     if (b0 < b1) {
-      load_x(0, b0);
-      if (b0 + 1 < b1) load_x(1, b0 + 1);
 #pragma unroll
-      for (int d = 0; d < D; ++d) {
-        if (b0 + d < b1) load_w(d, b0 + d);
+      for (int d = 0; d < 2; ++d) {
+        if (b0 + d < b1) {
+          load_x(d, b0 + d);
+          load_w(d, b0 + d);
+        }
         asm volatile("" ::: "memory");
       }
     }
@@ -191,9 +195,9 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
       }
     }
     __syncthreads();
-    for (int b = b0; b < b1; b += D) {
+    for (int b = b0; b < b1; b += 2) {
 #pragma unroll
-      for (int d = 0; d < D; ++d) {
+      for (int d = 0; d < 2; ++d) {
         if (b + d < b1) {   // the same for the whole wave
           u32x4_t w[TILES];
 #pragma unroll
@@ -234,12 +238,6 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
             for (int j = 0; j < NT; ++j) {
               u32x4_t f[PARTS];
               fx[d & 1][j][s].split(f);
-              if constexpr (SHORT) {
-                if (x_chunk(b + d, s) >= xchunks) {
-#pragma unroll
-                  for (int e = 0; e < PARTS; ++e) f[e] = u32x4_t{0, 0, 0, 0};
-                }
-              }
 #pragma unroll
               for (int e = 0; e < PARTS; ++e) {
                 sx[j] = mfma_chunk<DT_BF16>(ones, f[e], sx[j]);
@@ -256,9 +254,10 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
           }
           if constexpr (!SHORT) flush(128 * (b + d) / p.group);
         }
-        // the tokens first: loads return in order, and these are waited for first
-        if (b + d + 2 < b1) load_x(d, b + d + 2);
-        if (b + d + D < b1) load_w(d, b + d + D);
+        if (b + d + 2 < b1) {
+          load_x(d, b + d + 2);
+          load_w(d, b + d + 2);
+        }
       }
     }
   }
@@ -299,7 +298,7 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
   st_cols<DT, 4>(p.out + at, v);
 }
 
-template <int DT, int NT, int RW, int D, bool UP>
+template <int DT, int NT, int RW, bool UP>
 static void launch_quant_nt(const QuantParams& p, hipStream_t st) {
   constexpr int TILES = (UP ? 2 : 1) * RW;
   const dim3 grid((unsigned)((p.cols + 16 * RW - 1) / (16 * RW)),
@@ -311,10 +310,10 @@ static void launch_quant_nt(const QuantParams& p, hipStream_t st) {
                 "dynamic LDS of a launch");
   const size_t lds = scales > sums ? scales : sums;
   if (p.group < 128)
-    hipLaunchKernelGGL((quant_rows_kernel<DT, NT, RW, D, UP, true>), grid, dim3(QP_THREADS), lds,
+    hipLaunchKernelGGL((quant_rows_kernel<DT, NT, RW, UP, true>), grid, dim3(QP_THREADS), lds,
                        st, p);
   else
-    hipLaunchKernelGGL((quant_rows_kernel<DT, NT, RW, D, UP, false>), grid, dim3(QP_THREADS), lds,
+    hipLaunchKernelGGL((quant_rows_kernel<DT, NT, RW, UP, false>), grid, dim3(QP_THREADS), lds,
                        st, p);
 }
 
@@ -324,18 +323,21 @@ static void launch_quant_nt(const QuantParams& p, hipStream_t st) {
 // 22 and 17, 32 rows 38 and 24; float32 1 row 27 and 19; 4096 x 4096, 128
 // workgroups, 16 rows 8.2 and 9.9).  Gate and up share the tokens already, which
 // is enough for few rows (2 x 8192 x 4096 of 4 rows 13.2 and 15.0, of 16 17.1 and
-// 16.5; float32 of 4 rows 22 and 19).  More blocks in flight than two a wave,
-// beside 16 waves a CU, only cost registers (1 row 13.0 us with 2, 14.0 with 4).
+// 16.5; float32 of 4 rows 22 and 19), and with two token tiles of float32 two row
+// tiles spill.  Deeper rings (4 blocks: 1 row of 8192 x 8192 14.0 us), 16 waves (1
+// row of 1024 x 8192 7.5 and 7.4 us) and no loads for the tokens there are none
+// of (the same) were no faster.
 template <int DT, bool UP>
 static void launch_quant_dt(const QuantParams& p, hipStream_t st) {
   const int64_t wide = (int64_t)((p.cols + 31) / 32) * ((p.n + 31) / 32);
-  const bool two = wide >= 256 && !(UP && DT == DT_BF16 && p.n <= 8);
+  const bool two = wide >= 256 && !(UP && (DT == DT_BF16 ? p.n <= 8 : p.n > 16));
   if (p.n <= 16) {
-    if (two) launch_quant_nt<DT, 1, 2, 2, UP>(p, st);
-    else launch_quant_nt<DT, 1, 1, 2, UP>(p, st);
+    if (two) launch_quant_nt<DT, 1, 2, UP>(p, st);
+    else launch_quant_nt<DT, 1, 1, UP>(p, st);
   } else {
-    if (two) launch_quant_nt<DT, 2, 2, 2, UP>(p, st);
-    else launch_quant_nt<DT, 2, 1, 2, UP>(p, st);
+    if constexpr (!(UP && DT == DT_F32))
+      if (two) return launch_quant_nt<DT, 2, 2, UP>(p, st);
+    launch_quant_nt<DT, 2, 1, UP>(p, st);
   }
 }
 

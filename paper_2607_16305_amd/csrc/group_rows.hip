@@ -208,10 +208,11 @@ hipError_t launch_group_rows(int groups, int64_t n, const int32_t* pick, int32_t
                              int32_t* offsets, hipStream_t st) {
   const int range = (groups + GR_BLOCKS - 1) / GR_BLOCKS;
   const int ranges = (groups + range - 1) / range;
-  // a CU a segment, and steps for each of them
+  // a CU a segment, and a step for each of them (25509 ids of one group in one
+  // segment 21 us)
   const int64_t steps = (n + GR_STEP - 1) / GR_STEP;
   int64_t segments = range == 1 ? GR_BLOCKS / ranges : 1;
-  segments = segments < steps / GR_WAVES ? segments : steps / GR_WAVES;
+  if (segments > steps) segments = steps;
   if (segments < 1) segments = 1;
   hipLaunchKernelGGL(group_rows_kernel, dim3((unsigned)(ranges * segments)), dim3(GR_THREADS), 0,
                      st, pick, (int)n, groups, range, (int)segments, rows, offsets);

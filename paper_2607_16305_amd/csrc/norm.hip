@@ -152,13 +152,14 @@ __device__ __forceinline__ void rn_store_quant(char* row, int c, const float (&y
 
 // A row on a team of T threads, at most CH chunks a thread, kept in registers.
 template <int DT, int T, int CH, bool ONE>
-__global__ __launch_bounds__(RN_THREADS, CH < 8 || DT == DT_F32 ? 4 : 3) void residual_norm_kernel(NormParams p) {
-  constexpr int E = rn_elems<DT>();
-  __shared__ float red_s[RN_THREADS / 64];
-  __shared__ uint32_t red_m[RN_THREADS / 64];
+__global__ __launch_bounds__(T > RN_THREADS ? T : RN_THREADS,
+                             CH < 8 || DT == DT_F32 ? 4 : 3) void residual_norm_kernel(NormParams p) {
+  constexpr int E = rn_elems<DT>(), BLOCK = T > RN_THREADS ? T : RN_THREADS;
+  __shared__ float red_s[BLOCK / 64];
+  __shared__ uint32_t red_m[BLOCK / 64];
   const int t = threadIdx.x & (T - 1);
-  const int64_t row = (int64_t)blockIdx.x * (RN_THREADS / T) + threadIdx.x / T;
-  if (row >= p.n) return;   // T < RN_THREADS: whole waves, and no barrier is used
+  const int64_t row = (int64_t)blockIdx.x * (BLOCK / T) + threadIdx.x / T;
+  if (row >= p.n) return;   // T < BLOCK: whole waves, and no barrier is used
   const char* h = p.hidden + row * p.row_bytes;
   const char* add = p.add + row * p.parts * p.row_bytes;
   const float* pw = p.part_w != nullptr ? p.part_w + row * p.parts : nullptr;
@@ -298,19 +299,27 @@ __global__ __launch_bounds__(RN_THREADS) void residual_norm_wide_kernel(NormPara
 
 template <int DT, int T, int CH>
 static void launch_norm_t(const NormParams& p, hipStream_t st) {
-  const int64_t rows = RN_THREADS / T;
+  constexpr int BLOCK = T > RN_THREADS ? T : RN_THREADS;
+  const int64_t rows = BLOCK / T;
   const dim3 grid((unsigned)((p.n + rows - 1) / rows));
   if (p.parts == 1)
-    hipLaunchKernelGGL((residual_norm_kernel<DT, T, CH, true>), grid, dim3(RN_THREADS), 0, st, p);
+    hipLaunchKernelGGL((residual_norm_kernel<DT, T, CH, true>), grid, dim3(BLOCK), 0, st, p);
   else
-    hipLaunchKernelGGL((residual_norm_kernel<DT, T, CH, false>), grid, dim3(RN_THREADS), 0, st, p);
+    hipLaunchKernelGGL((residual_norm_kernel<DT, T, CH, false>), grid, dim3(BLOCK), 0, st, p);
 }
 
+// A wave a row while that is two chunks a thread, else 256 threads; 1024 while
+// every row has a CU of its own, where the time is one thread's chain of loads
+// (2 rows of 7360 in two parts 8.8 -> 5.1 us, 256 rows of 4096 in eight
+// 9.6 -> 7.2; 512 such rows 12.0 -> 13.7).
 template <int DT>
 static void launch_norm(const NormParams& p, hipStream_t st) {
+  const bool few = p.n <= 256;
   if (p.chunks <= 64) launch_norm_t<DT, 64, 1>(p, st);
   else if (p.chunks <= 128) launch_norm_t<DT, 64, 2>(p, st);
   else if (p.chunks <= 256) launch_norm_t<DT, 256, 1>(p, st);
+  else if (p.chunks <= 1024 && few) launch_norm_t<DT, 1024, 1>(p, st);
+  else if (p.chunks <= 2048 && few) launch_norm_t<DT, 1024, 2>(p, st);
   else if (p.chunks <= 512) launch_norm_t<DT, 256, 2>(p, st);
   else if (p.chunks <= 1024) launch_norm_t<DT, 256, 4>(p, st);
   else if (p.chunks <= 2048) launch_norm_t<DT, 256, 8>(p, st);

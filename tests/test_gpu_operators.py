@@ -96,6 +96,15 @@ def test_norm_parity(lk, dtype, n, d, parts, weighted):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [3, 256, 257])
+@pytest.mark.parametrize("d,parts", [(1160, 1), (1160, 2), (2056, 1), (2056, 3), (4104, 1),
+                                     (4104, 2), (8184, 1), (8184, 3), (16384, 1), (16384, 2)])
+def test_norm_teams(lk, dtype, n, d, parts):
+    """either side of the row count that a row's team of threads depends on"""
+    _check_norm(*_norm_case(lk, dtype, n, d, parts, parts > 1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [512, 40000])
 @pytest.mark.parametrize("kw", [
     dict(hidden_out=None, out=True, quant=False), dict(hidden_out=None, out=False, quant=True),

@@ -451,6 +451,10 @@ __global__ __launch_bounds__(GM_THREADS) void grouped_mid_kernel(GroupedParams p
 // numbered, workgroup s takes tiles s, s + GT_GRID, ...; where they lie is
 // found GT_WINDOW at a time, in one pass over the offsets (GtPlan).
 constexpr int GT_THREADS = 512, GT_GRID = 256, GT_WINDOW = 64;
+// Column tiles of a band: the 32 tiles that an XCD has at a time are then four
+// blocks of weights by eight of tokens (16 groups of 2048 rows, 4096 x 4096 in
+// e4m3, 658 us row by row, 627 in bands of 4, 636 of 8).
+constexpr int GT_BAND = 4;
 enum : int { GT_WHOLE = 0, GT_HALF = 1 };   // 256 x 256, 128 x 256
 
 struct GtLds {
@@ -483,13 +487,14 @@ __device__ __forceinline__ GtPlan gt_plan(int blocks, int own_halves, int tn) {
   return pl;
 }
 
-// PgLoads with the stages taken in a circle from stage `rot`
+// PgLoads with the stages taken in another order: in aligned blocks of a power
+// of two, stage s ^ turn.
 template <class S>
 struct GtLoads : PgLoads<S> {
-  int rot;
+  int turn, blocked;   // turn is below the power; stages in whole blocks
   __device__ __forceinline__ int at(int stage) const {
-    const int s = (stage < this->last ? stage : this->last) + rot;
-    return (s <= this->last ? s : s - this->last - 1) * 128;
+    const int s = stage < this->last ? stage : this->last;
+    return (s < blocked ? s ^ turn : s) * 128;
   }
   __device__ __forceinline__ void a(int h, int stage, char* dst) const {
     const int k = at(stage);
@@ -553,11 +558,26 @@ __device__ __forceinline__ void grouped_tile(const GroupedParams& p, char* lds, 
     }
   }
   f32x4_t acc[2][2][MI][NJ];
-  // a group of one row block reads its weights once, a whole row of 128 bytes in
-  // every stage: begun at a stage of its own, the tiles in flight do not all
-  // read the same few channels (64 rows each in 64 groups of 2048 x 2048 161 ->
-  // 139 us)
-  ld.rot = gb - ga <= 128 ? (int)((unsigned)(grp * 8 + n0 / 64) % (unsigned)nst) : 0;
+  // Rows lie a multiple of some KiB apart, so tiles that are at the same stage
+  // read the same few channels of L2 and of memory: each takes the stages in an
+  // order of its own.  A group of one row block, whose weights are read once,
+  // has all stages to choose from (64 groups of 64 rows, 2048 x 2048, 161 -> 139
+  // us).  Else what an XCD's tiles read has to stay in its L2 meanwhile: eight
+  // stages, the same order for tiles of the same rows, another one in every XCD
+  // (16 groups of 2048 rows, 4096 x 4096 in e4m3, 627 -> 540 us; 16 stages 547; 32
+  // groups of 1024 rows, 4096 x 4096 in bf16, 1120 -> 969).  float32, whose stages
+  // last longer, does without (8 groups of 1024 rows, 2048 x 2048, 567 and 620).
+  int power = 1;
+  ld.turn = 0;
+  if (gb - ga <= 128) {
+    while (2 * power <= nst) power *= 2;
+    ld.turn = grp * 8 + n0 / 64;
+  } else if (DT != DT_F32) {
+    power = 8;
+    ld.turn = blockIdx.x / (8 * GT_BAND) + blockIdx.x;
+  }
+  ld.turn &= power - 1;
+  ld.blocked = nst & -power;
   L.run(nst, ld, acc, [](int, int) {});
 
   // the chunks past the last whole stage, zeros behind them
@@ -693,8 +713,10 @@ __global__ __launch_bounds__(GT_THREADS, 2) void grouped_tiles_kernel(GroupedPar
       int b, h;
       blocks(g, b, h);
       const int64_t lo = at * tn, hi = (at + b) * tn;
-      auto whole = [&](int64_t u) {
-        return make_int4(g, (int)(u / tn) * 256, (int)(u % tn) * TC, GT_WHOLE);
+      auto whole = [&](int64_t u) {   // bands of GT_BAND column tiles, the group's rows in each
+        const int v = (int)u, w0 = v / (GT_BAND * b) * GT_BAND, in = v - w0 * b;
+        const int w = tn - w0 < GT_BAND ? tn - w0 : GT_BAND;
+        return make_int4(g, in / w * 256, (w0 + in % w) * TC, GT_WHOLE);
       };
       mark(lo, hi < pl.whole ? hi : pl.whole, whole);
       if (h != 0)

@@ -247,10 +247,14 @@ __global__ __launch_bounds__(GM_THREADS) void grouped_mid_kernel(GroupedParams p
   constexpr int ODT = DT == DT_E4M3 ? DT_BF16 : DT;
   constexpr int OES = ODT == DT_BF16 ? 2 : 4;
   constexpr int COLS = UP ? 32 : 64;
-  __shared__ __attribute__((aligned(1024))) char lds[NS][S::STAGE];
-  __shared__ int find_lds[GP_FIND_LDS];
-  __shared__ int32_t row_src[RT], row_dst[RT];
-  __shared__ float row_xs[RT];
+  // one object, as in the large tiles' kernel below
+  constexpr int STAGES = NS * S::STAGE;
+  __shared__ __attribute__((aligned(1024))) char smem[STAGES + 4 * (GP_FIND_LDS + 3 * RT)];
+  char (*lds)[S::STAGE] = reinterpret_cast<char (*)[S::STAGE]>(smem);
+  int32_t* row_src = reinterpret_cast<int32_t*>(smem + STAGES);
+  int32_t* row_dst = row_src + RT;
+  float* row_xs = reinterpret_cast<float*>(row_dst + RT);
+  int* find_lds = row_dst + 2 * RT;
   const int tn = (p.cols + COLS - 1) / COLS;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -565,16 +569,12 @@ __device__ __forceinline__ void grouped_tile(const GroupedParams& p, char* lds, 
   // us).  Else what an XCD's tiles read has to stay in its L2 meanwhile: eight
   // stages, the same order for tiles of the same rows, another one in every XCD
   // (16 groups of 2048 rows, 4096 x 4096 in e4m3, 627 -> 540 us; 16 stages 547; 32
-  // groups of 1024 rows, 4096 x 4096 in bf16, 1120 -> 969).  float32, whose stages
-  // last longer, does without (8 groups of 1024 rows, 2048 x 2048, 567 and 620).
-  int power = 1;
-  ld.turn = 0;
+  // groups of 1024 rows, 4096 x 4096 in bf16, 1120 -> 969; float32 the same).
+  int power = 8;
+  ld.turn = blockIdx.x / (8 * GT_BAND) + blockIdx.x;
   if (gb - ga <= 128) {
-    while (2 * power <= nst) power *= 2;
+    for (power = 1; 2 * power <= nst;) power *= 2;
     ld.turn = grp * 8 + n0 / 64;
-  } else if (DT != DT_F32) {
-    power = 8;
-    ld.turn = blockIdx.x / (8 * GT_BAND) + blockIdx.x;
   }
   ld.turn &= power - 1;
   ld.blocked = nst & -power;
@@ -658,8 +658,12 @@ __device__ __forceinline__ void grouped_tile(const GroupedParams& p, char* lds, 
 
 template <int DT, bool UP>
 __global__ __launch_bounds__(GT_THREADS, 2) void grouped_tiles_kernel(GroupedParams p) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * PgShape<4, 2>::BUF];
-  __shared__ GtLds gl;
+  // One object: the compiler puts a wait for every load into LDS before a read of
+  // one of several (16 groups of 2048 rows, 4096 x 4096 in e4m3, 532 -> 506 us, 64 of 1024,
+  // 2048 x 2048 in bf16, 573 -> 522).
+  constexpr int STAGES = 2 * PgShape<4, 2>::BUF;
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES + sizeof(GtLds)];
+  GtLds& gl = *reinterpret_cast<GtLds*>(lds + STAGES);
   constexpr int TC = UP ? 128 : 256;   // output columns of a tile
   const int tn = (p.cols + TC - 1) / TC;
   // neighbouring tiles on one XCD

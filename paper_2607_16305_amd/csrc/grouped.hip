@@ -785,7 +785,11 @@ static void launch_mid(const GroupedParams& p, hipStream_t st) {
 // Up to 4 rows a group (float32, bound by the matrix cores, 8) the few-rows
 // kernel: 64 groups of 2048 x 2048, it and 32-row tiles, 1 row 92 and 94 us, 4
 // rows 101 and 95, 16 rows 147 and 97 (537 MB of weights: 5.5 TB/s); 8 groups of
-// 1 row, 1024 x 2048, 11 and 17.
+// 1 row, 1024 x 2048, 11 and 17.  Also while its workgroups, whose waves share
+// K, are no more than the CUs (float32 without an up half twice that): 4 groups of
+// 11 rows, 2048 x 256, 7.9 and 9.0 us, float32 10.6 and 25.0; one of 128 rows, 2048
+// x 1024, 12.6 and 9.3; but not with two matrices a wave in fewer bits (4 groups of
+// 11 rows, 2048 x 256, 10.1 and 9.1, float32 17.1 and 25.4).
 // Then tiles of 32 rows, of 64 above 32 rows a group where these are enough
 // (64 rows 140 and 112 us; one group of 512 rows 14 and 18), with deep rings
 // while all tiles are resident at once (one group of 512 rows 14 us with 4
@@ -805,6 +809,9 @@ static hipError_t launch_grouped_dt(const GroupedParams& p, hipStream_t st) {
   const int64_t tn64 = (p.cols + (UP ? 31 : 63)) / (UP ? 32 : 64);
   // half a row tile of padding a group, half of the groups with a half tile
   const int64_t tiles64 = (p.m / 64 + used / 2 + 1) * tn64;
+  constexpr int few = DT == DT_F32 ? (UP ? 256 : 512) : (UP ? 0 : 256);
+  const int64_t tiles16 =
+      used * ((p.m + 16 * used - 1) / (16 * used)) * (int64_t)((p.cols + 15) / 16);
   auto rounds = [](int64_t n) { return (double)((n + GT_GRID - 1) / GT_GRID); };
   const double round = DT == DT_F32 ? 3000. : DT == DT_E4M3 ? 2150. : 2000.;
   const double large = rounds(p.m / 256 * tn) +
@@ -814,7 +821,7 @@ static hipError_t launch_grouped_dt(const GroupedParams& p, hipStream_t st) {
                     (p.picks == 0 || p.x_rows * p.k_bytes < ((int64_t)1 << 32));
   if (p.m > 64 * used && large * round < (double)tiles64 && p.k_bytes >= 128 && near)
     hipLaunchKernelGGL((grouped_tiles_kernel<DT, UP>), dim3(GT_GRID), dim3(GT_THREADS), 0, st, p);
-  else if (p.m <= (DT == DT_F32 ? 8 : 4) * used)
+  else if (p.m <= (DT == DT_F32 ? 8 : 4) * used || tiles16 <= few)
     launch_rows<DT, UP>(p, st);
   else if (p.m <= 32 * used || tiles64 <= 256) {
     if ((p.m / 32 + used / 2 + 1) * tn64 <= 768) launch_mid<DT, 4, 1, UP>(p, st);

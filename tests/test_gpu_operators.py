@@ -286,6 +286,17 @@ def test_grouped_kernels(lk, dtype, up, sizes, d_in, d_out):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("up", [False, True])
+@pytest.mark.parametrize("sizes,d_in,d_out", [
+    ([300, 17, 0, 90], 272, 1032), ([129, 128, 0, 3, 250], 1040, 520), ([40, 9, 33] * 5, 16, 552),
+    ([64, 11], 2064, 72), ([33], 1040, 512), ([4] * 9 + [60], 528, 136)])
+def test_grouped_between_few_and_many_rows(lk, dtype, up, sizes, d_in, d_out):
+    """either side of the rule between the few-rows kernel and the rings"""
+    _grouped_case(lk, dtype, sizes, d_in, d_out, up)
+    _grouped_case(lk, dtype, sizes, d_in, d_out, up, 2, True, m=sum(sizes) + 3)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("sizes,d_in,d_out", KERNELS)
 def test_grouped_kernels_gather_and_scatter(lk, dtype, sizes, d_in, d_out):
     _grouped_case(lk, dtype, sizes, d_in, d_out, False, 2, True, m=sum(sizes) + 30)

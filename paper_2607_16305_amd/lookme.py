@@ -397,16 +397,24 @@ def _refuse(msg):
 
 
 def _tensor(name, t, dtype, shape, device):
-    """t's address; refuses another type, shape or device, and strides."""
-    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+    """t's address; refuses another type, shape or device (an index, as of
+    Tensor.get_device), and strides."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
     if t.dtype is not dtype:
         _refuse(f"{name} is {t.dtype}, not {dtype}")
     if t.shape != shape:
         _refuse(f"{name} has the shape {tuple(t.shape)}, not {tuple(shape)}")
-    if t.device != device:
-        _refuse(f"{name} is on {t.device}, not on {device}")
+    if t.get_device() != device:
+        _refuse(f"{name} is on {t.device}, other tensors are elsewhere")
     _refuse(f"{name} is not contiguous")
+
+
+def _first(name, t):
+    """the address of the tensor that gives type, sizes and device"""
+    if not t.is_contiguous():
+        _refuse(f"{name} is not contiguous")
+    return t.data_ptr()
 
 
 def _dtype_code(name, t):
@@ -419,13 +427,12 @@ def _dtype_code(name, t):
 def _call(name, device, stream, *args):
     """The entry point on `stream` (None: the current one) of the tensors'
     device, which is a GPU."""
-    if device.type != "cuda":
-        _refuse(f"tensors on {device}: device memory is needed")
-    index = device.index
-    if index != torch._C._cuda_getDevice():
+    if device < 0:
+        _refuse("tensors that are not in device memory")
+    if device != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             return _call(name, device, stream, *args)
-    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)
+    raw = torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
     status = getattr(_lib or load(), name)(*args, raw)
     if status != LOOKME_OK:
         _check(status)
@@ -437,13 +444,13 @@ def residual_norm(hidden, weight=None, eps=1e-6, add=None, part_w=None, hidden_o
     [n, parts, d]; part_w [n, parts] float32; weight [d]; the outputs
     hidden_out (may be hidden), out [n, d], out_quant [n, d] float8_e4m3fn
     with scale_out [n] float32."""
-    dev, dt = hidden.device, hidden.dtype
+    dev, dt = hidden.get_device(), hidden.dtype
     code = _dtype_code("hidden", hidden)
     if hidden.dim() != 2:
         _refuse(f"hidden has {hidden.dim()} dimensions, not 2")
     rows = hidden.shape
     n, d = rows
-    p_hidden = _tensor("hidden", hidden, dt, rows, dev)
+    p_hidden = _first("hidden", hidden)
     parts, p_add, p_part = 0, None, None
     if add is not None:
         if add.dim() == 2:
@@ -472,7 +479,7 @@ def residual_norm(hidden, weight=None, eps=1e-6, add=None, part_w=None, hidden_o
 def group_rows(pick, groups, rows_out, offsets_out, stream=None):
     """lookme_group_rows on torch tensors: pick (any shape, n entries) and
     rows_out (as many) int32, offsets_out [groups + 1] int32."""
-    dev, n, i32 = pick.device, pick.numel(), torch.int32
+    dev, n, i32 = pick.get_device(), pick.numel(), torch.int32
     if rows_out.numel() != n:
         _refuse(f"rows_out has {rows_out.numel()} entries, not {n}")
     _call("lookme_group_rows", dev, stream, groups, n, _tensor("pick", pick, i32, pick.shape, dev),
@@ -486,7 +493,7 @@ def grouped_product(x, w, offsets, out, rows=None, picks=1, w_up=None, scatter=F
     for float8_e4m3fn: x [x_rows, d_in], w and w_up [groups, d_out, d_in],
     offsets [groups + 1] int32, out [m, d_out], rows [m] int32.  With rows,
     entry i reads x[rows[i] // picks] (picks = 0: x[i]); without, x[i]."""
-    dev, dt = x.device, x.dtype
+    dev, dt = x.get_device(), x.dtype
     quant = dt is torch.float8_e4m3fn
     code = 0 if quant else _dtype_code("x", x)
     if x.dim() != 2 or w.dim() != 3 or out.dim() != 2:
@@ -494,7 +501,7 @@ def grouped_product(x, w, offsets, out, rows=None, picks=1, w_up=None, scatter=F
     x_rows, d_in = x.shape
     groups, d_out, _ = shape = w.shape
     m = out.shape[0]
-    p_x = _tensor("x", x, dt, x.shape, dev)
+    p_x = _first("x", x)
     p_w = _tensor("w", w, dt, (groups, d_out, d_in), dev)
     p_up = None if w_up is None else _tensor("w_up", w_up, dt, shape, dev)
     p_off = _tensor("offsets", offsets, torch.int32, (groups + 1,), dev)
@@ -519,15 +526,14 @@ def grouped_product(x, w, offsets, out, rows=None, picks=1, w_up=None, scatter=F
           p_rows, picks, p_off, p_w, p_ws, p_up, p_us, p_out, int(scatter))
 
 
-def _quant_matrix(name, x, w, scale, zero):
+def _quant_matrix(name, dev, dt, d_in, w, scale, zero):
     """(d_out, group, addresses of w, scale and zero)"""
-    dev, d_in = x.device, x.shape[1]
     shape = scale.shape
     d_out, groups = shape
     if groups < 1 or d_in % groups != 0:
         _refuse(f"scale has {groups} groups for {d_in} columns")
     return (d_out, d_in // groups, _tensor(name, w, torch.uint8, (d_out, d_in // 2), dev),
-            _tensor("its scale", scale, x.dtype, shape, dev),
+            _tensor("its scale", scale, dt, shape, dev),
             None if zero is None else _tensor("its zero", zero, torch.uint8, shape, dev))
 
 
@@ -535,13 +541,13 @@ def quant_product(x, w, scale, out, zero=None, add=None, stream=None):
     """lookme_quant_product on torch tensors: x [n, d_in], w [d_out, d_in / 2]
     uint8, scale [d_out, groups], zero [d_out, groups] uint8, add and out
     [n, d_out] (out may be add)."""
-    dev, dt = x.device, x.dtype
+    dev, dt = x.get_device(), x.dtype
     code = _dtype_code("x", x)
     if x.dim() != 2 or scale.dim() != 2:
         _refuse("x and scale have 2 dimensions")
     n, d_in = x.shape
-    p_x = _tensor("x", x, dt, x.shape, dev)
-    d_out, group, p_w, p_s, p_z = _quant_matrix("w", x, w, scale, zero)
+    p_x = _first("x", x)
+    d_out, group, p_w, p_s, p_z = _quant_matrix("w", dev, dt, d_in, w, scale, zero)
     p_out = _tensor("out", out, dt, (n, d_out), dev)
     p_add = None if add is None else _tensor("add", add, dt, (n, d_out), dev)
     _call("lookme_quant_product", dev, stream, code, n, d_in, d_out, group, p_x, p_w, p_s, p_z,
@@ -551,14 +557,14 @@ def quant_product(x, w, scale, out, zero=None, add=None, stream=None):
 def quant_swiglu(x, w_gate, s_gate, w_up, s_up, out, z_gate=None, z_up=None, stream=None):
     """lookme_quant_swiglu on torch tensors, each matrix as for quant_product;
     out [n, d_ff]."""
-    dev, dt = x.device, x.dtype
+    dev, dt = x.get_device(), x.dtype
     code = _dtype_code("x", x)
     if x.dim() != 2 or s_gate.dim() != 2 or s_up.dim() != 2:
         _refuse("x and the scales have 2 dimensions")
     n, d_in = x.shape
-    p_x = _tensor("x", x, dt, x.shape, dev)
-    d_ff, group, *gate = _quant_matrix("w_gate", x, w_gate, s_gate, z_gate)
-    d_up, group_up, *up = _quant_matrix("w_up", x, w_up, s_up, z_up)
+    p_x = _first("x", x)
+    d_ff, group, *gate = _quant_matrix("w_gate", dev, dt, d_in, w_gate, s_gate, z_gate)
+    d_up, group_up, *up = _quant_matrix("w_up", dev, dt, d_in, w_up, s_up, z_up)
     if (d_up, group_up) != (d_ff, group):
         _refuse("w_gate and w_up differ in size or group")
     p_out = _tensor("out", out, dt, (n, d_ff), dev)

@@ -472,21 +472,38 @@ struct GtLds {
   int before[2][GT_THREADS];
 };
 
+// When the longest of GT_GRID workgroups is done, in hundredths of a whole tile's
+// time, with the whole tiles dealt in turn and then the halves, in whose later
+// turns the workgroups without a tile of the last round of whole ones are first.
+template <int DT>
+__host__ __device__ __forceinline__ int64_t gt_span(int64_t whole, int64_t halves) {
+  constexpr int HALF = DT == DT_F32 ? 55 : 65;
+  const int64_t full = whole / GT_GRID * 100, busy = whole % GT_GRID, free = GT_GRID - busy;
+  if (halves <= free) return full + (busy != 0 ? 100 : halves != 0 ? HALF : 0);
+  const int64_t turn = (halves - free - 1) / GT_GRID, in = (halves - free - 1) % GT_GRID;
+  return full + (in < free ? HALF * (2 + turn) : 100 + HALF * (1 + turn));
+}
+// The whole tiles of the last round to be cut in two: all or none, whichever is
+// done earlier.
+template <int DT>
+__host__ __device__ __forceinline__ int64_t gt_cut(int64_t whole, int64_t halves) {
+  const int64_t rem = whole % GT_GRID;
+  return gt_span<DT>(whole - rem, halves + 2 * rem) < gt_span<DT>(whole, halves) ? rem : 0;
+}
+
 // The launch's tiles: a group has a row block for every 256 rows, a last one of
-// at most 128 rows as a half; when the last round of whole tiles would be at
-// most half full its tiles are cut in halves too (a round of halves takes 0.73
-// of a whole one's time).
+// at most 128 rows as a half.
 struct GtPlan {
   int64_t whole, halves, cut;   // whole tiles, the groups' own halves, whole tiles cut in two
   int64_t units;
 };
+template <int DT>
 __device__ __forceinline__ GtPlan gt_plan(int blocks, int own_halves, int tn) {
   GtPlan pl;
   const int64_t all = (int64_t)blocks * tn;
-  const int64_t rem = all % GT_GRID;
-  pl.cut = rem <= GT_GRID / 2 ? rem : 0;
-  pl.whole = all - pl.cut;
   pl.halves = (int64_t)own_halves * tn;
+  pl.cut = gt_cut<DT>(all, pl.halves);
+  pl.whole = all - pl.cut;
   pl.units = pl.whole + pl.halves + 2 * pl.cut;
   return pl;
 }
@@ -695,20 +712,25 @@ __global__ __launch_bounds__(GT_THREADS, 2) void grouped_tiles_kernel(GroupedPar
     }
   }
   __syncthreads();
-  const GtPlan pl = gt_plan(__builtin_amdgcn_readfirstlane(gl.total[0]),
-                            __builtin_amdgcn_readfirstlane(gl.total[1]), tn);
+  const GtPlan pl = gt_plan<DT>(__builtin_amdgcn_readfirstlane(gl.total[0]),
+                                __builtin_amdgcn_readfirstlane(gl.total[1]), tn);
 
-  for (int64_t k0 = 0; slot + k0 * GT_GRID < pl.units; k0 += GT_WINDOW) {
+  // this workgroup's unit number k: from the halves' second turn on those without
+  // a tile in the last round of whole ones are the first
+  const int64_t last = pl.whole / GT_GRID;
+  const int turned = (slot - (int)(pl.whole % GT_GRID)) & (GT_GRID - 1);
+  auto unit = [&](int64_t k) { return k * GT_GRID + (k > last ? turned : slot); };
+
+  for (int64_t k0 = 0; unit(k0) < pl.units; k0 += GT_WINDOW) {
     __syncthreads();
     if (threadIdx.x < GT_WINDOW) gl.tile[threadIdx.x] = make_int4(-1, 0, 0, 0);
     __syncthreads();
     // this workgroup's tiles among [lo, hi) that lie in the window
     auto mark = [&](int64_t lo, int64_t hi, auto&& where) {
-      int64_t k = lo <= slot ? 0 : (lo - slot + GT_GRID - 1) / GT_GRID;
-      for (k = k < k0 ? k0 : k; k < k0 + GT_WINDOW; ++k) {
-        const int64_t u = slot + k * GT_GRID;
+      for (int64_t k = lo / GT_GRID < k0 ? k0 : lo / GT_GRID; k < k0 + GT_WINDOW; ++k) {
+        const int64_t u = unit(k);
         if (u >= hi) break;
-        gl.tile[k - k0] = where(u - lo);
+        if (u >= lo) gl.tile[k - k0] = where(u - lo);
       }
     };
     int64_t at = gl.before[0][threadIdx.x], athalf = gl.before[1][threadIdx.x];
@@ -790,18 +812,18 @@ static void launch_mid(const GroupedParams& p, hipStream_t st) {
 // 11 rows, 2048 x 256, 7.9 and 9.0 us, float32 10.6 and 25.0; one of 128 rows, 2048
 // x 1024, 12.6 and 9.3; but not with two matrices a wave in fewer bits (4 groups of
 // 11 rows, 2048 x 256, 10.1 and 9.1, float32 17.1 and 25.4).
-// Then tiles of 32 rows, of 64 above 32 rows a group where these are enough
-// (64 rows 140 and 112 us; one group of 512 rows 14 and 18), with deep rings
-// while all tiles are resident at once (one group of 512 rows 14 us with 4
-// stages, 15 with 3; of 2048 rows on 64-row tiles 32 us with 2, 42 with 4), and
-// for float32 again where there are many (13 groups of 231 rows, 840 x 1160, 85
-// us with 2, 100 with 4; 16 of 256, 2048 x 2048, 344 and 321).
+// Then tiles of 32 rows, of 64 above 32 rows a group where these are enough (64
+// groups of 64 rows 148 and 114 us; one of 512 rows 12 and 14), with deep rings
+// while all tiles are resident at once (one group of 512 rows 12.4 us with 4
+// stages, 13.7 with 3; of 2048 rows on 64-row tiles 30.6 us with 2, 35.7 with 4),
+// and for float32 again where there are many (16 of 256 rows 309 us with 2, 301
+// with 4; 13 groups of 231 rows, 840 x 1160, 71 and 92).
 // The large tiles where their rounds cost less: one of 256 whole ones takes as
-// long as `round` 64 x 64 ones, one of halves 0.73 of that, float32 0.58 (bf16, 2048 x 2048,
-// 64-row tiles and large ones: 64 groups of 64 rows 111 and 139 us, of 128 178
-// and 151, of 256 308 and 202; 16 of 256 63 and 55; one of 2048 32 and 49;
-// e4m3 16 of 256 42 and 37, float32 16 of 256 328 and 286, 3 of 1000 rows,
-// 4096 x 4096, 853 and 776).
+// long as `round` 64 x 64 ones, one of halves 65% of that, float32 55% (2048 x
+// 2048, 64-row tiles and large ones, bf16: 64 groups of 64 rows 114 and 117 us, of
+// 96 169 and 120, of 256 293 and 170; 16 of 128 33 and 48, of 256 60 and 42; one of
+// 2048 31 and 39; e4m3 16 of 256 38 and 30, float32 309 and 268, of 512 592 and
+// 488; 64 groups of 80 rows on average 168 and 120, float32 609 and 531).
 template <int DT, bool UP>
 static hipError_t launch_grouped_dt(const GroupedParams& p, hipStream_t st) {
   const int64_t used = p.groups < p.m ? p.groups : p.m;
@@ -812,14 +834,20 @@ static hipError_t launch_grouped_dt(const GroupedParams& p, hipStream_t st) {
   constexpr int few = DT == DT_F32 ? (UP ? 256 : 512) : (UP ? 0 : 256);
   const int64_t tiles16 =
       used * ((p.m + 16 * used - 1) / (16 * used)) * (int64_t)((p.cols + 15) / 16);
-  auto rounds = [](int64_t n) { return (double)((n + GT_GRID - 1) / GT_GRID); };
-  const double round = DT == DT_F32 ? 3000. : DT == DT_E4M3 ? 2150. : 2000.;
-  const double large = rounds(p.m / 256 * tn) +
-                       (DT == DT_F32 ? 0.58 : 0.73) * rounds((used + 1) / 2 * tn);
+  // large tiles as the mean has it: up to 128 rows a half a group, up to 224 a whole
+  // one; above, where any place in a last block is as likely (float32, which loses
+  // most by a second round, above 128), a whole one for every 256 rows and for
+  // every second group a half
+  const bool half = p.m <= 128 * used, one = !half && DT != DT_F32 && p.m <= 224 * used;
+  const int64_t whole = half ? 0 : one ? used * tn : p.m * tn / 256;
+  const int64_t halves = half ? used * tn : one ? 0 : (used + 1) / 2 * tn;
+  const int64_t cut = gt_cut<DT>(whole, halves);
+  const int64_t span = gt_span<DT>(whole - cut, halves + 2 * cut);
+  const int64_t round = DT == DT_F32 ? 3340 : DT == DT_E4M3 ? 2400 : 2100;
   // (the phased kernel's lane offsets are 32-bit)
   const bool near = p.k_bytes < (4 << 20) &&
                     (p.picks == 0 || p.x_rows * p.k_bytes < ((int64_t)1 << 32));
-  if (p.m > 64 * used && large * round < (double)tiles64 && p.k_bytes >= 128 && near)
+  if (span * round < 100 * tiles64 && p.k_bytes >= 128 && near)
     hipLaunchKernelGGL((grouped_tiles_kernel<DT, UP>), dim3(GT_GRID), dim3(GT_THREADS), 0, st, p);
   else if (p.m <= (DT == DT_F32 ? 8 : 4) * used || tiles16 <= few)
     launch_rows<DT, UP>(p, st);

@@ -302,6 +302,19 @@ def test_grouped_kernels_gather_and_scatter(lk, dtype, sizes, d_in, d_out):
     _grouped_case(lk, dtype, sizes, d_in, d_out, False, 2, True, m=sum(sizes) + 30)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("up", [False, True])
+@pytest.mark.parametrize("sizes,d_in,d_out", [
+    ([100, 60, 128, 127, 129, 1, 0, 155] * 8, 144, 1000),
+    ([100, 60, 128, 127, 129, 1, 0, 155] * 8, 1184, 1000),
+    ([600, 424, 513, 511, 128, 896, 129, 895] * 2, 144, 4096),
+    ([300, 260, 200, 513, 17] * 6, 1040, 2056)])
+def test_grouped_large_tiles(lk, dtype, up, sizes, d_in, d_out):
+    """whole and half tiles, cut and not, in every type"""
+    _grouped_case(lk, dtype, sizes, d_in, d_out, up)
+    _grouped_case(lk, dtype, sizes, d_in, d_out, up, 2, True, m=sum(sizes) + 7)
+
+
 @pytest.mark.parametrize("rows,d_out,d_in", [(1, 160, 16), (5, 320, 16), (40, 320, 16)])
 def test_grouped_more_tiles_than_a_launch_has_workgroups(lk, rows, d_out, d_in):
     """the few-rows and ring kernels in several passes"""

@@ -115,6 +115,28 @@ def test_norm_outputs(lk, dtype, d, kw):
                             False, **kw))
 
 
+def test_norm_of_more_rows_than_a_launch(lk):
+    """rows in several launches, every operand moved on"""
+    block, times, d = 4099, 2050, 8   # over 2^23 rows
+    g = torch.Generator().manual_seed(4)
+    h = torch.randn((block, d), generator=g).to(BF).cuda()
+    a = torch.randn((block, 2, d), generator=g).to(BF).cuda()
+    w = torch.rand((block, 2), generator=g).cuda()
+
+    def run(h, a, w):
+        n = h.shape[0]
+        o, ho = (torch.empty((n, d), dtype=BF, device="cuda") for _ in range(2))
+        q = torch.empty((n, d), dtype=torch.float8_e4m3fn, device="cuda")
+        sc = torch.empty(n, device="cuda")
+        lk.residual_norm(h, add=a, part_w=w, hidden_out=ho, out=o, out_quant=q, scale_out=sc)
+        return ho, o, q.view(torch.uint8), sc
+
+    want = run(h, a, w)
+    got = run(h.repeat(times, 1), a.repeat(times, 1, 1), w.repeat(times, 1))
+    for x, y in zip(got, want):
+        assert (x.view(times, *y.shape) == y).all()
+
+
 @pytest.mark.parametrize("d", [512, 40000])
 def test_norm_leaves_out_parts_of_weight_zero(lk, d):
     """the rows of such parts may hold anything; all of them left out is H"""

@@ -11,11 +11,11 @@
 // the run again, where the list ran full) a wave counts the entries of each
 // group; a prefix sum over groups and waves gives every run its first slot in
 // each group, and a last pass over the list hands them out.
-// What bounds it is the instructions a CU issues for each id: for one of
-// another range two comparisons and two scalar counts for 64 of them (262144 ids
-// in 1024 groups alike 24 us, 11 TB/s out of L2; with Zipf(1) groups 50, the first
-// range having a quarter of the ids, more than its lists hold; 512 ids in 128
-// groups 4.1).
+// What bounds it is the instructions a CU issues for each id: for 64 of another
+// range a subtraction, whose borrow is the count of those below, an addition and
+// a comparison (262144 ids in 1024 groups alike 21 us, 13 TB/s out of L2; with
+// Zipf(1) groups 45, the largest being an eighth of the ids; 512 ids in 128 groups
+// 4.1).
 // The result does not depend on timing: counts are sums, and a run's slots are
 // handed out by its own wave alone.
 #include "common.h"
@@ -50,7 +50,7 @@ __global__ __launch_bounds__(GR_THREADS) void group_rows_kernel(
   const int g0 = (int)(blockIdx.x / segments) * range;
   const int seg = blockIdx.x % segments;
   const int size = groups - g0 < range ? groups - g0 : range;
-  const unsigned lo = (unsigned)g0, hi = (unsigned)(g0 + size);
+  const unsigned lo = (unsigned)g0, span = (unsigned)size;
 
   // steps of GR_STEP entries: the segment's, dealt to the waves in runs (a run
   // is at most 2^26 entries), and the others, dealt one by one
@@ -74,16 +74,17 @@ __global__ __launch_bounds__(GR_THREADS) void group_rows_kernel(
       for (int k = 0; k < GR_LOADS; ++k) v[k] = s + 64 * k + lane < n ? p[64 * k] : -1;
     }
   };
-  int less = 0, early = 0, listed = 0;   // the same in every lane
+  // a lane's ids below the range, and of the range ahead of the segment; the run's
+  // entries of the range (the same in every lane)
+  int lane_less = 0, lane_early = 0, listed = 0;
   for (int step = wv; step < steps; step += GR_WAVES) {
     if (step >= seg0 && step < seg1) continue;
     int v[GR_LOADS];
     load(step, v);
 #pragma unroll
     for (int k = 0; k < GR_LOADS; ++k) {
-      const uint64_t lower = __ballot((unsigned)v[k] < lo);
-      less += __popcll(lower);
-      if (step < seg0) early += __popcll(__ballot((unsigned)v[k] < hi) & ~lower);
+      lane_less += (unsigned)v[k] < lo ? 1 : 0;
+      if (step < seg0) lane_early += (unsigned)v[k] - lo < span ? 1 : 0;
     }
   }
   for (int step = run0; step < run1; ++step) {
@@ -91,15 +92,15 @@ __global__ __launch_bounds__(GR_THREADS) void group_rows_kernel(
     load(step, v);
 #pragma unroll
     for (int k = 0; k < GR_LOADS; ++k) {
-      const uint64_t lower = __ballot((unsigned)v[k] < lo);
-      const uint64_t mine = __ballot((unsigned)v[k] < hi) & ~lower;
-      less += __popcll(lower);
+      lane_less += (unsigned)v[k] < lo ? 1 : 0;
+      const unsigned j = (unsigned)v[k] - lo;   // group in the range
+      const uint64_t mine = __ballot(j < span);
       if (mine != 0) {
-        // (entry << 6 plus the group, in one addition of a scalar)
-        if (listed <= GR_LIST - 64 && __builtin_amdgcn_inverse_ballot_w64(mine))
-          list[wv][gr_slot(mine, listed)] =
-              (uint32_t)(lane << 6) + (uint32_t)v[k] +
-              (((uint32_t)((step - run0) * GR_STEP + 64 * k) << 6) - (uint32_t)g0);
+        // (a full list is written over at its end, and not read)
+        const int at = listed < GR_LIST - 64 ? listed : GR_LIST - 64;
+        if (__builtin_amdgcn_inverse_ballot_w64(mine))
+          list[wv][gr_slot(mine, at)] =
+              j + (uint32_t)(lane << 6) + ((uint32_t)((step - run0) * GR_STEP + 64 * k) << 6);
         listed += __popcll(mine);
       }
     }
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(GR_THREADS) void group_rows_kernel(
         load(step, v);
 #pragma unroll
         for (int k = 0; k < GR_LOADS; ++k)
-          fn((unsigned)v[k] >= lo && (unsigned)v[k] < hi, v[k] - g0,
+          fn((unsigned)v[k] - lo < span, v[k] - g0,
              step * GR_STEP + 64 * k + lane);
       }
     }
@@ -149,7 +150,8 @@ __global__ __launch_bounds__(GR_THREADS) void group_rows_kernel(
     });
   }
   cnt[wv][lane] = count;
-  if (lane == 0) {
+  const int less = wave_scan_incl(lane_less), early = wave_scan_incl(lane_early);
+  if (lane == 63) {
     below[wv] = less;
     ahead[wv] = early;
   }

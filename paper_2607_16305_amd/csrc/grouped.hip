@@ -48,7 +48,8 @@ __device__ __forceinline__ void gp_rows(const GroupedParams& p, int g, int64_t& 
 }
 
 // Tile number which(total) in the groups' order, count(rows) tiles a group; all
-// threads of the block.  t.g is -1 past the last tile.
+// threads of the block, which pass a barrier before the next call.  t.g is -1 past
+// the last tile.
 template <int THREADS, class Count, class Which>
 __device__ __forceinline__ void find_tile(const GroupedParams& p, int* lds, GpTile& t,
                                           Count&& count, Which&& which) {
@@ -56,37 +57,43 @@ __device__ __forceinline__ void find_tile(const GroupedParams& p, int* lds, GpTi
   const int first = threadIdx.x * per;
   const int last = first + per < p.groups ? first + per : p.groups;
   int sum = 0;
+  int64_t a = 0, b = 0;
   for (int g = first; g < last; ++g) {
-    int64_t a, b;
     gp_rows(p, g, a, b);
     sum += count(b - a);
   }
   if (threadIdx.x == 0) lds[0] = -1;
-  const int incl = block_scan_incl<THREADS / 64>(sum, lds + 3);
-  if (threadIdx.x == THREADS - 1) lds[2] = incl;
+  int incl = wave_scan_incl(sum), total = 0;
+  if ((threadIdx.x & 63) == 63) lds[4 + threadIdx.x / 64] = incl;
   __syncthreads();
-  const int unit = which(__builtin_amdgcn_readfirstlane(lds[2]));
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    const int s = lds[4 + w];
+    incl += w < (int)(threadIdx.x / 64) ? s : 0;
+    total += s;
+  }
+  const int unit = which(__builtin_amdgcn_readfirstlane(total));
   int at = incl - sum;
   if (at <= unit && unit < incl) {
-    for (int g = first; g < last; ++g) {
-      int64_t a, b;
-      gp_rows(p, g, a, b);
+    int g = first;
+    for (; g < last; ++g) {
+      if (per != 1) gp_rows(p, g, a, b);   // (else they are at hand)
       const int c = count(b - a);
-      if (unit < at + c) {
-        lds[0] = g;
-        lds[1] = unit - at;
-        break;
-      }
+      if (unit < at + c) break;
       at += c;
     }
+    lds[0] = g;
+    lds[1] = unit - at;
+    lds[2] = (int)a;   // at most 2^30
+    lds[3] = (int)b;
   }
   __syncthreads();
   t.g = __builtin_amdgcn_readfirstlane(lds[0]);
   t.idx = __builtin_amdgcn_readfirstlane(lds[1]);
-  __syncthreads();
-  if (t.g >= 0) gp_rows(p, t.g, t.a, t.b);
+  t.a = __builtin_amdgcn_readfirstlane(lds[2]);
+  t.b = __builtin_amdgcn_readfirstlane(lds[3]);
 }
-constexpr int GP_FIND_LDS = 3 + 16;
+constexpr int GP_FIND_LDS = 4 + 4;   // (of blocks of four waves)
 // Most workgroups of a launch: the number of tiles is the device's, and a launch
 // is for the most there can be, in passes of this many.
 constexpr int64_t GP_GRID = 65536;

@@ -39,53 +39,88 @@ struct GpTile {
   int64_t a, b;    // rows of the group
 };
 
-// rows [a, b) of group g, kept inside [0, m) whatever the offsets hold
-__device__ __forceinline__ void gp_rows(const GroupedParams& p, int g, int64_t& a, int64_t& b) {
+// rows [a, b) of group g, kept inside [0, m) whatever the offsets hold (m is at
+// most 2^30)
+__device__ __forceinline__ void gp_rows(const GroupedParams& p, int g, int& a, int& b) {
+  const int m = (int)p.m;
   a = p.offsets[g];
   b = p.offsets[g + 1];
-  a = a < 0 ? 0 : (a > p.m ? p.m : a);
-  b = b < a ? a : (b > p.m ? p.m : b);
+  a = a < 0 ? 0 : (a > m ? m : a);
+  b = b < a ? a : (b > m ? m : b);
 }
 
 // Tile number which(total) in the groups' order, count(rows) tiles a group; all
 // threads of the block, which pass a barrier before the next call.  t.g is -1 past
-// the last tile.
+// the last tile.  A wave counts a run of groups, 64 neighbours at a time; the one
+// that has the tile goes through its run again.  (A thread's groups side by side
+// are a load of 64 lines each: 4000 groups of one row, 256 x 512, 502 us, 368 so.)
 template <int THREADS, class Count, class Which>
 __device__ __forceinline__ void find_tile(const GroupedParams& p, int* lds, GpTile& t,
                                           Count&& count, Which&& which) {
+  const int lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int per = (p.groups + THREADS - 1) / THREADS;
-  const int first = threadIdx.x * per;
-  const int last = first + per < p.groups ? first + per : p.groups;
+  const int first = wv * 64 * per + lane;
+  int a = 0, b = 0;
+  // tiles of group g; its rows in (a, b).  No branch, so that several groups'
+  // loads are in flight.
+  auto tiles = [&](int g) {
+    gp_rows(p, g < p.groups ? g : p.groups - 1, a, b);
+    return g < p.groups ? count(b - a) : 0;
+  };
   int sum = 0;
-  int64_t a = 0, b = 0;
-  for (int g = first; g < last; ++g) {
-    gp_rows(p, g, a, b);
-    sum += count(b - a);
+  int k = 0;
+  for (; k + 8 <= per; k += 8) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sum += tiles(first + 64 * (k + u));
   }
+  for (; k < per; ++k) sum += tiles(first + 64 * k);
   if (threadIdx.x == 0) lds[0] = -1;
-  int incl = wave_scan_incl(sum), total = 0;
-  if ((threadIdx.x & 63) == 63) lds[4 + threadIdx.x / 64] = incl;
+  const int incl = wave_scan_incl(sum);
+  if (lane == 63) lds[4 + wv] = incl;
   __syncthreads();
+  int before = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < THREADS / 64; ++w) {
     const int s = lds[4 + w];
-    incl += w < (int)(threadIdx.x / 64) ? s : 0;
+    before += w < wv ? s : 0;
     total += s;
   }
   const int unit = which(__builtin_amdgcn_readfirstlane(total));
-  int at = incl - sum;
-  if (at <= unit && unit < incl) {
-    int g = first;
-    for (; g < last; ++g) {
-      if (per != 1) gp_rows(p, g, a, b);   // (else they are at hand)
-      const int c = count(b - a);
-      if (unit < at + c) break;
-      at += c;
+  int left = unit - __builtin_amdgcn_readfirstlane(before);   // in this wave's run
+  if (left >= 0 && left < lds[4 + wv]) {
+    int c = sum, end = incl, g = first;
+    if (per != 1) {
+      bool found = false;
+      for (int q = 0; q < per && !found; q += 4) {
+        int c4[4], a4[4], b4[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          c4[u] = tiles(first + 64 * (q + u));
+          a4[u] = a;
+          b4[u] = b;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (found) continue;
+          c = c4[u];
+          a = a4[u];
+          b = b4[u];
+          g = first + 64 * (q + u);
+          end = wave_scan_incl(c);
+          const int all = __builtin_amdgcn_readlane(end, 63);
+          found = left < all;
+          left -= found ? 0 : all;
+        }
+      }
+      if (!found) c = end = 0;   // (never, while nobody changes the offsets)
     }
-    lds[0] = g;
-    lds[1] = unit - at;
-    lds[2] = (int)a;   // at most 2^30
-    lds[3] = (int)b;
+    if (end - c <= left && left < end) {
+      lds[0] = g;
+      lds[1] = left - (end - c);
+      lds[2] = a;
+      lds[3] = b;
+    }
   }
   __syncthreads();
   t.g = __builtin_amdgcn_readfirstlane(lds[0]);
@@ -128,6 +163,7 @@ __device__ __forceinline__ float gp_value(float c, float u, float xs, float ws, 
 // few rows a group
 // ---------------------------------------------------------------------------
 constexpr int GS_THREADS = 256, GS_WAVES = 4;
+constexpr int64_t GS_BLOCKS = 8192;   // of a launch, above which each takes more
 
 // KS: waves that share the K of 16 weight rows; the workgroup's other waves take
 // other rows.  Two steps (64 bytes of K) are in flight a wave: more registers
@@ -152,14 +188,17 @@ __global__ __launch_bounds__(GS_THREADS) void grouped_rows_kernel(GroupedParams 
   const int s0 = kp * per;
   const int s1 = s0 + per < steps ? s0 + per : steps;
 
+  const int cblocks = (tiles_n + p.span - 1) / p.span;
+
   for (int64_t unit = blockIdx.x;; unit += gridDim.x) {
-    const int row_tile = (int)(unit / tiles_n);
+    const int row_tile = (int)(unit / cblocks);
     GpTile t;
     find_tile<GS_THREADS>(
-        p, find_lds, t, [](int64_t r) { return (int)((r + 15) / 16); },
+        p, find_lds, t, [](int r) { return (int)((unsigned)(r + 15) / 16); },
         [row_tile](int) { return row_tile; });
     if (t.g < 0) return;
-    const int c0 = (int)(unit - (int64_t)row_tile * tiles_n) * COLS + 16 * (wv / KS);
+    const int t0 = (int)(unit - (int64_t)row_tile * cblocks) * p.span;
+    const int t1 = t0 + p.span < tiles_n ? t0 + p.span : tiles_n;
 
     int64_t i = t.a + (int64_t)t.idx * 16 + n16, src, dst;
     const bool in = i < t.b;
@@ -167,75 +206,82 @@ __global__ __launch_bounds__(GS_THREADS) void grouped_rows_kernel(GroupedParams 
     const bool ok = gp_entry(p, i, src, dst) && in;
     const char* xp = p.x + src * p.k_bytes;
     const float xs = DT == DT_E4M3 ? p.x_scale[src] : 1.f;
-    const int wc = c0 + n16 < p.cols ? c0 + n16 : p.cols - 1;
-    const int64_t wrow = ((int64_t)t.g * p.cols + wc) * p.k_bytes;
-    const char* wp[MATS];
-    wp[0] = p.w + wrow;
-    if constexpr (UP) wp[1] = p.w_up + wrow;
 
-    f32x4_t acc[MATS];
+    for (int ct = t0; ct < t1; ++ct) {
+      const int c0 = ct * COLS + 16 * (wv / KS);
+      const int wc = c0 + n16 < p.cols ? c0 + n16 : p.cols - 1;
+      const int64_t wrow = ((int64_t)t.g * p.cols + wc) * p.k_bytes;
+      const char* wp[MATS];
+      wp[0] = p.w + wrow;
+      if constexpr (UP) wp[1] = p.w_up + wrow;
+
+      f32x4_t acc[MATS];
 #pragma unroll
-    for (int q = 0; q < MATS; ++q) acc[q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    u32x4_t fw[D][MATS], fx[D];
-    // unconditional loads from clamped addresses; chunks past K count as zero
-    auto load = [&](int d, int s) {
-      int c = 4 * s + g;
-      c = c < chunks ? c : chunks - 1;
+      for (int q = 0; q < MATS; ++q) acc[q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      u32x4_t fw[D][MATS], fx[D];
+      // unconditional loads from clamped addresses; chunks past K count as zero
+      auto load = [&](int d, int s) {
+        int c = 4 * s + g;
+        c = c < chunks ? c : chunks - 1;
 #pragma unroll
-      for (int q = 0; q < MATS; ++q) fw[d][q] = ld16(wp[q] + (int64_t)c * 16);
-      fx[d] = ld16(xp + (int64_t)c * 16);
-    };
-    if (s0 < s1) {
-#pragma unroll
-      for (int d = 0; d < D; ++d) {
-        load(d, s0 + d);
-        asm volatile("" ::: "memory");
-      }
-      for (int s = s0; s < s1; s += D) {
+        for (int q = 0; q < MATS; ++q) fw[d][q] = ld16(wp[q] + (int64_t)c * 16);
+        fx[d] = ld16(xp + (int64_t)c * 16);
+      };
+      if (s0 < s1) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
-          const bool live = s + d < s1 && 4 * (s + d) + g < chunks;
-          const u32x4_t none = {0, 0, 0, 0};
-          u32x4_t w[MATS];
+          load(d, s0 + d);
+          asm volatile("" ::: "memory");
+        }
+        for (int s = s0; s < s1; s += D) {
 #pragma unroll
-          for (int q = 0; q < MATS; ++q) w[q] = live ? fw[d][q] : none;
-          const u32x4_t x = live ? fx[d] : none;
-          load(d, s + d + D);
+          for (int d = 0; d < D; ++d) {
+            const bool live = s + d < s1 && 4 * (s + d) + g < chunks;
+            const u32x4_t none = {0, 0, 0, 0};
+            u32x4_t w[MATS];
 #pragma unroll
-          for (int q = 0; q < MATS; ++q) acc[q] = mfma_chunk<DT>(w[q], x, acc[q]);
+            for (int q = 0; q < MATS; ++q) w[q] = live ? fw[d][q] : none;
+            const u32x4_t x = live ? fx[d] : none;
+            load(d, s + d + D);
+#pragma unroll
+            for (int q = 0; q < MATS; ++q) acc[q] = mfma_chunk<DT>(w[q], x, acc[q]);
+          }
         }
       }
-    }
-    f32x4_t* mine = part + wv * (MATS * 64) + lane;
-    if (kp != 0) {
+      f32x4_t* mine = part + wv * (MATS * 64) + lane;
+      if (kp != 0) {
 #pragma unroll
-      for (int q = 0; q < MATS; ++q) mine[q * 64] = acc[q];
-    }
-    __syncthreads();   // (the next unit's find_tile keeps its writes behind these reads)
-    if (kp != 0) continue;
-#pragma unroll
-    for (int o = 1; o < KS; ++o)
-#pragma unroll
-      for (int q = 0; q < MATS; ++q) {
-        const f32x4_t v = mine[(o * MATS + q) * 64];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[q][r] += v[r];
+        for (int q = 0; q < MATS; ++q) mine[q * 64] = acc[q];
       }
-    // the lane holds columns c0 + 4 g + r of its token's row (cols is a multiple
-    // of 4)
-    const int col = c0 + 4 * g;
-    if (col >= p.cols || !ok) continue;
-    f32x4_t ws = {1.f, 1.f, 1.f, 1.f}, us = ws;
-    if constexpr (DT == DT_E4M3) {
-      const int64_t s = (int64_t)t.g * p.cols + col;
-      ws = *reinterpret_cast<const f32x4_t*>(p.w_scale + s);
-      if constexpr (UP) us = *reinterpret_cast<const f32x4_t*>(p.up_scale + s);
-    }
-    float v[4];
+      __syncthreads();
+      if (kp == 0) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      v[r] = gp_value<DT, UP>(acc[0][r], UP ? acc[MATS - 1][r] : 0.f, xs, ws[r], us[r]);
-    st_cols<ODT, 4>(p.out + (dst * p.cols + col) * OES, v);
+        for (int o = 1; o < KS; ++o)
+#pragma unroll
+          for (int q = 0; q < MATS; ++q) {
+            const f32x4_t v = mine[(o * MATS + q) * 64];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[q][r] += v[r];
+          }
+        // the lane holds columns c0 + 4 g + r of its token's row (cols is a multiple
+        // of 4)
+        const int col = c0 + 4 * g;
+        if (col < p.cols && ok) {
+          f32x4_t ws = {1.f, 1.f, 1.f, 1.f}, us = ws;
+          if constexpr (DT == DT_E4M3) {
+            const int64_t s = (int64_t)t.g * p.cols + col;
+            ws = *reinterpret_cast<const f32x4_t*>(p.w_scale + s);
+            if constexpr (UP) us = *reinterpret_cast<const f32x4_t*>(p.up_scale + s);
+          }
+          float v[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            v[r] = gp_value<DT, UP>(acc[0][r], UP ? acc[MATS - 1][r] : 0.f, xs, ws[r], us[r]);
+          st_cols<ODT, 4>(p.out + (dst * p.cols + col) * OES, v);
+        }
+      }
+      if (ct + 1 < t1) __syncthreads();   // (the next unit has find_tile's barriers)
+    }
   }
 }
 
@@ -282,7 +328,7 @@ __global__ __launch_bounds__(GM_THREADS) void grouped_mid_kernel(GroupedParams p
     // share its weights), neighbours on one XCD
     GpTile t;
     find_tile<GM_THREADS>(
-        p, find_lds, t, [tn](int64_t r) { return (int)((r + RT - 1) / RT) * tn; },
+        p, find_lds, t, [tn](int r) { return (int)((unsigned)(r + RT - 1) / RT) * tn; },
         [&](int total) {
           const int64_t left = total - base;
           const int n = (int)(left < (int64_t)gridDim.x ? left : (int64_t)gridDim.x);
@@ -559,8 +605,9 @@ __device__ __forceinline__ void grouped_tile(const GroupedParams& p, char* lds, 
   // a reload inside the stage loop waits for every load in flight
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));
-  int64_t ga, gb;
-  gp_rows(p, grp, ga, gb);
+  int ra, rb;
+  gp_rows(p, grp, ra, rb);
+  const int64_t ga = ra, gb = rb;
   __syncthreads();   // the tile before this one is done with its rows and stages
   if (tid < S::BM) {
     int64_t i = ga + m0 + tid, src, dst;
@@ -707,9 +754,9 @@ __global__ __launch_bounds__(GT_THREADS, 2) void grouped_tiles_kernel(GroupedPar
   // this thread's groups and the numbers of row blocks before them
   const int per = (p.groups + GT_THREADS - 1) / GT_THREADS;
   auto blocks = [&](int g, int& whole, int& half) {
-    int64_t a, b;
+    int a, b;
     gp_rows(p, g, a, b);
-    const int r = (int)(b - a), rem = r & 255;
+    const int r = b - a, rem = r & 255;
     half = rem > 0 && rem <= 128 ? 1 : 0;
     whole = (r >> 8) + (rem > 128 ? 1 : 0);
   };
@@ -793,19 +840,30 @@ __global__ __launch_bounds__(GT_THREADS, 2) void grouped_tiles_kernel(GroupedPar
 }
 
 // K over two waves, or over four where that is long (16 rows of one in 16
-// matrices of 4096 x 4096 114 -> 93 us) or the workgroups are few.
+// matrices of 4096 x 4096 114 -> 93 us) or the workgroups are few.  Where these
+// would be many, each takes several column tiles for the row tile it has found
+// (4000 groups of one row, 256 x 512, one column tile a workgroup and four: 368
+// and 252 us; from 4096 workgroups on 2 rows in 64 groups of 2048 x 2048 take 102
+// us instead of 90).
 template <int DT, bool UP>
-static void launch_rows(const GroupedParams& p, hipStream_t st) {
+static void launch_rows(GroupedParams p, hipStream_t st) {
   const int64_t most = p.m / 16 + p.groups;   // row tiles: one a group, one for each 16 rows
   const int64_t tiles = most < p.m ? most : p.m;
   auto grid = [&](int cols) {
-    const int64_t n = tiles * ((p.cols + cols - 1) / cols);
+    const int64_t tn = (p.cols + cols - 1) / cols;
+    int64_t blocks = GS_BLOCKS / tiles;
+    blocks = blocks < 1 ? 1 : blocks < tn ? blocks : tn;
+    p.span = (int)((tn + blocks - 1) / blocks);
+    const int64_t n = tiles * ((tn + p.span - 1) / p.span);
     return dim3((unsigned)(n < GP_GRID ? n : GP_GRID));
   };
-  if (p.k_bytes >= 8192 || tiles * ((p.cols + 31) / 32) < 1024)
-    hipLaunchKernelGGL((grouped_rows_kernel<DT, 4, UP>), grid(16), dim3(GS_THREADS), 0, st, p);
-  else
-    hipLaunchKernelGGL((grouped_rows_kernel<DT, 2, UP>), grid(32), dim3(GS_THREADS), 0, st, p);
+  if (p.k_bytes >= 8192 || tiles * ((p.cols + 31) / 32) < 1024) {
+    const dim3 n = grid(16);
+    hipLaunchKernelGGL((grouped_rows_kernel<DT, 4, UP>), n, dim3(GS_THREADS), 0, st, p);
+  } else {
+    const dim3 n = grid(32);
+    hipLaunchKernelGGL((grouped_rows_kernel<DT, 2, UP>), n, dim3(GS_THREADS), 0, st, p);
+  }
 }
 
 template <int DT, int NS, int TI, bool UP>

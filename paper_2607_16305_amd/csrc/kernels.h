@@ -314,6 +314,7 @@ struct GroupedParams {
   int groups, cols;
   int picks;                 // entry i reads row rows[i] / picks; 0: row i
   bool scatter;              // its output goes to row rows[i]; else to row i
+  int span;                  // column tiles of a workgroup (set by the launch)
 };
 constexpr int GROUPED_E4M3 = 2;   // dt of e4m3 operands (out in bf16)
 hipError_t launch_grouped(int dt, const GroupedParams& p, hipStream_t st);

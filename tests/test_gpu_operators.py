@@ -337,6 +337,16 @@ def test_grouped_large_tiles(lk, dtype, up, sizes, d_in, d_out):
     _grouped_case(lk, dtype, sizes, d_in, d_out, up, 2, True, m=sum(sizes) + 7)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("up", [False, True])
+@pytest.mark.parametrize("sizes", [[1, 0, 2] * 500, [0] * 700 + [3, 1] + [0] * 900 + [17] * 6 + [1],
+                                   [2] * 257, [40, 0, 25] * 300])
+def test_grouped_many_groups(lk, dtype, up, sizes):
+    """more groups than threads, and several column tiles a workgroup"""
+    _grouped_case(lk, dtype, sizes, 32, 520, up)
+    _grouped_case(lk, dtype, sizes, 32, 520, up, 2, True, m=sum(sizes) + 5)
+
+
 @pytest.mark.parametrize("rows,d_out,d_in", [(1, 160, 16), (5, 320, 16), (40, 320, 16)])
 def test_grouped_more_tiles_than_a_launch_has_workgroups(lk, rows, d_out, d_in):
     """the few-rows and ring kernels in several passes"""

@@ -859,10 +859,10 @@ static void launch_rows(GroupedParams p, hipStream_t st) {
   };
   if (p.k_bytes >= 8192 || tiles * ((p.cols + 31) / 32) < 1024) {
     const dim3 n = grid(16);
-    hipLaunchKernelGGL((grouped_rows_kernel<DT, 4, UP>), n, dim3(GS_THREADS), 0, st, p);
+    launch_kernel(grouped_rows_kernel<DT, 4, UP>, n, dim3(GS_THREADS), 0, st, p);
   } else {
     const dim3 n = grid(32);
-    hipLaunchKernelGGL((grouped_rows_kernel<DT, 2, UP>), n, dim3(GS_THREADS), 0, st, p);
+    launch_kernel(grouped_rows_kernel<DT, 2, UP>, n, dim3(GS_THREADS), 0, st, p);
   }
 }
 
@@ -872,9 +872,8 @@ static void launch_mid(const GroupedParams& p, hipStream_t st) {
   const int64_t most = p.m / RT + p.groups;
   int64_t tiles = (most < p.m ? most : p.m) * ((p.cols + COLS - 1) / COLS);
   tiles = (tiles + 7) / 8 * 8;   // xcd_remap deals whole rounds over the XCDs
-  hipLaunchKernelGGL((grouped_mid_kernel<DT, NS, TI, UP>),
-                     dim3((unsigned)(tiles < GP_GRID ? tiles : GP_GRID)), dim3(GM_THREADS), 0, st,
-                     p);
+  launch_kernel(grouped_mid_kernel<DT, NS, TI, UP>,
+                dim3((unsigned)(tiles < GP_GRID ? tiles : GP_GRID)), dim3(GM_THREADS), 0, st, p);
 }
 
 // The host knows the groups' number and their rows together, so the rules go
@@ -924,7 +923,7 @@ static hipError_t launch_grouped_dt(const GroupedParams& p, hipStream_t st) {
   const bool near = p.k_bytes < (4 << 20) &&
                     (p.picks == 0 || p.x_rows * p.k_bytes < ((int64_t)1 << 32));
   if (span * round < 100 * tiles64 && p.k_bytes >= 128 && near)
-    hipLaunchKernelGGL((grouped_tiles_kernel<DT, UP>), dim3(GT_GRID), dim3(GT_THREADS), 0, st, p);
+    launch_kernel(grouped_tiles_kernel<DT, UP>, dim3(GT_GRID), dim3(GT_THREADS), 0, st, p);
   else if (p.m <= (DT == DT_F32 ? 8 : 4) * used || tiles16 <= few)
     launch_rows<DT, UP>(p, st);
   else if (p.m <= 32 * used || tiles64 <= 256) {

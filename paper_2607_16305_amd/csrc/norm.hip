@@ -307,9 +307,9 @@ static void launch_norm_t(const NormParams& p, hipStream_t st) {
   const int64_t rows = BLOCK / T;
   const dim3 grid((unsigned)((p.n + rows - 1) / rows));
   if (p.parts == 1)
-    hipLaunchKernelGGL((residual_norm_kernel<DT, T, CH, true>), grid, dim3(BLOCK), 0, st, p);
+    launch_kernel(residual_norm_kernel<DT, T, CH, true>, grid, dim3(BLOCK), 0, st, p);
   else
-    hipLaunchKernelGGL((residual_norm_kernel<DT, T, CH, false>), grid, dim3(BLOCK), 0, st, p);
+    launch_kernel(residual_norm_kernel<DT, T, CH, false>, grid, dim3(BLOCK), 0, st, p);
 }
 
 // A wave a row while that is two chunks a thread, else 256 threads; 1024 while
@@ -328,8 +328,7 @@ static void launch_norm(const NormParams& p, hipStream_t st) {
   else if (p.chunks <= 1024) launch_norm_t<DT, 256, 4>(p, st);
   else if (p.chunks <= 2048) launch_norm_t<DT, 256, 8>(p, st);
   else
-    hipLaunchKernelGGL((residual_norm_wide_kernel<DT>), dim3((unsigned)p.n), dim3(RN_THREADS), 0,
-                       st, p);
+    launch_kernel(residual_norm_wide_kernel<DT>, dim3((unsigned)p.n), dim3(RN_THREADS), 0, st, p);
 }
 
 hipError_t launch_residual_norm(int dt, int64_t n, int d, const void* hidden, int parts,

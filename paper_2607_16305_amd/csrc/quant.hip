@@ -310,11 +310,9 @@ static void launch_quant_nt(const QuantParams& p, hipStream_t st) {
                 "dynamic LDS of a launch");
   const size_t lds = scales > sums ? scales : sums;
   if (p.group < 128)
-    hipLaunchKernelGGL((quant_rows_kernel<DT, NT, RW, UP, true>), grid, dim3(QP_THREADS), lds,
-                       st, p);
+    launch_kernel(quant_rows_kernel<DT, NT, RW, UP, true>, grid, dim3(QP_THREADS), lds, st, p);
   else
-    hipLaunchKernelGGL((quant_rows_kernel<DT, NT, RW, UP, false>), grid, dim3(QP_THREADS), lds,
-                       st, p);
+    launch_kernel(quant_rows_kernel<DT, NT, RW, UP, false>, grid, dim3(QP_THREADS), lds, st, p);
 }
 
 // Two row tiles a wave where these are a workgroup for every CU: the tokens,

@@ -396,11 +396,12 @@ def _refuse(msg):
     raise LookmeError(LOOKME_ERR_INVALID, msg)
 
 
-def _tensor(name, t, dtype, shape, device):
-    """t's address; refuses another type, shape or device (an index, as of
-    Tensor.get_device), and strides."""
-    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
-        return t.data_ptr()
+# The helpers below check their tensors in place, and call this for what it says
+# where one is not as it must be: a call a tensor is 0.1 us of the 6 that a whole
+# call takes on the host, 2.6 of them the launch.
+def _wrong(name, t, dtype, shape, device):
+    """refuses tensor t for its type, shape, device (an index, as of
+    Tensor.get_device) or strides"""
     if t.dtype is not dtype:
         _refuse(f"{name} is {t.dtype}, not {dtype}")
     if t.shape != shape:
@@ -410,17 +411,18 @@ def _tensor(name, t, dtype, shape, device):
     _refuse(f"{name} is not contiguous")
 
 
-def _first(name, t):
-    """the address of the tensor that gives type, sizes and device"""
-    if not t.is_contiguous():
-        _refuse(f"{name} is not contiguous")
+def _tensor(name, t, dtype, shape, device):
+    """t's address, for the rarer tensors"""
+    if (t.dtype is not dtype or t.shape != shape or t.get_device() != device
+            or not t.is_contiguous()):
+        _wrong(name, t, dtype, shape, device)
     return t.data_ptr()
 
 
-def _dtype_code(name, t):
-    code = DTYPE_CODE.get(t.dtype)
+def _dtype_code(name, dtype):
+    code = DTYPE_CODE.get(dtype)
     if code is None:
-        _refuse(f"{name} is {t.dtype}: float32 or bfloat16")
+        _refuse(f"{name} is {dtype}: float32 or bfloat16")
     return code
 
 
@@ -444,35 +446,50 @@ def residual_norm(hidden, weight=None, eps=1e-6, add=None, part_w=None, hidden_o
     [n, parts, d]; part_w [n, parts] float32; weight [d]; the outputs
     hidden_out (may be hidden), out [n, d], out_quant [n, d] float8_e4m3fn
     with scale_out [n] float32."""
-    dev, dt = hidden.get_device(), hidden.dtype
-    code = _dtype_code("hidden", hidden)
-    if hidden.dim() != 2:
-        _refuse(f"hidden has {hidden.dim()} dimensions, not 2")
-    rows = hidden.shape
+    dev, dt, rows = hidden.get_device(), hidden.dtype, hidden.shape
+    code = _dtype_code("hidden", dt)
+    if len(rows) != 2:
+        _refuse(f"hidden has {len(rows)} dimensions, not 2")
     n, d = rows
-    p_hidden = _first("hidden", hidden)
-    parts, p_add, p_part = 0, None, None
+    if not hidden.is_contiguous():
+        _wrong("hidden", hidden, dt, rows, dev)
+    parts = 0
+    p_add = p_part = p_weight = p_sum = p_out = p_quant = p_scale = None
     if add is not None:
         if add.dim() == 2:
-            parts, p_add = 1, _tensor("add", add, dt, rows, dev)
+            parts, shape = 1, rows
         else:
             parts = add.shape[1] if add.dim() == 3 else 0
-            p_add = _tensor("add", add, dt, (n, parts, d), dev)
-            if parts == 0:
-                p_add = None
+            shape = (n, parts, d)
+        if (add.dtype is not dt or add.shape != shape or add.get_device() != dev
+                or not add.is_contiguous()):
+            _wrong("add", add, dt, shape, dev)
+        if parts != 0:
+            p_add = add.data_ptr()
     if part_w is not None:
         p_part = _tensor("part_w", part_w, torch.float32, (n, parts), dev)
         if parts == 0:
             p_part = None
-    p_weight = None if weight is None else _tensor("weight", weight, dt, (d,), dev)
-    p_sum = None if hidden_out is None else _tensor("hidden_out", hidden_out, dt, rows, dev)
-    p_out = None if out is None else _tensor("out", out, dt, rows, dev)
-    p_quant = p_scale = None
+    if weight is not None:
+        if (weight.dtype is not dt or weight.shape != (d,) or weight.get_device() != dev
+                or not weight.is_contiguous()):
+            _wrong("weight", weight, dt, (d,), dev)
+        p_weight = weight.data_ptr()
+    if hidden_out is not None:
+        if (hidden_out.dtype is not dt or hidden_out.shape != rows
+                or hidden_out.get_device() != dev or not hidden_out.is_contiguous()):
+            _wrong("hidden_out", hidden_out, dt, rows, dev)
+        p_sum = hidden_out.data_ptr()
+    if out is not None:
+        if (out.dtype is not dt or out.shape != rows or out.get_device() != dev
+                or not out.is_contiguous()):
+            _wrong("out", out, dt, rows, dev)
+        p_out = out.data_ptr()
     if out_quant is not None:
         p_quant = _tensor("out_quant", out_quant, torch.float8_e4m3fn, rows, dev)
     if scale_out is not None:
         p_scale = _tensor("scale_out", scale_out, torch.float32, (n,), dev)
-    _call("lookme_residual_norm", dev, stream, code, n, d, p_hidden, parts, p_add, p_part,
+    _call("lookme_residual_norm", dev, stream, code, n, d, hidden.data_ptr(), parts, p_add, p_part,
           p_weight, eps, p_sum, p_out, p_quant, p_scale)
 
 
@@ -482,9 +499,15 @@ def group_rows(pick, groups, rows_out, offsets_out, stream=None):
     dev, n, i32 = pick.get_device(), pick.numel(), torch.int32
     if rows_out.numel() != n:
         _refuse(f"rows_out has {rows_out.numel()} entries, not {n}")
-    _call("lookme_group_rows", dev, stream, groups, n, _tensor("pick", pick, i32, pick.shape, dev),
-          _tensor("rows_out", rows_out, i32, rows_out.shape, dev),
-          _tensor("offsets_out", offsets_out, i32, (groups + 1,), dev))
+    if pick.dtype is not i32 or not pick.is_contiguous():
+        _wrong("pick", pick, i32, pick.shape, dev)
+    if rows_out.dtype is not i32 or rows_out.get_device() != dev or not rows_out.is_contiguous():
+        _wrong("rows_out", rows_out, i32, rows_out.shape, dev)
+    if (offsets_out.dtype is not i32 or offsets_out.shape != (groups + 1,)
+            or offsets_out.get_device() != dev or not offsets_out.is_contiguous()):
+        _wrong("offsets_out", offsets_out, i32, (groups + 1,), dev)
+    _call("lookme_group_rows", dev, stream, groups, n, pick.data_ptr(), rows_out.data_ptr(),
+          offsets_out.data_ptr())
 
 
 def grouped_product(x, w, offsets, out, rows=None, picks=1, w_up=None, scatter=False,
@@ -493,28 +516,45 @@ def grouped_product(x, w, offsets, out, rows=None, picks=1, w_up=None, scatter=F
     for float8_e4m3fn: x [x_rows, d_in], w and w_up [groups, d_out, d_in],
     offsets [groups + 1] int32, out [m, d_out], rows [m] int32.  With rows,
     entry i reads x[rows[i] // picks] (picks = 0: x[i]); without, x[i]."""
-    dev, dt = x.get_device(), x.dtype
+    dev, dt, i32 = x.get_device(), x.dtype, torch.int32
     quant = dt is torch.float8_e4m3fn
-    code = 0 if quant else _dtype_code("x", x)
-    if x.dim() != 2 or w.dim() != 3 or out.dim() != 2:
+    code = 0 if quant else _dtype_code("x", dt)
+    x_shape, shape, out_shape = x.shape, w.shape, out.shape
+    if len(x_shape) != 2 or len(shape) != 3 or len(out_shape) != 2:
         _refuse("x and out have 2 dimensions, w has 3")
-    x_rows, d_in = x.shape
-    groups, d_out, _ = shape = w.shape
-    m = out.shape[0]
-    p_x = _first("x", x)
-    p_w = _tensor("w", w, dt, (groups, d_out, d_in), dev)
-    p_up = None if w_up is None else _tensor("w_up", w_up, dt, shape, dev)
-    p_off = _tensor("offsets", offsets, torch.int32, (groups + 1,), dev)
-    p_out = _tensor("out", out, torch.bfloat16 if quant else dt, (m, d_out), dev)
+    x_rows, d_in = x_shape
+    groups, d_out, _ = shape
+    m = out_shape[0]
+    if not x.is_contiguous():
+        _wrong("x", x, dt, x_shape, dev)
+    if w.dtype is not dt or shape[2] != d_in or w.get_device() != dev or not w.is_contiguous():
+        _wrong("w", w, dt, (groups, d_out, d_in), dev)
+    if (offsets.dtype is not i32 or offsets.shape != (groups + 1,)
+            or offsets.get_device() != dev or not offsets.is_contiguous()):
+        _wrong("offsets", offsets, i32, (groups + 1,), dev)
+    out_dt = torch.bfloat16 if quant else dt
+    if (out.dtype is not out_dt or out_shape[1] != d_out or out.get_device() != dev
+            or not out.is_contiguous()):
+        _wrong("out", out, out_dt, (m, d_out), dev)
+    p_up = p_rows = None
+    if w_up is not None:
+        if (w_up.dtype is not dt or w_up.shape != shape or w_up.get_device() != dev
+                or not w_up.is_contiguous()):
+            _wrong("w_up", w_up, dt, shape, dev)
+        p_up = w_up.data_ptr()
     if rows is None:
-        p_rows, picks = None, 0
+        picks = 0
     else:
-        p_rows = _tensor("rows", rows, torch.int32, (m,), dev)
+        if (rows.dtype is not i32 or rows.shape != (m,) or rows.get_device() != dev
+                or not rows.is_contiguous()):
+            _wrong("rows", rows, i32, (m,), dev)
+        p_rows = rows.data_ptr()
     if not quant:
         if x_scale is not None or w_scale is not None or w_up_scale is not None:
             _refuse(f"scales given for {dt}")
-        return _call("lookme_grouped_product", dev, stream, code, groups, m, d_in, d_out, p_x,
-                     x_rows, p_rows, picks, p_off, p_w, p_up, p_out, int(scatter))
+        return _call("lookme_grouped_product", dev, stream, code, groups, m, d_in, d_out,
+                     x.data_ptr(), x_rows, p_rows, picks, offsets.data_ptr(), w.data_ptr(), p_up,
+                     out.data_ptr(), int(scatter))
     if x_scale is None or w_scale is None:
         _refuse("float8_e4m3fn needs x_scale and w_scale")
     f32 = torch.float32
@@ -522,53 +562,63 @@ def grouped_product(x, w, offsets, out, rows=None, picks=1, w_up=None, scatter=F
     p_ws = _tensor("w_scale", w_scale, f32, (groups, d_out), dev)
     p_us = None if w_up_scale is None else _tensor("w_up_scale", w_up_scale, f32, (groups, d_out),
                                                    dev)
-    _call("lookme_grouped_product_quant", dev, stream, groups, m, d_in, d_out, p_x, p_xs, x_rows,
-          p_rows, picks, p_off, p_w, p_ws, p_up, p_us, p_out, int(scatter))
+    _call("lookme_grouped_product_quant", dev, stream, groups, m, d_in, d_out, x.data_ptr(), p_xs,
+          x_rows, p_rows, picks, offsets.data_ptr(), w.data_ptr(), p_ws, p_up, p_us,
+          out.data_ptr(), int(scatter))
 
 
 def _quant_matrix(name, dev, dt, d_in, w, scale, zero):
     """(d_out, group, addresses of w, scale and zero)"""
-    shape = scale.shape
+    shape, u8 = scale.shape, torch.uint8
     d_out, groups = shape
     if groups < 1 or d_in % groups != 0:
         _refuse(f"scale has {groups} groups for {d_in} columns")
-    return (d_out, d_in // groups, _tensor(name, w, torch.uint8, (d_out, d_in // 2), dev),
-            _tensor("its scale", scale, dt, shape, dev),
-            None if zero is None else _tensor("its zero", zero, torch.uint8, shape, dev))
+    if (w.dtype is not u8 or w.shape != (d_out, d_in // 2) or w.get_device() != dev
+            or not w.is_contiguous()):
+        _wrong(name, w, u8, (d_out, d_in // 2), dev)
+    if scale.dtype is not dt or scale.get_device() != dev or not scale.is_contiguous():
+        _wrong("its scale", scale, dt, shape, dev)
+    return (d_out, d_in // groups, w.data_ptr(), scale.data_ptr(),
+            None if zero is None else _tensor("its zero", zero, u8, shape, dev))
 
 
 def quant_product(x, w, scale, out, zero=None, add=None, stream=None):
     """lookme_quant_product on torch tensors: x [n, d_in], w [d_out, d_in / 2]
     uint8, scale [d_out, groups], zero [d_out, groups] uint8, add and out
     [n, d_out] (out may be add)."""
-    dev, dt = x.get_device(), x.dtype
-    code = _dtype_code("x", x)
-    if x.dim() != 2 or scale.dim() != 2:
+    dev, dt, shape = x.get_device(), x.dtype, x.shape
+    code = _dtype_code("x", dt)
+    if len(shape) != 2 or scale.dim() != 2:
         _refuse("x and scale have 2 dimensions")
-    n, d_in = x.shape
-    p_x = _first("x", x)
+    n, d_in = shape
+    if not x.is_contiguous():
+        _wrong("x", x, dt, shape, dev)
     d_out, group, p_w, p_s, p_z = _quant_matrix("w", dev, dt, d_in, w, scale, zero)
-    p_out = _tensor("out", out, dt, (n, d_out), dev)
+    if (out.dtype is not dt or out.shape != (n, d_out) or out.get_device() != dev
+            or not out.is_contiguous()):
+        _wrong("out", out, dt, (n, d_out), dev)
     p_add = None if add is None else _tensor("add", add, dt, (n, d_out), dev)
-    _call("lookme_quant_product", dev, stream, code, n, d_in, d_out, group, p_x, p_w, p_s, p_z,
-          p_add, p_out)
+    _call("lookme_quant_product", dev, stream, code, n, d_in, d_out, group, x.data_ptr(), p_w, p_s,
+          p_z, p_add, out.data_ptr())
 
 
 def quant_swiglu(x, w_gate, s_gate, w_up, s_up, out, z_gate=None, z_up=None, stream=None):
     """lookme_quant_swiglu on torch tensors, each matrix as for quant_product;
     out [n, d_ff]."""
-    dev, dt = x.get_device(), x.dtype
-    code = _dtype_code("x", x)
-    if x.dim() != 2 or s_gate.dim() != 2 or s_up.dim() != 2:
+    dev, dt, shape = x.get_device(), x.dtype, x.shape
+    code = _dtype_code("x", dt)
+    if len(shape) != 2 or s_gate.dim() != 2 or s_up.dim() != 2:
         _refuse("x and the scales have 2 dimensions")
-    n, d_in = x.shape
-    p_x = _first("x", x)
+    n, d_in = shape
+    if not x.is_contiguous():
+        _wrong("x", x, dt, shape, dev)
     d_ff, group, *gate = _quant_matrix("w_gate", dev, dt, d_in, w_gate, s_gate, z_gate)
     d_up, group_up, *up = _quant_matrix("w_up", dev, dt, d_in, w_up, s_up, z_up)
     if (d_up, group_up) != (d_ff, group):
         _refuse("w_gate and w_up differ in size or group")
     p_out = _tensor("out", out, dt, (n, d_ff), dev)
-    _call("lookme_quant_swiglu", dev, stream, code, n, d_in, d_ff, group, p_x, *gate, *up, p_out)
+    _call("lookme_quant_swiglu", dev, stream, code, n, d_in, d_ff, group, x.data_ptr(), *gate, *up,
+          p_out)
 
 
 def lookme_destroy(h):

@@ -887,6 +887,10 @@ static void launch_mid(const GroupedParams& p, hipStream_t st) {
 // 11 rows, 2048 x 256, 7.9 and 9.0 us, float32 10.6 and 25.0; one of 128 rows, 2048
 // x 1024, 12.6 and 9.3; but not with two matrices a wave in fewer bits (4 groups of
 // 11 rows, 2048 x 256, 10.1 and 9.1, float32 17.1 and 25.4).
+// And up to 32 rows a group where these are no more than the groups that a thread
+// looks through for a tile, which this kernel does once for several column tiles
+// (10 rows in 16000 groups of 512 x 64 1.1 and 4.5 ms, 30 in 8000 of 256 x 128 0.60
+// and 0.86; 20 in 4000 of 512 x 512 1.23 and 0.75).
 // Then tiles of 32 rows, of 64 above 32 rows a group where these are enough (64
 // groups of 64 rows 148 and 114 us; one of 512 rows 12 and 14), with deep rings
 // while all tiles are resident at once (one group of 512 rows 12.4 us with 4
@@ -924,7 +928,8 @@ static hipError_t launch_grouped_dt(const GroupedParams& p, hipStream_t st) {
                     (p.picks == 0 || p.x_rows * p.k_bytes < ((int64_t)1 << 32));
   if (span * round < 100 * tiles64 && p.k_bytes >= 128 && near)
     launch_kernel(grouped_tiles_kernel<DT, UP>, dim3(GT_GRID), dim3(GT_THREADS), 0, st, p);
-  else if (p.m <= (DT == DT_F32 ? 8 : 4) * used || tiles16 <= few)
+  else if (p.m <= (DT == DT_F32 ? 8 : 4) * used || tiles16 <= few ||
+           (p.m <= 32 * used && p.m <= (p.groups / GS_THREADS) * used))
     launch_rows<DT, UP>(p, st);
   else if (p.m <= 32 * used || tiles64 <= 256) {
     if ((p.m / 32 + used / 2 + 1) * tn64 <= 768) launch_mid<DT, 4, 1, UP>(p, st);

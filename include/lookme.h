@@ -637,9 +637,10 @@ lookme_status_t lookme_grouped_product_quant(int32_t groups, int64_t m, int32_t 
  * lookme_quant_product -- a product of few rows (decoded tokens) with weights
  * of 4 bits, in groups along d_in that share a scale and a zero point:
  *   out[t, c] = round(add[t, c] + sum_G scale[c, G] sum_{k in G} (q[c, k] - zero[c, G]) x[t, k])
- * The products are exact, the sums float32, no weight is rounded.  Every 16
- * rows (32 from 17 on) read the weights again: for many rows unpack them once.
- * A row of x with an infinity or a NaN gives NaN.
+ * The products (q - zero) x are exact, the sums float32 sums of them, no weight
+ * is rounded.  Every 16 rows (32 from 17 on) read the weights again: many rows
+ * are better multiplied with weights that the caller has unpacked.
+ * A row of x with an infinity or a NaN, and a sum past float32's range, give NaN.
  *   dtype  lookme_dtype_t of x, scale, add and out (no handle)
  *   group  32, 64 or a multiple of 128; d_in a multiple of it
  *   w      [d_out, d_in / 2] bytes: byte j of a row holds q[2 j] in its low

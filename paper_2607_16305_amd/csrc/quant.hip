@@ -6,17 +6,24 @@
 //
 // Bound by the weights' stream out of HBM.  A wave takes 16 weight rows and
 // 16 NT tokens on the matrix cores.  A lane's 16 bytes are 32 weights of a row;
-// two nibbles at a time become two bf16 values 16 + q in two instructions
-// (0x4180 + 8 q: exact), so that
-//   sum (q - z) x = sum (16 + q) x - (16 + z) sum x,
-// with sum x from a product with ones.  Every product is exact in float32 and
-// the group's scale multiplies its float32 sum: no weight is rounded.  float32
-// tokens are three bf16 values (8 + 8 + 8 bits of the significand), three
+// a nibble in a byte of its own is the e4m3 value q / 512, which a conversion
+// turns into the float32 q for two of them at a time; q - z, at most 8 bits of
+// significand, is exact in bf16.  So every product is exact in float32, the sums
+// are float32 sums of these products and nothing else, and the group's scale
+// multiplies its sum: no weight is rounded.  (Two instructions for two nibbles
+// give 16 + q, with (16 + z) sum x taken off afterwards: no faster, 8192 x 8192 of 1,
+// 16 and 64 rows 15.1, 18.5 and 45.1 us against 15.3, 18.5 and 45.3, and its sums
+// lose what the result is when sum x is large beside it: relative errors of
+// 4e-5 instead of 1e-7 for tokens of mean 5, of 4e-2 where only one token value of
+// 12345 stands before a weight of zero.)
+// float32 tokens are three bf16 values (8 + 8 + 8 bits of the significand), three
 // products a step.
-// The scales and zero points of a workgroup's rows wait in LDS as float32.  All
-// workgroups are resident at once: what a call takes beyond its launch is the
-// weights at 5 TB/s, or the instructions (95 a wave for 128 x 16 weights, 55
-// with two row tiles), whichever is longer, and two latencies of HBM.
+// The scales and zero points of a workgroup's rows wait in LDS as float32.  What a
+// call takes beyond its launch is the weights at 5 TB/s, or the instructions (115 a
+// wave for 128 x 16 weights), whichever is longer, and two latencies of HBM, while
+// its workgroups are all resident: one to three a CU, by their registers.  More of
+// them (there are cols / 16 x n / 16, half as many for every second tile a wave
+// has) take their turns.
 #include "common.h"
 #include "kernels.h"
 #include "tile_gemm.h"
@@ -26,18 +33,18 @@ namespace lookme {
 constexpr int QP_WAVES = 8, QP_THREADS = 64 * QP_WAVES;
 constexpr int QP_GROUPS = 128;   // groups whose scales are in LDS at a time
 
-// 8 nibbles as the bf16 values 16 + q of nibbles (0, 4), (1, 5), (2, 6), (3, 7)
-__device__ __forceinline__ u32x4_t qp_expand(uint32_t u) {
-  constexpr uint32_t M = 0x00780078u, B = 0x41804180u;
-  return u32x4_t{((u << 3) & M) | B, ((u >> 1) & M) | B, ((u >> 5) & M) | B, ((u >> 9) & M) | B};
-}
-
-// eight bf16 values in the order of qp_expand
-__device__ __forceinline__ u32x4_t qp_order(u32x4_t x) {
-  return u32x4_t{__builtin_amdgcn_perm(x[2], x[0], 0x05040100u),
-                 __builtin_amdgcn_perm(x[2], x[0], 0x07060302u),
-                 __builtin_amdgcn_perm(x[3], x[1], 0x05040100u),
-                 __builtin_amdgcn_perm(x[3], x[1], 0x07060302u)};
+// 8 nibbles less a zero point as bf16, in their order
+__device__ __forceinline__ u32x4_t qp_expand(uint32_t u, float z) {
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  const uint32_t even = u & 0x0F0F0F0Fu, odd = (u >> 4) & 0x0F0F0F0Fu;
+  const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f, false);
+  const f32x2_t b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f, false);
+  const f32x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(even, 512.f, true);
+  const f32x2_t d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(odd, 512.f, true);
+  auto pair = [z](float lo, float hi) {   // (the lower halves are zero)
+    return __builtin_amdgcn_perm(as_u32(hi - z), as_u32(lo - z), 0x07060302u);
+  };
+  return u32x4_t{pair(a[0], b[0]), pair(a[1], b[1]), pair(c[0], d[0]), pair(c[1], d[1])};
 }
 
 // regs r of lane group g hold words 4 g + r of a row's 64 bytes; afterwards
@@ -64,7 +71,7 @@ struct QpFrag {
   }
   __device__ __forceinline__ void split(u32x4_t (&f)[PARTS]) const {
     if constexpr (DT == DT_BF16) {
-      f[0] = qp_order(raw[0]);
+      f[0] = raw[0];
     } else {
       uint32_t h[3][8];
 #pragma unroll
@@ -75,12 +82,11 @@ struct QpFrag {
         h[1][e] = as_u32(r1) & 0xFFFF0000u;
         h[2][e] = as_u32(r1 - as_f32(h[1][e]));
       }
-      // pairs (0, 4), (1, 5), (2, 6), (3, 7): upper halves
 #pragma unroll
       for (int q = 0; q < 3; ++q)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          f[q][e] = __builtin_amdgcn_perm(h[q][e + 4], h[q][e], 0x07060302u);
+          f[q][e] = __builtin_amdgcn_perm(h[q][2 * e + 1], h[q][2 * e], 0x07060302u);
     }
   }
 };
@@ -98,7 +104,7 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
   constexpr int PARTS = QpFrag<DT>::PARTS;
   static_assert(RW * NT <= QP_WAVES, "a wave an output tile");
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  // [group][tile][scale, 16 + zero][16 rows]
+  // [group][tile][scale, zero][16 rows]
   float (*sz)[TILES][2][16] = reinterpret_cast<float (*)[TILES][2][16]>(lds);
   f32x4_t* part = reinterpret_cast<f32x4_t*>(lds);
   const int lane = threadIdx.x & 63;
@@ -191,7 +197,7 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
           sz[k][q][0][r & 15] = bf16lo(reinterpret_cast<const uint16_t*>(m.scale)[at + k]);
         else
           sz[k][q][0][r & 15] = reinterpret_cast<const float*>(m.scale)[at + k];
-        sz[k][q][1][r & 15] = 16.f + (m.zero != nullptr ? (float)m.zero[at + k] : 8.f);
+        sz[k][q][1][r & 15] = m.zero != nullptr ? (float)m.zero[at + k] : 8.f;
       }
     }
     __syncthreads();
@@ -205,54 +211,60 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
             w[q] = fw[d][q];
             if constexpr (SHORT) qp_transpose(w[q]);
           }
-          f32x4_t sp[TILES][NT], sx[NT];
+          const int block = b + d;
+          // a block's group, among those in LDS; of SHORT ones that of step s (of the
+          // steps past K the last one)
+          const int whole = SHORT ? 0 : 128 * block / p.group - first;
+          auto of = [&](int s) {
+            const int grp = (4 * block + s) >> (p.group == 32 ? 0 : 1);
+            return (grp < groups ? grp : groups - 1) - first;
+          };
+          float z[TILES];
+          auto zeros = [&](int grp) {
 #pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            sx[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int q = 0; q < TILES; ++q) z[q] = sz[grp][q][1][n16];
+          };
+          f32x4_t sp[TILES][NT];
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int q = 0; q < TILES; ++q) sp[q][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-          }
           auto flush = [&](int grp) {   // the group's sums, scaled, into acc
 #pragma unroll
             for (int q = 0; q < TILES; ++q) {
-              const f32x4_t s = *reinterpret_cast<const f32x4_t*>(&sz[grp - first][q][0][4 * g]);
-              const f32x4_t z = *reinterpret_cast<const f32x4_t*>(&sz[grp - first][q][1][4 * g]);
+              const f32x4_t s = *reinterpret_cast<const f32x4_t*>(&sz[grp][q][0][4 * g]);
 #pragma unroll
               for (int j = 0; j < NT; ++j) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                  acc[q][j][r] = fmaf(s[r], fmaf(-z[r], sx[j][r], sp[q][j][r]), acc[q][j][r]);
+                for (int r = 0; r < 4; ++r) acc[q][j][r] = fmaf(s[r], sp[q][j][r], acc[q][j][r]);
                 sp[q][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
               }
             }
-#pragma unroll
-            for (int j = 0; j < NT; ++j) sx[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
           };
+          if constexpr (!SHORT) zeros(whole);
 #pragma unroll
           for (int s = 0; s < 4; ++s) {
-            const u32x4_t ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+            if constexpr (SHORT)
+              if (p.group == 32 || (s & 1) == 0) zeros(of(s));
             u32x4_t a[TILES];
 #pragma unroll
-            for (int q = 0; q < TILES; ++q) a[q] = qp_expand(w[q][s]);
+            for (int q = 0; q < TILES; ++q) a[q] = qp_expand(w[q][s], z[q]);
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               u32x4_t f[PARTS];
               fx[d & 1][j][s].split(f);
 #pragma unroll
-              for (int e = 0; e < PARTS; ++e) {
-                sx[j] = mfma_chunk<DT_BF16>(ones, f[e], sx[j]);
+              for (int e = 0; e < PARTS; ++e)
 #pragma unroll
                 for (int q = 0; q < TILES; ++q)
                   sp[q][j] = mfma_chunk<DT_BF16>(a[q], f[e], sp[q][j]);
-              }
             }
             if constexpr (SHORT) {
               // (K may end inside the last block)
-              const int k = 128 * (b + d) + 32 * s;
-              if (k < p.k && (p.group == 32 || (s & 1) != 0)) flush(k / p.group);
+              if (128 * block + 32 * s < p.k && (p.group == 32 || (s & 1) != 0)) flush(of(s));
             }
           }
-          if constexpr (!SHORT) flush(128 * (b + d) / p.group);
+          if constexpr (!SHORT) flush(whole);
         }
         if (b + d + 2 < b1) {
           load_x(d, b + d + 2);
@@ -281,6 +293,9 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) sum[q][r] += v[r];
     }
+    // an infinity becomes a NaN, as the parts of a float32 one are
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sum[q][r] = fmaf(sum[q][r], 0.f, sum[q][r]);
   }
   const int col = c0 + 16 * i + 4 * g;
   const int64_t t = t0 + 16 * j + n16;

@@ -615,8 +615,9 @@ lookme_status_t lookme_grouped_product(int32_t dtype, int32_t groups, int64_t m,
 /*
  * lookme_grouped_product_quant -- lookme_grouped_product on e4m3 operands with
  * a float32 scale a row, out in bf16:
- *   out[dst, c] = round(x_scale[src] w_scale[g, c] sum_k w[g, c, k] x[src, k])
- * (with w_up: both sums scaled, then silu(.) * .).
+ *   out[dst, c] = round(sum_k w[g, c, k] x[src, k] * x_scale[src] * w_scale[g, c])
+ * (with w_up: both sums scaled, then silu(.) * .), from left to right in float32:
+ * the sum times x_scale, as the real row has it, has to be in its range.
  *   x [x_rows, d_in] e4m3, x_scale [x_rows] (out_quant and scale_out of
  *   lookme_residual_norm); w, w_up [groups, d_out, d_in] e4m3, w_scale,
  *   up_scale [groups, d_out]; w_up and up_scale both or neither

@@ -24,7 +24,7 @@
 //       and by the stores of a tile, 8 us in 63, which meet those of all others.
 //
 // e4m3 operands carry a float32 scale a row, applied once to the float32 sum:
-// out = round(xs ws sum).
+// out = round((sum xs) ws).
 #include "common.h"
 #include "kernels.h"
 #include "tile_gemm.h"
@@ -149,12 +149,14 @@ __device__ __forceinline__ bool gp_entry(const GroupedParams& p, int64_t i, int6
   return true;
 }
 
-// float32 sums of one output and of its up half, made an output value
+// float32 sums of one output and of its up half, made an output value.  The scales
+// one after the other: their product may pass the range that the result keeps, and
+// a sum of zero is zero.
 template <int DT, bool UP>
 __device__ __forceinline__ float gp_value(float c, float u, float xs, float ws, float us) {
   if constexpr (DT == DT_E4M3) {
-    c *= xs * ws;
-    u *= xs * us;
+    c = c * xs * ws;
+    u = u * xs * us;
   }
   return UP ? silu_f(c) * u : c;
 }

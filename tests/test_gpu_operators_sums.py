@@ -7,7 +7,7 @@ import torch
 
 from tests import operators as R
 from tests import operators_exact as X
-from tests.test_gpu_operators import BF, DT, E4M3, F32, QUANT, _close, _say, lk  # noqa: F401
+from tests.test_gpu_operators import BF, DT, E4M3, KERNELS, QUANT, _close, _offsets, _say, lk  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +69,50 @@ def test_quant_weights_of_zero_leave_a_value_out(lk, dtype, zero, n, group):  # 
     out = torch.empty((n, d_out), dtype=DT[dtype], device="cuda")
     lk.quant_product(*_cuda(x, R.pack(q), s), out, zero=None if z is None else z.cuda())
     assert torch.equal(out.cpu(), want.to(DT[dtype]))
+
+
+# ---------------------------------------------------------------------------
+# e4m3 grouped products
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("up", [False, True])
+@pytest.mark.parametrize("sizes,d_in,d_out", KERNELS)
+def test_grouped_scales_whose_product_has_no_float32(lk, sizes, d_in, d_out, up):  # noqa: F811
+    """rows and columns of very large and very small scales: a sum of zero stays
+    zero, a small result keeps its digits.  Up to two values of a row are not 0, so the sums
+    are exact; two roundings of the scaled sum and one of the output"""
+    _say("grouped scales", sizes[:8], d_in, d_out, up)
+    g = torch.Generator().manual_seed(11)
+    G, m = len(sizes), sum(sizes)
+    x = torch.zeros((m, d_in))
+    for _ in range(2):
+        x[torch.arange(m), torch.randint(0, d_in, (m,), generator=g)] = \
+            2.0 ** torch.randint(-3, 9, (m,), generator=g)
+    w = torch.randint(1, 16, (G, d_out, d_in), generator=g).float()
+    kind = torch.arange(m) % 4        # sums of zero, small, large, and ordinary
+    x[kind == 0] = 0
+    xs = (1 + torch.rand((m,), generator=g)) * torch.tensor([2.0 ** 100, 2.0 ** -70, 2.0 ** 70, 1.0])[kind]
+    of = torch.arange(d_out) % 3
+    ws = (1 + torch.rand((G, d_out), generator=g)) * torch.tensor([2.0 ** 40, 2.0 ** -72, 1.0])[of]
+    out = torch.full((m, d_out), -7.0, dtype=BF, device="cuda")
+    off = _offsets(sizes)
+    kw = dict(w_up=w.to(E4M3).cuda(), w_up_scale=torch.ones((G, d_out), device="cuda")) if up else {}
+    lk.grouped_product(x.to(E4M3).cuda(), w.to(E4M3).cuda(), off.cuda(), out, x_scale=xs.cuda(),
+                       w_scale=ws.cuda(), **kw)
+    got, inside = out.cpu(), 0
+    assert (got[kind == 0] == 0).all(), "sums of zero"
+    for i in range(G):
+        a, b = int(off[i]), int(off[i + 1])
+        s = x[a:b].double() @ w[i].double().T
+        v = s * xs[a:b, None].double() * ws[i].double()
+        e = 3 * R.U32 * v.abs()
+        if up:
+            u = s * xs[a:b, None].double()
+            v, e = R.silu_product(v, e, u, 2 * R.U32 * u.abs())
+        # (bf16's numbers end at 2^128, its steps at 2^-133)
+        e = e + R.HALF[BF] * v.abs() * (1 + 2 ** -7) + 2.0 ** -134
+        fits = v.abs() < 2.0 ** 127
+        inside += int(fits.sum())
+        r = got[a:b].double()
+        assert (((r - v).abs() <= e) | ~fits).all(), f"group {i}"
+    assert inside >= 0.7 * got.numel()   # (but most of one row in four)

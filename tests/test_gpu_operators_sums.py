@@ -116,3 +116,27 @@ def test_grouped_scales_whose_product_has_no_float32(lk, sizes, d_in, d_out, up)
         r = got[a:b].double()
         assert (((r - v).abs() <= e) | ~fits).all(), f"group {i}"
     assert inside >= 0.7 * got.numel()   # (but most of one row in four)
+
+
+@pytest.mark.parametrize("sizes,d_in,d_out", KERNELS)
+def test_grouped_e4m3_blocks_of_eight(lk, sizes, d_in, d_out):  # noqa: F811
+    """products of 2^16 and -2^16 in two blocks of 8 neighbouring values, and one of 1 in a third
+    or one of 8 beside the first: both are there in every kernel"""
+    _say("grouped blocks", sizes[:8], d_in, d_out)
+    g = torch.Generator().manual_seed(12)
+    m, G = sum(sizes), len(sizes)
+    block = torch.stack([torch.randperm(d_in // 8, generator=g)[:3] for _ in range(m)]) * 8
+    at = block + torch.randint(0, 8, (m, 3), generator=g)
+    beside = block[:, 0] + (at[:, 0] % 8 + 1 + torch.randint(0, 7, (m,), generator=g)) % 8
+    i, third = torch.arange(m), torch.arange(m) % 2 == 0
+    x = torch.zeros((m, d_in))
+    x[i, at[:, 0]], x[i, at[:, 1]] = 256.0, -256.0
+    x[i, at[:, 2]] = torch.where(third, 1.0 / 256, 0.0)     # an e4m3 value, of weight 256: 1
+    x[i, beside] = torch.where(third, 0.0, 1.0 / 32)        # 8 = 2^-13 of 2^16
+    out = torch.empty((m, d_out), dtype=BF, device="cuda")
+    w = torch.full((G, d_out, d_in), 256.0).to(E4M3)
+    lk.grouped_product(x.to(E4M3).cuda(), w.cuda(), _offsets(sizes).cuda(), out,
+                       x_scale=torch.ones(m, device="cuda"),
+                       w_scale=torch.ones((G, d_out), device="cuda"))
+    want = torch.where(third, 1.0, 8.0)[:, None].expand(m, d_out)
+    assert torch.equal(out.cpu().float(), want)

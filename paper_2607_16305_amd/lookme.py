@@ -428,9 +428,12 @@ def _dtype_code(name, dtype):
 
 def _call(name, device, stream, *args):
     """The entry point on `stream` (None: the current one) of the tensors'
-    device, which is a GPU."""
+    device, which is a GPU.  A stream of another device is refused: the kernel
+    would run there, on memory that it may not reach."""
     if device < 0:
         _refuse("tensors that are not in device memory")
+    if stream is not None and not isinstance(stream, int) and stream.device_index != device:
+        _refuse(f"the stream is of device {stream.device_index}, the tensors are on {device}")
     if device != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
             return _call(name, device, stream, *args)

@@ -24,6 +24,7 @@ LOOKME_SCORE_DOT, LOOKME_SCORE_COS = 0, 1
 LOOKME_KMAX = 32
 LOOKME_NOALLOC_MAX_ROWS = 131072
 LOOKME_MAX_GROUPS = 16384
+INT32 = 1 << 31     # one past the largest int32_t, as which the library takes most sizes
 
 STATUS_NAMES = {0: "OK", 1: "INVALID", 2: "UNSUPPORTED", 3: "WORKSPACE", 4: "HIP"}
 
@@ -347,20 +348,30 @@ def inject_text(table, pos, ids, hidden, kept=None, count=None, stream=None):
                        hidden.shape[1], stream)
 
 
+def _int32(*sizes):
+    """refuses a size that ctypes would cut to 32 bits"""
+    for v in sizes:
+        if not -INT32 <= v < INT32:
+            _refuse(f"{v} does not fit 32 bits")
+
+
 def lookme_residual_norm(dtype, n, d, hidden, parts, add, part_w, weight, eps, hidden_out, out,
                          out_quant, scale_out, stream=None):
+    _int32(dtype, d, parts)
     _check(load().lookme_residual_norm(dtype, n, d, _ptr(hidden), parts, _ptr(add), _ptr(part_w),
                                        _ptr(weight), eps, _ptr(hidden_out), _ptr(out),
                                        _ptr(out_quant), _ptr(scale_out), _stream(stream)))
 
 
 def lookme_group_rows(groups, n, pick, rows_out, offsets_out, stream=None):
+    _int32(groups)
     _check(load().lookme_group_rows(groups, n, _ptr(pick), _ptr(rows_out), _ptr(offsets_out),
                                     _stream(stream)))
 
 
 def lookme_grouped_product(dtype, groups, m, d_in, d_out, x, x_rows, rows, picks, offsets, w,
                            w_up, out, scatter, stream=None):
+    _int32(dtype, groups, d_in, d_out, picks, scatter)
     _check(load().lookme_grouped_product(dtype, groups, m, d_in, d_out, _ptr(x), x_rows,
                                          _ptr(rows), picks, _ptr(offsets), _ptr(w), _ptr(w_up),
                                          _ptr(out), scatter, _stream(stream)))
@@ -368,6 +379,7 @@ def lookme_grouped_product(dtype, groups, m, d_in, d_out, x, x_rows, rows, picks
 
 def lookme_grouped_product_quant(groups, m, d_in, d_out, x, x_scale, x_rows, rows, picks,
                                  offsets, w, w_scale, w_up, up_scale, out, scatter, stream=None):
+    _int32(groups, d_in, d_out, picks, scatter)
     _check(load().lookme_grouped_product_quant(groups, m, d_in, d_out, _ptr(x), _ptr(x_scale),
                                                x_rows, _ptr(rows), picks, _ptr(offsets), _ptr(w),
                                                _ptr(w_scale), _ptr(w_up), _ptr(up_scale),
@@ -375,6 +387,7 @@ def lookme_grouped_product_quant(groups, m, d_in, d_out, x, x_scale, x_rows, row
 
 
 def lookme_quant_product(dtype, n, d_in, d_out, group, x, w, scale, zero, add, out, stream=None):
+    _int32(dtype, d_in, d_out, group)
     _check(load().lookme_quant_product(dtype, n, d_in, d_out, group, _ptr(x), _ptr(w),
                                        _ptr(scale), _ptr(zero), _ptr(add), _ptr(out),
                                        _stream(stream)))
@@ -382,6 +395,7 @@ def lookme_quant_product(dtype, n, d_in, d_out, group, x, w, scale, zero, add, o
 
 def lookme_quant_swiglu(dtype, n, d_in, d_ff, group, x, w_gate, scale_gate, zero_gate, w_up,
                         scale_up, zero_up, out, stream=None):
+    _int32(dtype, d_in, d_ff, group)
     _check(load().lookme_quant_swiglu(dtype, n, d_in, d_ff, group, _ptr(x), _ptr(w_gate),
                                       _ptr(scale_gate), _ptr(zero_gate), _ptr(w_up),
                                       _ptr(scale_up), _ptr(zero_up), _ptr(out),
@@ -454,6 +468,8 @@ def residual_norm(hidden, weight=None, eps=1e-6, add=None, part_w=None, hidden_o
     if len(rows) != 2:
         _refuse(f"hidden has {len(rows)} dimensions, not 2")
     n, d = rows
+    if d >= INT32:
+        _int32(d)
     if not hidden.is_contiguous():
         _wrong("hidden", hidden, dt, rows, dev)
     parts = 0
@@ -464,6 +480,8 @@ def residual_norm(hidden, weight=None, eps=1e-6, add=None, part_w=None, hidden_o
         else:
             parts = add.shape[1] if add.dim() == 3 else 0
             shape = (n, parts, d)
+            if parts >= INT32:
+                _int32(parts)
         if (add.dtype is not dt or add.shape != shape or add.get_device() != dev
                 or not add.is_contiguous()):
             _wrong("add", add, dt, shape, dev)
@@ -502,6 +520,8 @@ def group_rows(pick, groups, rows_out, offsets_out, stream=None):
     dev, n, i32 = pick.get_device(), pick.numel(), torch.int32
     if rows_out.numel() != n:
         _refuse(f"rows_out has {rows_out.numel()} entries, not {n}")
+    if groups >= INT32:
+        _int32(groups)
     if pick.dtype is not i32 or not pick.is_contiguous():
         _wrong("pick", pick, i32, pick.shape, dev)
     if rows_out.dtype is not i32 or rows_out.get_device() != dev or not rows_out.is_contiguous():
@@ -528,6 +548,8 @@ def grouped_product(x, w, offsets, out, rows=None, picks=1, w_up=None, scatter=F
     x_rows, d_in = x_shape
     groups, d_out, _ = shape
     m = out_shape[0]
+    if d_in >= INT32 or d_out >= INT32 or groups >= INT32 or not -INT32 <= picks < INT32:
+        _int32(d_in, d_out, groups, picks)
     if not x.is_contiguous():
         _wrong("x", x, dt, x_shape, dev)
     if w.dtype is not dt or shape[2] != d_in or w.get_device() != dev or not w.is_contiguous():
@@ -574,6 +596,8 @@ def _quant_matrix(name, dev, dt, d_in, w, scale, zero):
     """(d_out, group, addresses of w, scale and zero)"""
     shape, u8 = scale.shape, torch.uint8
     d_out, groups = shape
+    if d_in >= INT32 or d_out >= INT32:
+        _int32(d_in, d_out)
     if groups < 1 or d_in % groups != 0:
         _refuse(f"scale has {groups} groups for {d_in} columns")
     if (w.dtype is not u8 or w.shape != (d_out, d_in // 2) or w.get_device() != dev

@@ -847,35 +847,29 @@ __global__ __launch_bounds__(GT_THREADS, 2) void grouped_tiles_kernel(GroupedPar
 // (4000 groups of one row, 256 x 512, one column tile a workgroup and four: 368
 // and 252 us; from 4096 workgroups on 2 rows in 64 groups of 2048 x 2048 take 102
 // us instead of 90).
-template <int DT, bool UP>
-static void launch_rows(GroupedParams p, hipStream_t st) {
-  const int64_t most = p.m / 16 + p.groups;   // row tiles: one a group, one for each 16 rows
-  const int64_t tiles = most < p.m ? most : p.m;
-  auto grid = [&](int cols) {
-    const int64_t tn = (p.cols + cols - 1) / cols;
-    int64_t blocks = GS_BLOCKS / tiles;
-    blocks = blocks < 1 ? 1 : blocks < tn ? blocks : tn;
-    p.span = (int)((tn + blocks - 1) / blocks);
-    const int64_t n = tiles * ((tn + p.span - 1) / p.span);
-    return dim3((unsigned)(n < GP_GRID ? n : GP_GRID));
-  };
-  if (p.k_bytes >= 8192 || tiles * ((p.cols + 31) / 32) < 1024) {
-    const dim3 n = grid(16);
-    launch_kernel(grouped_rows_kernel<DT, 4, UP>, n, dim3(GS_THREADS), 0, st, p);
-  } else {
-    const dim3 n = grid(32);
-    launch_kernel(grouped_rows_kernel<DT, 2, UP>, n, dim3(GS_THREADS), 0, st, p);
-  }
+static void plan_rows(int64_t m, int groups, int cols, int64_t k_bytes, GroupedPlan* pl) {
+  const int64_t most = m / 16 + groups;   // row tiles: one a group, one for each 16 rows
+  const int64_t tiles = most < m ? most : m;
+  pl->kernel = GROUPED_ROWS;
+  pl->rows = 16;
+  pl->depth = k_bytes >= 8192 || tiles * ((cols + 31) / 32) < 1024 ? 4 : 2;
+  const int64_t per = 16 * (GS_WAVES / pl->depth);   // columns of a column tile
+  const int64_t tn = (cols + per - 1) / per;
+  int64_t blocks = GS_BLOCKS / tiles;
+  blocks = blocks < 1 ? 1 : blocks < tn ? blocks : tn;
+  pl->span = (int)((tn + blocks - 1) / blocks);
+  const int64_t n = tiles * ((tn + pl->span - 1) / pl->span);
+  pl->blocks = (int)(n < GP_GRID ? n : GP_GRID);
 }
 
-template <int DT, int NS, int TI, bool UP>
-static void launch_mid(const GroupedParams& p, hipStream_t st) {
-  constexpr int RT = 32 * TI, COLS = UP ? 32 : 64;
-  const int64_t most = p.m / RT + p.groups;
-  int64_t tiles = (most < p.m ? most : p.m) * ((p.cols + COLS - 1) / COLS);
+static void plan_ring(int64_t m, int groups, int64_t tn, int depth, int rows, GroupedPlan* pl) {
+  const int64_t most = m / rows + groups;
+  int64_t tiles = (most < m ? most : m) * tn;
   tiles = (tiles + 7) / 8 * 8;   // xcd_remap deals whole rounds over the XCDs
-  launch_kernel(grouped_mid_kernel<DT, NS, TI, UP>,
-                dim3((unsigned)(tiles < GP_GRID ? tiles : GP_GRID)), dim3(GM_THREADS), 0, st, p);
+  pl->kernel = GROUPED_RING;
+  pl->depth = depth;
+  pl->rows = rows;
+  pl->blocks = (int)(tiles < GP_GRID ? tiles : GP_GRID);
 }
 
 // The host knows the groups' number and their rows together, so the rules go
@@ -906,55 +900,85 @@ static void launch_mid(const GroupedParams& p, hipStream_t st) {
 // 2048 31 and 39; e4m3 16 of 256 38 and 30, float32 309 and 268, of 512 592 and
 // 488; 64 groups of 80 rows on average 168 and 120, float32 609 and 531).
 template <int DT, bool UP>
-static hipError_t launch_grouped_dt(const GroupedParams& p, hipStream_t st) {
-  const int64_t used = p.groups < p.m ? p.groups : p.m;
-  const int64_t tn = (p.cols + (UP ? 127 : 255)) / (UP ? 128 : 256);
-  const int64_t tn64 = (p.cols + (UP ? 31 : 63)) / (UP ? 32 : 64);
+static GroupedPlan plan_dt(int64_t m, int groups, int cols, int64_t k_bytes, int picks,
+                           int64_t x_rows) {
+  const int64_t used = groups < m ? groups : m;
+  const int64_t tn = (cols + (UP ? 127 : 255)) / (UP ? 128 : 256);
+  const int64_t tn64 = (cols + (UP ? 31 : 63)) / (UP ? 32 : 64);
   // half a row tile of padding a group, half of the groups with a half tile
-  const int64_t tiles64 = (p.m / 64 + used / 2 + 1) * tn64;
+  const int64_t tiles64 = (m / 64 + used / 2 + 1) * tn64;
   constexpr int few = DT == DT_F32 ? (UP ? 256 : 512) : (UP ? 0 : 256);
-  const int64_t tiles16 =
-      used * ((p.m + 16 * used - 1) / (16 * used)) * (int64_t)((p.cols + 15) / 16);
+  const int64_t tiles16 = used * ((m + 16 * used - 1) / (16 * used)) * (int64_t)((cols + 15) / 16);
   // large tiles as the mean has it: up to 128 rows a half a group, up to 224 a whole
   // one; above, where any place in a last block is as likely (float32, which loses
   // most by a second round, above 128), a whole one for every 256 rows and for
   // every second group a half
-  const bool half = p.m <= 128 * used, one = !half && DT != DT_F32 && p.m <= 224 * used;
-  const int64_t whole = half ? 0 : one ? used * tn : p.m * tn / 256;
+  const bool half = m <= 128 * used, one = !half && DT != DT_F32 && m <= 224 * used;
+  const int64_t whole = half ? 0 : one ? used * tn : m * tn / 256;
   const int64_t halves = half ? used * tn : one ? 0 : (used + 1) / 2 * tn;
   const int64_t cut = gt_cut<DT>(whole, halves);
   const int64_t span = gt_span<DT>(whole - cut, halves + 2 * cut);
   const int64_t round = DT == DT_F32 ? 3340 : DT == DT_E4M3 ? 2400 : 2100;
   // (the phased kernel's lane offsets are 32-bit)
-  const bool near = p.k_bytes < (4 << 20) &&
-                    (p.picks == 0 || p.x_rows * p.k_bytes < ((int64_t)1 << 32));
-  if (span * round < 100 * tiles64 && p.k_bytes >= 128 && near)
-    launch_kernel(grouped_tiles_kernel<DT, UP>, dim3(GT_GRID), dim3(GT_THREADS), 0, st, p);
-  else if (p.m <= (DT == DT_F32 ? 8 : 4) * used || tiles16 <= few ||
-           (p.m <= 32 * used && p.m <= (p.groups / GS_THREADS) * used))
-    launch_rows<DT, UP>(p, st);
-  else if (p.m <= 32 * used || tiles64 <= 256) {
-    if ((p.m / 32 + used / 2 + 1) * tn64 <= 768) launch_mid<DT, 4, 1, UP>(p, st);
-    else launch_mid<DT, 3, 1, UP>(p, st);
-  } else if (tiles64 <= 512 || (DT == DT_F32 && tiles64 > 1024)) {
-    launch_mid<DT, 4, 2, UP>(p, st);
+  const bool near = k_bytes < (4 << 20) &&
+                    (picks == 0 || x_rows * k_bytes < ((int64_t)1 << 32));
+  GroupedPlan pl{};
+  if (span * round < 100 * tiles64 && k_bytes >= 128 && near) {
+    pl.kernel = GROUPED_TILES;
+    pl.blocks = GT_GRID;
+  } else if (m <= (DT == DT_F32 ? 8 : 4) * used || tiles16 <= few ||
+             (m <= 32 * used && m <= (groups / GS_THREADS) * used)) {
+    plan_rows(m, groups, cols, k_bytes, &pl);
+  } else if (m <= 32 * used || tiles64 <= 256) {
+    plan_ring(m, groups, tn64, (m / 32 + used / 2 + 1) * tn64 <= 768 ? 4 : 3, 32, &pl);
   } else {
-    launch_mid<DT, 2, 2, UP>(p, st);
+    plan_ring(m, groups, tn64, tiles64 <= 512 || (DT == DT_F32 && tiles64 > 1024) ? 4 : 2, 64,
+              &pl);
   }
-  return hipGetLastError();
+  return pl;
+}
+
+template <int DT, bool UP>
+static void launch_plan(GroupedParams p, const GroupedPlan& pl, hipStream_t st) {
+  const dim3 grid((unsigned)pl.blocks);
+  p.span = pl.span;
+  if (pl.kernel == GROUPED_TILES)
+    launch_kernel(grouped_tiles_kernel<DT, UP>, grid, dim3(GT_THREADS), 0, st, p);
+  else if (pl.kernel == GROUPED_ROWS && pl.depth == 4)
+    launch_kernel(grouped_rows_kernel<DT, 4, UP>, grid, dim3(GS_THREADS), 0, st, p);
+  else if (pl.kernel == GROUPED_ROWS)
+    launch_kernel(grouped_rows_kernel<DT, 2, UP>, grid, dim3(GS_THREADS), 0, st, p);
+  else if (pl.rows == 32 && pl.depth == 4)
+    launch_kernel(grouped_mid_kernel<DT, 4, 1, UP>, grid, dim3(GM_THREADS), 0, st, p);
+  else if (pl.rows == 32)
+    launch_kernel(grouped_mid_kernel<DT, 3, 1, UP>, grid, dim3(GM_THREADS), 0, st, p);
+  else if (pl.depth == 4)
+    launch_kernel(grouped_mid_kernel<DT, 4, 2, UP>, grid, dim3(GM_THREADS), 0, st, p);
+  else
+    launch_kernel(grouped_mid_kernel<DT, 2, 2, UP>, grid, dim3(GM_THREADS), 0, st, p);
+}
+
+GroupedPlan grouped_plan(int dt, bool up, int64_t m, int groups, int cols, int64_t k_bytes,
+                         int picks, int64_t x_rows) {
+  const auto plan = dt == DT_BF16 ? (up ? plan_dt<DT_BF16, true> : plan_dt<DT_BF16, false>)
+                    : dt == DT_F32 ? (up ? plan_dt<DT_F32, true> : plan_dt<DT_F32, false>)
+                                   : (up ? plan_dt<DT_E4M3, true> : plan_dt<DT_E4M3, false>);
+  return plan(m, groups, cols, k_bytes, picks, x_rows);
 }
 
 hipError_t launch_grouped(int dt, const GroupedParams& p, hipStream_t st) {
   if (p.m == 0) return hipSuccess;
   const bool up = p.w_up != nullptr;
+  const GroupedPlan pl = grouped_plan(dt, up, p.m, p.groups, p.cols, p.k_bytes, p.picks, p.x_rows);
   switch (dt) {
-    case DT_BF16: return up ? launch_grouped_dt<DT_BF16, true>(p, st)
-                            : launch_grouped_dt<DT_BF16, false>(p, st);
-    case DT_F32: return up ? launch_grouped_dt<DT_F32, true>(p, st)
-                           : launch_grouped_dt<DT_F32, false>(p, st);
-    default: return up ? launch_grouped_dt<DT_E4M3, true>(p, st)
-                       : launch_grouped_dt<DT_E4M3, false>(p, st);
+    case DT_BF16: up ? launch_plan<DT_BF16, true>(p, pl, st)
+                     : launch_plan<DT_BF16, false>(p, pl, st); break;
+    case DT_F32: up ? launch_plan<DT_F32, true>(p, pl, st)
+                    : launch_plan<DT_F32, false>(p, pl, st); break;
+    default: up ? launch_plan<DT_E4M3, true>(p, pl, st)
+                : launch_plan<DT_E4M3, false>(p, pl, st);
   }
+  return hipGetLastError();
 }
 
 }  // namespace lookme

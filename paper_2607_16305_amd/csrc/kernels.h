@@ -328,6 +328,16 @@ struct GroupedParams {
   int span;                  // column tiles of a workgroup (set by the launch)
 };
 constexpr int GROUPED_E4M3 = 2;   // dt of e4m3 operands (out in bf16)
+enum : int { GROUPED_ROWS = 0, GROUPED_RING = 1, GROUPED_TILES = 2 };
+struct GroupedPlan {
+  int kernel;
+  int depth;                 // ROWS: waves that share K; RING: stages
+  int rows;                  // of a tile (ROWS and RING)
+  int span;                  // ROWS: column tiles of a workgroup
+  int blocks;                // workgroups
+};
+GroupedPlan grouped_plan(int dt, bool up, int64_t m, int groups, int cols, int64_t k_bytes,
+                         int picks, int64_t x_rows);
 hipError_t launch_grouped(int dt, const GroupedParams& p, hipStream_t st);
 
 // ---- products with 4-bit weights (quant.hip) -------------------------------

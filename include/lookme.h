@@ -578,7 +578,8 @@ lookme_status_t lookme_residual_norm(int32_t dtype, int64_t n, int32_t d, const 
  *   offsets_out [groups + 1] int32: group g's entries are rows_out[offsets[g]
  *               .. offsets[g + 1]); offsets[groups] is the number of entries
  * 1 <= groups <= LOOKME_MAX_GROUPS, n <= 2^30.  n = 0 writes zero offsets.
- * Needs no handle and no workspace.
+ * Needs no handle and no workspace; for that every one of up to 256 workgroups
+ * reads all ids, so it is meant for a batch's picks (up to some 2^22).
  */
 lookme_status_t lookme_group_rows(int32_t groups, int64_t n, const int32_t* pick,
                                   int32_t* rows_out, int32_t* offsets_out, void* stream);
@@ -658,10 +659,11 @@ lookme_status_t lookme_quant_product(int32_t dtype, int64_t n, int32_t d_in, int
                                      void* out, void* stream);
 
 /*
- * lookme_quant_swiglu -- the gate and up half of the SwiGLU fusion of Eq. 10
- * (lookme_set_fusion) on such weights: out[t, :] = round(silu(W_gate x[t, :])
- * * (W_up x[t, :])).  lookme_quant_product with add is the other half:
- * hidden + W_down u.  Arguments as above, out [n, d_ff].
+ * lookme_quant_swiglu -- gate and up of a SwiGLU layer (the form that the fusion
+ * of Eq. 10 has; lookme_set_fusion itself takes no such weights) on 4-bit
+ * weights: out[t, :] = round(silu(W_gate x[t, :]) * (W_up x[t, :])).
+ * lookme_quant_product with add is the other half: hidden + W_down u.
+ * Arguments as above, out [n, d_ff].
  */
 lookme_status_t lookme_quant_swiglu(int32_t dtype, int64_t n, int32_t d_in, int32_t d_ff,
                                     int32_t group, const void* x, const void* w_gate,

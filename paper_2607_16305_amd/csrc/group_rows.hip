@@ -4,7 +4,7 @@
 //
 // One launch and no scratch.  A workgroup owns a range of consecutive groups and
 // (with fewer groups than CUs) one of several segments of the entries, and reads
-// all the ids (they stay in L2): those below the range count towards where its
+// all the ids (2^18 of them are 1 MiB and stay in L2; see below): those below the range count towards where its
 // rows begin, those of its group ahead of its segment towards where its own
 // begin.  In its segment its waves own runs of consecutive entries, and each
 // lists its run's entries of the range in order in LDS.  Over its list (or over
@@ -14,8 +14,10 @@
 // What bounds it is the instructions a CU issues for each id: for 64 of another
 // range a subtraction, whose borrow is the count of those below, an addition and
 // a comparison (262144 ids in 1024 groups alike 21 us, 13 TB/s out of L2; with
-// Zipf(1) groups 45, the largest being an eighth of the ids; 512 ids in 128 groups
-// 4.1).
+// Zipf(1) groups 45, the largest being an eighth of the ids, and 130 where the
+// largest ones are neighbours and so share a workgroup; 512 ids in 128 groups 4.1).
+// The time grows with the ids, 2^20 in 1024 groups alike 71 us and 2^22 275, until
+// the lists run full: 2^24 take 7.3 ms.
 // The result does not depend on timing: counts are sums, and a run's slots are
 // handed out by its own wave alone.
 #include "common.h"

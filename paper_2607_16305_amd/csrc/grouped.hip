@@ -17,8 +17,9 @@
 //       operands through a ring of stages in LDS.
 //   grouped_tiles_kernel  many rows a group: 256 x 256 and 128 x 256 tiles on the
 //       phased loop of phase_gemm.h, one workgroup a CU that takes tile after
-//       tile: 64 groups of 1024 rows, 2048 x 2048 in bf16, 517 us, 1063 TFLOP/s;
-//       32 of 4096 x 4096 885, 1242; 16 of 2048 rows, 4096 x 4096 in e4m3, 497, 2210.
+//       tile: 64 groups of 1024 rows, 2048 x 2048 in bf16, 517 to 573 us by run and
+//       card, 1063 to 959 TFLOP/s; 32 of 4096 x 4096 885 to 902, 1242 to 1219; 16 of
+//       2048 rows, 4096 x 4096 in e4m3, 497 to 566, 2210 to 1940.
 //       Bound by the stage stream out of L2 beside the fragment reads (the matrix
 //       cores are busy 55% of the time, at the 2.0 GHz that such a load leaves)
 //       and by the stores of a tile, 8 us in 63, which meet those of all others.
@@ -873,7 +874,9 @@ static void plan_ring(int64_t m, int groups, int64_t tn, int depth, int rows, Gr
 }
 
 // The host knows the groups' number and their rows together, so the rules go
-// by the mean; a group far from it is computed on tiles that fit it less well.
+// by the mean; a group far from it is computed on tiles that fit it less well: 64
+// groups of 512 rows among 960 empty ones, 1024 x 1024 in bf16, 305 us on tiles
+// of 32 rows, without the empty ones 83 (float32, 128 rows each, 525 and 155).
 //
 // Up to 4 rows a group (float32, bound by the matrix cores, 8) the few-rows
 // kernel: 64 groups of 2048 x 2048, it and 32-row tiles, 1 row 92 and 94 us, 4
@@ -889,16 +892,22 @@ static void plan_ring(int64_t m, int groups, int64_t tn, int depth, int rows, Gr
 // and 0.86; 20 in 4000 of 512 x 512 1.23 and 0.75).
 // Then tiles of 32 rows, of 64 above 32 rows a group where these are enough (64
 // groups of 64 rows 148 and 114 us; one of 512 rows 12 and 14), with deep rings
-// while all tiles are resident at once (one group of 512 rows 12.4 us with 4
-// stages, 13.7 with 3; of 2048 rows on 64-row tiles 30.6 us with 2, 35.7 with 4),
-// and for float32 again where there are many (16 of 256 rows 309 us with 2, 301
-// with 4; 13 groups of 231 rows, 840 x 1160, 71 and 92).
+// while all tiles are resident at once: four stages of 32 rows leave three
+// workgroups a CU (768), of 64 rows two (512) (one group of 512 rows 12.4 us with 4
+// stages, 13.7 with 3; of 2048 rows on 64-row tiles 30.6 us with 2, 35.7 with 4).
+// float32, which the matrix cores bound, takes two stages only between 512 and 1024
+// tiles of 64 rows, which are all resident with two and not with four (13 groups of
+// 231 rows, 840 x 1160, 71 and 92), and four again beyond (16 of 256 rows 309 us with
+// 2, 301 with 4).
 // The large tiles where their rounds cost less: one of 256 whole ones takes as
 // long as `round` 64 x 64 ones, one of halves 65% of that, float32 55% (2048 x
 // 2048, 64-row tiles and large ones, bf16: 64 groups of 64 rows 114 and 117 us, of
 // 96 169 and 120, of 256 293 and 170; 16 of 128 33 and 48, of 256 60 and 42; one of
-// 2048 31 and 39; e4m3 16 of 256 38 and 30, float32 309 and 268, of 512 592 and
-// 488; 64 groups of 80 rows on average 168 and 120, float32 609 and 531).
+// 2048 31 and 39; e4m3 16 of 256 38 and 30; 64 groups of 80 rows on average 168 and
+// 120).  For float32, whose large tiles lose most by a round that is not full,
+// the rule supposes groups of any size, and keeps even ones of 256, 512 or 80 rows,
+// which would fill it, on rings (16 of 256 rows 309 us, on large tiles 268; of 512
+// 576 and 492; 64 of 80 626 and 540; 13 groups of 231 rows, 840 x 1160, 72 and 154).
 template <int DT, bool UP>
 static GroupedPlan plan_dt(int64_t m, int groups, int cols, int64_t k_bytes, int picks,
                            int64_t x_rows) {

@@ -1,5 +1,7 @@
-// Products of few rows with weights of 4 bits and scales (and zero points) by
-// groups along K, the form in which the fusion of Eq. 10 serves single tokens:
+// Products of few rows, of decoded tokens, with weights of 4 bits and scales (and
+// zero points) by groups along K: a projection with its residual sum, or the gate
+// and up half of a SwiGLU layer (the form of Eq. 10; the handle's own fusion takes
+// bf16 and float32 weights):
 //
 //   out = round(add + sum_G s_G sum_{k in G} (q_k - z_G) x_k), or
 //   out = round(silu(gate) * up) of two such sums.
@@ -19,11 +21,11 @@
 // float32 tokens are three bf16 values (8 + 8 + 8 bits of the significand), three
 // products a step.
 // The scales and zero points of a workgroup's rows wait in LDS as float32.  What a
-// call takes beyond its launch is the weights at 5 TB/s, or the instructions (115 a
-// wave for 128 x 16 weights), whichever is longer, and two latencies of HBM, while
-// its workgroups are all resident: one to three a CU, by their registers.  More of
-// them (there are cols / 16 x n / 16, half as many for every second tile a wave
-// has) take their turns.
+// call takes beyond its launch is the weights at 5 TB/s, or the instructions (120 a
+// wave for 128 x 16 weights, 102 with two row tiles), whichever is longer, and two
+// latencies of HBM, while its workgroups are all resident: one to three a CU, by
+// their registers.  More of them (there are cols / 16 x n / 16, half as many for
+// every second tile a wave has) take their turns.
 #include "common.h"
 #include "kernels.h"
 #include "tile_gemm.h"

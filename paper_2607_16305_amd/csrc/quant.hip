@@ -333,13 +333,13 @@ static void launch_quant_nt(const QuantParams& p, hipStream_t st) {
 }
 
 // Two row tiles a wave where these are a workgroup for every CU: the tokens,
-// which every wave reads from L2 and orders for itself, then serve twice the
-// weights (8192 x 8192 of bf16, one tile and two: 1 row 13.0 and 12.7 us, 16 rows
-// 22 and 17, 32 rows 38 and 24; float32 1 row 27 and 19; 4096 x 4096, 128
-// workgroups, 16 rows 8.2 and 9.9).  Gate and up share the tokens already, which
-// is enough for few rows (2 x 8192 x 4096 of 4 rows 13.2 and 15.0, of 16 17.1 and
-// 16.5; float32 of 4 rows 22 and 19), and with two token tiles of float32 two row
-// tiles spill.  Deeper rings (4 blocks: 1 row of 8192 x 8192 14.0 us), 16 waves (1
+// which every wave reads from L2 for itself, then serve twice the weights (8192 x
+// 8192 of bf16 out of HBM, one tile and two: 1 row 15.0 and 14.6 us, 16 rows 23.9
+// and 18.3, 32 rows 36.5 and 25.1; float32 1 row 28.2 and 20.1; 4096 x 4096, 128
+// workgroups, 16 rows 8.6 and 10.1).  Gate and up share the tokens already, which
+// is enough for few rows (2 x 8192 x 4096 of 4 rows 14.2 and 16.9, of 16 17.4 and
+// 17.6, of 32 27.2 and 21.3; float32 of 4 rows 24.5 and 21.3), and with two token
+// tiles of float32 two row tiles spill.  Deeper rings (4 blocks: 1 row of 8192 x 8192 14.0 us), 16 waves (1
 // row of 1024 x 8192 7.5 and 7.4 us) and no loads for the tokens there are none
 // of (the same) were no faster.
 template <int DT, bool UP>

@@ -221,9 +221,8 @@ hipError_t launch_group_rows(int groups, int64_t n, const int32_t* pick, int32_t
   int64_t segments = range == 1 ? GR_BLOCKS / ranges : 1;
   if (segments > steps) segments = steps;
   if (segments < 1) segments = 1;
-  launch_kernel(group_rows_kernel, dim3((unsigned)(ranges * segments)), dim3(GR_THREADS), 0, st,
-                pick, (int)n, groups, range, (int)segments, rows, offsets);
-  return hipGetLastError();
+  return launch_kernel(group_rows_kernel, dim3((unsigned)(ranges * segments)), dim3(GR_THREADS), 0,
+                       st, pick, (int)n, groups, range, (int)segments, rows, offsets);
 }
 
 }  // namespace lookme

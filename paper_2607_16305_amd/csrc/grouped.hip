@@ -948,23 +948,22 @@ static GroupedPlan plan_dt(int64_t m, int groups, int cols, int64_t k_bytes, int
 }
 
 template <int DT, bool UP>
-static void launch_plan(GroupedParams p, const GroupedPlan& pl, hipStream_t st) {
+static hipError_t launch_plan(GroupedParams p, const GroupedPlan& pl, hipStream_t st) {
   const dim3 grid((unsigned)pl.blocks);
   p.span = pl.span;
   if (pl.kernel == GROUPED_TILES)
-    launch_kernel(grouped_tiles_kernel<DT, UP>, grid, dim3(GT_THREADS), 0, st, p);
-  else if (pl.kernel == GROUPED_ROWS && pl.depth == 4)
-    launch_kernel(grouped_rows_kernel<DT, 4, UP>, grid, dim3(GS_THREADS), 0, st, p);
-  else if (pl.kernel == GROUPED_ROWS)
-    launch_kernel(grouped_rows_kernel<DT, 2, UP>, grid, dim3(GS_THREADS), 0, st, p);
-  else if (pl.rows == 32 && pl.depth == 4)
-    launch_kernel(grouped_mid_kernel<DT, 4, 1, UP>, grid, dim3(GM_THREADS), 0, st, p);
-  else if (pl.rows == 32)
-    launch_kernel(grouped_mid_kernel<DT, 3, 1, UP>, grid, dim3(GM_THREADS), 0, st, p);
-  else if (pl.depth == 4)
-    launch_kernel(grouped_mid_kernel<DT, 4, 2, UP>, grid, dim3(GM_THREADS), 0, st, p);
-  else
-    launch_kernel(grouped_mid_kernel<DT, 2, 2, UP>, grid, dim3(GM_THREADS), 0, st, p);
+    return launch_kernel(grouped_tiles_kernel<DT, UP>, grid, dim3(GT_THREADS), 0, st, p);
+  if (pl.kernel == GROUPED_ROWS && pl.depth == 4)
+    return launch_kernel(grouped_rows_kernel<DT, 4, UP>, grid, dim3(GS_THREADS), 0, st, p);
+  if (pl.kernel == GROUPED_ROWS)
+    return launch_kernel(grouped_rows_kernel<DT, 2, UP>, grid, dim3(GS_THREADS), 0, st, p);
+  if (pl.rows == 32 && pl.depth == 4)
+    return launch_kernel(grouped_mid_kernel<DT, 4, 1, UP>, grid, dim3(GM_THREADS), 0, st, p);
+  if (pl.rows == 32)
+    return launch_kernel(grouped_mid_kernel<DT, 3, 1, UP>, grid, dim3(GM_THREADS), 0, st, p);
+  if (pl.depth == 4)
+    return launch_kernel(grouped_mid_kernel<DT, 4, 2, UP>, grid, dim3(GM_THREADS), 0, st, p);
+  return launch_kernel(grouped_mid_kernel<DT, 2, 2, UP>, grid, dim3(GM_THREADS), 0, st, p);
 }
 
 GroupedPlan grouped_plan(int dt, bool up, int64_t m, int groups, int cols, int64_t k_bytes,
@@ -980,14 +979,13 @@ hipError_t launch_grouped(int dt, const GroupedParams& p, hipStream_t st) {
   const bool up = p.w_up != nullptr;
   const GroupedPlan pl = grouped_plan(dt, up, p.m, p.groups, p.cols, p.k_bytes, p.picks, p.x_rows);
   switch (dt) {
-    case DT_BF16: up ? launch_plan<DT_BF16, true>(p, pl, st)
-                     : launch_plan<DT_BF16, false>(p, pl, st); break;
-    case DT_F32: up ? launch_plan<DT_F32, true>(p, pl, st)
-                    : launch_plan<DT_F32, false>(p, pl, st); break;
-    default: up ? launch_plan<DT_E4M3, true>(p, pl, st)
-                : launch_plan<DT_E4M3, false>(p, pl, st);
+    case DT_BF16: return up ? launch_plan<DT_BF16, true>(p, pl, st)
+                            : launch_plan<DT_BF16, false>(p, pl, st);
+    case DT_F32: return up ? launch_plan<DT_F32, true>(p, pl, st)
+                           : launch_plan<DT_F32, false>(p, pl, st);
+    default: return up ? launch_plan<DT_E4M3, true>(p, pl, st)
+                       : launch_plan<DT_E4M3, false>(p, pl, st);
   }
-  return hipGetLastError();
 }
 
 }  // namespace lookme

@@ -12,14 +12,18 @@
 namespace lookme {
 
 // A launch without the call configuration that hipLaunchKernelGGL pushes and pops
-// (2.79 -> 2.60 us of host time); its status is the next hipGetLastError.
+// (2.79 -> 2.60 us of host time).  Returns the launch's own status: the thread's last
+// error may be one that another call of the program's has left.
 template <class T>
 struct SameType { using type = T; };
 template <class... A>
-inline void launch_kernel(void (*kernel)(A...), dim3 grid, dim3 block, size_t lds, hipStream_t st,
-                          typename SameType<A>::type... a) {
+inline hipError_t launch_kernel(void (*kernel)(A...), dim3 grid, dim3 block, size_t lds,
+                                hipStream_t st, typename SameType<A>::type... a) {
   void* args[] = {const_cast<void*>(static_cast<const void*>(&a))...};
-  (void)hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, args, lds, st);
+  const hipError_t e =
+      hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, args, lds, st);
+  if (e != hipSuccess) (void)hipGetLastError();   // reported here, not to the next who asks
+  return e;
 }
 
 // ---- projection: q[l, t, :] = round(x[t, :] . Wt[l]^T) --------------------

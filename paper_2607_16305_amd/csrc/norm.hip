@@ -302,14 +302,13 @@ __global__ __launch_bounds__(RN_THREADS) void residual_norm_wide_kernel(NormPara
 }
 
 template <int DT, int T, int CH>
-static void launch_norm_t(const NormParams& p, hipStream_t st) {
+static hipError_t launch_norm_t(const NormParams& p, hipStream_t st) {
   constexpr int BLOCK = T > RN_THREADS ? T : RN_THREADS;
   const int64_t rows = BLOCK / T;
   const dim3 grid((unsigned)((p.n + rows - 1) / rows));
   if (p.parts == 1)
-    launch_kernel(residual_norm_kernel<DT, T, CH, true>, grid, dim3(BLOCK), 0, st, p);
-  else
-    launch_kernel(residual_norm_kernel<DT, T, CH, false>, grid, dim3(BLOCK), 0, st, p);
+    return launch_kernel(residual_norm_kernel<DT, T, CH, true>, grid, dim3(BLOCK), 0, st, p);
+  return launch_kernel(residual_norm_kernel<DT, T, CH, false>, grid, dim3(BLOCK), 0, st, p);
 }
 
 // A wave a row while that is two chunks a thread, else 256 threads; 1024 while
@@ -317,18 +316,18 @@ static void launch_norm_t(const NormParams& p, hipStream_t st) {
 // (2 rows of 7360 in two parts 8.8 -> 5.1 us, 256 rows of 4096 in eight
 // 9.6 -> 7.2; 512 such rows 12.0 -> 13.7).
 template <int DT>
-static void launch_norm(const NormParams& p, hipStream_t st) {
+static hipError_t launch_norm(const NormParams& p, hipStream_t st) {
   const bool few = p.n <= 256;
-  if (p.chunks <= 64) launch_norm_t<DT, 64, 1>(p, st);
-  else if (p.chunks <= 128) launch_norm_t<DT, 64, 2>(p, st);
-  else if (p.chunks <= 256) launch_norm_t<DT, 256, 1>(p, st);
-  else if (p.chunks <= 1024 && few) launch_norm_t<DT, 1024, 1>(p, st);
-  else if (p.chunks <= 2048 && few) launch_norm_t<DT, 1024, 2>(p, st);
-  else if (p.chunks <= 512) launch_norm_t<DT, 256, 2>(p, st);
-  else if (p.chunks <= 1024) launch_norm_t<DT, 256, 4>(p, st);
-  else if (p.chunks <= 2048) launch_norm_t<DT, 256, 8>(p, st);
-  else
-    launch_kernel(residual_norm_wide_kernel<DT>, dim3((unsigned)p.n), dim3(RN_THREADS), 0, st, p);
+  if (p.chunks <= 64) return launch_norm_t<DT, 64, 1>(p, st);
+  if (p.chunks <= 128) return launch_norm_t<DT, 64, 2>(p, st);
+  if (p.chunks <= 256) return launch_norm_t<DT, 256, 1>(p, st);
+  if (p.chunks <= 1024 && few) return launch_norm_t<DT, 1024, 1>(p, st);
+  if (p.chunks <= 2048 && few) return launch_norm_t<DT, 1024, 2>(p, st);
+  if (p.chunks <= 512) return launch_norm_t<DT, 256, 2>(p, st);
+  if (p.chunks <= 1024) return launch_norm_t<DT, 256, 4>(p, st);
+  if (p.chunks <= 2048) return launch_norm_t<DT, 256, 8>(p, st);
+  return launch_kernel(residual_norm_wide_kernel<DT>, dim3((unsigned)p.n), dim3(RN_THREADS), 0, st,
+                       p);
 }
 
 hipError_t launch_residual_norm(int dt, int64_t n, int d, const void* hidden, int parts,
@@ -352,8 +351,8 @@ hipError_t launch_residual_norm(int dt, int64_t n, int d, const void* hidden, in
   p.inv_d = 1.f / (float)d;
   for (int64_t row = 0; row < n; row += RN_ROWS) {
     p.n = n - row < RN_ROWS ? n - row : RN_ROWS;
-    if (dt == DT_BF16) launch_norm<DT_BF16>(p, st);
-    else launch_norm<DT_F32>(p, st);
+    const hipError_t e = dt == DT_BF16 ? launch_norm<DT_BF16>(p, st) : launch_norm<DT_F32>(p, st);
+    if (e != hipSuccess) return e;
     const int64_t bytes = RN_ROWS * p.row_bytes;
     p.hidden += bytes;
     if (p.add != nullptr) p.add += bytes * parts;
@@ -365,7 +364,7 @@ hipError_t launch_residual_norm(int dt, int64_t n, int d, const void* hidden, in
       p.scale_out += RN_ROWS;
     }
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace lookme

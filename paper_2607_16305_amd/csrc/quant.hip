@@ -316,7 +316,7 @@ __global__ __launch_bounds__(QP_THREADS) void quant_rows_kernel(QuantParams p) {
 }
 
 template <int DT, int NT, int RW, bool UP>
-static void launch_quant_nt(const QuantParams& p, hipStream_t st) {
+static hipError_t launch_quant_nt(const QuantParams& p, hipStream_t st) {
   constexpr int TILES = (UP ? 2 : 1) * RW;
   const dim3 grid((unsigned)((p.cols + 16 * RW - 1) / (16 * RW)),
                   (unsigned)((p.n + 16 * NT - 1) / (16 * NT)));
@@ -327,9 +327,9 @@ static void launch_quant_nt(const QuantParams& p, hipStream_t st) {
                 "dynamic LDS of a launch");
   const size_t lds = scales > sums ? scales : sums;
   if (p.group < 128)
-    launch_kernel(quant_rows_kernel<DT, NT, RW, UP, true>, grid, dim3(QP_THREADS), lds, st, p);
-  else
-    launch_kernel(quant_rows_kernel<DT, NT, RW, UP, false>, grid, dim3(QP_THREADS), lds, st, p);
+    return launch_kernel(quant_rows_kernel<DT, NT, RW, UP, true>, grid, dim3(QP_THREADS), lds, st,
+                         p);
+  return launch_kernel(quant_rows_kernel<DT, NT, RW, UP, false>, grid, dim3(QP_THREADS), lds, st, p);
 }
 
 // Two row tiles a wave where these are a workgroup for every CU: the tokens,
@@ -343,29 +343,22 @@ static void launch_quant_nt(const QuantParams& p, hipStream_t st) {
 // row of 1024 x 8192 7.5 and 7.4 us) and no loads for the tokens there are none
 // of (the same) were no faster.
 template <int DT, bool UP>
-static void launch_quant_dt(const QuantParams& p, hipStream_t st) {
+static hipError_t launch_quant_dt(const QuantParams& p, hipStream_t st) {
   const int64_t wide = (int64_t)((p.cols + 31) / 32) * ((p.n + 31) / 32);
   const bool two = wide >= 256 && !(UP && (DT == DT_BF16 ? p.n <= 8 : p.n > 16));
   if (p.n <= 16) {
-    if (two) launch_quant_nt<DT, 1, 2, UP>(p, st);
-    else launch_quant_nt<DT, 1, 1, UP>(p, st);
-  } else {
-    if constexpr (!(UP && DT == DT_F32))
-      if (two) return launch_quant_nt<DT, 2, 2, UP>(p, st);
-    launch_quant_nt<DT, 2, 1, UP>(p, st);
+    return two ? launch_quant_nt<DT, 1, 2, UP>(p, st) : launch_quant_nt<DT, 1, 1, UP>(p, st);
   }
+  if constexpr (!(UP && DT == DT_F32))
+    if (two) return launch_quant_nt<DT, 2, 2, UP>(p, st);
+  return launch_quant_nt<DT, 2, 1, UP>(p, st);
 }
 
 hipError_t launch_quant(int dt, const QuantParams& p, hipStream_t st) {
   if (p.n == 0) return hipSuccess;
-  if (dt == DT_BF16) {
-    if (p.up) launch_quant_dt<DT_BF16, true>(p, st);
-    else launch_quant_dt<DT_BF16, false>(p, st);
-  } else {
-    if (p.up) launch_quant_dt<DT_F32, true>(p, st);
-    else launch_quant_dt<DT_F32, false>(p, st);
-  }
-  return hipGetLastError();
+  if (dt == DT_BF16)
+    return p.up ? launch_quant_dt<DT_BF16, true>(p, st) : launch_quant_dt<DT_BF16, false>(p, st);
+  return p.up ? launch_quant_dt<DT_F32, true>(p, st) : launch_quant_dt<DT_F32, false>(p, st);
 }
 
 }  // namespace lookme

@@ -538,8 +538,10 @@ lookme_status_t lookme_inject_text(int32_t dtype, const void* table, int64_t voc
  *   hidden_out[t, :] = s,  out[t, :] = round(y)
  *   scale_out[t] = max(max|y| / 448, 2^-126),  out_quant[t, :] = e4m3(y / scale_out[t])
  * float32 throughout (part j into partial sum j mod 4, these one after another,
- * then hidden), one rounding (ties to even) into each output.  A part of
- * weight 0 is left out whatever its row holds.
+ * then hidden; y times the reciprocal of scale_out), one rounding (ties to even)
+ * into each output.  The squares are summed as they are: a finite row whose sum
+ * of squares passes float32's range gives 0 in out.  A part of weight 0 is left
+ * out whatever its row holds.
  * A row with a NaN or an infinity gives what IEEE arithmetic gives (NaN in
  * out and scale_out).
  *   dtype      lookme_dtype_t of hidden, add, weight, hidden_out and out (no

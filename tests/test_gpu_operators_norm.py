@@ -44,3 +44,20 @@ def test_norm_of_a_sum_that_is_not_stored(lk, dtype, d, parts, weighted, n):  # 
             assert torch.equal(q1.view(torch.uint8), q.view(torch.uint8))
             assert torch.equal(sc1, sc)
     assert torch.equal(hd.cpu(), h) and torch.equal(ad.cpu().nan_to_num(), add.nan_to_num())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [512, 4096, 40000])
+def test_norm_of_rows_whose_squares_leave_float32(lk, dtype, d):  # noqa: F811
+    """values from 2^64 on give 0, of 2^63 the norm; a row beside them is its own"""
+    _say("norm of huge rows", dtype, d)
+    h = torch.ones((4, d), dtype=DT[dtype])
+    h[1], h[2, 1:] = 2.0 ** 64, 0
+    h[2, 0] = 2.0 ** 63
+    hd = h.cuda()
+    o = torch.full_like(hd, 7.0)
+    q, sc = torch.zeros((4, d), dtype=E4M3, device="cuda"), torch.zeros(4, device="cuda")
+    lk.residual_norm(hd, eps=0.0, out=o, out_quant=q, scale_out=sc)
+    assert (o[1] == 0).all() and (q[1].float() == 0).all() and float(sc[1]) == 2.0 ** -126
+    assert torch.equal(o[0], o[3]) and ((o[0].double() - 1).abs() <= 2.0 ** -8).all()
+    assert abs(float(o[2, 0]) / d ** 0.5 - 1) <= 2.0 ** -8 and (o[2, 1:] == 0).all()

@@ -71,6 +71,26 @@ def test_quant_weights_of_zero_leave_a_value_out(lk, dtype, zero, n, group):  # 
     assert torch.equal(out.cpu(), want.to(DT[dtype]))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,d_out", [(2 ** 20 - 16, 8), (3, 2 ** 21 + 8), (40, 2 ** 18)])
+def test_quant_products_of_the_most_rows_and_columns(lk, dtype, n, d_out):  # noqa: F811
+    _say("quant large", dtype, n, d_out)
+    x, w, s, z = X.quant_case(16, 64, 4096, 32, DT[dtype], True)
+    xs, ws = x.repeat(-(-n // 16), 1)[:n], w.repeat(-(-d_out // 4096), 1)[:d_out]
+    ss, zs = (t.repeat(-(-d_out // 4096), 1)[:d_out] for t in (s, z))
+    out = torch.empty((n, d_out), dtype=DT[dtype], device="cuda")
+    lk.quant_product(*_cuda(xs, ws, ss), out, zero=zs.cuda())
+    want = X.quant_sums(x, w, s, z).to(DT[dtype]).cuda()
+    for a in range(0, n, 16):
+        if n <= 64 or a % 65536 == 0 or a + 16 >= n:
+            for b in range(0, d_out, 4096):
+                got = out[a:a + 16, b:b + 4096]
+                assert torch.equal(got, want[:got.shape[0], :got.shape[1]]), (a, b)
+    full = out[:n // 16 * 16]
+    if d_out < 4096:
+        assert (full.view(-1, 16, d_out) == want[:, :d_out]).all()
+
+
 # ---------------------------------------------------------------------------
 # e4m3 grouped products
 # ---------------------------------------------------------------------------

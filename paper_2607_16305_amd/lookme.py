@@ -446,7 +446,7 @@ def _call(name, device, stream, *args):
     would run there, on memory that it may not reach."""
     if device < 0:
         _refuse("tensors that are not in device memory")
-    if stream is not None and not isinstance(stream, int) and stream.device_index != device:
+    if stream is not None and getattr(stream, "device_index", device) != device:
         _refuse(f"the stream is of device {stream.device_index}, the tensors are on {device}")
     if device != torch._C._cuda_getDevice():
         with torch.cuda.device(device):

@@ -39,7 +39,8 @@ def test_a_stream_of_another_device_is_refused(calls):
 def test_a_stream_of_the_tensors_device_and_an_address_are_passed_on(calls):
     lk._call("lookme_group_rows", 0, _stream(0), 8)
     lk._call("lookme_group_rows", 0, 77, 8)
-    assert calls == [("lookme_group_rows", (8, 1234)), ("lookme_group_rows", (8, 77))]
+    lk._call("lookme_group_rows", 0, types.SimpleNamespace(cuda_stream=5), 8)   # says no device
+    assert [c[1] for c in calls] == [(8, 1234), (8, 77), (8, 5)]
 
 
 BIG = 2 ** 32           # cut to 32 bits, BIG + 64 is 64

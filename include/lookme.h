@@ -674,6 +674,136 @@ lookme_status_t lookme_quant_swiglu(int32_t dtype, int64_t n, int32_t d_in, int3
                                     const uint8_t* zero_up, void* out, void* stream);
 
 /*
+ * Attention of a layer, the Delta = Attn(H_in) that lookme_select and lookme_gate
+ * take: lookme_head_norm_rotary makes q and k of a product's rows,
+ * lookme_cache_write keeps k and v in 4 bits, lookme_cache_attention attends over
+ * what is kept; its rows are the input of the output projection.
+ *
+ * The rows of q, k, v and out may have any stride: row t, head h, element j of x is
+ * x[t * x_stride + h * head_dim + j], x_stride in elements, at least heads *
+ * head_dim and, times the element size, a multiple of 16 bytes.
+ */
+
+/*
+ * lookme_head_norm_rotary -- the root-mean-square norm of each head of the queries
+ * and keys with the rotation of their positions, in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * weight            (norm = 0: y = x)
+ *   a_i = pos[axis[i], t] * freq[i],  c_i = factor cos a_i,  s_i = factor sin a_i
+ *   z = y_first c_i - y_second s_i,  z' = y_first s_i + y_second c_i   (i < rot / 2)
+ * for the elements (i, i + rot / 2), or (2 i, 2 i + 1) with interleaved; elements
+ * from rot on keep y.  float32, one rounding into the output; the angle is reduced
+ * in float64, so far positions keep theirs.  freq holds what a model scales for
+ * long contexts, factor the scale of its rotation.
+ *   q, q_out [n, q_heads, head_dim], k, k_out [n, k_heads, head_dim] with strides
+ *            as above; an output may be its input, with the same stride, else they
+ *            do not overlap.  k_heads = 0: no k (its pointers are not used)
+ *   norm     0 or 1; q_weight, k_weight [head_dim] or NULL (1), NULL for norm = 0
+ *   rot      rotated elements: even, in [0, head_dim]; 0: no rotation (pos, axis and
+ *            freq NULL)
+ *   pos      [axes, n] int32, a token's position on every axis (row and column of an
+ *            image beside the order of the text); any int32
+ *   axis     [rot / 2] int32 in [0, axes) (clamped), or NULL (axis 0)
+ *   freq     [rot / 2] float32, finite, |pos freq| below 2^40
+ * head_dim * elem_size a multiple of 16 bytes, head_dim at most 256.  n = 0 does
+ * nothing.  Needs no handle and no workspace.
+ */
+lookme_status_t lookme_head_norm_rotary(int32_t dtype, int64_t n, int32_t head_dim,
+                                        int32_t q_heads, const void* q, int64_t q_stride,
+                                        void* q_out, int64_t q_out_stride, int32_t k_heads,
+                                        const void* k, int64_t k_stride, void* k_out,
+                                        int64_t k_out_stride, int32_t norm, const void* q_weight,
+                                        const void* k_weight, float eps, int32_t rot,
+                                        int32_t interleaved, int32_t axes, const int32_t* pos,
+                                        const int32_t* axis, const float* freq, float factor,
+                                        void* stream);
+
+/*
+ * The cache of 4 bits, [pages, kv_heads, page / 32, 34 head_dim] bytes: page p
+ * holds `page` tokens (a power of two in [32, 2^20]) of every head, slot p * page +
+ * i is its token i.  32 neighbouring values of a head (of a token's k or v) share a
+ * scale 2^(byte - 127); a value is a sign bit and three bits for 0, .5, 1, 1.5, 2,
+ * 3, 4, 6.  The byte is the smallest E + 127 with max|x| <= 7 2^E, in [27, 252]
+ * (below, values become zeros; above, they saturate at 6 2^125), or 255 where one
+ * of the 32 is not finite: the block then reads as NaN.  The code is the nearest
+ * value's, of two as near the even code.
+ *   A tile of 32 tokens of a head, d = head_dim, u = d / 16; dim, dim + 1 of an
+ * even dim share a byte, dim in its low half:
+ *   k of token t:  byte t d/2 + (dim % 32 / 8) d/8 + (dim / 32) 4 + dim % 8 / 2
+ *   v of token t:  byte 16 d + ((t % 16 / 4 * 16 + dim / u) 8 + t % 4 + 4 (t / 16)) u/2
+ *                  + dim % u / 2
+ *   scales:        k 32 d + t d/32 + dim / 32
+ *                  v 33 d + dim / 32 * 32 + t % 16 / 4 * 8 + t % 4 + 4 (t / 16)
+ * head_dim 64, 128 or 256; pages * page at most 2^31; kv_heads at most 4096.
+ */
+
+/*
+ * lookme_cache_write -- keeps k and v, [n, kv_heads, head_dim] with strides as
+ * above, in the slots of their rows:
+ *   slots [n] int32; a slot outside [0, pages * page) (-1 for a padded row) is not
+ *         written.  Two rows with one slot race.
+ * Other tokens of a tile keep their bytes.  A function of each row alone, the same
+ * bytes whatever the batch.  n = 0 does nothing.  Needs no workspace.
+ */
+lookme_status_t lookme_cache_write(int32_t dtype, int64_t n, int32_t kv_heads, int32_t head_dim,
+                                   const void* k, int64_t k_stride, const void* v,
+                                   int64_t v_stride, const int32_t* slots, int64_t pages,
+                                   int32_t page, void* cache, void* stream);
+
+/*
+ * lookme_cache_read -- the values that the slots hold (exact in either dtype), to
+ * k_out and v_out, [n, kv_heads, head_dim] with strides as above, one of them may
+ * be NULL.  Rows whose slot is out of range are left as they were.
+ */
+lookme_status_t lookme_cache_read(int32_t dtype, int64_t n, int32_t kv_heads, int32_t head_dim,
+                                  const int32_t* slots, int64_t pages, int32_t page,
+                                  const void* cache, void* k_out, int64_t k_stride, void* v_out,
+                                  int64_t v_stride, void* stream);
+
+/*
+ * lookme_cache_attention -- attention over the cache: for sequence b, its row i of m
+ * = q_offsets[b + 1] - q_offsets[b] rows, and query head h,
+ *   s_t = scale <q[q_offsets[b] + i, h], k_t>,  p = softmax over the visible t,
+ *   out[q_offsets[b] + i, h] = round(sum_t p_t v_t)
+ * with k_t, v_t of key head h / (q_heads / kv_heads), token t of sequence b.
+ * Visible are t < lengths[b], with causal also t <= lengths[b] - m + i: the rows are
+ * the sequence's last m tokens, already written.  Without causal the cache may be
+ * another sequence's, say an image encoder's states.  A row that sees no token (or
+ * whose scores are all minus infinity) gives 0.  Tokens that a row does not see do
+ * not touch it, whatever their bytes; a visible block that is not finite gives NaN.
+ *   n          rows of q and out, [n, q_heads, head_dim] with strides as above;
+ *              out may be q, with the same stride
+ *   q_offsets  [batch + 1] int32, ascending, in [0, n] (clamped); NULL: row b is
+ *              sequence b's (n = batch).  Rows of no sequence are left as they were
+ *   lengths    [batch] int32: the sequences' tokens, clamped to [0, max_pages * page]
+ *   pages      [batch, max_pages] int32: token t of sequence b is token t % page of
+ *              page pages[b, t / page].  Pages behind a length are not read; a page
+ *              outside [0, num_pages) leaves its tokens out
+ *   scale      positive and finite
+ *   workspace  lookme_cache_attention_workspace bytes, 256-byte aligned (may be NULL
+ *              where that is 0).  Nothing is kept in it between calls, but calls that
+ *              may overlap on the GPU need one each.
+ * float32 scores and sums; k and v are exact.  bf16: p is rounded to bf16 before
+ * it multiplies v.  q_heads a multiple of kv_heads, n * q_heads at most 2^29,
+ * batch * kv_heads at most 2^22, max_pages * page at most 2^30.  n = 0 does nothing.
+ */
+lookme_status_t lookme_cache_attention(int32_t dtype, int64_t n, int32_t batch, int32_t q_heads,
+                                       int32_t kv_heads, int32_t head_dim, const void* q,
+                                       int64_t q_stride, const int32_t* q_offsets,
+                                       const int32_t* lengths, const int32_t* pages,
+                                       int32_t max_pages, int64_t num_pages, int32_t page,
+                                       const void* cache, float scale, int32_t causal, void* out,
+                                       int64_t out_stride, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of such a call, at most LOOKME_ATTENTION_WORKSPACE.  No HIP
+ * call is made. */
+#define LOOKME_ATTENTION_WORKSPACE ((size_t)64 << 20)
+lookme_status_t lookme_cache_attention_workspace(int32_t dtype, int64_t n, int32_t batch,
+                                                 int32_t q_heads, int32_t kv_heads,
+                                                 int32_t head_dim, int32_t max_pages,
+                                                 int32_t page, size_t* bytes);
+
+/*
  * Measurement support (not part of the method).  When enabled, each kernel
  * group that route/lookup/inject launches is bracketed by a pair of HIP timing
  * events recorded on the call's stream; the Level-2 scoring launch of the

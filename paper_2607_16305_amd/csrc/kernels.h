@@ -361,4 +361,58 @@ struct QuantParams {
 };
 hipError_t launch_quant(int dt, const QuantParams& p, hipStream_t st);
 
+// ---- head norms and rotary positions (rotary.hip) --------------------------
+struct RotarySide {
+  const char* x;             // row t, head h at x + t stride + h head_bytes
+  char* out;
+  const char* weight;        // [d] or null (1)
+  int64_t stride, out_stride;   // bytes
+};
+struct RotaryParams {
+  RotarySide q, k;
+  const int32_t* pos;        // [axes, n]: pos_stride entries an axis
+  const int32_t* axis;       // [rot / 2] or null (axis 0)
+  const float* freq;         // [rot / 2]
+  int64_t n, pos_stride;
+  int q_heads, k_heads, head_bytes, chunks, rot, axes;
+  bool norm, interleaved;
+  float eps, inv_d, factor;
+  int tokens, span;          // of a workgroup (set by the launch)
+};
+hipError_t launch_head_norm_rotary(int dt, const RotaryParams& p, hipStream_t st);
+
+// ---- the 4-bit cache (cache4.h, cache.hip) ---------------------------------
+struct CacheParams {
+  const char *k, *v;         // write: rows of [heads, d]
+  char *k_out, *v_out;       // read: the same; one may be null
+  int64_t k_stride, v_stride;   // bytes
+  const int32_t* slots;      // [n]: page << page_log2 | place
+  uint8_t* cache;            // [pages, heads, page / 32, 34 d]
+  int64_t n, slots_all;
+  int heads, d, page_log2;
+};
+hipError_t launch_cache_write(int dt, const CacheParams& p, hipStream_t st);
+hipError_t launch_cache_read(int dt, const CacheParams& p, hipStream_t st);
+
+// ---- attention over the 4-bit cache (attend.hip) ---------------------------
+struct AttendParams {
+  const char* q;             // row i, head h at q + i q_stride + h head_bytes
+  char* out;
+  const uint8_t* cache;
+  const int32_t* pages;      // [batch, max_pages]
+  const int32_t* lengths;    // [batch]
+  const int32_t* q_offsets;  // [batch + 1] or null (one row each)
+  float* part;               // workspace: outputs, then maxima and sums
+  int64_t q_stride, out_stride;   // bytes
+  int n, batch, q_heads, kv_heads, max_pages, num_pages, page_log2;
+  bool causal;
+  float scale_log2;
+  int target;                // work units that the cut of the keys aims at; 0: no cut
+  int units_most;            // workgroups of the launch
+};
+// Bytes of workspace of a call (0: none needed).
+size_t attend_workspace(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
+                        int64_t tokens);
+hipError_t launch_attend(int dt, int d, AttendParams p, hipStream_t st);
+
 }  // namespace lookme

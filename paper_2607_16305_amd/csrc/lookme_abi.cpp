@@ -356,6 +356,92 @@ lookme_status_t grouped_params(int32_t groups, int64_t m, int32_t d_in, int32_t 
   return LOOKME_OK;
 }
 
+// rows of heads at a stride (in elements): whole 16-byte chunks, rows apart
+lookme_status_t check_stride(int64_t stride, int32_t heads, int32_t head_dim, int es,
+                             const char* name) {
+  if (stride < (int64_t)heads * head_dim)
+    return fail(LOOKME_ERR_INVALID, "%s %lld is below a row's %lld elements", name,
+                (long long)stride, (long long)heads * head_dim);
+  if (stride > (int64_t)1 << 31)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%s %lld exceeds 2^31", name, (long long)stride);
+  if (stride * es % 16 != 0)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%s times the element size must be a multiple of 16",
+                name);
+  return LOOKME_OK;
+}
+
+lookme_status_t check_heads(int32_t heads, const char* name) {
+  if (heads < 1) return fail(LOOKME_ERR_INVALID, "%s must be >= 1 (got %d)", name, heads);
+  if (heads > 4096) return fail(LOOKME_ERR_UNSUPPORTED, "%s %d exceeds 4096", name, heads);
+  return LOOKME_OK;
+}
+
+int log2_of(int32_t v) {
+  int l = 0;
+  while ((1 << l) < v) ++l;
+  return l;
+}
+
+// the geometry of a 4-bit cache, without its pages
+lookme_status_t check_cache(int32_t dtype, int32_t kv_heads, int32_t head_dim, int32_t page) {
+  LOOKME_TRY(check_dtype(dtype));
+  LOOKME_TRY(check_heads(kv_heads, "kv_heads"));
+  if (head_dim < 1) return fail(LOOKME_ERR_INVALID, "head_dim must be positive");
+  if (head_dim != 64 && head_dim != 128 && head_dim != 256)
+    return fail(LOOKME_ERR_UNSUPPORTED, "head_dim %d: 64, 128 or 256", head_dim);
+  if (page < 1) return fail(LOOKME_ERR_INVALID, "page must be positive (got %d)", page);
+  if (page < 32 || page > 1 << 20 || (page & (page - 1)) != 0)
+    return fail(LOOKME_ERR_UNSUPPORTED, "page %d: a power of two in [32, 2^20]", page);
+  return LOOKME_OK;
+}
+
+lookme_status_t check_pages(int64_t pages, int32_t page) {
+  if (pages < 1) return fail(LOOKME_ERR_INVALID, "%lld pages", (long long)pages);
+  if (pages > ((int64_t)1 << 31) / page)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%lld pages of %d tokens exceed 2^31", (long long)pages,
+                page);
+  return LOOKME_OK;
+}
+
+lookme_status_t check_attention(int32_t dtype, int64_t n, int32_t batch, int32_t q_heads,
+                                int32_t kv_heads, int32_t head_dim, int32_t max_pages,
+                                int32_t page) {
+  LOOKME_TRY(check_cache(dtype, kv_heads, head_dim, page));
+  LOOKME_TRY(check_rows(n));
+  LOOKME_TRY(check_heads(q_heads, "q_heads"));
+  if (q_heads % kv_heads != 0)
+    return fail(LOOKME_ERR_INVALID, "%d query heads for %d key heads", q_heads, kv_heads);
+  if (batch < 0) return fail(LOOKME_ERR_INVALID, "batch must be >= 0 (got %d)", batch);
+  if (max_pages < 1) return fail(LOOKME_ERR_INVALID, "max_pages must be >= 1 (got %d)", max_pages);
+  if ((int64_t)max_pages * page > (int64_t)1 << 30)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%d pages of %d tokens a sequence exceed 2^30", max_pages,
+                page);
+  if (n * q_heads > (int64_t)1 << 29 || (int64_t)batch * kv_heads > (int64_t)1 << 22)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%lld rows of %d heads exceed 2^29, or %d sequences of %d "
+                "key heads 2^22", (long long)n, q_heads, batch, kv_heads);
+  return LOOKME_OK;
+}
+
+lookme_status_t cache_params(int32_t dtype, int64_t n, int32_t kv_heads, int32_t head_dim,
+                             const int32_t* slots, int64_t pages, int32_t page, const void* cache,
+                             lookme::CacheParams* p) {
+  LOOKME_TRY(check_cache(dtype, kv_heads, head_dim, page));
+  LOOKME_TRY(check_rows(n));
+  LOOKME_TRY(check_pages(pages, page));
+  if (n > 0) {
+    LOOKME_TRY(check_ptr(slots, "slots"));
+    LOOKME_TRY(check_ptr(cache, "cache"));
+  }
+  p->slots = slots;
+  p->cache = static_cast<uint8_t*>(const_cast<void*>(cache));
+  p->n = n;
+  p->slots_all = pages * page;
+  p->heads = kv_heads;
+  p->d = head_dim;
+  p->page_log2 = log2_of(page);
+  return LOOKME_OK;
+}
+
 lookme_status_t check_quant(int32_t dtype, int64_t n, int32_t d_in, int32_t d_out, int32_t group) {
   LOOKME_TRY(check_dtype(dtype));
   if (n < 0) return fail(LOOKME_ERR_INVALID, "n must be >= 0 (got %lld)", (long long)n);
@@ -1381,6 +1467,199 @@ lookme_status_t lookme_quant_swiglu(int32_t dtype, int64_t n, int32_t d_in, int3
   p.up = true;
   return hip_status(lookme::launch_quant(dtype, p, static_cast<hipStream_t>(stream)),
                     "quant swiglu launch");
+}
+
+lookme_status_t lookme_head_norm_rotary(int32_t dtype, int64_t n, int32_t head_dim,
+                                        int32_t q_heads, const void* q, int64_t q_stride,
+                                        void* q_out, int64_t q_out_stride, int32_t k_heads,
+                                        const void* k, int64_t k_stride, void* k_out,
+                                        int64_t k_out_stride, int32_t norm, const void* q_weight,
+                                        const void* k_weight, float eps, int32_t rot,
+                                        int32_t interleaved, int32_t axes, const int32_t* pos,
+                                        const int32_t* axis, const float* freq, float factor,
+                                        void* stream) {
+  LOOKME_TRY(check_dtype(dtype));
+  LOOKME_TRY(check_rows(n));
+  const int es = elem_size(dtype);
+  LOOKME_TRY(check_width(head_dim, es, "head_dim"));
+  if (head_dim > 256) return fail(LOOKME_ERR_UNSUPPORTED, "head_dim %d exceeds 256", head_dim);
+  LOOKME_TRY(check_heads(q_heads, "q_heads"));
+  if (k_heads != 0) LOOKME_TRY(check_heads(k_heads, "k_heads"));
+  LOOKME_TRY(check_stride(q_stride, q_heads, head_dim, es, "q_stride"));
+  LOOKME_TRY(check_stride(q_out_stride, q_heads, head_dim, es, "q_out_stride"));
+  if (k_heads != 0) {
+    LOOKME_TRY(check_stride(k_stride, k_heads, head_dim, es, "k_stride"));
+    LOOKME_TRY(check_stride(k_out_stride, k_heads, head_dim, es, "k_out_stride"));
+  }
+  if (norm != 0 && norm != 1) return fail(LOOKME_ERR_INVALID, "norm must be 0 or 1");
+  if (norm == 0 && (q_weight != nullptr || k_weight != nullptr))
+    return fail(LOOKME_ERR_INVALID, "a weight given without norm");
+  if (!(eps >= 0.f)) return fail(LOOKME_ERR_INVALID, "eps must be >= 0");
+  if (rot < 0 || rot > head_dim || rot % 2 != 0)
+    return fail(LOOKME_ERR_INVALID, "rot %d: even, in [0, head_dim]", rot);
+  if (interleaved != 0 && interleaved != 1)
+    return fail(LOOKME_ERR_INVALID, "interleaved must be 0 or 1");
+  if (rot == 0 && (pos != nullptr || axis != nullptr || freq != nullptr))
+    return fail(LOOKME_ERR_INVALID, "positions given for rot = 0");
+  if (rot > 0 && axes < 1) return fail(LOOKME_ERR_INVALID, "axes must be >= 1 (got %d)", axes);
+  if (!(factor - factor == 0.f)) return fail(LOOKME_ERR_INVALID, "factor must be finite");
+  if (n == 0) return LOOKME_OK;
+  LOOKME_TRY(check_ptr(q, "q"));
+  LOOKME_TRY(check_ptr(q_out, "q_out"));
+  if (k_heads != 0) {
+    LOOKME_TRY(check_ptr(k, "k"));
+    LOOKME_TRY(check_ptr(k_out, "k_out"));
+  }
+  if ((q_out == q && q_out_stride != q_stride) ||
+      (k_heads != 0 && k_out == k && k_out_stride != k_stride))
+    return fail(LOOKME_ERR_INVALID, "an output that is its input needs the same stride");
+  LOOKME_TRY(check_optional(q_weight, "q_weight"));
+  LOOKME_TRY(check_optional(k_weight, "k_weight"));
+  if (rot > 0) {
+    LOOKME_TRY(check_ptr(pos, "pos"));
+    LOOKME_TRY(check_optional(axis, "axis"));
+    LOOKME_TRY(check_ptr(freq, "freq"));
+  }
+  lookme::RotaryParams p{};
+  p.q = {static_cast<const char*>(q), static_cast<char*>(q_out),
+         static_cast<const char*>(q_weight), q_stride * es, q_out_stride * es};
+  p.k = {static_cast<const char*>(k), static_cast<char*>(k_out),
+         static_cast<const char*>(k_weight), k_stride * es, k_out_stride * es};
+  p.pos = pos;
+  p.axis = axis;
+  p.freq = freq;
+  p.n = p.pos_stride = n;
+  p.q_heads = q_heads;
+  p.k_heads = k_heads;
+  p.head_bytes = head_dim * es;
+  p.chunks = p.head_bytes / 16;
+  p.rot = rot;
+  p.axes = axes;
+  p.norm = norm != 0;
+  p.interleaved = interleaved != 0;
+  p.eps = eps;
+  p.inv_d = 1.f / (float)head_dim;
+  p.factor = factor;
+  return hip_status(lookme::launch_head_norm_rotary(dtype, p, static_cast<hipStream_t>(stream)),
+                    "head norm launch");
+}
+
+lookme_status_t lookme_cache_write(int32_t dtype, int64_t n, int32_t kv_heads, int32_t head_dim,
+                                   const void* k, int64_t k_stride, const void* v,
+                                   int64_t v_stride, const int32_t* slots, int64_t pages,
+                                   int32_t page, void* cache, void* stream) {
+  lookme::CacheParams p{};
+  LOOKME_TRY(cache_params(dtype, n, kv_heads, head_dim, slots, pages, page, cache, &p));
+  const int es = elem_size(dtype);
+  LOOKME_TRY(check_stride(k_stride, kv_heads, head_dim, es, "k_stride"));
+  LOOKME_TRY(check_stride(v_stride, kv_heads, head_dim, es, "v_stride"));
+  if (n == 0) return LOOKME_OK;
+  LOOKME_TRY(check_ptr(k, "k"));
+  LOOKME_TRY(check_ptr(v, "v"));
+  p.k = static_cast<const char*>(k);
+  p.v = static_cast<const char*>(v);
+  p.k_stride = k_stride * es;
+  p.v_stride = v_stride * es;
+  return hip_status(lookme::launch_cache_write(dtype, p, static_cast<hipStream_t>(stream)),
+                    "cache write launch");
+}
+
+lookme_status_t lookme_cache_read(int32_t dtype, int64_t n, int32_t kv_heads, int32_t head_dim,
+                                  const int32_t* slots, int64_t pages, int32_t page,
+                                  const void* cache, void* k_out, int64_t k_stride, void* v_out,
+                                  int64_t v_stride, void* stream) {
+  lookme::CacheParams p{};
+  LOOKME_TRY(cache_params(dtype, n, kv_heads, head_dim, slots, pages, page, cache, &p));
+  const int es = elem_size(dtype);
+  if (n == 0) return LOOKME_OK;
+  if (k_out == nullptr && v_out == nullptr) return fail(LOOKME_ERR_INVALID, "no output given");
+  if (k_out != nullptr) {
+    LOOKME_TRY(check_stride(k_stride, kv_heads, head_dim, es, "k_stride"));
+    LOOKME_TRY(check_ptr(k_out, "k_out"));
+  }
+  if (v_out != nullptr) {
+    LOOKME_TRY(check_stride(v_stride, kv_heads, head_dim, es, "v_stride"));
+    LOOKME_TRY(check_ptr(v_out, "v_out"));
+  }
+  p.k_out = static_cast<char*>(k_out);
+  p.v_out = static_cast<char*>(v_out);
+  p.k_stride = k_stride * es;
+  p.v_stride = v_stride * es;
+  return hip_status(lookme::launch_cache_read(dtype, p, static_cast<hipStream_t>(stream)),
+                    "cache read launch");
+}
+
+lookme_status_t lookme_cache_attention_workspace(int32_t dtype, int64_t n, int32_t batch,
+                                                 int32_t q_heads, int32_t kv_heads,
+                                                 int32_t head_dim, int32_t max_pages,
+                                                 int32_t page, size_t* bytes) {
+  if (bytes == nullptr) return fail(LOOKME_ERR_INVALID, "bytes is NULL");
+  LOOKME_TRY(check_attention(dtype, n, batch, q_heads, kv_heads, head_dim, max_pages, page));
+  *bytes = n == 0 || batch == 0
+               ? 0
+               : lookme::attend_workspace(dtype, n, batch, q_heads, kv_heads, head_dim,
+                                          (int64_t)max_pages * page);
+  return LOOKME_OK;
+}
+
+lookme_status_t lookme_cache_attention(int32_t dtype, int64_t n, int32_t batch, int32_t q_heads,
+                                       int32_t kv_heads, int32_t head_dim, const void* q,
+                                       int64_t q_stride, const int32_t* q_offsets,
+                                       const int32_t* lengths, const int32_t* pages,
+                                       int32_t max_pages, int64_t num_pages, int32_t page,
+                                       const void* cache, float scale, int32_t causal, void* out,
+                                       int64_t out_stride, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  LOOKME_TRY(check_attention(dtype, n, batch, q_heads, kv_heads, head_dim, max_pages, page));
+  LOOKME_TRY(check_pages(num_pages, page));
+  const int es = elem_size(dtype);
+  LOOKME_TRY(check_stride(q_stride, q_heads, head_dim, es, "q_stride"));
+  LOOKME_TRY(check_stride(out_stride, q_heads, head_dim, es, "out_stride"));
+  if (q_offsets == nullptr && n != batch)
+    return fail(LOOKME_ERR_INVALID, "%lld rows for %d sequences without q_offsets", (long long)n,
+                batch);
+  if (!(scale > 0.f) || !(scale - scale == 0.f))
+    return fail(LOOKME_ERR_INVALID, "scale must be positive and finite");
+  if (causal != 0 && causal != 1) return fail(LOOKME_ERR_INVALID, "causal must be 0 or 1");
+  if (n == 0 || batch == 0) return LOOKME_OK;
+  LOOKME_TRY(check_ptr(q, "q"));
+  LOOKME_TRY(check_optional(q_offsets, "q_offsets"));
+  LOOKME_TRY(check_ptr(lengths, "lengths"));
+  LOOKME_TRY(check_ptr(pages, "pages"));
+  LOOKME_TRY(check_ptr(cache, "cache"));
+  LOOKME_TRY(check_ptr(out, "out"));
+  if (out == q && out_stride != q_stride)
+    return fail(LOOKME_ERR_INVALID, "an output that is its input needs the same stride");
+  const size_t need = lookme::attend_workspace(dtype, n, batch, q_heads, kv_heads, head_dim,
+                                               (int64_t)max_pages * page);
+  if (need > 0) {
+    if (workspace == nullptr || workspace_bytes < need)
+      return fail(LOOKME_ERR_WORKSPACE, "needs %zu bytes of workspace (got %zu)", need,
+                  workspace == nullptr ? (size_t)0 : workspace_bytes);
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+      return fail(LOOKME_ERR_INVALID, "the workspace must be 256-byte aligned");
+  }
+  lookme::AttendParams p{};
+  p.q = static_cast<const char*>(q);
+  p.out = static_cast<char*>(out);
+  p.cache = static_cast<const uint8_t*>(cache);
+  p.pages = pages;
+  p.lengths = lengths;
+  p.q_offsets = q_offsets;
+  p.part = static_cast<float*>(workspace);
+  p.q_stride = q_stride * es;
+  p.out_stride = out_stride * es;
+  p.n = (int)n;
+  p.batch = batch;
+  p.q_heads = q_heads;
+  p.kv_heads = kv_heads;
+  p.max_pages = max_pages;
+  p.num_pages = (int)num_pages;
+  p.page_log2 = log2_of(page);
+  p.causal = causal != 0;
+  p.scale_log2 = scale * 1.44269504088896340736f;
+  return hip_status(lookme::launch_attend(dtype, head_dim, p, static_cast<hipStream_t>(stream)),
+                    "attention launch");
 }
 
 }  // extern "C"

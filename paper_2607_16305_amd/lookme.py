@@ -24,6 +24,7 @@ LOOKME_SCORE_DOT, LOOKME_SCORE_COS = 0, 1
 LOOKME_KMAX = 32
 LOOKME_NOALLOC_MAX_ROWS = 131072
 LOOKME_MAX_GROUPS = 16384
+LOOKME_ATTENTION_WORKSPACE = 64 << 20
 INT32 = 1 << 31     # one past the largest int32_t, as which the library takes most sizes
 
 STATUS_NAMES = {0: "OK", 1: "INVALID", 2: "UNSUPPORTED", 3: "WORKSPACE", 4: "HIP"}
@@ -40,7 +41,9 @@ EXPORTED = ("lookme_create", "lookme_workspace_size", "lookme_set_workspace", "l
             "lookme_destroy", "lookme_last_error",
             "lookme_profile_enable", "lookme_profile_read", "lookme_inject_noalloc",
             "lookme_residual_norm", "lookme_group_rows", "lookme_grouped_product",
-            "lookme_grouped_product_quant", "lookme_quant_product", "lookme_quant_swiglu")
+            "lookme_grouped_product_quant", "lookme_quant_product", "lookme_quant_swiglu",
+            "lookme_head_norm_rotary", "lookme_cache_write", "lookme_cache_read",
+            "lookme_cache_attention", "lookme_cache_attention_workspace")
 
 GROUPS = ("project", "route", "bucket", "score", "norm", "select", "inject")
 
@@ -134,6 +137,27 @@ def load():
                                  ctypes.c_int32, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
         "lookme_quant_swiglu": [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
                                 ctypes.c_int32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
+        "lookme_head_norm_rotary": [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                    ctypes.c_int32, _vp, ctypes.c_int64, _vp, ctypes.c_int64,
+                                    ctypes.c_int32, _vp, ctypes.c_int64, _vp, ctypes.c_int64,
+                                    ctypes.c_int32, _vp, _vp, ctypes.c_float, ctypes.c_int32,
+                                    ctypes.c_int32, ctypes.c_int32, _vp, _vp, _vp,
+                                    ctypes.c_float, _vp],
+        "lookme_cache_write": [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                               _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, ctypes.c_int64,
+                               ctypes.c_int32, _vp, _vp],
+        "lookme_cache_read": [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _vp,
+                              ctypes.c_int64, ctypes.c_int32, _vp, _vp, ctypes.c_int64, _vp,
+                              ctypes.c_int64, _vp],
+        "lookme_cache_attention": [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                   ctypes.c_int32, ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp,
+                                   _vp, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, _vp,
+                                   ctypes.c_float, ctypes.c_int32, _vp, ctypes.c_int64, _vp,
+                                   ctypes.c_size_t, _vp],
+        "lookme_cache_attention_workspace": [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                             ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                             ctypes.c_int32, ctypes.c_int32,
+                                             ctypes.POINTER(ctypes.c_size_t)],
         "lookme_destroy": [_vp],
         "lookme_profile_enable": [_vp, ctypes.c_int32],
         "lookme_profile_read": [_vp, ctypes.c_int32, ctypes.POINTER(ctypes.c_int64),
@@ -402,6 +426,53 @@ def lookme_quant_swiglu(dtype, n, d_in, d_ff, group, x, w_gate, scale_gate, zero
                                       _stream(stream)))
 
 
+def lookme_head_norm_rotary(dtype, n, head_dim, q_heads, q, q_stride, q_out, q_out_stride, k_heads,
+                            k, k_stride, k_out, k_out_stride, norm, q_weight, k_weight, eps, rot,
+                            interleaved, axes, pos, axis, freq, factor, stream=None):
+    _int32(dtype, head_dim, q_heads, k_heads, norm, rot, interleaved, axes)
+    _check(load().lookme_head_norm_rotary(dtype, n, head_dim, q_heads, _ptr(q), q_stride,
+                                          _ptr(q_out), q_out_stride, k_heads, _ptr(k), k_stride,
+                                          _ptr(k_out), k_out_stride, norm, _ptr(q_weight),
+                                          _ptr(k_weight), eps, rot, interleaved, axes, _ptr(pos),
+                                          _ptr(axis), _ptr(freq), factor, _stream(stream)))
+
+
+def lookme_cache_write(dtype, n, kv_heads, head_dim, k, k_stride, v, v_stride, slots, pages, page,
+                       cache, stream=None):
+    _int32(dtype, kv_heads, head_dim, page)
+    _check(load().lookme_cache_write(dtype, n, kv_heads, head_dim, _ptr(k), k_stride, _ptr(v),
+                                     v_stride, _ptr(slots), pages, page, _ptr(cache),
+                                     _stream(stream)))
+
+
+def lookme_cache_read(dtype, n, kv_heads, head_dim, slots, pages, page, cache, k_out, k_stride,
+                      v_out, v_stride, stream=None):
+    _int32(dtype, kv_heads, head_dim, page)
+    _check(load().lookme_cache_read(dtype, n, kv_heads, head_dim, _ptr(slots), pages, page,
+                                    _ptr(cache), _ptr(k_out), k_stride, _ptr(v_out), v_stride,
+                                    _stream(stream)))
+
+
+def lookme_cache_attention(dtype, n, batch, q_heads, kv_heads, head_dim, q, q_stride, q_offsets,
+                           lengths, pages, max_pages, num_pages, page, cache, scale, causal, out,
+                           out_stride, workspace, workspace_bytes, stream=None):
+    _int32(dtype, batch, q_heads, kv_heads, head_dim, max_pages, page, causal)
+    _check(load().lookme_cache_attention(dtype, n, batch, q_heads, kv_heads, head_dim, _ptr(q),
+                                         q_stride, _ptr(q_offsets), _ptr(lengths), _ptr(pages),
+                                         max_pages, num_pages, page, _ptr(cache), scale, causal,
+                                         _ptr(out), out_stride, _ptr(workspace), workspace_bytes,
+                                         _stream(stream)))
+
+
+def lookme_cache_attention_workspace(dtype, n, batch, q_heads, kv_heads, head_dim, max_pages,
+                                     page) -> int:
+    _int32(dtype, batch, q_heads, kv_heads, head_dim, max_pages, page)
+    out = ctypes.c_size_t()
+    _check(load().lookme_cache_attention_workspace(dtype, n, batch, q_heads, kv_heads, head_dim,
+                                                   max_pages, page, ctypes.byref(out)))
+    return out.value
+
+
 # The same on torch tensors: sizes come from the shapes, which are checked (the
 # C side sees pointers only), and the call runs on the tensors' device.  These
 # are called once a layer and token, so they keep their own time short.
@@ -646,6 +717,153 @@ def quant_swiglu(x, w_gate, s_gate, w_up, s_up, out, z_gate=None, z_up=None, str
     p_out = _tensor("out", out, dt, (n, d_ff), dev)
     _call("lookme_quant_swiglu", dev, stream, code, n, d_in, d_ff, group, x.data_ptr(), *gate, *up,
           p_out)
+
+
+def _heads(name, t, dtype, n, heads, d, device):
+    """(address, stride of a row) of t [n, heads, d], whose rows may lie apart"""
+    if t.dtype is not dtype or t.shape != (n, heads, d) or t.get_device() != device:
+        _wrong(name, t, dtype, (n, heads, d), device)
+    row, head, one = t.stride()
+    if n > 1:
+        if row < heads * d:
+            _refuse(f"the rows of {name} overlap (stride {row})")
+    else:
+        row = heads * d
+    if t.numel() and ((one != 1 and d > 1) or (head != d and heads > 1)):
+        _refuse(f"the heads of {name} do not lie side by side (strides {t.stride()})")
+    return t.data_ptr(), row
+
+
+def head_norm_rotary(q, q_out, k=None, k_out=None, norm=True, q_weight=None, k_weight=None,
+                     eps=1e-6, pos=None, freq=None, axis=None, factor=1.0, interleaved=False,
+                     stream=None):
+    """lookme_head_norm_rotary on torch tensors: q and q_out [n, q_heads, d], k and
+    k_out [n, k_heads, d] (rows may lie apart, as in a product of q, k and v; outputs
+    may be their inputs); q_weight and k_weight [d]; pos [n] or [axes, n] int32, freq
+    [rot / 2] float32, axis [rot / 2] int32.  Without freq nothing is rotated."""
+    dev, dt = q.get_device(), q.dtype
+    code = _dtype_code("q", dt)
+    if q.dim() != 3:
+        _refuse(f"q has {q.dim()} dimensions, not 3")
+    n, q_heads, d = q.shape
+    if d >= INT32 or q_heads >= INT32:
+        _int32(d, q_heads)
+    p_q, q_row = _heads("q", q, dt, n, q_heads, d, dev)
+    p_qo, qo_row = _heads("q_out", q_out, dt, n, q_heads, d, dev)
+    k_heads, p_k, k_row, p_ko, ko_row = 0, None, 0, None, 0
+    if (k is None) != (k_out is None):
+        _refuse("k and k_out go together")
+    if k is not None:
+        k_heads = k.shape[1] if k.dim() == 3 else 0
+        if k_heads >= INT32:
+            _int32(k_heads)
+        p_k, k_row = _heads("k", k, dt, n, k_heads, d, dev)
+        p_ko, ko_row = _heads("k_out", k_out, dt, n, k_heads, d, dev)
+    elif k_weight is not None:
+        _refuse("k_weight given without k")
+    p_qw = None if q_weight is None else _tensor("q_weight", q_weight, dt, (d,), dev)
+    p_kw = None if k_weight is None else _tensor("k_weight", k_weight, dt, (d,), dev)
+    rot, axes, p_pos, p_axis, p_freq = 0, 1, None, None, None
+    if freq is not None:
+        rot = 2 * freq.numel()
+        if pos is None:
+            _refuse("freq given without pos")
+        axes = pos.shape[0] if pos.dim() == 2 else 1
+        if rot >= INT32 or axes >= INT32:
+            _int32(rot, axes)
+        p_freq = _tensor("freq", freq, torch.float32, (rot // 2,), dev)
+        p_pos = _tensor("pos", pos, torch.int32, (axes, n) if pos.dim() == 2 else (n,), dev)
+        if axis is not None:
+            p_axis = _tensor("axis", axis, torch.int32, (rot // 2,), dev)
+        elif axes > 1:
+            _refuse(f"positions of {axes} axes need axis")
+        if rot == 0:
+            p_pos = p_axis = p_freq = None
+    elif pos is not None or axis is not None:
+        _refuse("positions given without freq")
+    _call("lookme_head_norm_rotary", dev, stream, code, n, d, q_heads, p_q, q_row, p_qo, qo_row,
+          k_heads, p_k, k_row, p_ko, ko_row, int(norm), p_qw, p_kw, eps, rot, int(interleaved),
+          axes, p_pos, p_axis, p_freq, factor)
+
+
+def cache_shape(pages, kv_heads, page, head_dim):
+    """The shape of a 4-bit cache (a uint8 tensor) of `pages` pages of `page` tokens"""
+    return (pages, kv_heads, page // 32, 34 * head_dim)
+
+
+def _cache(cache, dev):
+    """(pages, kv_heads, page, head_dim, address) of a 4-bit cache"""
+    shape = cache.shape
+    if len(shape) != 4 or shape[3] % 34 != 0:
+        _refuse(f"cache has the shape {tuple(shape)}, not [pages, kv_heads, page / 32, 34 d]")
+    if cache.dtype is not torch.uint8 or cache.get_device() != dev or not cache.is_contiguous():
+        _wrong("cache", cache, torch.uint8, shape, dev)
+    pages, heads, tiles, width = shape
+    if heads >= INT32 or tiles >= INT32 // 32 or width >= INT32:
+        _int32(heads, 32 * tiles, width)
+    return pages, heads, 32 * tiles, width // 34, cache.data_ptr()
+
+
+def cache_write(k, v, slots, cache, stream=None):
+    """lookme_cache_write on torch tensors: k and v [n, kv_heads, d] (rows may lie
+    apart), slots [n] int32, cache [pages, kv_heads, page / 32, 34 d] uint8."""
+    dev, dt = k.get_device(), k.dtype
+    code = _dtype_code("k", dt)
+    pages, heads, page, d, p_c = _cache(cache, dev)
+    n = k.shape[0] if k.dim() == 3 else 0
+    p_k, k_row = _heads("k", k, dt, n, heads, d, dev)
+    p_v, v_row = _heads("v", v, dt, n, heads, d, dev)
+    p_s = _tensor("slots", slots, torch.int32, (n,), dev)
+    _call("lookme_cache_write", dev, stream, code, n, heads, d, p_k, k_row, p_v, v_row, p_s, pages,
+          page, p_c)
+
+
+def cache_read(slots, cache, k_out=None, v_out=None, stream=None):
+    """lookme_cache_read on torch tensors: slots [n] int32, cache as for
+    cache_write, k_out and v_out [n, kv_heads, d] (rows may lie apart), one of them
+    may be None."""
+    one = v_out if k_out is None else k_out
+    if one is None:
+        _refuse("no output given")
+    dev, dt, n = slots.get_device(), one.dtype, slots.numel()
+    code = _dtype_code("the output", dt)
+    pages, heads, page, d, p_c = _cache(cache, dev)
+    p_s = _tensor("slots", slots, torch.int32, (n,), dev)
+    p_k, k_row = (None, 0) if k_out is None else _heads("k_out", k_out, dt, n, heads, d, dev)
+    p_v, v_row = (None, 0) if v_out is None else _heads("v_out", v_out, dt, n, heads, d, dev)
+    _call("lookme_cache_read", dev, stream, code, n, heads, d, p_s, pages, page, p_c, p_k, k_row,
+          p_v, v_row)
+
+
+def cache_attention(q, cache, pages, lengths, out, workspace=None, q_offsets=None, scale=None,
+                    causal=True, stream=None):
+    """lookme_cache_attention on torch tensors: q and out [n, q_heads, d] (rows may
+    lie apart; out may be q), cache as for cache_write, pages [batch, max_pages],
+    lengths [batch] and q_offsets [batch + 1] int32 (None: a row each), scale d ** -0.5
+    if None, workspace uint8 (of LOOKME_ATTENTION_WORKSPACE bytes for every call, or
+    what lookme_cache_attention_workspace gives for one)."""
+    dev, dt, i32 = q.get_device(), q.dtype, torch.int32
+    code = _dtype_code("q", dt)
+    if q.dim() != 3 or pages.dim() != 2:
+        _refuse("q has 3 dimensions, pages has 2")
+    n, q_heads, _ = q.shape
+    num_pages, kv_heads, page, d, p_c = _cache(cache, dev)
+    batch, max_pages = pages.shape
+    if batch >= INT32 or max_pages >= INT32 or q_heads >= INT32:
+        _int32(batch, max_pages, q_heads)
+    p_q, q_row = _heads("q", q, dt, n, q_heads, d, dev)
+    p_o, o_row = _heads("out", out, dt, n, q_heads, d, dev)
+    if (pages.dtype is not i32 or pages.get_device() != dev or not pages.is_contiguous()):
+        _wrong("pages", pages, i32, pages.shape, dev)
+    p_l = _tensor("lengths", lengths, i32, (batch,), dev)
+    p_off = None if q_offsets is None else _tensor("q_offsets", q_offsets, i32, (batch + 1,), dev)
+    p_w, w_bytes = None, 0
+    if workspace is not None:
+        w_bytes = workspace.numel()
+        p_w = _tensor("workspace", workspace, torch.uint8, workspace.shape, dev)
+    _call("lookme_cache_attention", dev, stream, code, n, batch, q_heads, kv_heads, d, p_q, q_row,
+          p_off, p_l, pages.data_ptr(), max_pages, num_pages, page, p_c,
+          d ** -0.5 if scale is None else scale, int(causal), p_o, o_row, p_w, w_bytes)
 
 
 def lookme_destroy(h):

@@ -211,8 +211,13 @@ __device__ __forceinline__ float at_weight(float m, float M) {
 // ---------------------------------------------------------------------------
 // RT tiles of 16 rows a wave, WR waves along the rows, WT along the tokens
 // ---------------------------------------------------------------------------
+constexpr int at_waves(int dt, int d, int rt) {
+  const int bf16 = d == 64 ? (rt == 1 ? 4 : 3) : d == 128 ? (rt == 1 ? 3 : 2) : rt == 1 ? 2 : 1;
+  return dt == DT_BF16 || bf16 == 1 ? bf16 : bf16 - 1;
+}
+
 template <int DT, int D, int RT, int WR, int WT>
-__global__ __launch_bounds__(64 * WR * WT) void attend_kernel(AttendParams p) {
+__global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kernel(AttendParams p) {
   constexpr int U = D / 16, M = D / 32, BR = 16 * RT * WR, TERMS = at_terms<DT>();
   constexpr int ES = DT == DT_BF16 ? 2 : 4;
   __shared__ f32x4_t join[WT > 1 ? WT / 2 * WR : 1][RT * U][WT > 1 ? 64 : 1];
@@ -300,168 +305,182 @@ __global__ __launch_bounds__(64 * WR * WT) void attend_kernel(AttendParams p) {
   const int full = row0 < R ? last_of(row0) : -1;    // every row sees the tokens up to here
   const int tiles_log2 = p.page_log2 - 5;
   const int32_t* pages = p.pages + (int64_t)u.b * p.max_pages;
-  auto tile_at = [&](int t, bool* ok) {
-    const int id = pages[t >> tiles_log2];
-    *ok = id >= 0 && id < p.num_pages;
-    const int64_t page = *ok ? id : 0;
+  auto page_of = [&](int t) { return pages[t >> tiles_log2]; };
+  auto held = [&](int id) { return id >= 0 && id < p.num_pages; };
+  auto tile_at = [&](int t, int id) {
+    const int64_t page = held(id) ? id : 0;
     return p.cache + (((page * p.kv_heads + h) << tiles_log2) + (t & ((1 << tiles_log2) - 1))) *
                          (int64_t)(34 * D);
   };
-
-  AttendTile<D> cur, next;
-  bool ok = false, next_ok = false;
-  if (first + wt < end) at_load(cur, tile_at(first + wt, &ok));
-  for (int t = first + wt; t < end; t += WT) {
-    if (t + WT < end) at_load(next, tile_at(t + WT, &next_ok));
-    if (ok) {
-      // scores of 32 tokens
-      f32x4_t s[RT][2];
+  auto step = [&](AttendTile<D>& cur, int t, int id) {
+    if (!held(id)) return;
+    // scores of 32 tokens
+    f32x4_t s[RT][2];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
+    for (int half = 0; half < 2; ++half) {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[rt][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int rt = 0; rt < RT; ++rt) s[rt][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int m = 0; m < M; ++m) {
-          const float scale = at_scale(at_byte(cur.ks[half][m / 4], m % 4));
-          u32x4_t k;
+      for (int m = 0; m < M; ++m) {
+        const float scale = at_scale(at_byte(cur.ks[half][m / 4], m % 4));
+        u32x4_t k;
 #pragma unroll
-          for (int b = 0; b < 4; ++b) k[b] = c4_pair(cur.k[half][m], scale, b);
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int x = TERMS - 1; x >= 0; --x)
-              s[rt][half] = mfma_chunk<DT_BF16>(k, q[rt][m][x], s[rt][half]);
-        }
-      }
-      // tokens that a row does not see, and, where a block of v is not finite (or
-      // behind the last token, where anything may be), values that must not meet the
-      // weight 0
-      const int t0 = t * C4_TILE;
-      const bool edge = t0 + C4_TILE - 1 > full;
-      if (edge) {
+        for (int b = 0; b < 4; ++b) k[b] = c4_pair(cur.k[half][m], scale, b);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-          for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (t0 + 16 * half + 4 * c + i > last[rt]) s[rt][half][i] = -INFINITY;
-      }
-      // (a byte of 255: its complement is 0)
-      const uint32_t inv0 = ~cur.vs[0], inv1 = ~cur.vs[1];
-      const uint32_t holes = (((inv0 - 0x01010101u) & ~inv0) | ((inv1 - 0x01010101u) & ~inv1)) &
-                             0x80808080u;
-      uint32_t nan_rows[RT];
-      const bool careful = __any(holes != 0 || t0 + C4_TILE > u.seq.len);
-      if (careful) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) nan_rows[rt] = 0;
-        for (int g = 0; g < M; ++g) {
-          bool ok2;
-          uint32_t vs[2];
-          at_load_words(vs, tile_at(t, &ok2) + 33 * D + g * 32 + c * 8);
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const bool hole = at_byte(vs[x / 4], x % 4) == C4_NAN;
-            const int token = t0 + 4 * c + x % 4 + 16 * (x / 4);
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-              nan_rows[rt] |= (hole && token <= last[rt] ? 1u : 0u) << g;
-          }
-        }
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          nan_rows[rt] |= __shfl_xor(nan_rows[rt], 16, 64);
-          nan_rows[rt] |= __shfl_xor(nan_rows[rt], 32, 64);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if ((nan_rows[rt] >> ((4 * c + i) * U / 32)) & 1u)
-#pragma unroll
-              for (int m = 0; m < U; ++m) acc[rt][m][i] = as_f32(0x7FC00000u);
-        }
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          const int token = t0 + 4 * c + x % 4 + 16 * (x / 4);
-          if (token >= u.seq.len || at_byte(cur.vs[x / 4], x % 4) == C4_NAN) {
-            const int bit = 8 * (x % 4);
-            cur.vs[x / 4] = (cur.vs[x / 4] & ~(0xFFu << bit)) | (127u << bit);
-            if constexpr (U == 4) {
-              cur.v[x / 2] &= x % 2 == 0 ? 0xFFFF0000u : 0x0000FFFFu;
-            } else {
-#pragma unroll
-              for (int w = 0; w < U / 8; ++w) cur.v[x * (U / 8) + w] = 0;
-            }
-          }
-        }
-      }
-      // running maximum
-      float mx[RT];
-      bool grown = false;
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        mx[rt] = s[rt][0][0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) mx[rt] = fmaxf(mx[rt], s[rt][e / 4][e % 4]);
-        grown |= mx[rt] > top_next[rt];
-      }
-      if (__any(grown)) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          const float now = fmaxf(top[rt], at_row_max(mx[rt]));
-          const float b = now == -INFINITY ? 0.f : now * scl;
-          const float f = top[rt] == -INFINITY ? 0.f : exp2f(base[rt] - b);
-          top[rt] = now;
-          top_next[rt] = now + slack;
-          base[rt] = b;
-          sum[rt] *= f;
-#pragma unroll
-          for (int m = 0; m < U; ++m) acc[rt][m] *= f;
-        }
-      }
-      // weights
-      u32x4_t w[RT][TERMS];
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float e[8];
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          e[x] = __builtin_amdgcn_exp2f(fmaf(s[rt][x / 4][x % 4], scl, -base[rt]));
-          sum[rt] += e[x];
-        }
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          uint32_t o[TERMS];
-          at_split<DT>(e[2 * x], e[2 * x + 1], o);
-#pragma unroll
-          for (int k = 0; k < TERMS; ++k) w[rt][k][x] = o[k];
-        }
-      }
-      // outputs: byte b of a token's unit holds the lane's dims 2 b and 2 b + 1
-#pragma unroll
-      for (int b = 0; b < U / 2; ++b) {
-        uint32_t pair[8];
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          const int byte = x * (U / 2) + b;
-          pair[x] = c4_pair(cur.v[byte / 4], at_scale(at_byte(cur.vs[x / 4], x % 4)), byte % 4);
-        }
-        u32x4_t lo, hi;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          lo[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x05040100u);
-          hi[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x07060302u);
-        }
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-          for (int k = TERMS - 1; k >= 0; --k) {
-            acc[rt][2 * b] = mfma_chunk<DT_BF16>(lo, w[rt][k], acc[rt][2 * b]);
-            acc[rt][2 * b + 1] = mfma_chunk<DT_BF16>(hi, w[rt][k], acc[rt][2 * b + 1]);
-          }
+          for (int x = TERMS - 1; x >= 0; --x)
+            s[rt][half] = mfma_chunk<DT_BF16>(k, q[rt][m][x], s[rt][half]);
       }
     }
-    cur = next;
-    ok = next_ok;
+    // tokens that a row does not see, and, where a block of v is not finite (or
+    // behind the last token, where anything may be), values that must not meet the
+    // weight 0
+    const int t0 = t * C4_TILE;
+    const bool edge = t0 + C4_TILE - 1 > full;
+    if (edge) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (t0 + 16 * half + 4 * c + i > last[rt]) s[rt][half][i] = -INFINITY;
+    }
+    // (a byte of 255: its complement is 0)
+    const uint32_t inv0 = ~cur.vs[0], inv1 = ~cur.vs[1];
+    const uint32_t holes = (((inv0 - 0x01010101u) & ~inv0) | ((inv1 - 0x01010101u) & ~inv1)) &
+                           0x80808080u;
+    uint32_t nan_rows[RT];
+    const bool careful = __any(holes != 0 || t0 + C4_TILE > u.seq.len);
+    if (careful) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) nan_rows[rt] = 0;
+      for (int g = 0; g < M; ++g) {
+        uint32_t vs[2];
+        at_load_words(vs, tile_at(t, id) + 33 * D + g * 32 + c * 8);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const bool hole = at_byte(vs[x / 4], x % 4) == C4_NAN;
+          const int token = t0 + 4 * c + x % 4 + 16 * (x / 4);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+            nan_rows[rt] |= (hole && token <= last[rt] ? 1u : 0u) << g;
+        }
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        nan_rows[rt] |= __shfl_xor(nan_rows[rt], 16, 64);
+        nan_rows[rt] |= __shfl_xor(nan_rows[rt], 32, 64);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if ((nan_rows[rt] >> ((4 * c + i) * U / 32)) & 1u)
+#pragma unroll
+            for (int m = 0; m < U; ++m) acc[rt][m][i] = as_f32(0x7FC00000u);
+      }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const int token = t0 + 4 * c + x % 4 + 16 * (x / 4);
+        if (token >= u.seq.len || at_byte(cur.vs[x / 4], x % 4) == C4_NAN) {
+          const int bit = 8 * (x % 4);
+          cur.vs[x / 4] = (cur.vs[x / 4] & ~(0xFFu << bit)) | (127u << bit);
+          if constexpr (U == 4) {
+            cur.v[x / 2] &= x % 2 == 0 ? 0xFFFF0000u : 0x0000FFFFu;
+          } else {
+#pragma unroll
+            for (int w = 0; w < U / 8; ++w) cur.v[x * (U / 8) + w] = 0;
+          }
+        }
+      }
+    }
+    // running maximum
+    float mx[RT];
+    bool grown = false;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      mx[rt] = s[rt][0][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) mx[rt] = fmaxf(mx[rt], s[rt][e / 4][e % 4]);
+      grown |= mx[rt] > top_next[rt];
+    }
+    if (__any(grown)) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const float now = fmaxf(top[rt], at_row_max(mx[rt]));
+        const float b = now == -INFINITY ? 0.f : now * scl;
+        const float f = top[rt] == -INFINITY ? 0.f : exp2f(base[rt] - b);
+        top[rt] = now;
+        top_next[rt] = now + slack;
+        base[rt] = b;
+        sum[rt] *= f;
+#pragma unroll
+        for (int m = 0; m < U; ++m) acc[rt][m] *= f;
+      }
+    }
+    // weights
+    u32x4_t w[RT][TERMS];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float e[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        e[x] = __builtin_amdgcn_exp2f(fmaf(s[rt][x / 4][x % 4], scl, -base[rt]));
+        sum[rt] += e[x];
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        uint32_t o[TERMS];
+        at_split<DT>(e[2 * x], e[2 * x + 1], o);
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) w[rt][k][x] = o[k];
+      }
+    }
+    // outputs: byte b of a token's unit holds the lane's dims 2 b and 2 b + 1
+#pragma unroll
+    for (int b = 0; b < U / 2; ++b) {
+      uint32_t pair[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const int byte = x * (U / 2) + b;
+        pair[x] = c4_pair(cur.v[byte / 4], at_scale(at_byte(cur.vs[x / 4], x % 4)), byte % 4);
+      }
+      u32x4_t lo, hi;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        lo[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x05040100u);
+        hi[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x07060302u);
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int k = TERMS - 1; k >= 0; --k) {
+          acc[rt][2 * b] = mfma_chunk<DT_BF16>(lo, w[rt][k], acc[rt][2 * b]);
+          acc[rt][2 * b + 1] = mfma_chunk<DT_BF16>(hi, w[rt][k], acc[rt][2 * b + 1]);
+        }
+    }
+  };
+
+  // Two tiles in registers by turns: one is multiplied while the other is on its way,
+  // and the page of the one after it
+  AttendTile<D> even, odd;
+  int t = first + wt;
+  if (t < end) {
+    int id = page_of(t), next = page_of(t + WT < end ? t + WT : t);
+    at_load(even, tile_at(t, id));
+    while (true) {
+      int after = page_of(t + 2 * WT < end ? t + 2 * WT : t);
+      if (t + WT < end) at_load(odd, tile_at(t + WT, next));
+      step(even, t, id);
+      t += WT;
+      if (t >= end) break;
+      id = page_of(t + 2 * WT < end ? t + 2 * WT : t);
+      if (t + WT < end) at_load(even, tile_at(t + WT, after));
+      step(odd, t, next);
+      t += WT;
+      if (t >= end) break;
+      next = id;
+      id = after;
+    }
   }
 
   // the waves along the tokens join

@@ -60,7 +60,8 @@ struct AttendUnit {
   int64_t part;           // index among the units whose keys are cut
 };
 
-__device__ __forceinline__ float wave_sum(float v) {
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
   return v;
@@ -82,6 +83,14 @@ __device__ __forceinline__ bool at_unit(const AttendParams& p, int64_t unit, boo
       work += (float)blocks * (float)((s.len + C4_TILE - 1) / C4_TILE);
     }
     work = wave_sum(work) * (float)p.kv_heads;
+  } else {
+    // without a cut the blocks of rows of one key head read the same keys: a
+    // neighbourhood of units for each XCD, so that they meet in its L2
+    int all = 0;
+    for (int b = lane; b < p.batch; b += 64)
+      all += (int)(((int64_t)at_seq(p, b).rows * G + BR - 1) / BR * p.kv_heads);
+    unit = xcd_remap((int)unit, wave_sum(all));
+    if (unit < 0) return false;
   }
   int chunk = 0x7FFFFFFF;
   if (p.target > 0) {
@@ -229,8 +238,7 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
   const int G = p.q_heads / p.kv_heads;
 
   AttendUnit u;
-  const int unit = xcd_remap(blockIdx.x, gridDim.x);
-  if (unit < 0 || !at_unit<BR>(p, unit, false, &u)) return;
+  if (!at_unit<BR>(p, blockIdx.x, false, &u)) return;
   const int R = u.seq.rows * G, blocks = (R + BR - 1) / BR;
   const int blk = blocks - 1 - u.local % blocks;     // the longest first
   const int hs = u.local / blocks, split = hs % u.splits, h = hs / u.splits;

@@ -18,12 +18,14 @@
 // signs; the output has the same step), float32 rows take q and p as three bf16
 // values each, which hold all 24 bits.
 #include "cache4.h"
+#include "dtl.h"
 #include "kernels.h"
 
 namespace lookme {
 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
 // Fewest tiles of a work unit; the rescaling waits until a maximum has grown by
 // 2^AT_SLACK.
@@ -89,7 +91,7 @@ __device__ __forceinline__ bool at_unit(const AttendParams& p, int64_t unit, boo
     int all = 0;
     for (int b = lane; b < p.batch; b += 64)
       all += (int)(((int64_t)at_seq(p, b).rows * G + BR - 1) / BR * p.kv_heads);
-    unit = xcd_remap((int)unit, wave_sum(all));
+    unit = __builtin_amdgcn_readfirstlane(xcd_remap((int)unit, wave_sum(all)));
     if (unit < 0) return false;
   }
   int chunk = 0x7FFFFFFF;
@@ -146,9 +148,9 @@ __device__ __forceinline__ void at_load_words(uint32_t (&w)[N], const uint8_t* p
   if constexpr (N == 1) {
     w[0] = *reinterpret_cast<const uint32_t*>(p);
   } else if constexpr (N == 2) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    w[0] = v.x;
-    w[1] = v.y;
+    const u32x2_t v = *reinterpret_cast<const u32x2_t*>(p);
+    w[0] = v[0];
+    w[1] = v[1];
   } else {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
@@ -177,8 +179,11 @@ __device__ __forceinline__ void at_load(AttendTile<D>& t, const uint8_t* tile) {
 
 __device__ __forceinline__ uint32_t at_byte(uint32_t w, int i) { return (w >> (8 * i)) & 0xFFu; }
 
-// a finite block's scale, or NaN's bits as the conversion takes them
-__device__ __forceinline__ float at_scale(uint32_t byte) { return as_f32(byte << 23); }
+// The scale of byte i of w: the conversion takes a float's exponent and nothing else of
+// it, so the other bytes may stand in its sign and significand (255: NaN)
+__device__ __forceinline__ float at_scale(uint32_t w, int i) {
+  return as_f32(i == 3 ? w >> 1 : w << (23 - 8 * i));
+}
 
 // x as `terms` bf16 values that add up to it
 template <int DT>
@@ -224,14 +229,32 @@ constexpr int at_waves(int dt, int d, int rt) {
   const int bf16 = d == 64 ? (rt == 1 ? 4 : 3) : d == 128 ? (rt == 1 ? 3 : 2) : rt == 1 ? 2 : 1;
   return dt == DT_BF16 || bf16 == 1 ? bf16 : bf16 - 1;
 }
+// tiles of a wave's ring in LDS, one of them being multiplied
+constexpr int at_ring(int dt, int d) { return d == 64 ? 4 : d == 128 ? 3 : 2; }
+
+// A tile on its way into LDS: 1 KB an instruction, the last one on some of the lanes
+template <int D>
+constexpr int at_instr() {
+  return 34 * D / 1024 + 1;
+}
+template <int D>
+__device__ __forceinline__ void at_issue(const uint8_t* tile, char* dst) {
+  const int lane = threadIdx.x & 63;
+  constexpr int FULL = 34 * D / 1024, REST = 34 * D % 1024 / 16;
+#pragma unroll
+  for (int i = 0; i < FULL; ++i) load_lds16(tile + i * 1024 + lane * 16, dst + i * 1024);
+  if (lane < REST) load_lds16(tile + FULL * 1024 + lane * 16, dst + FULL * 1024);
+}
 
 template <int DT, int D, int RT, int WR, int WT>
 __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kernel(AttendParams p) {
   constexpr int U = D / 16, M = D / 32, BR = 16 * RT * WR, TERMS = at_terms<DT>();
   constexpr int ES = DT == DT_BF16 ? 2 : 4;
-  __shared__ f32x4_t join[WT > 1 ? WT / 2 * WR : 1][RT * U][WT > 1 ? 64 : 1];
-  __shared__ float join_m[WT > 1 ? WT / 2 * WR : 1][RT][WT > 1 ? 64 : 1];
-  __shared__ float join_l[WT > 1 ? WT / 2 * WR : 1][RT][WT > 1 ? 64 : 1];
+  // the waves' rings of tiles, then what they join
+  constexpr int NB = at_ring(DT, D), TILE = 34 * D;
+  constexpr int JOIN = WT > 1 ? WT / 2 * WR * RT * (U * 1024 + 512) : 16;
+  constexpr int RING = WT > 1 ? WT * WR * NB * TILE : 16;
+  __shared__ __attribute__((aligned(1024))) char smem[RING > JOIN ? RING : JOIN];
   const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wt = wave % WT, wr = wave / WT;
@@ -250,42 +273,51 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
   const int end_row = row0 + 16 * RT < R ? row0 + 16 * RT : R;
   const int block_end = blk * BR + BR < R ? blk * BR + BR : R;
   int last[RT];
-  int64_t q_row[RT];
   u32x4_t q[RT][M][TERMS];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = row0 + rt * 16 + j;
-    const bool valid = r < R;
-    last[rt] = valid ? last_of(r) : -1;
-    const int i = valid ? r / G : 0;
-    q_row[rt] = valid ? (int64_t)(u.seq.q0 + i) : -1;
-    const char* src = p.q + (u.seq.q0 + i) * p.q_stride +
-                      ((int64_t)h * G + (valid ? r - i * G : 0)) * D * ES;
+    last[rt] = r < R ? last_of(r) : -1;
+  }
+  auto load_q = [&]() {
 #pragma unroll
-    for (int m = 0; m < M; ++m) {
-      if constexpr (DT == DT_BF16) {
-        q[rt][m][0] = valid ? ld16(src + (32 * m + 8 * c) * 2) : u32x4_t{0, 0, 0, 0};
-      } else {
-        u32x4_t a{0, 0, 0, 0}, b{0, 0, 0, 0};
-        if (valid) {
-          a = ld16(src + (32 * m + 8 * c) * 4);
-          b = ld16(src + (32 * m + 8 * c) * 4 + 16);
-        }
-        const f32x4_t af = __builtin_bit_cast(f32x4_t, a), bf = __builtin_bit_cast(f32x4_t, b);
+    for (int rt = 0; rt < RT; ++rt) {
+      const int r = row0 + rt * 16 + j, i = r < R ? r / G : 0;
+      const char* src = p.q + (u.seq.q0 + i) * p.q_stride +
+                        ((int64_t)h * G + (r < R ? r - i * G : 0)) * D * ES;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          uint32_t w[TERMS], x[TERMS];
-          at_split<DT>(af[2 * e], af[2 * e + 1], w);
-          at_split<DT>(bf[2 * e], bf[2 * e + 1], x);
+      for (int m = 0; m < M; ++m) {
+        if constexpr (DT == DT_BF16) {
+          q[rt][m][0] = r < R ? ld16(src + (32 * m + 8 * c) * 2) : u32x4_t{0, 0, 0, 0};
+        } else {
+          u32x4_t a{0, 0, 0, 0}, b{0, 0, 0, 0};
+          if (r < R) {
+            a = ld16(src + (32 * m + 8 * c) * 4);
+            b = ld16(src + (32 * m + 8 * c) * 4 + 16);
+          }
+          const f32x4_t af = __builtin_bit_cast(f32x4_t, a), bf = __builtin_bit_cast(f32x4_t, b);
 #pragma unroll
-          for (int k = 0; k < TERMS; ++k) {
-            q[rt][m][k][e] = w[k];
-            q[rt][m][k][2 + e] = x[k];
+          for (int e = 0; e < 2; ++e) {
+            uint32_t w[TERMS], x[TERMS];
+            at_split<DT>(af[2 * e], af[2 * e + 1], w);
+            at_split<DT>(bf[2 * e], bf[2 * e + 1], x);
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k) {
+              q[rt][m][k][e] = w[k];
+              q[rt][m][k][2 + e] = x[k];
+            }
           }
         }
       }
     }
-  }
+    // (waited for here, once: the compiler would wait for every load in the loop)
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) asm volatile("" : "+v"(q[rt][m][k]));
+  };
 
   f32x4_t acc[RT][U];
   float top[RT], top_next[RT], base[RT], sum[RT];   // maximum; where it is renewed; in powers of two
@@ -312,7 +344,9 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
   }
   const int full = row0 < R ? last_of(row0) : -1;    // every row sees the tokens up to here
   const int tiles_log2 = p.page_log2 - 5;
-  const int32_t* pages = p.pages + (int64_t)u.b * p.max_pages;
+  // (scalar loads, which the counts of loads in flight below leave out)
+  typedef const __attribute__((address_space(4))) int32_t* scalar_ptr_t;
+  const scalar_ptr_t pages = (scalar_ptr_t)(uintptr_t)(p.pages + (int64_t)u.b * p.max_pages);
   auto page_of = [&](int t) { return pages[t >> tiles_log2]; };
   auto held = [&](int id) { return id >= 0 && id < p.num_pages; };
   auto tile_at = [&](int t, int id) {
@@ -320,8 +354,7 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
     return p.cache + (((page * p.kv_heads + h) << tiles_log2) + (t & ((1 << tiles_log2) - 1))) *
                          (int64_t)(34 * D);
   };
-  auto step = [&](AttendTile<D>& cur, int t, int id) {
-    if (!held(id)) return;
+  auto step = [&](AttendTile<D>& cur, int t, const uint8_t* tile) {
     // scores of 32 tokens
     f32x4_t s[RT][2];
 #pragma unroll
@@ -330,7 +363,7 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
       for (int rt = 0; rt < RT; ++rt) s[rt][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int m = 0; m < M; ++m) {
-        const float scale = at_scale(at_byte(cur.ks[half][m / 4], m % 4));
+        const float scale = at_scale(cur.ks[half][m / 4], m % 4);
         u32x4_t k;
 #pragma unroll
         for (int b = 0; b < 4; ++b) k[b] = c4_pair(cur.k[half][m], scale, b);
@@ -366,7 +399,7 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
       for (int rt = 0; rt < RT; ++rt) nan_rows[rt] = 0;
       for (int g = 0; g < M; ++g) {
         uint32_t vs[2];
-        at_load_words(vs, tile_at(t, id) + 33 * D + g * 32 + c * 8);
+        at_load_words(vs, tile + 33 * D + g * 32 + c * 8);
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
           const bool hole = at_byte(vs[x / 4], x % 4) == C4_NAN;
@@ -450,7 +483,7 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
         const int byte = x * (U / 2) + b;
-        pair[x] = c4_pair(cur.v[byte / 4], at_scale(at_byte(cur.vs[x / 4], x % 4)), byte % 4);
+        pair[x] = c4_pair(cur.v[byte / 4], at_scale(cur.vs[x / 4], x % 4), byte % 4);
       }
       u32x4_t lo, hi;
 #pragma unroll
@@ -468,26 +501,65 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
     }
   };
 
-  // Two tiles in registers by turns: one is multiplied while the other is on its way,
-  // and the page of the one after it
-  AttendTile<D> even, odd;
   int t = first + wt;
-  if (t < end) {
-    int id = page_of(t), next = page_of(t + WT < end ? t + WT : t);
-    at_load(even, tile_at(t, id));
-    while (true) {
-      int after = page_of(t + 2 * WT < end ? t + 2 * WT : t);
-      if (t + WT < end) at_load(odd, tile_at(t + WT, next));
-      step(even, t, id);
-      t += WT;
-      if (t >= end) break;
-      id = page_of(t + 2 * WT < end ? t + 2 * WT : t);
-      if (t + WT < end) at_load(even, tile_at(t + WT, after));
-      step(odd, t, next);
-      t += WT;
-      if (t >= end) break;
-      next = id;
-      id = after;
+  if constexpr (WT > 1) {
+    // The wave's own ring: NB - 1 tiles on their way while one is multiplied, no
+    // barrier, the page of the next one ahead of them.  `bad`: bit i, the tile i turns
+    // ahead is on no page.
+    char* ring = smem + wave * (NB * TILE);
+    uint32_t bad = 0;
+    int id = t < end ? page_of(t) : 0, slot = 0;
+    auto issue = [&](int x, int at) {
+      at_issue<D>(tile_at(x, id), ring + at * TILE);
+      bad |= (held(id) ? 0u : 1u) << (NB - 1);
+      id = page_of(x + WT < end ? x + WT : x);
+    };
+#pragma unroll
+    for (int i = 0; i < NB - 1; ++i) {
+      bad >>= 1;
+      if (t + i * WT < end) issue(t + i * WT, i);
+    }
+    load_q();
+    for (; t < end; t += WT) {
+      bad >>= 1;
+      if (t + (NB - 1) * WT < end) {
+        issue(t + (NB - 1) * WT, slot == 0 ? NB - 1 : slot - 1);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 1) * at_instr<D>()) : "memory");
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+      if ((bad & 1u) == 0) {
+        AttendTile<D> cur;
+        const uint8_t* tile = reinterpret_cast<const uint8_t*>(ring + slot * TILE);
+        at_load(cur, tile);
+        step(cur, t, tile);
+      }
+      slot = slot == NB - 1 ? 0 : slot + 1;
+      asm volatile("" ::: "memory");
+    }
+    __syncthreads();   // the rings are free for the join
+  } else {
+    // Two tiles in registers by turns: one is multiplied while the other is on its
+    // way, and the page of the one after it
+    AttendTile<D> even, odd;
+    if (t < end) {
+      load_q();
+      int id = page_of(t), next = page_of(t + WT < end ? t + WT : t);
+      at_load(even, tile_at(t, id));
+      while (true) {
+        int after = page_of(t + 2 * WT < end ? t + 2 * WT : t);
+        if (t + WT < end) at_load(odd, tile_at(t + WT, next));
+        if (held(id)) step(even, t, tile_at(t, id));
+        t += WT;
+        if (t >= end) break;
+        id = page_of(t + 2 * WT < end ? t + 2 * WT : t);
+        if (t + WT < end) at_load(even, tile_at(t + WT, after));
+        if (held(next)) step(odd, t, tile_at(t, next));
+        t += WT;
+        if (t >= end) break;
+        next = id;
+        id = after;
+      }
     }
   }
 
@@ -501,26 +573,28 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
   if constexpr (WT > 1) {
 #pragma unroll
     for (int step = WT / 2; step > 0; step >>= 1) {
-      const int slot = wr * (WT / 2) + (wt & (step - 1));
+      char* slot = smem + (wr * (WT / 2) + (wt & (step - 1))) * (RT * (U * 1024 + 512));
+      f32x4_t* join = reinterpret_cast<f32x4_t*>(slot) + lane;
+      float* ml = reinterpret_cast<float*>(slot + RT * U * 1024) + lane;
       if (wt >= step && wt < 2 * step) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          join_m[slot][rt][lane] = ref[rt];
-          join_l[slot][rt][lane] = sum[rt];
+          ml[rt * 128] = ref[rt];
+          ml[rt * 128 + 64] = sum[rt];
 #pragma unroll
-          for (int m = 0; m < U; ++m) join[slot][rt * U + m][lane] = acc[rt][m];
+          for (int m = 0; m < U; ++m) join[(rt * U + m) * 64] = acc[rt][m];
         }
       }
       __syncthreads();
       if (wt < step) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          const float other = join_m[slot][rt][lane], most = fmaxf(ref[rt], other);
+          const float other = ml[rt * 128], most = fmaxf(ref[rt], other);
           const float a = at_weight(ref[rt], most), b = at_weight(other, most);
           ref[rt] = most;
-          sum[rt] = sum[rt] * a + join_l[slot][rt][lane] * b;
+          sum[rt] = sum[rt] * a + ml[rt * 128 + 64] * b;
 #pragma unroll
-          for (int m = 0; m < U; ++m) acc[rt][m] = acc[rt][m] * a + join[slot][rt * U + m][lane] * b;
+          for (int m = 0; m < U; ++m) acc[rt][m] = acc[rt][m] * a + join[(rt * U + m) * 64] * b;
         }
       }
       if (step > 1) __syncthreads();
@@ -531,8 +605,8 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
   // a lane holds dims 4 c u .. 4 c u + 4 u - 1 of its rows
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    if (q_row[rt] < 0) continue;
     const int r = row0 + rt * 16 + j;
+    if (r >= R) continue;
     if (u.splits > 1) {
       const int64_t at = (u.part + u.local) * BR + (r - blk * BR);
       float* dst = p.part + at * D + 4 * c * U;
@@ -550,7 +624,7 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
       continue;
     }
     const float inv = sum[rt] == 0.f ? 0.f : 1.f / sum[rt];
-    char* dst = p.out + q_row[rt] * p.out_stride + ((int64_t)h * G + r % G) * D * ES + 4 * c * U * ES;
+    char* dst = p.out + (int64_t)(u.seq.q0 + r / G) * p.out_stride + ((int64_t)h * G + r % G) * D * ES + 4 * c * U * ES;
     float o[4 * U];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -561,7 +635,7 @@ __global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kern
       u32x4_t v;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        if constexpr (DT == DT_BF16) v[k] = pack_bf16x2(o[8 * x + 2 * k], o[8 * x + 2 * k + 1]);
+        if constexpr (DT == DT_BF16) v[k] = at_pack(o[8 * x + 2 * k], o[8 * x + 2 * k + 1]);
         else v[k] = as_u32(o[4 * x + k]);
       }
       st16(dst + 16 * x, v);
@@ -637,8 +711,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
   acc *= sum == 0.f ? 0.f : 1.f / sum;
   char* dst = p.out + row * p.out_stride + ((int64_t)head * D + 4 * l) * ES;
   if constexpr (DT == DT_BF16)
-    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc[0], acc[1]),
-                                                pack_bf16x2(acc[2], acc[3]));
+    *reinterpret_cast<uint2*>(dst) = make_uint2(at_pack(acc[0], acc[1]), at_pack(acc[2], acc[3]));
   else
     *reinterpret_cast<f32x4_t*>(dst) = acc;
 }

@@ -177,8 +177,6 @@ __device__ __forceinline__ void at_load(AttendTile<D>& t, const uint8_t* tile) {
   at_load_words(t.vs, tile + 33 * D + j * (D / 16) / 32 * 32 + c * 8);
 }
 
-__device__ __forceinline__ uint32_t at_byte(uint32_t w, int i) { return (w >> (8 * i)) & 0xFFu; }
-
 // The scale of byte i of w: the conversion takes a float's exponent and nothing else of
 // it, so the other bytes may stand in its sign and significand (255: NaN)
 __device__ __forceinline__ float at_scale(uint32_t w, int i) {
@@ -212,10 +210,6 @@ __device__ __forceinline__ float at_row_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16, 64));
   return fmaxf(v, __shfl_xor(v, 32, 64));
 }
-__device__ __forceinline__ float at_row_sum(float v) {
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
-}
 
 // Weight of a part whose maximum is m, of M over all (both in powers of two)
 __device__ __forceinline__ float at_weight(float m, float M) {
@@ -223,14 +217,366 @@ __device__ __forceinline__ float at_weight(float m, float M) {
 }
 
 // ---------------------------------------------------------------------------
-// RT tiles of 16 rows a wave, WR waves along the rows, WT along the tokens
+// a wave's rows, RT tiles of 16: running maxima and sums over the tokens so far
 // ---------------------------------------------------------------------------
-constexpr int at_waves(int dt, int d, int rt) {
-  const int bf16 = d == 64 ? (rt == 1 ? 4 : 3) : d == 128 ? (rt == 1 ? 3 : 2) : rt == 1 ? 2 : 1;
-  return dt == DT_BF16 || bf16 == 1 ? bf16 : bf16 - 1;
+// A lane holds, of row j of each tile, dims (4 c + i) u + m in acc[.][m][i]; the
+// sum of the row's weights is acc[.][u], the product with a row of ones, which
+// the matrix cores do while the vector instructions are what is short.
+template <int D, int RT>
+struct AttendRows {
+  static constexpr int U = D / 16;
+  f32x4_t acc[RT][U + 1];
+  float top[RT], next[RT], base[RT];   // maximum, where it is renewed, in powers of two
+  int last[RT];                        // the last token that the row sees
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      top[rt] = next[rt] = -INFINITY;
+      base[rt] = 0.f;
+#pragma unroll
+      for (int m = 0; m <= U; ++m) acc[rt][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // scores of the tile from token t0 that a row does not see
+  __device__ __forceinline__ void mask(f32x4_t (&s)[RT][2], int t0) const {
+    const int c = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (t0 + 16 * half + 4 * c + i > last[rt]) s[rt][half][i] = -INFINITY;
+  }
+
+  // NaN into the dims of the blocks of v that are not finite (byte 255 among the tile's
+  // scales) of rows that see them.  The products take such blocks as zeros, which
+  // would meet weights of 0 otherwise.
+  __device__ __forceinline__ void holes(const uint8_t* scales, int t0) {
+    const int c = (threadIdx.x & 63) >> 4;
+    uint32_t nan_rows[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) nan_rows[rt] = 0;
+    for (int g = 0; g < D / 32; ++g) {
+      uint32_t vs[2];
+      at_load_words(vs, scales + g * 32 + c * 8);
+      for (int x = 0; x < 8; ++x) {
+        const bool hole = ((vs[x / 4] >> (8 * (x % 4))) & 0xFFu) == (uint32_t)C4_NAN;
+        const int token = t0 + 4 * c + x % 4 + 16 * (x / 4);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+          nan_rows[rt] |= (hole && token <= last[rt] ? 1u : 0u) << g;
+      }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      nan_rows[rt] |= __shfl_xor(nan_rows[rt], 16, 64);
+      nan_rows[rt] |= __shfl_xor(nan_rows[rt], 32, 64);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if ((nan_rows[rt] >> ((4 * c + i) * U / 32)) & 1u)
+#pragma unroll
+          for (int m = 0; m < U; ++m) acc[rt][m][i] = as_f32(0x7FC00000u);
+    }
+  }
+
+  // Scores into weights 2^(s scl - base).  The maximum is renewed, and what there is
+  // rescaled, only when a score has passed it by 2^AT_SLACK: p stays far from
+  // float32's ends, and most tiles need neither.
+  template <int DT>
+  __device__ __forceinline__ void weights(const f32x4_t (&s)[RT][2], float scl, float slack,
+                                          u32x4_t (&w)[RT][at_terms<DT>()]) {
+    float mx[RT];
+    bool grown = false;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      mx[rt] = s[rt][0][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) mx[rt] = fmaxf(mx[rt], s[rt][e / 4][e % 4]);
+      grown |= mx[rt] > next[rt];
+    }
+    if (__any(grown)) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const float now = fmaxf(top[rt], at_row_max(mx[rt]));
+        const float b = now == -INFINITY ? 0.f : now * scl;
+        const float f = top[rt] == -INFINITY ? 0.f : exp2f(base[rt] - b);
+        top[rt] = now;
+        next[rt] = now + slack;
+        base[rt] = b;
+#pragma unroll
+        for (int m = 0; m <= U; ++m) acc[rt][m] *= f;
+      }
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float e[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        e[x] = __builtin_amdgcn_exp2f(fmaf(s[rt][x / 4][x % 4], scl, -base[rt]));
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        uint32_t o[at_terms<DT>()];
+        at_split<DT>(e[2 * x], e[2 * x + 1], o);
+#pragma unroll
+        for (int k = 0; k < at_terms<DT>(); ++k) w[rt][k][x] = o[k];
+      }
+    }
+  }
+
+  // acc[.][m] += v^T w
+  template <int TERMS>
+  __device__ __forceinline__ void add(int m, u32x4_t v, const u32x4_t (&w)[RT][TERMS]) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int k = TERMS - 1; k >= 0; --k)
+        acc[rt][m] = mfma_chunk<DT_BF16>(v, w[rt][k], acc[rt][m]);
+  }
+  template <int TERMS>
+  __device__ __forceinline__ void add_ones(const u32x4_t (&w)[RT][TERMS]) {
+    add(U, u32x4_t{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, w);
+  }
+
+  __device__ __forceinline__ float ref(int rt) const {
+    return top[rt] == -INFINITY ? -INFINITY : base[rt];
+  }
+
+  // Joins tile rt of a wave that left its rows at `other` (acc, then ref); ref_rt: this
+  // wave's, renewed
+  static constexpr int LEFT = RT * ((U + 1) * 1024 + 256);   // bytes
+  __device__ __forceinline__ void leave(char* to, const float (&refs)[RT]) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      reinterpret_cast<float*>(to + RT * (U + 1) * 1024)[rt * 64 + lane] = refs[rt];
+#pragma unroll
+      for (int m = 0; m <= U; ++m)
+        reinterpret_cast<f32x4_t*>(to)[(rt * (U + 1) + m) * 64 + lane] = acc[rt][m];
+    }
+  }
+  __device__ __forceinline__ void join(const char* from, float (&refs)[RT]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const float other = reinterpret_cast<const float*>(from + RT * (U + 1) * 1024)[rt * 64 + lane];
+      const float most = fmaxf(refs[rt], other);
+      const float a = at_weight(refs[rt], most), b = at_weight(other, most);
+      refs[rt] = most;
+#pragma unroll
+      for (int m = 0; m <= U; ++m)
+        acc[rt][m] = acc[rt][m] * a +
+                     reinterpret_cast<const f32x4_t*>(from)[(rt * (U + 1) + m) * 64 + lane] * b;
+    }
+  }
+};
+
+// What the waves of a unit know of it
+struct AttendBlock {
+  AttendUnit u;
+  int G, R, blk, h, split;   // heads of a key head, rows, block of rows, key head, part of the keys
+  int first, end;            // the part's tiles
+};
+
+template <int BR>
+__device__ __forceinline__ bool at_block(const AttendParams& p, AttendBlock* k) {
+  if (!at_unit<BR>(p, blockIdx.x, false, &k->u)) return false;
+  k->G = p.q_heads / p.kv_heads;
+  k->R = k->u.seq.rows * k->G;
+  const int blocks = (k->R + BR - 1) / BR, hs = k->u.local / blocks;
+  k->blk = blocks - 1 - k->u.local % blocks;     // the longest first
+  k->h = hs / k->u.splits;
+  k->split = hs % k->u.splits;
+  const int end_row = k->blk * BR + BR < k->R ? k->blk * BR + BR : k->R;
+  const int seen = p.causal ? k->u.seq.len - k->u.seq.rows + (end_row - 1) / k->G + 1 : k->u.seq.len;
+  const int tiles = seen > 0 ? (seen + C4_TILE - 1) / C4_TILE : 0;   // (early rows may see none)
+  const int per = (tiles + k->u.splits - 1) / k->u.splits;
+  k->first = k->split * per;
+  k->end = k->first + per < tiles ? k->first + per : tiles;
+  return true;
+}
+
+// The last token that row r sees
+__device__ __forceinline__ int at_last(const AttendParams& p, const AttendBlock& k, int r) {
+  return p.causal ? k.u.seq.len - k.u.seq.rows + r / k.G : k.u.seq.len - 1;
+}
+
+// Where the block's tiles are
+template <int D>
+struct AttendPages {
+  // (scalar loads, which the counts of loads in flight below leave out)
+  typedef const __attribute__((address_space(4))) int32_t* scalar_ptr_t;
+  scalar_ptr_t pages;
+  const uint8_t* cache;
+  int tiles_log2, num_pages, kv_heads, h;
+
+  __device__ __forceinline__ AttendPages(const AttendParams& p, const AttendBlock& k)
+      : pages((scalar_ptr_t)(uintptr_t)(p.pages + (int64_t)k.u.b * p.max_pages)),
+        cache(p.cache), tiles_log2(p.page_log2 - 5), num_pages(p.num_pages),
+        kv_heads(p.kv_heads), h(k.h) {}
+  __device__ __forceinline__ int id(int t) const { return pages[t >> tiles_log2]; }
+  __device__ __forceinline__ bool held(int id) const { return id >= 0 && id < num_pages; }
+  __device__ __forceinline__ const uint8_t* tile(int t, int id) const {
+    const int64_t page = held(id) ? id : 0;
+    return cache + (((page * kv_heads + h) << tiles_log2) + (t & ((1 << tiles_log2) - 1))) *
+                       (int64_t)(34 * D);
+  }
+};
+
+// The queries of RT tiles from row row0 as matrix operands
+template <int DT, int D, int RT>
+__device__ __forceinline__ void at_queries(const AttendParams& p, const AttendBlock& k, int row0,
+                                           u32x4_t (&q)[RT][D / 32][at_terms<DT>()]) {
+  constexpr int TERMS = at_terms<DT>(), ES = DT == DT_BF16 ? 2 : 4;
+  const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = row0 + rt * 16 + j, i = r < k.R ? r / k.G : 0;
+    const char* src = p.q + (k.u.seq.q0 + i) * p.q_stride +
+                      ((int64_t)k.h * k.G + (r < k.R ? r - i * k.G : 0)) * D * ES;
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m) {
+      if constexpr (DT == DT_BF16) {
+        q[rt][m][0] = r < k.R ? ld16(src + (32 * m + 8 * c) * 2) : u32x4_t{0, 0, 0, 0};
+      } else {
+        u32x4_t a{0, 0, 0, 0}, b{0, 0, 0, 0};
+        if (r < k.R) {
+          a = ld16(src + (32 * m + 8 * c) * 4);
+          b = ld16(src + (32 * m + 8 * c) * 4 + 16);
+        }
+        const f32x4_t af = __builtin_bit_cast(f32x4_t, a), bf = __builtin_bit_cast(f32x4_t, b);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          uint32_t w[TERMS], x[TERMS];
+          at_split<DT>(af[2 * e], af[2 * e + 1], w);
+          at_split<DT>(bf[2 * e], bf[2 * e + 1], x);
+#pragma unroll
+          for (int n = 0; n < TERMS; ++n) {
+            q[rt][m][n][e] = w[n];
+            q[rt][m][n][2 + e] = x[n];
+          }
+        }
+      }
+    }
+  }
+  // (waited for here, once: the compiler would wait for every load in the loop)
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+      for (int n = 0; n < TERMS; ++n) asm volatile("" : "+v"(q[rt][m][n]));
+}
+
+// The outputs of a wave's rows, or what a part of the keys gives for them
+template <int DT, int D, int RT, int BR>
+__device__ __forceinline__ void at_store(const AttendParams& p, const AttendBlock& k, int row0,
+                                         const AttendRows<D, RT>& a, const float (&refs)[RT]) {
+  constexpr int U = D / 16, ES = DT == DT_BF16 ? 2 : 4;
+  const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = row0 + rt * 16 + j;
+    if (r >= k.R) continue;
+    const float sum = a.acc[rt][U][0];
+    if (k.u.splits > 1) {
+      const int64_t at = (k.u.part + k.u.local) * BR + (r - k.blk * BR);
+      float* dst = p.part + at * D + 4 * c * U;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int m = 0; m < U; m += 4)
+          *reinterpret_cast<f32x4_t*>(dst + i * U + m) =
+              f32x4_t{a.acc[rt][m][i], a.acc[rt][m + 1][i], a.acc[rt][m + 2][i],
+                      a.acc[rt][m + 3][i]};
+      if (c == 0)
+        *reinterpret_cast<f32x2_t*>(p.part + (int64_t)2 * p.target * BR * D + at * 2) =
+            f32x2_t{refs[rt], sum};
+      continue;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int i = r / k.G;
+    char* dst = p.out + (int64_t)(k.u.seq.q0 + i) * p.out_stride +
+                ((int64_t)k.h * k.G + (r - i * k.G)) * D * ES + 4 * c * U * ES;
+    float o[4 * U];
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4)
+#pragma unroll
+      for (int m = 0; m < U; ++m) o[i4 * U + m] = a.acc[rt][m][i4] * inv;
+#pragma unroll
+    for (int x = 0; x < 4 * U * ES / 16; ++x) {
+      u32x4_t v;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        if constexpr (DT == DT_BF16) v[n] = at_pack(o[8 * x + 2 * n], o[8 * x + 2 * n + 1]);
+        else v[n] = as_u32(o[4 * x + n]);
+      }
+      st16(dst + 16 * x, v);
+    }
+  }
+}
+
+// Whether one of 8 scale bytes is 255 (its complement is 0)
+__device__ __forceinline__ bool at_hole(const uint32_t (&vs)[2]) {
+  const uint32_t a = ~vs[0], b = ~vs[1];
+  return ((((a - 0x01010101u) & ~a) | ((b - 0x01010101u) & ~b)) & 0x80808080u) != 0;
+}
+
+// Zeros in the place of the lane's tokens whose block of v is not finite, or which lie
+// behind the last one, where anything may be
+template <int D>
+__device__ __forceinline__ void at_fill_holes(uint32_t (&v)[D / 16], uint32_t (&vs)[2], int t0,
+                                              int len) {
+  constexpr int U = D / 16;
+  const int c = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    const int token = t0 + 4 * c + x % 4 + 16 * (x / 4), bit = 8 * (x % 4);
+    if (token >= len || ((vs[x / 4] >> bit) & 0xFFu) == (uint32_t)C4_NAN) {
+      vs[x / 4] = (vs[x / 4] & ~(0xFFu << bit)) | (127u << bit);
+      if constexpr (U == 4) {
+        v[x / 2] &= x % 2 == 0 ? 0xFFFF0000u : 0x0000FFFFu;
+      } else {
+#pragma unroll
+        for (int w = 0; w < U / 8; ++w) v[x * (U / 8) + w] = 0;
+      }
+    }
+  }
+}
+
+// Operand m = 2 b and 2 b + 1 of v: byte b of a token's unit holds these dims
+template <int D>
+__device__ __forceinline__ void at_v_operands(const uint32_t (&v)[D / 16], const uint32_t (&vs)[2],
+                                              int b, u32x4_t* lo, u32x4_t* hi) {
+  uint32_t pair[8];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    const int byte = x * (D / 32) + b;
+    pair[x] = c4_pair(v[byte / 4], at_scale(vs[x / 4], x % 4), byte % 4);
+  }
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    (*lo)[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x05040100u);
+    (*hi)[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x07060302u);
+  }
+}
+
+__device__ __forceinline__ u32x4_t at_k_operand(uint32_t k, float scale) {
+  return u32x4_t{c4_pair(k, scale, 0), c4_pair(k, scale, 1), c4_pair(k, scale, 2),
+                 c4_pair(k, scale, 3)};
+}
+
+// ---------------------------------------------------------------------------
+// few rows a key head (a decode step): 16 a unit, its waves along the tokens
+// ---------------------------------------------------------------------------
+constexpr int AF_WAVES = 4;
+constexpr int af_occupancy(int dt, int d) {
+  return d == 64 ? 4 : d == 128 ? 3 : dt == DT_BF16 ? 2 : 1;
 }
 // tiles of a wave's ring in LDS, one of them being multiplied
-constexpr int at_ring(int dt, int d) { return d == 64 ? 4 : d == 128 ? 3 : 2; }
+constexpr int af_ring(int d) { return d == 64 ? 4 : 2; }
 
 // A tile on its way into LDS: 1 KB an instruction, the last one on some of the lanes
 template <int D>
@@ -242,405 +588,254 @@ __device__ __forceinline__ void at_issue(const uint8_t* tile, char* dst) {
   const int lane = threadIdx.x & 63;
   constexpr int FULL = 34 * D / 1024, REST = 34 * D % 1024 / 16;
 #pragma unroll
-  for (int i = 0; i < FULL; ++i) load_lds16(tile + i * 1024 + lane * 16, dst + i * 1024);
-  if (lane < REST) load_lds16(tile + FULL * 1024 + lane * 16, dst + FULL * 1024);
+  for (int i = 0; i < FULL; ++i) load_lds16_nt(tile + i * 1024 + lane * 16, dst + i * 1024);
+  if (lane < REST) load_lds16_nt(tile + FULL * 1024 + lane * 16, dst + FULL * 1024);
 }
 
-template <int DT, int D, int RT, int WR, int WT>
-__global__ __launch_bounds__(64 * WR * WT, at_waves(DT, D, RT)) void attend_kernel(AttendParams p) {
-  constexpr int U = D / 16, M = D / 32, BR = 16 * RT * WR, TERMS = at_terms<DT>();
-  constexpr int ES = DT == DT_BF16 ? 2 : 4;
+template <int DT, int D>
+__global__ __launch_bounds__(64 * AF_WAVES, af_occupancy(DT, D))
+void attend_few_kernel(AttendParams p) {
+  constexpr int U = D / 16, M = D / 32, BR = 16, TERMS = at_terms<DT>();
+  constexpr int NB = af_ring(D), TILE = 34 * D;
+  constexpr int RING = AF_WAVES * NB * TILE, JOIN = AF_WAVES / 2 * AttendRows<D, 1>::LEFT;
   // the waves' rings of tiles, then what they join
-  constexpr int NB = at_ring(DT, D), TILE = 34 * D;
-  constexpr int JOIN = WT > 1 ? WT / 2 * WR * RT * (U * 1024 + 512) : 16;
-  constexpr int RING = WT > 1 ? WT * WR * NB * TILE : 16;
   __shared__ __attribute__((aligned(1024))) char smem[RING > JOIN ? RING : JOIN];
-  const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
+  const int lane = threadIdx.x & 63, j = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wt = wave % WT, wr = wave / WT;
-  const int G = p.q_heads / p.kv_heads;
-
-  AttendUnit u;
-  if (!at_unit<BR>(p, blockIdx.x, false, &u)) return;
-  const int R = u.seq.rows * G, blocks = (R + BR - 1) / BR;
-  const int blk = blocks - 1 - u.local % blocks;     // the longest first
-  const int hs = u.local / blocks, split = hs % u.splits, h = hs / u.splits;
-
-  // rows, their last visible token, their queries
-  const int row0 = blk * BR + wr * RT * 16;
-  const int shift = u.seq.len - u.seq.rows;
-  auto last_of = [&](int r) { return p.causal ? shift + r / G : u.seq.len - 1; };
-  const int end_row = row0 + 16 * RT < R ? row0 + 16 * RT : R;
-  const int block_end = blk * BR + BR < R ? blk * BR + BR : R;
-  int last[RT];
-  u32x4_t q[RT][M][TERMS];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int r = row0 + rt * 16 + j;
-    last[rt] = r < R ? last_of(r) : -1;
-  }
-  auto load_q = [&]() {
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int r = row0 + rt * 16 + j, i = r < R ? r / G : 0;
-      const char* src = p.q + (u.seq.q0 + i) * p.q_stride +
-                        ((int64_t)h * G + (r < R ? r - i * G : 0)) * D * ES;
-#pragma unroll
-      for (int m = 0; m < M; ++m) {
-        if constexpr (DT == DT_BF16) {
-          q[rt][m][0] = r < R ? ld16(src + (32 * m + 8 * c) * 2) : u32x4_t{0, 0, 0, 0};
-        } else {
-          u32x4_t a{0, 0, 0, 0}, b{0, 0, 0, 0};
-          if (r < R) {
-            a = ld16(src + (32 * m + 8 * c) * 4);
-            b = ld16(src + (32 * m + 8 * c) * 4 + 16);
-          }
-          const f32x4_t af = __builtin_bit_cast(f32x4_t, a), bf = __builtin_bit_cast(f32x4_t, b);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            uint32_t w[TERMS], x[TERMS];
-            at_split<DT>(af[2 * e], af[2 * e + 1], w);
-            at_split<DT>(bf[2 * e], bf[2 * e + 1], x);
-#pragma unroll
-            for (int k = 0; k < TERMS; ++k) {
-              q[rt][m][k][e] = w[k];
-              q[rt][m][k][2 + e] = x[k];
-            }
-          }
-        }
-      }
-    }
-    // (waited for here, once: the compiler would wait for every load in the loop)
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-      for (int m = 0; m < M; ++m)
-#pragma unroll
-        for (int k = 0; k < TERMS; ++k) asm volatile("" : "+v"(q[rt][m][k]));
-  };
-
-  f32x4_t acc[RT][U];
-  float top[RT], top_next[RT], base[RT], sum[RT];   // maximum; where it is renewed; in powers of two
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    top[rt] = top_next[rt] = -INFINITY;
-    base[rt] = sum[rt] = 0.f;
-#pragma unroll
-    for (int m = 0; m < U; ++m) acc[rt][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  AttendBlock k;
+  if (!at_block<BR>(p, &k)) return;
+  const int row0 = k.blk * BR;
+  AttendRows<D, 1> rows;
+  rows.clear();
+  rows.last[0] = row0 + j < k.R ? at_last(p, k, row0 + j) : -1;
+  const int full = at_last(p, k, row0);      // every row sees the tokens up to here
   const float scl = p.scale_log2, slack = AT_SLACK / scl;
+  const AttendPages<D> pages(p, k);
 
-  // the part's tiles, of which this wave takes every WT-th
-  const int seen = last_of(block_end - 1) + 1;       // (rows before the first token see none)
-  const int block_tiles = seen > 0 ? (seen + C4_TILE - 1) / C4_TILE : 0;
-  const int per = (block_tiles + u.splits - 1) / u.splits;
-  const int first = split * per;
-  int end = first + per < block_tiles ? first + per : block_tiles;
-  if (row0 < R) {
-    const int own = last_of(end_row - 1) / C4_TILE + 1;   // no less than the block's first rows'
-    end = own < end ? own : end;
-  } else {
-    end = first;
-  }
-  const int full = row0 < R ? last_of(row0) : -1;    // every row sees the tokens up to here
-  const int tiles_log2 = p.page_log2 - 5;
-  // (scalar loads, which the counts of loads in flight below leave out)
-  typedef const __attribute__((address_space(4))) int32_t* scalar_ptr_t;
-  const scalar_ptr_t pages = (scalar_ptr_t)(uintptr_t)(p.pages + (int64_t)u.b * p.max_pages);
-  auto page_of = [&](int t) { return pages[t >> tiles_log2]; };
-  auto held = [&](int id) { return id >= 0 && id < p.num_pages; };
-  auto tile_at = [&](int t, int id) {
-    const int64_t page = held(id) ? id : 0;
-    return p.cache + (((page * p.kv_heads + h) << tiles_log2) + (t & ((1 << tiles_log2) - 1))) *
-                         (int64_t)(34 * D);
+  // The wave's own ring: NB - 1 tiles on their way while one is multiplied, no barrier,
+  // the page of the next one ahead of them.  `bad`: bit i, the tile i turns ahead is on
+  // no page.
+  char* ring = smem + wave * (NB * TILE);
+  uint32_t bad = 0;
+  int t = k.first + wave, slot = 0;
+  int id = t < k.end ? pages.id(t) : 0;
+  auto issue = [&](int x, int at) {
+    at_issue<D>(pages.tile(x, id), ring + at * TILE);
+    bad |= (pages.held(id) ? 0u : 1u) << (NB - 1);
+    id = pages.id(x + AF_WAVES < k.end ? x + AF_WAVES : x);
   };
-  auto step = [&](AttendTile<D>& cur, int t, const uint8_t* tile) {
-    // scores of 32 tokens
-    f32x4_t s[RT][2];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
+  for (int i = 0; i < NB - 1; ++i) {
+    bad >>= 1;
+    if (t + i * AF_WAVES < k.end) issue(t + i * AF_WAVES, i);
+  }
+  u32x4_t q[1][M][TERMS];
+  at_queries<DT, D, 1>(p, k, row0, q);
+  for (; t < k.end; t += AF_WAVES) {
+    bad >>= 1;
+    if (t + (NB - 1) * AF_WAVES < k.end) {
+      issue(t + (NB - 1) * AF_WAVES, slot == 0 ? NB - 1 : slot - 1);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 1) * at_instr<D>()) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    if ((bad & 1u) == 0) {
+      const uint8_t* tile = reinterpret_cast<const uint8_t*>(ring + slot * TILE);
+      AttendTile<D> cur;
+      at_load(cur, tile);
+      const int t0 = t * C4_TILE;
+      f32x4_t s[1][2];
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) s[rt][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int half = 0; half < 2; ++half) {
+        s[0][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int m = 0; m < M; ++m) {
-        const float scale = at_scale(cur.ks[half][m / 4], m % 4);
-        u32x4_t k;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) k[b] = c4_pair(cur.k[half][m], scale, b);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+        for (int m = 0; m < M; ++m) {
+          const u32x4_t kv = at_k_operand(cur.k[half][m], at_scale(cur.ks[half][m / 4], m % 4));
 #pragma unroll
           for (int x = TERMS - 1; x >= 0; --x)
-            s[rt][half] = mfma_chunk<DT_BF16>(k, q[rt][m][x], s[rt][half]);
+            s[0][half] = mfma_chunk<DT_BF16>(kv, q[0][m][x], s[0][half]);
+        }
+      }
+      if (t0 + C4_TILE - 1 > full) rows.mask(s, t0);
+      const bool hole = __any(at_hole(cur.vs));
+      if (hole) rows.holes(tile + 33 * D, t0);
+      if (hole || t0 + C4_TILE > k.u.seq.len) at_fill_holes<D>(cur.v, cur.vs, t0, k.u.seq.len);
+      u32x4_t w[1][TERMS];
+      rows.template weights<DT>(s, scl, slack, w);
+      rows.add_ones(w);
+#pragma unroll
+      for (int b = 0; b < U / 2; ++b) {
+        u32x4_t lo, hi;
+        at_v_operands<D>(cur.v, cur.vs, b, &lo, &hi);
+        rows.add(2 * b, lo, w);
+        rows.add(2 * b + 1, hi, w);
       }
     }
-    // tokens that a row does not see, and, where a block of v is not finite (or
-    // behind the last token, where anything may be), values that must not meet the
-    // weight 0
-    const int t0 = t * C4_TILE;
-    const bool edge = t0 + C4_TILE - 1 > full;
-    if (edge) {
+    slot = slot == NB - 1 ? 0 : slot + 1;
+    asm volatile("" ::: "memory");
+  }
+
+  float refs[1] = {rows.ref(0)};
+  __syncthreads();   // the rings are free for the join
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+  for (int step = AF_WAVES / 2; step > 0; step >>= 1) {
+    char* left = smem + (wave & (step - 1)) * AttendRows<D, 1>::LEFT;
+    if (wave >= step && wave < 2 * step) rows.leave(left, refs);
+    __syncthreads();
+    if (wave < step) rows.join(left, refs);
+    if (step > 1) __syncthreads();
+  }
+  if (wave == 0) at_store<DT, D, 1, BR>(p, k, row0, rows, refs);
+}
+
+// ---------------------------------------------------------------------------
+// many rows a key head (prefill, cross attention): the waves of a workgroup along
+// the rows, RT tiles of 16 each; a tile of the cache is unpacked once, a quarter by
+// each wave, and read as matrix operands from LDS
+// ---------------------------------------------------------------------------
+constexpr int AM_WAVES = 4;
+template <int DT, int D>
+constexpr int am_row_tiles() {
+  return DT == DT_BF16 ? 2 : D == 256 ? 1 : D == 128 ? 2 : 3;
+}
+constexpr int am_occupancy(int d) { return d == 256 ? 1 : 2; }
+
+// A wave's share of a tile: D / 64 of the 2 D / 32 operands of k, and of the D / 32 pairs of
+// operands of v (d = 64: k by the last two waves, v by the first two)
+template <int D>
+struct AttendShare {
+  static constexpr int M = D / 32, U = D / 16;
+  static constexpr int KN = D == 64 ? 2 : D / 64, VN = D == 64 ? 1 : D / 128;
+  uint32_t k[KN], ks, v[U], vs[2];
+  __device__ __forceinline__ void load(const uint8_t* tile, int wave) {
+    const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
+    const int half = D == 64 ? wave & 1 : wave >> 1, m0 = D == 64 ? 0 : (wave & 1) * KN;
+    at_load_words(k, tile + (16 * half + j) * (D / 2) + c * (D / 8) + 4 * m0);
+    const uint8_t* at = tile + 32 * D + (16 * half + j) * M + m0;
+    if constexpr (KN == 2) ks = *reinterpret_cast<const uint16_t*>(at);
+    else ks = *reinterpret_cast<const uint32_t*>(at);
+    at_load_words(v, tile + 16 * D + (c * 16 + j) * (D / 4));
+    at_load_words(vs, tile + 33 * D + j * U / 32 * 32 + c * 8);
+  }
+  // operand n of the tile at lds + n 1024: k of the halves, then v
+  __device__ __forceinline__ void unpack(char* lds, int wave, int t0, int len, bool hole) {
+    const int lane = threadIdx.x & 63;
+    char* to = lds + lane * 16;
+    if (D != 64 || wave >= 2) {
+      const int n0 = D == 64 ? (wave & 1) * M : wave * KN;
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (t0 + 16 * half + 4 * c + i > last[rt]) s[rt][half][i] = -INFINITY;
+      for (int n = 0; n < KN; ++n) st16(to + (n0 + n) * 1024, at_k_operand(k[n], at_scale(ks, n)));
     }
-    // (a byte of 255: its complement is 0)
-    const uint32_t inv0 = ~cur.vs[0], inv1 = ~cur.vs[1];
-    const uint32_t holes = (((inv0 - 0x01010101u) & ~inv0) | ((inv1 - 0x01010101u) & ~inv1)) &
-                           0x80808080u;
-    uint32_t nan_rows[RT];
-    const bool careful = __any(holes != 0 || t0 + C4_TILE > u.seq.len);
-    if (careful) {
+    if (D != 64 || wave < 2) {
+      if (hole || t0 + C4_TILE > len) at_fill_holes<D>(v, vs, t0, len);
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) nan_rows[rt] = 0;
-      for (int g = 0; g < M; ++g) {
-        uint32_t vs[2];
-        at_load_words(vs, tile + 33 * D + g * 32 + c * 8);
+      for (int n = 0; n < VN; ++n) {
+        const int b = wave * VN + n;      // byte b of every token's unit, as byte 0
+        uint32_t pair[8];
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
-          const bool hole = at_byte(vs[x / 4], x % 4) == C4_NAN;
-          const int token = t0 + 4 * c + x % 4 + 16 * (x / 4);
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-            nan_rows[rt] |= (hole && token <= last[rt] ? 1u : 0u) << g;
+          uint32_t word;
+          if constexpr (U == 4) word = v[x / 2] >> (16 * (x % 2));
+          else if constexpr (U == 8) word = v[x];
+          else word = b < 4 ? v[2 * x] : v[2 * x + 1];
+          pair[x] = c4_pair(word >> (8 * (b & 3)), at_scale(vs[x / 4], x % 4), 0);
         }
-      }
+        u32x4_t lo, hi;
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        nan_rows[rt] |= __shfl_xor(nan_rows[rt], 16, 64);
-        nan_rows[rt] |= __shfl_xor(nan_rows[rt], 32, 64);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if ((nan_rows[rt] >> ((4 * c + i) * U / 32)) & 1u)
-#pragma unroll
-            for (int m = 0; m < U; ++m) acc[rt][m][i] = as_f32(0x7FC00000u);
-      }
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const int token = t0 + 4 * c + x % 4 + 16 * (x / 4);
-        if (token >= u.seq.len || at_byte(cur.vs[x / 4], x % 4) == C4_NAN) {
-          const int bit = 8 * (x % 4);
-          cur.vs[x / 4] = (cur.vs[x / 4] & ~(0xFFu << bit)) | (127u << bit);
-          if constexpr (U == 4) {
-            cur.v[x / 2] &= x % 2 == 0 ? 0xFFFF0000u : 0x0000FFFFu;
-          } else {
-#pragma unroll
-            for (int w = 0; w < U / 8; ++w) cur.v[x * (U / 8) + w] = 0;
-          }
+        for (int x = 0; x < 4; ++x) {
+          lo[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x05040100u);
+          hi[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x07060302u);
         }
-      }
-    }
-    // running maximum
-    float mx[RT];
-    bool grown = false;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      mx[rt] = s[rt][0][0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) mx[rt] = fmaxf(mx[rt], s[rt][e / 4][e % 4]);
-      grown |= mx[rt] > top_next[rt];
-    }
-    if (__any(grown)) {
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const float now = fmaxf(top[rt], at_row_max(mx[rt]));
-        const float b = now == -INFINITY ? 0.f : now * scl;
-        const float f = top[rt] == -INFINITY ? 0.f : exp2f(base[rt] - b);
-        top[rt] = now;
-        top_next[rt] = now + slack;
-        base[rt] = b;
-        sum[rt] *= f;
-#pragma unroll
-        for (int m = 0; m < U; ++m) acc[rt][m] *= f;
-      }
-    }
-    // weights
-    u32x4_t w[RT][TERMS];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float e[8];
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        e[x] = __builtin_amdgcn_exp2f(fmaf(s[rt][x / 4][x % 4], scl, -base[rt]));
-        sum[rt] += e[x];
-      }
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        uint32_t o[TERMS];
-        at_split<DT>(e[2 * x], e[2 * x + 1], o);
-#pragma unroll
-        for (int k = 0; k < TERMS; ++k) w[rt][k][x] = o[k];
-      }
-    }
-    // outputs: byte b of a token's unit holds the lane's dims 2 b and 2 b + 1
-#pragma unroll
-    for (int b = 0; b < U / 2; ++b) {
-      uint32_t pair[8];
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const int byte = x * (U / 2) + b;
-        pair[x] = c4_pair(cur.v[byte / 4], at_scale(cur.vs[x / 4], x % 4), byte % 4);
-      }
-      u32x4_t lo, hi;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        lo[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x05040100u);
-        hi[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x07060302u);
-      }
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int k = TERMS - 1; k >= 0; --k) {
-          acc[rt][2 * b] = mfma_chunk<DT_BF16>(lo, w[rt][k], acc[rt][2 * b]);
-          acc[rt][2 * b + 1] = mfma_chunk<DT_BF16>(hi, w[rt][k], acc[rt][2 * b + 1]);
-        }
-    }
-  };
-
-  int t = first + wt;
-  if constexpr (WT > 1) {
-    // The wave's own ring: NB - 1 tiles on their way while one is multiplied, no
-    // barrier, the page of the next one ahead of them.  `bad`: bit i, the tile i turns
-    // ahead is on no page.
-    char* ring = smem + wave * (NB * TILE);
-    uint32_t bad = 0;
-    int id = t < end ? page_of(t) : 0, slot = 0;
-    auto issue = [&](int x, int at) {
-      at_issue<D>(tile_at(x, id), ring + at * TILE);
-      bad |= (held(id) ? 0u : 1u) << (NB - 1);
-      id = page_of(x + WT < end ? x + WT : x);
-    };
-#pragma unroll
-    for (int i = 0; i < NB - 1; ++i) {
-      bad >>= 1;
-      if (t + i * WT < end) issue(t + i * WT, i);
-    }
-    load_q();
-    for (; t < end; t += WT) {
-      bad >>= 1;
-      if (t + (NB - 1) * WT < end) {
-        issue(t + (NB - 1) * WT, slot == 0 ? NB - 1 : slot - 1);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NB - 1) * at_instr<D>()) : "memory");
-      } else {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      }
-      if ((bad & 1u) == 0) {
-        AttendTile<D> cur;
-        const uint8_t* tile = reinterpret_cast<const uint8_t*>(ring + slot * TILE);
-        at_load(cur, tile);
-        step(cur, t, tile);
-      }
-      slot = slot == NB - 1 ? 0 : slot + 1;
-      asm volatile("" ::: "memory");
-    }
-    __syncthreads();   // the rings are free for the join
-  } else {
-    // Two tiles in registers by turns: one is multiplied while the other is on its
-    // way, and the page of the one after it
-    AttendTile<D> even, odd;
-    if (t < end) {
-      load_q();
-      int id = page_of(t), next = page_of(t + WT < end ? t + WT : t);
-      at_load(even, tile_at(t, id));
-      while (true) {
-        int after = page_of(t + 2 * WT < end ? t + 2 * WT : t);
-        if (t + WT < end) at_load(odd, tile_at(t + WT, next));
-        if (held(id)) step(even, t, tile_at(t, id));
-        t += WT;
-        if (t >= end) break;
-        id = page_of(t + 2 * WT < end ? t + 2 * WT : t);
-        if (t + WT < end) at_load(even, tile_at(t + WT, after));
-        if (held(next)) step(odd, t, tile_at(t, next));
-        t += WT;
-        if (t >= end) break;
-        next = id;
-        id = after;
+        st16(to + (2 * M + 2 * b) * 1024, lo);
+        st16(to + (2 * M + 2 * b + 1) * 1024, hi);
       }
     }
   }
+};
 
-  // the waves along the tokens join
-  float ref[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    sum[rt] = at_row_sum(sum[rt]);
-    ref[rt] = top[rt] == -INFINITY ? -INFINITY : base[rt];
-  }
-  if constexpr (WT > 1) {
-#pragma unroll
-    for (int step = WT / 2; step > 0; step >>= 1) {
-      char* slot = smem + (wr * (WT / 2) + (wt & (step - 1))) * (RT * (U * 1024 + 512));
-      f32x4_t* join = reinterpret_cast<f32x4_t*>(slot) + lane;
-      float* ml = reinterpret_cast<float*>(slot + RT * U * 1024) + lane;
-      if (wt >= step && wt < 2 * step) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          ml[rt * 128] = ref[rt];
-          ml[rt * 128 + 64] = sum[rt];
-#pragma unroll
-          for (int m = 0; m < U; ++m) join[(rt * U + m) * 64] = acc[rt][m];
-        }
-      }
-      __syncthreads();
-      if (wt < step) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          const float other = ml[rt * 128], most = fmaxf(ref[rt], other);
-          const float a = at_weight(ref[rt], most), b = at_weight(other, most);
-          ref[rt] = most;
-          sum[rt] = sum[rt] * a + ml[rt * 128 + 64] * b;
-#pragma unroll
-          for (int m = 0; m < U; ++m) acc[rt][m] = acc[rt][m] * a + join[(rt * U + m) * 64] * b;
-        }
-      }
-      if (step > 1) __syncthreads();
-    }
-    if (wt != 0) return;
-  }
-
-  // a lane holds dims 4 c u .. 4 c u + 4 u - 1 of its rows
+template <int DT, int D>
+__global__ __launch_bounds__(64 * AM_WAVES, am_occupancy(D))
+void attend_many_kernel(AttendParams p) {
+  constexpr int U = D / 16, M = D / 32, TERMS = at_terms<DT>(), RT = am_row_tiles<DT, D>();
+  constexpr int BR = 16 * RT * AM_WAVES, STAGE = 4 * M * 1024;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  const int lane = threadIdx.x & 63, j = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  AttendBlock k;
+  if (!at_block<BR>(p, &k)) return;
+  const int row0 = k.blk * BR + wave * RT * 16;
+  AttendRows<D, RT> rows;
+  rows.clear();
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = row0 + rt * 16 + j;
-    if (r >= R) continue;
-    if (u.splits > 1) {
-      const int64_t at = (u.part + u.local) * BR + (r - blk * BR);
-      float* dst = p.part + at * D + 4 * c * U;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int m = 0; m < U; m += 4)
-          *reinterpret_cast<f32x4_t*>(dst + i * U + m) =
-              f32x4_t{acc[rt][m][i], acc[rt][m + 1][i], acc[rt][m + 2][i], acc[rt][m + 3][i]};
-      if (c == 0) {
-        float* ml = p.part + (int64_t)2 * p.target * BR * D + at * 2;
-        ml[0] = ref[rt];
-        ml[1] = sum[rt];
+    rows.last[rt] = r < k.R ? at_last(p, k, r) : -1;
+  }
+  // every row of the wave sees the tokens up to `full`, none sees one behind `most`
+  const int full = row0 < k.R ? at_last(p, k, row0) : -1;
+  const int end_row = row0 + 16 * RT < k.R ? row0 + 16 * RT : k.R;
+  const int most = row0 < k.R ? at_last(p, k, end_row - 1) : -1;
+  const float scl = p.scale_log2, slack = AT_SLACK / scl;
+  const AttendPages<D> pages(p, k);
+
+  // Tile t is multiplied out of one half of LDS while t + 1 is unpacked into the other
+  // and t + 2 on its way into registers; one barrier a tile.
+  AttendShare<D> share;
+  u32x4_t q[RT][M][TERMS];
+  int t = k.first;
+  if (t < k.end) {
+    int id = pages.id(t), id1 = pages.id(t + 1 < k.end ? t + 1 : t);
+    share.load(pages.tile(t, id), wave);
+    at_queries<DT, D, RT>(p, k, row0, q);
+    bool hole = __any(at_hole(share.vs));
+    share.unpack(smem, wave, t * C4_TILE, k.u.seq.len, hole);
+    if (t + 1 < k.end) share.load(pages.tile(t + 1, id1), wave);
+    __syncthreads();
+    for (; t < k.end; ++t) {
+      const char* ops = smem + ((t - k.first) & 1) * STAGE + lane * 16;
+      const int t0 = t * C4_TILE;
+      const int id2 = pages.id(t + 2 < k.end ? t + 2 : t);
+      bool next_hole = false;
+      if (t + 1 < k.end) {
+        next_hole = __any(at_hole(share.vs));
+        share.unpack(smem + ((t + 1 - k.first) & 1) * STAGE, wave, t0 + C4_TILE, k.u.seq.len,
+                     next_hole);
+        if (t + 2 < k.end) share.load(pages.tile(t + 2, id2), wave);
       }
-      continue;
-    }
-    const float inv = sum[rt] == 0.f ? 0.f : 1.f / sum[rt];
-    char* dst = p.out + (int64_t)(u.seq.q0 + r / G) * p.out_stride + ((int64_t)h * G + r % G) * D * ES + 4 * c * U * ES;
-    float o[4 * U];
+      if (pages.held(id) && t0 <= most) {
+        f32x4_t s[RT][2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int half = 0; half < 2; ++half) {
 #pragma unroll
-      for (int m = 0; m < U; ++m) o[i * U + m] = acc[rt][m][i] * inv;
+          for (int rt = 0; rt < RT; ++rt) s[rt][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < 4 * U * ES / 16; ++x) {
-      u32x4_t v;
+          for (int m = 0; m < M; ++m) {
+            const u32x4_t kv = ld16(ops + (half * M + m) * 1024);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if constexpr (DT == DT_BF16) v[k] = at_pack(o[8 * x + 2 * k], o[8 * x + 2 * k + 1]);
-        else v[k] = as_u32(o[4 * x + k]);
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+              for (int x = TERMS - 1; x >= 0; --x)
+                s[rt][half] = mfma_chunk<DT_BF16>(kv, q[rt][m][x], s[rt][half]);
+          }
+        }
+        if (t0 + C4_TILE - 1 > full) rows.mask(s, t0);
+        if (hole) rows.holes(pages.tile(t, id) + 33 * D, t0);
+        u32x4_t w[RT][TERMS];
+        rows.template weights<DT>(s, scl, slack, w);
+        rows.add_ones(w);
+#pragma unroll
+        for (int m = 0; m < U; ++m) rows.add(m, ld16(ops + (2 * M + m) * 1024), w);
       }
-      st16(dst + 16 * x, v);
+      id = id1;
+      id1 = id2;
+      hole = next_hole;
+      __syncthreads();
     }
   }
+  float refs[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) refs[rt] = rows.ref(rt);
+  at_store<DT, D, RT, BR>(p, k, row0, rows, refs);
 }
 
 // Joins the parts of a row's keys: a workgroup a row and query head.
@@ -726,9 +921,10 @@ struct AttendPlan {
   int64_t units;    // workgroups
 };
 
-template <int DT, int D>
-constexpr int at_row_tiles() {
-  return DT == DT_F32 && D == 256 ? 1 : 2;
+template <int DT>
+static int many_block(int d) {
+  return 16 * AM_WAVES * (d == 64 ? am_row_tiles<DT, 64>()
+                                  : d == 128 ? am_row_tiles<DT, 128>() : am_row_tiles<DT, 256>());
 }
 
 static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
@@ -736,9 +932,9 @@ static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_
   const int G = q_heads / kv_heads;
   AttendPlan a{};
   a.rows = n * G > (int64_t)16 * batch;
-  a.block = !a.rows ? 16 : dt == DT_F32 && d == 256 ? 64 : 128;
+  a.block = !a.rows ? 16 : dt == DT_BF16 ? many_block<DT_BF16>(d) : many_block<DT_F32>(d);
   const int64_t whole = (n * G / a.block + batch) * kv_heads;
-  a.target = a.rows ? 240 : 1024;
+  a.target = a.rows ? 240 : 768;
   if (whole >= a.target || tokens <= AT_MIN_TILES * C4_TILE) a.target = 0;
   a.units = whole + (a.target > 0 ? a.target + 64 : 0);
   return a;
@@ -756,13 +952,13 @@ static hipError_t launch_attend_d(AttendParams p, hipStream_t st) {
                                    (int64_t)p.max_pages << p.page_log2);
   p.target = a.target;
   const dim3 grid((unsigned)((a.units + 7) / 8 * 8));
-  constexpr int RT = at_row_tiles<DT, D>();
   const hipError_t e =
-      a.rows ? launch_kernel(attend_kernel<DT, D, RT, 4, 1>, grid, dim3(256), 0, st, p)
-             : launch_kernel(attend_kernel<DT, D, 1, 1, 4>, grid, dim3(256), 0, st, p);
+      a.rows ? launch_kernel(attend_many_kernel<DT, D>, grid, dim3(64 * AM_WAVES), 0, st, p)
+             : launch_kernel(attend_few_kernel<DT, D>, grid, dim3(64 * AF_WAVES), 0, st, p);
   if (e != hipSuccess || a.target == 0) return e;
   const dim3 rows((unsigned)((int64_t)p.n * p.q_heads));
-  return a.rows ? launch_kernel(attend_join_kernel<DT, D, 64 * RT>, rows, dim3(256), 0, st, p)
+  constexpr int BLOCK = 16 * AM_WAVES * am_row_tiles<DT, D>();
+  return a.rows ? launch_kernel(attend_join_kernel<DT, D, BLOCK>, rows, dim3(256), 0, st, p)
                 : launch_kernel(attend_join_kernel<DT, D, 16>, rows, dim3(256), 0, st, p);
 }
 

@@ -163,7 +163,7 @@ __device__ __forceinline__ void at_load_words(uint32_t (&w)[N], const uint8_t* p
 
 template <int D>
 __device__ __forceinline__ void at_load(AttendTile<D>& t, const uint8_t* tile) {
-  const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
+  const uint32_t lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
 #pragma unroll
   for (int s = 0; s < 2; ++s)
     at_load_words(t.k[s], tile + (16 * s + j) * (D / 2) + c * (D / 8));
@@ -282,12 +282,10 @@ struct AttendRows {
     }
   }
 
-  // Scores into weights 2^(s scl - base).  The maximum is renewed, and what there is
-  // rescaled, only when a score has passed it by 2^AT_SLACK: p stays far from
-  // float32's ends, and most tiles need neither.
-  template <int DT>
-  __device__ __forceinline__ void weights(const f32x4_t (&s)[RT][2], float scl, float slack,
-                                          u32x4_t (&w)[RT][at_terms<DT>()]) {
+  // The maximum is renewed, and what there is rescaled, only when a score has passed
+  // it by 2^AT_SLACK: the weights stay far from float32's ends, and most tiles need
+  // neither.
+  __device__ __forceinline__ void renew(const f32x4_t (&s)[RT][2], float scl, float slack) {
     float mx[RT];
     bool grown = false;
 #pragma unroll
@@ -310,6 +308,12 @@ struct AttendRows {
         for (int m = 0; m <= U; ++m) acc[rt][m] *= f;
       }
     }
+  }
+
+  // Scores into weights 2^(s scl - base)
+  template <int DT>
+  __device__ __forceinline__ void weights(const f32x4_t (&s)[RT][2], float scl,
+                                          u32x4_t (&w)[RT][at_terms<DT>()]) const {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       float e[8];
@@ -409,19 +413,19 @@ struct AttendPages {
   // (scalar loads, which the counts of loads in flight below leave out)
   typedef const __attribute__((address_space(4))) int32_t* scalar_ptr_t;
   scalar_ptr_t pages;
-  const uint8_t* cache;
-  int tiles_log2, num_pages, kv_heads, h;
+  const uint8_t* head;       // the key head's tiles of page 0
+  int64_t page_bytes;
+  int tiles_log2, num_pages;
 
   __device__ __forceinline__ AttendPages(const AttendParams& p, const AttendBlock& k)
       : pages((scalar_ptr_t)(uintptr_t)(p.pages + (int64_t)k.u.b * p.max_pages)),
-        cache(p.cache), tiles_log2(p.page_log2 - 5), num_pages(p.num_pages),
-        kv_heads(p.kv_heads), h(k.h) {}
+        head(p.cache + ((int64_t)k.h << (p.page_log2 - 5)) * (34 * D)),
+        page_bytes(((int64_t)p.kv_heads << (p.page_log2 - 5)) * (34 * D)),
+        tiles_log2(p.page_log2 - 5), num_pages(p.num_pages) {}
   __device__ __forceinline__ int id(int t) const { return pages[t >> tiles_log2]; }
   __device__ __forceinline__ bool held(int id) const { return id >= 0 && id < num_pages; }
   __device__ __forceinline__ const uint8_t* tile(int t, int id) const {
-    const int64_t page = held(id) ? id : 0;
-    return cache + (((page * kv_heads + h) << tiles_log2) + (t & ((1 << tiles_log2) - 1))) *
-                       (int64_t)(34 * D);
+    return head + (held(id) ? id : 0) * page_bytes + (t & ((1 << tiles_log2) - 1)) * (34 * D);
   }
 };
 
@@ -534,6 +538,7 @@ __device__ __forceinline__ void at_fill_holes(uint32_t (&v)[D / 16], uint32_t (&
 #pragma unroll
   for (int x = 0; x < 8; ++x) {
     const int token = t0 + 4 * c + x % 4 + 16 * (x / 4), bit = 8 * (x % 4);
+    asm volatile("");   // (rare: not to be turned into selects on everybody's way)
     if (token >= len || ((vs[x / 4] >> bit) & 0xFFu) == (uint32_t)C4_NAN) {
       vs[x / 4] = (vs[x / 4] & ~(0xFFu << bit)) | (127u << bit);
       if constexpr (U == 4) {
@@ -660,8 +665,9 @@ void attend_few_kernel(AttendParams p) {
       const bool hole = __any(at_hole(cur.vs));
       if (hole) rows.holes(tile + 33 * D, t0);
       if (hole || t0 + C4_TILE > k.u.seq.len) at_fill_holes<D>(cur.v, cur.vs, t0, k.u.seq.len);
+      rows.renew(s, scl, slack);
       u32x4_t w[1][TERMS];
-      rows.template weights<DT>(s, scl, slack, w);
+      rows.template weights<DT>(s, scl, w);
       rows.add_ones(w);
 #pragma unroll
       for (int b = 0; b < U / 2; ++b) {
@@ -700,55 +706,64 @@ constexpr int am_row_tiles() {
 }
 constexpr int am_occupancy(int d) { return d == 256 ? 1 : 2; }
 
-// A wave's share of a tile: D / 64 of the 2 D / 32 operands of k, and of the D / 32 pairs of
-// operands of v (d = 64: k by the last two waves, v by the first two)
+// A wave's share of a tile: D / 64 of the D / 16 operands of k, and of the D / 32 pairs of
+// operands of v D / 128 (d = 64: k by the last two waves, v by the first two)
 template <int D>
 struct AttendShare {
   static constexpr int M = D / 32, U = D / 16;
   static constexpr int KN = D == 64 ? 2 : D / 64, VN = D == 64 ? 1 : D / 128;
-  uint32_t k[KN], ks, v[U], vs[2];
-  __device__ __forceinline__ void load(const uint8_t* tile, int wave) {
-    const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
-    const int half = D == 64 ? wave & 1 : wave >> 1, m0 = D == 64 ? 0 : (wave & 1) * KN;
-    at_load_words(k, tile + (16 * half + j) * (D / 2) + c * (D / 8) + 4 * m0);
-    const uint8_t* at = tile + 32 * D + (16 * half + j) * M + m0;
-    if constexpr (KN == 2) ks = *reinterpret_cast<const uint16_t*>(at);
-    else ks = *reinterpret_cast<const uint32_t*>(at);
-    at_load_words(v, tile + 16 * D + (c * 16 + j) * (D / 4));
-    at_load_words(vs, tile + 33 * D + j * U / 32 * 32 + c * 8);
+  uint32_t k[KN], ks, v[U], vs[2], vs_ahead[2];   // (the next tile's scales of v, to look for holes)
+  uint32_t at_k, at_ks, at_v, at_vs;   // of the lane's bytes in a tile
+  __device__ __forceinline__ AttendShare(int wave) {
+    const uint32_t lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
+    const uint32_t half = D == 64 ? wave & 1 : wave >> 1, m0 = D == 64 ? 0 : (wave & 1) * KN;
+    at_k = (16 * half + j) * (D / 2) + c * (D / 8) + 4 * m0;
+    at_ks = 32 * D + (16 * half + j) * M + m0;
+    at_v = 16 * D + (c * 16 + j) * (D / 4);
+    at_vs = 33 * D + j * U / 32 * 32 + c * 8;
   }
-  // operand n of the tile at lds + n 1024: k of the halves, then v
-  __device__ __forceinline__ void unpack(char* lds, int wave, int t0, int len, bool hole) {
-    const int lane = threadIdx.x & 63;
-    char* to = lds + lane * 16;
-    if (D != 64 || wave >= 2) {
-      const int n0 = D == 64 ? (wave & 1) * M : wave * KN;
+  __device__ __forceinline__ void load_k(const uint8_t* tile) {
+    at_load_words(k, tile + at_k);
+    if constexpr (KN == 2) ks = *reinterpret_cast<const uint16_t*>(tile + at_ks);
+    else ks = *reinterpret_cast<const uint32_t*>(tile + at_ks);
+  }
+  __device__ __forceinline__ void load_v(const uint8_t* tile, const uint8_t* next) {
+    at_load_words(v, tile + at_v);
+    vs[0] = vs_ahead[0];
+    vs[1] = vs_ahead[1];
+    at_load_words(vs_ahead, next + at_vs);
+  }
+  // operands at lds + n 1024
+  __device__ __forceinline__ void unpack_k(char* lds, int wave) const {
+    if (D == 64 && wave < 2) return;
+    const int n0 = D == 64 ? (wave & 1) * M : wave * KN;
+    char* to = lds + (threadIdx.x & 63) * 16;
 #pragma unroll
-      for (int n = 0; n < KN; ++n) st16(to + (n0 + n) * 1024, at_k_operand(k[n], at_scale(ks, n)));
-    }
-    if (D != 64 || wave < 2) {
-      if (hole || t0 + C4_TILE > len) at_fill_holes<D>(v, vs, t0, len);
+    for (int n = 0; n < KN; ++n) st16(to + (n0 + n) * 1024, at_k_operand(k[n], at_scale(ks, n)));
+  }
+  __device__ __forceinline__ void unpack_v(char* lds, int wave) const {
+    if (D == 64 && wave >= 2) return;
+    char* to = lds + (threadIdx.x & 63) * 16;
 #pragma unroll
-      for (int n = 0; n < VN; ++n) {
-        const int b = wave * VN + n;      // byte b of every token's unit, as byte 0
-        uint32_t pair[8];
+    for (int n = 0; n < VN; ++n) {
+      const int b = wave * VN + n;      // byte b of every token's unit, as byte 0
+      uint32_t pair[8];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          uint32_t word;
-          if constexpr (U == 4) word = v[x / 2] >> (16 * (x % 2));
-          else if constexpr (U == 8) word = v[x];
-          else word = b < 4 ? v[2 * x] : v[2 * x + 1];
-          pair[x] = c4_pair(word >> (8 * (b & 3)), at_scale(vs[x / 4], x % 4), 0);
-        }
-        u32x4_t lo, hi;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          lo[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x05040100u);
-          hi[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x07060302u);
-        }
-        st16(to + (2 * M + 2 * b) * 1024, lo);
-        st16(to + (2 * M + 2 * b + 1) * 1024, hi);
+      for (int x = 0; x < 8; ++x) {
+        uint32_t word;
+        if constexpr (U == 4) word = v[x / 2] >> (16 * (x % 2));
+        else if constexpr (U == 8) word = v[x];
+        else word = b < 4 ? v[2 * x] : v[2 * x + 1];
+        pair[x] = c4_pair(word >> (8 * (b & 3)), at_scale(vs[x / 4], x % 4), 0);
       }
+      u32x4_t lo, hi;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        lo[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x05040100u);
+        hi[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], 0x07060302u);
+      }
+      st16(to + 2 * b * 1024, lo);
+      st16(to + (2 * b + 1) * 1024, hi);
     }
   }
 };
@@ -771,65 +786,101 @@ void attend_many_kernel(AttendParams p) {
     const int r = row0 + rt * 16 + j;
     rows.last[rt] = r < k.R ? at_last(p, k, r) : -1;
   }
-  // every row of the wave sees the tokens up to `full`, none sees one behind `most`
-  const int full = row0 < k.R ? at_last(p, k, row0) : -1;
-  const int end_row = row0 + 16 * RT < k.R ? row0 + 16 * RT : k.R;
-  const int most = row0 < k.R ? at_last(p, k, end_row - 1) : -1;
+  const int full = row0 < k.R ? at_last(p, k, row0) : -1;   // every row sees the tokens up to here
   const float scl = p.scale_log2, slack = AT_SLACK / scl;
   const AttendPages<D> pages(p, k);
 
-  // Tile t is multiplied out of one half of LDS while t + 1 is unpacked into the other
-  // and t + 2 on its way into registers; one barrier a tile.
-  AttendShare<D> share;
+  // In one turn, of tile t: the scores of tile t + 1 (matrix cores) beside the weights of t
+  // (vector instructions), then the outputs of t beside the unpacking of k of t + 2 and
+  // v of t + 1 into the halves of LDS that the last turn has read; one barrier.
+  char* const lds_k = smem;
+  char* const lds_v = smem + STAGE;
+  constexpr int HALF = STAGE / 2;
+  AttendShare<D> share(wave);
   u32x4_t q[RT][M][TERMS];
-  int t = k.first;
-  if (t < k.end) {
-    int id = pages.id(t), id1 = pages.id(t + 1 < k.end ? t + 1 : t);
-    share.load(pages.tile(t, id), wave);
-    at_queries<DT, D, RT>(p, k, row0, q);
-    bool hole = __any(at_hole(share.vs));
-    share.unpack(smem, wave, t * C4_TILE, k.u.seq.len, hole);
-    if (t + 1 < k.end) share.load(pages.tile(t + 1, id1), wave);
-    __syncthreads();
-    for (; t < k.end; ++t) {
-      const char* ops = smem + ((t - k.first) & 1) * STAGE + lane * 16;
-      const int t0 = t * C4_TILE;
-      const int id2 = pages.id(t + 2 < k.end ? t + 2 : t);
-      bool next_hole = false;
-      if (t + 1 < k.end) {
-        next_hole = __any(at_hole(share.vs));
-        share.unpack(smem + ((t + 1 - k.first) & 1) * STAGE, wave, t0 + C4_TILE, k.u.seq.len,
-                     next_hole);
-        if (t + 2 < k.end) share.load(pages.tile(t + 2, id2), wave);
-      }
-      if (pages.held(id) && t0 <= most) {
-        f32x4_t s[RT][2];
+  const int turns = k.end - k.first;
+  if (turns > 0) {
+    auto at = [&](int i) { return k.first + (i < turns ? i : turns - 1); };
+    auto scores = [&](f32x4_t (&s)[RT][2], const char* ops) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+      for (int half = 0; half < 2; ++half) {
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) s[rt][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int rt = 0; rt < RT; ++rt) s[rt][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int m = 0; m < M; ++m) {
-            const u32x4_t kv = ld16(ops + (half * M + m) * 1024);
+        for (int m = 0; m < M; ++m) {
+          const u32x4_t kv = ld16(ops + (half * M + m) * 1024 + lane * 16);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+          for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-              for (int x = TERMS - 1; x >= 0; --x)
-                s[rt][half] = mfma_chunk<DT_BF16>(kv, q[rt][m][x], s[rt][half]);
-          }
+            for (int x = TERMS - 1; x >= 0; --x)
+              s[rt][half] = mfma_chunk<DT_BF16>(kv, q[rt][m][x], s[rt][half]);
         }
-        if (t0 + C4_TILE - 1 > full) rows.mask(s, t0);
-        if (hole) rows.holes(pages.tile(t, id) + 33 * D, t0);
-        u32x4_t w[RT][TERMS];
-        rows.template weights<DT>(s, scl, slack, w);
-        rows.add_ones(w);
+      }
+    };
+    // a tile's scores as its rows see them; a tile on no page is seen by none
+    auto seen = [&](f32x4_t (&s)[RT][2], int i, int id) {
+      const int t0 = at(i) * C4_TILE;
+      if (!pages.held(id)) rows.mask(s, 0x7FFFFF00);
+      else if (t0 + C4_TILE - 1 > full) rows.mask(s, t0);
+      rows.renew(s, scl, slack);
+    };
+    // v that has come: its holes filled
+    bool hole = false;
+    auto mend = [&](int i) {
+      const int t0 = at(i) * C4_TILE;
+      hole = __any(at_hole(share.vs));
+      if (hole || t0 + C4_TILE > k.u.seq.len)
+        at_fill_holes<D>(share.v, share.vs, t0, k.u.seq.len);
+    };
+    int id = pages.id(at(0)), id1 = pages.id(at(1)), id2 = pages.id(at(2));
+    const uint8_t* tile = pages.tile(at(0), id);
+    const uint8_t* tile1 = pages.tile(at(1), id1);
+    at_load_words(share.vs_ahead, tile + share.at_vs);
+    share.load_k(tile);
+    share.load_v(tile, tile1);
+    at_queries<DT, D, RT>(p, k, row0, q);
+    share.unpack_k(lds_k, wave);
+    mend(0);
+    share.unpack_v(lds_v, wave);
+    tile = pages.tile(at(2), id2);
+    share.load_k(tile1);
+    share.load_v(tile1, tile);
+    share.unpack_k(lds_k + HALF, wave);
+    share.load_k(tile);
+    __syncthreads();
+    f32x4_t s[RT][2];
+    scores(s, lds_k);
+    seen(s, 0, id);
+    for (int i = 0; i < turns; ++i) {
+      const bool was_hole = hole;
+      mend(i + 1);
+      const int id3 = pages.id(at(i + 3));
+      f32x4_t ahead[RT][2];
+      scores(ahead, lds_k + ((i + 1) & 1) * HALF);
+      u32x4_t w[RT][TERMS];
+      rows.template weights<DT>(s, scl, w);
+      const char* ops = lds_v + (i & 1) * HALF + lane * 16;
+      rows.add_ones(w);
 #pragma unroll
-        for (int m = 0; m < U; ++m) rows.add(m, ld16(ops + (2 * M + m) * 1024), w);
+      for (int m = 0; m < U; ++m) rows.add(m, ld16(ops + m * 1024), w);
+      share.unpack_k(lds_k + (i & 1) * HALF, wave);
+      share.unpack_v(lds_v + ((i + 1) & 1) * HALF, wave);
+      const uint8_t* far = pages.tile(at(i + 3), id3);
+      share.load_v(tile, far);
+      share.load_k(far);
+      tile = far;
+      if (was_hole && pages.held(id)) rows.holes(pages.tile(at(i), id) + 33 * D, at(i) * C4_TILE);
+      __syncthreads();
+      if (i + 1 < turns) {
+        seen(ahead, i + 1, id1);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) s[rt][half] = ahead[rt][half];
       }
       id = id1;
       id1 = id2;
-      hole = next_hole;
-      __syncthreads();
+      id2 = id3;
     }
   }
   float refs[RT];

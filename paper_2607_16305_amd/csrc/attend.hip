@@ -712,26 +712,26 @@ template <int D>
 struct AttendShare {
   static constexpr int M = D / 32, U = D / 16;
   static constexpr int KN = D == 64 ? 2 : D / 64, VN = D == 64 ? 1 : D / 128;
-  uint32_t k[KN], ks, v[U], vs[2], vs_ahead[2];   // (the next tile's scales of v, to look for holes)
+  uint32_t k[KN], ks, v[U];
   uint32_t at_k, at_ks, at_v, at_vs;   // of the lane's bytes in a tile
+  uint32_t ks_shift;                   // of its scales of k in their word
   __device__ __forceinline__ AttendShare(int wave) {
     const uint32_t lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
     const uint32_t half = D == 64 ? wave & 1 : wave >> 1, m0 = D == 64 ? 0 : (wave & 1) * KN;
     at_k = (16 * half + j) * (D / 2) + c * (D / 8) + 4 * m0;
     at_ks = 32 * D + (16 * half + j) * M + m0;
+    ks_shift = at_ks % 4 * 8;
+    at_ks -= at_ks % 4;
     at_v = 16 * D + (c * 16 + j) * (D / 4);
     at_vs = 33 * D + j * U / 32 * 32 + c * 8;
   }
   __device__ __forceinline__ void load_k(const uint8_t* tile) {
     at_load_words(k, tile + at_k);
-    if constexpr (KN == 2) ks = *reinterpret_cast<const uint16_t*>(tile + at_ks);
-    else ks = *reinterpret_cast<const uint32_t*>(tile + at_ks);
+    ks = *reinterpret_cast<const uint32_t*>(tile + at_ks);
   }
-  __device__ __forceinline__ void load_v(const uint8_t* tile, const uint8_t* next) {
-    at_load_words(v, tile + at_v);
-    vs[0] = vs_ahead[0];
-    vs[1] = vs_ahead[1];
-    at_load_words(vs_ahead, next + at_vs);
+  __device__ __forceinline__ void load_v(const uint8_t* tile) { at_load_words(v, tile + at_v); }
+  __device__ __forceinline__ void load_scales(const uint8_t* tile, uint32_t (&vs)[2]) const {
+    at_load_words(vs, tile + at_vs);
   }
   // operands at lds + n 1024
   __device__ __forceinline__ void unpack_k(char* lds, int wave) const {
@@ -739,9 +739,10 @@ struct AttendShare {
     const int n0 = D == 64 ? (wave & 1) * M : wave * KN;
     char* to = lds + (threadIdx.x & 63) * 16;
 #pragma unroll
-    for (int n = 0; n < KN; ++n) st16(to + (n0 + n) * 1024, at_k_operand(k[n], at_scale(ks, n)));
+    for (int n = 0; n < KN; ++n)
+      st16(to + (n0 + n) * 1024, at_k_operand(k[n], at_scale(ks >> ks_shift, n)));
   }
-  __device__ __forceinline__ void unpack_v(char* lds, int wave) const {
+  __device__ __forceinline__ void unpack_v(char* lds, int wave, const uint32_t (&vs)[2]) const {
     if (D == 64 && wave >= 2) return;
     char* to = lds + (threadIdx.x & 63) * 16;
 #pragma unroll
@@ -820,42 +821,48 @@ void attend_many_kernel(AttendParams p) {
     // a tile's scores as its rows see them; a tile on no page is seen by none
     auto seen = [&](f32x4_t (&s)[RT][2], int i, int id) {
       const int t0 = at(i) * C4_TILE;
-      if (!pages.held(id)) rows.mask(s, 0x7FFFFF00);
-      else if (t0 + C4_TILE - 1 > full) rows.mask(s, t0);
+      if (t0 + C4_TILE - 1 > full) rows.mask(s, t0);
+      if (!pages.held(id)) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[rt][e / 4][e % 4] = -INFINITY;
+      }
       rows.renew(s, scl, slack);
     };
-    // v that has come: its holes filled
-    bool hole = false;
-    auto mend = [&](int i) {
+    bool hole = false;   // in the tile whose v was unpacked last
+    auto mend = [&](int i, uint32_t (&vs)[2]) {
       const int t0 = at(i) * C4_TILE;
-      hole = __any(at_hole(share.vs));
-      if (hole || t0 + C4_TILE > k.u.seq.len)
-        at_fill_holes<D>(share.v, share.vs, t0, k.u.seq.len);
+      hole = __any(at_hole(vs));
+      if (hole || t0 + C4_TILE > k.u.seq.len) at_fill_holes<D>(share.v, vs, t0, k.u.seq.len);
     };
+    uint32_t vs_even[2], vs_odd[2];
+    f32x4_t s_even[RT][2], s_odd[RT][2];
     int id = pages.id(at(0)), id1 = pages.id(at(1)), id2 = pages.id(at(2));
     const uint8_t* tile = pages.tile(at(0), id);
-    const uint8_t* tile1 = pages.tile(at(1), id1);
-    at_load_words(share.vs_ahead, tile + share.at_vs);
     share.load_k(tile);
-    share.load_v(tile, tile1);
+    share.load_v(tile);
+    share.load_scales(tile, vs_odd);
     at_queries<DT, D, RT>(p, k, row0, q);
     share.unpack_k(lds_k, wave);
-    mend(0);
-    share.unpack_v(lds_v, wave);
-    tile = pages.tile(at(2), id2);
-    share.load_k(tile1);
-    share.load_v(tile1, tile);
-    share.unpack_k(lds_k + HALF, wave);
+    mend(0, vs_odd);
+    share.unpack_v(lds_v, wave, vs_odd);
+    tile = pages.tile(at(1), id1);
     share.load_k(tile);
+    share.load_v(tile);
+    share.load_scales(tile, vs_even);
+    share.unpack_k(lds_k + HALF, wave);
+    tile = pages.tile(at(2), id2);
+    share.load_k(tile);
+    share.load_scales(tile, vs_odd);
     __syncthreads();
-    f32x4_t s[RT][2];
-    scores(s, lds_k);
-    seen(s, 0, id);
-    for (int i = 0; i < turns; ++i) {
+    scores(s_even, lds_k);
+    seen(s_even, 0, id);
+    // (even and odd turns: what is loaded or computed for a later one keeps its registers)
+    auto turn = [&](int i, const f32x4_t (&s)[RT][2], f32x4_t (&ahead)[RT][2], uint32_t (&vs)[2]) {
       const bool was_hole = hole;
-      mend(i + 1);
+      mend(i + 1, vs);
       const int id3 = pages.id(at(i + 3));
-      f32x4_t ahead[RT][2];
       scores(ahead, lds_k + ((i + 1) & 1) * HALF);
       u32x4_t w[RT][TERMS];
       rows.template weights<DT>(s, scl, w);
@@ -864,23 +871,24 @@ void attend_many_kernel(AttendParams p) {
 #pragma unroll
       for (int m = 0; m < U; ++m) rows.add(m, ld16(ops + m * 1024), w);
       share.unpack_k(lds_k + (i & 1) * HALF, wave);
-      share.unpack_v(lds_v + ((i + 1) & 1) * HALF, wave);
-      const uint8_t* far = pages.tile(at(i + 3), id3);
-      share.load_v(tile, far);
-      share.load_k(far);
-      tile = far;
+      share.unpack_v(lds_v + ((i + 1) & 1) * HALF, wave, vs);
+      share.load_v(tile);
+      tile = pages.tile(at(i + 3), id3);
+      share.load_k(tile);
+      share.load_scales(tile, vs);
       if (was_hole && pages.held(id)) rows.holes(pages.tile(at(i), id) + 33 * D, at(i) * C4_TILE);
       __syncthreads();
-      if (i + 1 < turns) {
-        seen(ahead, i + 1, id1);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-          for (int half = 0; half < 2; ++half) s[rt][half] = ahead[rt][half];
-      }
+      if (i + 1 < turns) seen(ahead, i + 1, id1);
       id = id1;
       id1 = id2;
       id2 = id3;
+    };
+    int i = 0;
+    while (true) {
+      turn(i, s_even, s_odd, vs_even);
+      if (++i == turns) break;
+      turn(i, s_odd, s_even, vs_odd);
+      if (++i == turns) break;
     }
   }
   float refs[RT];

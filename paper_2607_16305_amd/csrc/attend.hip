@@ -17,6 +17,8 @@
 // weights p to bf16 for the second product (half a step, 2^-8 relative, of independent
 // signs; the output has the same step), float32 rows take q and p as three bf16
 // values each, which hold all 24 bits.
+#include <type_traits>
+
 #include "cache4.h"
 #include "dtl.h"
 #include "kernels.h"
@@ -295,7 +297,7 @@ struct AttendRows {
       for (int e = 1; e < 8; ++e) mx[rt] = fmaxf(mx[rt], s[rt][e / 4][e % 4]);
       grown |= mx[rt] > next[rt];
     }
-    if (__any(grown)) {
+    if (__builtin_expect(__any(grown), 0)) {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         const float now = fmaxf(top[rt], at_row_max(mx[rt]));
@@ -661,10 +663,12 @@ void attend_few_kernel(AttendParams p) {
             s[0][half] = mfma_chunk<DT_BF16>(kv, q[0][m][x], s[0][half]);
         }
       }
-      if (t0 + C4_TILE - 1 > full) rows.mask(s, t0);
       const bool hole = __any(at_hole(cur.vs));
-      if (hole) rows.holes(tile + 33 * D, t0);
-      if (hole || t0 + C4_TILE > k.u.seq.len) at_fill_holes<D>(cur.v, cur.vs, t0, k.u.seq.len);
+      if (__builtin_expect(hole || t0 + C4_TILE - 1 > full, 0)) {
+        rows.mask(s, t0);
+        if (hole) rows.holes(tile + 33 * D, t0);
+        at_fill_holes<D>(cur.v, cur.vs, t0, k.u.seq.len);
+      }
       rows.renew(s, scl, slack);
       u32x4_t w[1][TERMS];
       rows.template weights<DT>(s, scl, w);
@@ -820,21 +824,17 @@ void attend_many_kernel(AttendParams p) {
     };
     // a tile's scores as its rows see them; a tile on no page is seen by none
     auto seen = [&](f32x4_t (&s)[RT][2], int i, int id) {
-      const int t0 = at(i) * C4_TILE;
-      if (t0 + C4_TILE - 1 > full) rows.mask(s, t0);
-      if (!pages.held(id)) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) s[rt][e / 4][e % 4] = -INFINITY;
-      }
+      const int t0 = (k.first + i) * C4_TILE;
+      if (__builtin_expect(t0 + C4_TILE - 1 > full || !pages.held(id), 0))
+        rows.mask(s, pages.held(id) ? t0 : 0x7FFFFF00);
       rows.renew(s, scl, slack);
     };
     bool hole = false;   // in the tile whose v was unpacked last
     auto mend = [&](int i, uint32_t (&vs)[2]) {
-      const int t0 = at(i) * C4_TILE;
+      const int t0 = (k.first + i) * C4_TILE;
       hole = __any(at_hole(vs));
-      if (hole || t0 + C4_TILE > k.u.seq.len) at_fill_holes<D>(share.v, vs, t0, k.u.seq.len);
+      if (__builtin_expect(hole || t0 + C4_TILE > k.u.seq.len, 0))
+        at_fill_holes<D>(share.v, vs, t0, k.u.seq.len);
     };
     uint32_t vs_even[2], vs_odd[2];
     f32x4_t s_even[RT][2], s_odd[RT][2];
@@ -858,36 +858,44 @@ void attend_many_kernel(AttendParams p) {
     __syncthreads();
     scores(s_even, lds_k);
     seen(s_even, 0, id);
+    // (all loads waited for: the loop counts its own)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) asm volatile("" : "+v"(vs_even[x]), "+v"(vs_odd[x]));
     // (even and odd turns: what is loaded or computed for a later one keeps its registers)
-    auto turn = [&](int i, const f32x4_t (&s)[RT][2], f32x4_t (&ahead)[RT][2], uint32_t (&vs)[2]) {
+    auto turn = [&](auto odd, int i, const f32x4_t (&s)[RT][2], f32x4_t (&ahead)[RT][2],
+                    uint32_t (&vs)[2]) {
+      constexpr int HERE = decltype(odd)::value ? HALF : 0, THERE = HALF - HERE;
       const bool was_hole = hole;
       mend(i + 1, vs);
       const int id3 = pages.id(at(i + 3));
-      scores(ahead, lds_k + ((i + 1) & 1) * HALF);
+      scores(ahead, lds_k + THERE);
       u32x4_t w[RT][TERMS];
       rows.template weights<DT>(s, scl, w);
-      const char* ops = lds_v + (i & 1) * HALF + lane * 16;
+      const char* ops = lds_v + HERE + lane * 16;
       rows.add_ones(w);
 #pragma unroll
       for (int m = 0; m < U; ++m) rows.add(m, ld16(ops + m * 1024), w);
-      share.unpack_k(lds_k + (i & 1) * HALF, wave);
-      share.unpack_v(lds_v + ((i + 1) & 1) * HALF, wave, vs);
+      share.unpack_k(lds_k + HERE, wave);
+      share.unpack_v(lds_v + THERE, wave, vs);
       share.load_v(tile);
       tile = pages.tile(at(i + 3), id3);
       share.load_k(tile);
       share.load_scales(tile, vs);
-      if (was_hole && pages.held(id)) rows.holes(pages.tile(at(i), id) + 33 * D, at(i) * C4_TILE);
+      if (__builtin_expect(was_hole, 0)) {
+        if (pages.held(id))
+          rows.holes(pages.tile(at(i), id) + 33 * D, (k.first + i) * C4_TILE);
+      }
       __syncthreads();
-      if (i + 1 < turns) seen(ahead, i + 1, id1);
+      seen(ahead, i + 1, id1);   // (behind the last tile: of no use, and of no harm)
       id = id1;
       id1 = id2;
       id2 = id3;
     };
     int i = 0;
     while (true) {
-      turn(i, s_even, s_odd, vs_even);
+      turn(std::false_type(), i, s_even, s_odd, vs_even);
       if (++i == turns) break;
-      turn(i, s_odd, s_even, vs_odd);
+      turn(std::true_type(), i, s_odd, s_even, vs_odd);
       if (++i == turns) break;
     }
   }

@@ -829,10 +829,9 @@ void attend_many_kernel(AttendParams p) {
         rows.mask(s, pages.held(id) ? t0 : 0x7FFFFF00);
       rows.renew(s, scl, slack);
     };
-    bool hole = false;   // in the tile whose v was unpacked last
-    auto mend = [&](int i, uint32_t (&vs)[2]) {
+    bool hole, hole1;   // in v of tiles i and i + 1
+    auto mend = [&](int i, bool hole, uint32_t (&vs)[2]) {
       const int t0 = (k.first + i) * C4_TILE;
-      hole = __any(at_hole(vs));
       if (__builtin_expect(hole || t0 + C4_TILE > k.u.seq.len, 0))
         at_fill_holes<D>(share.v, vs, t0, k.u.seq.len);
     };
@@ -845,7 +844,8 @@ void attend_many_kernel(AttendParams p) {
     share.load_scales(tile, vs_odd);
     at_queries<DT, D, RT>(p, k, row0, q);
     share.unpack_k(lds_k, wave);
-    mend(0, vs_odd);
+    hole = __any(at_hole(vs_odd));
+    mend(0, hole, vs_odd);
     share.unpack_v(lds_v, wave, vs_odd);
     tile = pages.tile(at(1), id1);
     share.load_k(tile);
@@ -858,15 +858,12 @@ void attend_many_kernel(AttendParams p) {
     __syncthreads();
     scores(s_even, lds_k);
     seen(s_even, 0, id);
-    // (all loads waited for: the loop counts its own)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) asm volatile("" : "+v"(vs_even[x]), "+v"(vs_odd[x]));
+    hole1 = __any(at_hole(vs_even));
     // (even and odd turns: what is loaded or computed for a later one keeps its registers)
     auto turn = [&](auto odd, int i, const f32x4_t (&s)[RT][2], f32x4_t (&ahead)[RT][2],
-                    uint32_t (&vs)[2]) {
+                    uint32_t (&vs)[2], const uint32_t (&vs_next)[2]) {
       constexpr int HERE = decltype(odd)::value ? HALF : 0, THERE = HALF - HERE;
-      const bool was_hole = hole;
-      mend(i + 1, vs);
+      mend(i + 1, hole1, vs);
       const int id3 = pages.id(at(i + 3));
       scores(ahead, lds_k + THERE);
       u32x4_t w[RT][TERMS];
@@ -877,25 +874,28 @@ void attend_many_kernel(AttendParams p) {
       for (int m = 0; m < U; ++m) rows.add(m, ld16(ops + m * 1024), w);
       share.unpack_k(lds_k + HERE, wave);
       share.unpack_v(lds_v + THERE, wave, vs);
+      const bool hole2 = __any(at_hole(vs_next));   // (these have come, the loads below have not)
       share.load_v(tile);
       tile = pages.tile(at(i + 3), id3);
       share.load_k(tile);
       share.load_scales(tile, vs);
-      if (__builtin_expect(was_hole, 0)) {
+      if (__builtin_expect(hole, 0)) {
         if (pages.held(id))
           rows.holes(pages.tile(at(i), id) + 33 * D, (k.first + i) * C4_TILE);
       }
       __syncthreads();
       seen(ahead, i + 1, id1);   // (behind the last tile: of no use, and of no harm)
+      hole = hole1;
+      hole1 = hole2;
       id = id1;
       id1 = id2;
       id2 = id3;
     };
     int i = 0;
     while (true) {
-      turn(std::false_type(), i, s_even, s_odd, vs_even);
+      turn(std::false_type(), i, s_even, s_odd, vs_even, vs_odd);
       if (++i == turns) break;
-      turn(std::true_type(), i, s_odd, s_even, vs_odd);
+      turn(std::true_type(), i, s_odd, s_even, vs_odd, vs_even);
       if (++i == turns) break;
     }
   }

@@ -61,7 +61,7 @@ __device__ __forceinline__ AttendSeq at_seq(const AttendParams& p, int b) {
 struct AttendUnit {
   AttendSeq seq;
   int b, local, splits;   // sequence, index among its units, parts of its keys
-  int64_t part;           // index among the units whose keys are cut
+  int part;               // index among the units whose keys are cut, of its sequence's first
 };
 
 template <class T>
@@ -73,51 +73,45 @@ __device__ __forceinline__ T wave_sum(T v) {
 
 // Unit `unit` of the batch, the same for every lane of the wave.  The keys of all
 // sequences are cut into parts of about the same size, so that there are about
-// p.target units in all, whatever the lengths.  ROWS: a unit is a row of blocks
-// all of whose parts count as one (for joining them).
+// p.target units in all, whatever the lengths.
 template <int BR>
-__device__ __forceinline__ bool at_unit(const AttendParams& p, int64_t unit, bool joined,
-                                        AttendUnit* u) {
+__device__ __forceinline__ bool at_unit(const AttendParams& p, int64_t unit, AttendUnit* u) {
   const int lane = threadIdx.x & 63, G = p.q_heads / p.kv_heads;
-  float work = 0.f;
+  auto blocks_of = [&](const AttendSeq& s) {
+    return (int)(((int64_t)s.rows * G + BR - 1) / BR) * p.kv_heads;
+  };
+  AttendSeq s{0, 0, 0};       // of sequence lane, or of the 64 that are looked at
+  if (lane < p.batch) s = at_seq(p, lane);
+  int chunk = 0x7FFFFFFF;     // tiles of a part
   if (p.target > 0) {
-    for (int b = lane; b < p.batch; b += 64) {
-      const AttendSeq s = at_seq(p, b);
-      const int64_t blocks = ((int64_t)s.rows * G + BR - 1) / BR;
-      work += (float)blocks * (float)((s.len + C4_TILE - 1) / C4_TILE);
+    float work = (float)blocks_of(s) * (float)((s.len + C4_TILE - 1) / C4_TILE);
+    for (int b = lane + 64; b < p.batch; b += 64) {
+      const AttendSeq o = at_seq(p, b);
+      work += (float)blocks_of(o) * (float)((o.len + C4_TILE - 1) / C4_TILE);
     }
-    work = wave_sum(work) * (float)p.kv_heads;
+    const float c = ceilf(wave_sum(work) / (float)p.target);
+    chunk = c < (float)AT_MIN_TILES ? AT_MIN_TILES : c > 1e9f ? 1000000000 : (int)c;
   } else {
     // without a cut the blocks of rows of one key head read the same keys: a
     // neighbourhood of units for each XCD, so that they meet in its L2
-    int all = 0;
-    for (int b = lane; b < p.batch; b += 64)
-      all += (int)(((int64_t)at_seq(p, b).rows * G + BR - 1) / BR * p.kv_heads);
+    int all = blocks_of(s);
+    for (int b = lane + 64; b < p.batch; b += 64) all += blocks_of(at_seq(p, b));
     unit = __builtin_amdgcn_readfirstlane(xcd_remap((int)unit, wave_sum(all)));
     if (unit < 0) return false;
   }
-  int chunk = 0x7FFFFFFF;
-  if (p.target > 0) {
-    const float c = ceilf(work / (float)p.target);
-    chunk = c < (float)AT_MIN_TILES ? AT_MIN_TILES : c > 1e9f ? 1000000000 : (int)c;
-  }
   int64_t before = 0, parts = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    AttendSeq s{0, 0, 0};
-    int units = 0, splits = 1, cut = 0;
-    if (b0 + lane < p.batch) {
-      s = at_seq(p, b0 + lane);
-      const int64_t blocks = ((int64_t)s.rows * G + BR - 1) / BR * p.kv_heads;
-      const int tiles = (s.len + C4_TILE - 1) / C4_TILE;
-      splits = tiles > chunk ? (tiles + chunk - 1) / chunk : 1;
-      const int64_t all = blocks * splits;
-      const int most = all > AT_UNITS_OF_SEQ ? AT_UNITS_OF_SEQ : (int)all;
-      cut = splits > 1 ? most : 0;
-      units = joined ? (int)blocks : most;
+    if (b0 > 0) {
+      s = AttendSeq{0, 0, 0};
+      if (b0 + lane < p.batch) s = at_seq(p, b0 + lane);
     }
+    const int tiles = (s.len + C4_TILE - 1) / C4_TILE;
+    const int splits = tiles > chunk ? (tiles + chunk - 1) / chunk : 1;
+    const int64_t all = (int64_t)blocks_of(s) * splits;
+    const int units = all > AT_UNITS_OF_SEQ ? AT_UNITS_OF_SEQ : (int)all;
+    const int cut = splits > 1 ? units : 0;
     const int incl = wave_scan_incl(units), cut_incl = wave_scan_incl(cut);
-    const bool here = unit < before + incl;
-    const uint64_t found = __ballot(here);
+    const uint64_t found = __ballot(unit < before + incl);
     if (found != 0) {
       const int l = __ffsll((unsigned long long)found) - 1;
       u->b = b0 + l;
@@ -127,13 +121,25 @@ __device__ __forceinline__ bool at_unit(const AttendParams& p, int64_t unit, boo
       u->splits = __builtin_amdgcn_readlane(splits, l);
       u->local = (int)(unit - before - (__builtin_amdgcn_readlane(incl, l) -
                                         __builtin_amdgcn_readlane(units, l)));
-      u->part = parts + __builtin_amdgcn_readlane(cut_incl, l) - __builtin_amdgcn_readlane(cut, l);
+      u->part = (int)(parts + __builtin_amdgcn_readlane(cut_incl, l) -
+                      __builtin_amdgcn_readlane(cut, l));
       return true;
     }
     before += __builtin_amdgcn_readlane(incl, 63);
     parts += __builtin_amdgcn_readlane(cut_incl, 63);
   }
   return false;
+}
+
+// The workspace: p.target 2 units' outputs [BR, D], their rows' (maximum, sum), then for
+// every sequence (its first unit there, parts of its keys), for the join
+template <int D, int BR>
+__device__ __forceinline__ float* at_sums(const AttendParams& p) {
+  return p.part + (int64_t)2 * p.target * BR * D;
+}
+template <int D, int BR>
+__device__ __forceinline__ int* at_cuts(const AttendParams& p) {
+  return reinterpret_cast<int*>(at_sums<D, BR>(p) + (int64_t)2 * p.target * BR * 2);
 }
 
 // ---------------------------------------------------------------------------
@@ -386,15 +392,20 @@ struct AttendBlock {
   int first, end;            // the part's tiles
 };
 
-template <int BR>
+template <int D, int BR>
 __device__ __forceinline__ bool at_block(const AttendParams& p, AttendBlock* k) {
-  if (!at_unit<BR>(p, blockIdx.x, false, &k->u)) return false;
+  if (!at_unit<BR>(p, blockIdx.x, &k->u)) return false;
   k->G = p.q_heads / p.kv_heads;
   k->R = k->u.seq.rows * k->G;
   const int blocks = (k->R + BR - 1) / BR, hs = k->u.local / blocks;
   k->blk = blocks - 1 - k->u.local % blocks;     // the longest first
   k->h = hs / k->u.splits;
   k->split = hs % k->u.splits;
+  if (p.target > 0 && k->u.local == 0 && threadIdx.x == 0) {
+    int* cut = at_cuts<D, BR>(p) + 2 * k->u.b;
+    cut[0] = k->u.part;
+    cut[1] = k->u.splits;
+  }
   const int end_row = k->blk * BR + BR < k->R ? k->blk * BR + BR : k->R;
   const int seen = p.causal ? k->u.seq.len - k->u.seq.rows + (end_row - 1) / k->G + 1 : k->u.seq.len;
   const int tiles = seen > 0 ? (seen + C4_TILE - 1) / C4_TILE : 0;   // (early rows may see none)
@@ -488,7 +499,7 @@ __device__ __forceinline__ void at_store(const AttendParams& p, const AttendBloc
     if (r >= k.R) continue;
     const float sum = a.acc[rt][U][0];
     if (k.u.splits > 1) {
-      const int64_t at = (k.u.part + k.u.local) * BR + (r - k.blk * BR);
+      const int64_t at = (int64_t)(k.u.part + k.u.local) * BR + (r - k.blk * BR);
       float* dst = p.part + at * D + 4 * c * U;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -498,8 +509,7 @@ __device__ __forceinline__ void at_store(const AttendParams& p, const AttendBloc
               f32x4_t{a.acc[rt][m][i], a.acc[rt][m + 1][i], a.acc[rt][m + 2][i],
                       a.acc[rt][m + 3][i]};
       if (c == 0)
-        *reinterpret_cast<f32x2_t*>(p.part + (int64_t)2 * p.target * BR * D + at * 2) =
-            f32x2_t{refs[rt], sum};
+        reinterpret_cast<f32x2_t*>(at_sums<D, BR>(p))[at] = f32x2_t{refs[rt], sum};
       continue;
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -610,7 +620,7 @@ void attend_few_kernel(AttendParams p) {
   const int lane = threadIdx.x & 63, j = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   AttendBlock k;
-  if (!at_block<BR>(p, &k)) return;
+  if (!at_block<D, BR>(p, &k)) return;
   const int row0 = k.blk * BR;
   AttendRows<D, 1> rows;
   rows.clear();
@@ -782,7 +792,7 @@ void attend_many_kernel(AttendParams p) {
   const int lane = threadIdx.x & 63, j = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   AttendBlock k;
-  if (!at_block<BR>(p, &k)) return;
+  if (!at_block<D, BR>(p, &k)) return;
   const int row0 = k.blk * BR + wave * RT * 16;
   AttendRows<D, RT> rows;
   rows.clear();
@@ -905,77 +915,91 @@ void attend_many_kernel(AttendParams p) {
   at_store<DT, D, RT, BR>(p, k, row0, rows, refs);
 }
 
-// Joins the parts of a row's keys: a workgroup a row and query head.
-template <int DT, int D, int BR>
+// Joins the parts of a row's keys: W waves a row and query head.
+template <int DT, int D, int BR, int W>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
-  constexpr int ES = DT == DT_BF16 ? 2 : 4, L = D / 4, N = 256 / L;
-  __shared__ f32x4_t accs[N][L];
-  __shared__ float ms[N], ls[N];
-  const int G = p.q_heads / p.kv_heads;
-  const int row = blockIdx.x / p.q_heads, head = blockIdx.x % p.q_heads;   // (of all n rows)
+  constexpr int E = D / 64, AHEAD = 4;     // values of a lane, parts on their way
+  typedef float fe_t __attribute__((ext_vector_type(E)));
+  __shared__ fe_t accs[W][64];
+  __shared__ float ms[W], ls[W];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int at = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;   // of all rows' query heads
+  if (at >= p.n * p.q_heads) return;
+  const int row = at / p.q_heads, head = at - row * p.q_heads, G = p.q_heads / p.kv_heads;
   // the row's sequence
-  const int lane64 = threadIdx.x & 63;
   int b = row;
+  AttendSeq s{row, 1, 0};
   if (p.q_offsets != nullptr) {
     b = -1;
     for (int b0 = 0; b0 < p.batch && b < 0; b0 += 64) {
-      bool mine = false;
-      if (b0 + lane64 < p.batch) {
-        const AttendSeq s = at_seq(p, b0 + lane64);
-        mine = row >= s.q0 && row < s.q0 + s.rows;
+      AttendSeq o{0, 0, 0};
+      if (b0 + lane < p.batch) o = at_seq(p, b0 + lane);
+      const uint64_t found = __ballot(row >= o.q0 && row < o.q0 + o.rows);
+      if (found != 0) {
+        const int l = __ffsll((unsigned long long)found) - 1;
+        b = b0 + l;
+        s.q0 = __builtin_amdgcn_readlane(o.q0, l);
+        s.rows = __builtin_amdgcn_readlane(o.rows, l);
       }
-      const uint64_t found = __ballot(mine);
-      if (found != 0) b = b0 + __ffsll((unsigned long long)found) - 1;
     }
     if (b < 0) return;
   }
-  // the sequence's first unit, by the search that found the units
-  const AttendSeq s = at_seq(p, b);
-  AttendUnit u;
-  int64_t first = 0;
-  for (int a = lane64; a < b; a += 64) {
-    const AttendSeq o = at_seq(p, a);
-    first += ((int64_t)o.rows * G + BR - 1) / BR * p.kv_heads;
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) first += __shfl_xor((long long)first, d, 64);
-  if (!at_unit<BR>(p, first, true, &u) || u.splits <= 1) return;
-  const int R = s.rows * G, blocks = (R + BR - 1) / BR;
-  const int h = head / G, r = (row - s.q0) * G + head % G, blk = r / BR;
-  const int l = threadIdx.x % L, g = threadIdx.x / L;
-  const float* ml = p.part + (int64_t)2 * p.target * BR * D;
+  const int* cut = at_cuts<D, BR>(p) + 2 * b;
+  const int part = cut[0], splits = cut[1];
+  if (splits <= 1) return;
+  const int blocks = (s.rows * G + BR - 1) / BR;
+  const int h = head / G, r = (row - s.q0) * G + head - h * G, blk = r / BR;
+  const int64_t first = ((int64_t)part + (int64_t)h * splits * blocks + (blocks - 1 - blk)) * BR +
+                        (r - blk * BR);
+  const int64_t step = (int64_t)blocks * BR;
+  const f32x2_t* sums = reinterpret_cast<const f32x2_t*>(at_sums<D, BR>(p));
+  const fe_t* outs = reinterpret_cast<const fe_t*>(p.part) + lane;
   float m = -INFINITY, sum = 0.f;
-  f32x4_t acc{0.f, 0.f, 0.f, 0.f};
-  for (int x = g; x < u.splits; x += N) {
-    const int64_t unit = u.part + ((int64_t)h * u.splits + x) * blocks + (blocks - 1 - blk);
-    const int64_t at = unit * BR + (r - blk * BR);
-    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p.part + at * D + 4 * l);
-    const float om = ml[2 * at], ol = ml[2 * at + 1];
-    const float most = fmaxf(m, om), a = at_weight(m, most), c = at_weight(om, most);
-    m = most;
-    sum = sum * a + ol * c;
-    acc = acc * a + v * c;
-  }
-  accs[g][l] = acc;
-  if (l == 0) {
-    ms[g] = m;
-    ls[g] = sum;
-  }
-  __syncthreads();
-  if (g != 0) return;
+  fe_t acc = {};
+  for (int x0 = wave % W; x0 < splits; x0 += W * AHEAD) {
+    fe_t v[AHEAD];
+    f32x2_t ml[AHEAD];
 #pragma unroll
-  for (int x = 1; x < N; ++x) {
-    const float most = fmaxf(m, ms[x]), a = at_weight(m, most), c = at_weight(ms[x], most);
-    m = most;
-    sum = sum * a + ls[x] * c;
-    acc = acc * a + accs[x][l] * c;
+    for (int i = 0; i < AHEAD; ++i) {
+      const int x = x0 + i * W < splits ? x0 + i * W : x0;
+      ml[i] = sums[first + x * step];
+      v[i] = outs[(first + x * step) * 64];
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (x0 + i * W >= splits) break;
+      const float most = fmaxf(m, ml[i][0]), a = at_weight(m, most), c = at_weight(ml[i][0], most);
+      m = most;
+      sum = sum * a + ml[i][1] * c;
+      acc = acc * a + v[i] * c;
+    }
+  }
+  if constexpr (W > 1) {
+    accs[wave][lane] = acc;
+    if (lane == 0) {
+      ms[wave] = m;
+      ls[wave] = sum;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int x = 1; x < W; ++x) {
+      const float most = fmaxf(m, ms[x]), a = at_weight(m, most), c = at_weight(ms[x], most);
+      m = most;
+      sum = sum * a + ls[x] * c;
+      acc = acc * a + accs[x][lane] * c;
+    }
   }
   acc *= sum == 0.f ? 0.f : 1.f / sum;
-  char* dst = p.out + row * p.out_stride + ((int64_t)head * D + 4 * l) * ES;
-  if constexpr (DT == DT_BF16)
-    *reinterpret_cast<uint2*>(dst) = make_uint2(at_pack(acc[0], acc[1]), at_pack(acc[2], acc[3]));
-  else
-    *reinterpret_cast<f32x4_t*>(dst) = acc;
+  constexpr int ES = DT == DT_BF16 ? 2 : 4;
+  char* dst = p.out + row * p.out_stride + ((int64_t)head * D + E * lane) * ES;
+  if constexpr (DT == DT_F32) {
+    *reinterpret_cast<fe_t*>(dst) = acc;
+  } else {
+    typedef __bf16 be_t __attribute__((ext_vector_type(E)));
+    *reinterpret_cast<be_t*>(dst) = __builtin_convertvector(acc, be_t);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -1001,7 +1025,8 @@ static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_
   a.rows = n * G > (int64_t)16 * batch;
   a.block = !a.rows ? 16 : dt == DT_BF16 ? many_block<DT_BF16>(d) : many_block<DT_F32>(d);
   const int64_t whole = (n * G / a.block + batch) * kv_heads;
-  a.target = a.rows ? 240 : 768;
+  // (one round of resident workgroups; 512 of 128 rows and 128 dims are 68 MB)
+  a.target = a.rows ? (d == 64 ? 480 : d == 128 ? 480 : 240) : d == 64 ? 1024 : d == 128 ? 768 : dt == DT_BF16 ? 512 : 256;
   if (whole >= a.target || tokens <= AT_MIN_TILES * C4_TILE) a.target = 0;
   a.units = whole + (a.target > 0 ? a.target + 64 : 0);
   return a;
@@ -1010,7 +1035,7 @@ static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_
 size_t attend_workspace(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
                         int64_t tokens) {
   const AttendPlan a = attend_plan(dt, n, batch, q_heads, kv_heads, d, tokens);
-  return (size_t)2 * a.target * a.block * (d + 2) * 4;
+  return a.target == 0 ? 0 : (size_t)2 * a.target * a.block * (d + 2) * 4 + (size_t)batch * 8;
 }
 
 template <int DT, int D>
@@ -1023,10 +1048,13 @@ static hipError_t launch_attend_d(AttendParams p, hipStream_t st) {
       a.rows ? launch_kernel(attend_many_kernel<DT, D>, grid, dim3(64 * AM_WAVES), 0, st, p)
              : launch_kernel(attend_few_kernel<DT, D>, grid, dim3(64 * AF_WAVES), 0, st, p);
   if (e != hipSuccess || a.target == 0) return e;
-  const dim3 rows((unsigned)((int64_t)p.n * p.q_heads));
+  // a wave a row where that fills the chip, else a workgroup
+  const int64_t rows = (int64_t)p.n * p.q_heads;
   constexpr int BLOCK = 16 * AM_WAVES * am_row_tiles<DT, D>();
-  return a.rows ? launch_kernel(attend_join_kernel<DT, D, BLOCK>, rows, dim3(256), 0, st, p)
-                : launch_kernel(attend_join_kernel<DT, D, 16>, rows, dim3(256), 0, st, p);
+  const dim3 each((unsigned)rows), four((unsigned)((rows + 3) / 4));
+  if (a.rows) return launch_kernel(attend_join_kernel<DT, D, BLOCK, 1>, four, dim3(256), 0, st, p);
+  if (rows >= 4096) return launch_kernel(attend_join_kernel<DT, D, 16, 1>, four, dim3(256), 0, st, p);
+  return launch_kernel(attend_join_kernel<DT, D, 16, 4>, each, dim3(256), 0, st, p);
 }
 
 hipError_t launch_attend(int dt, int d, AttendParams p, hipStream_t st) {

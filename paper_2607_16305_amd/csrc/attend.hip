@@ -1026,7 +1026,7 @@ static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_
   a.block = !a.rows ? 16 : dt == DT_BF16 ? many_block<DT_BF16>(d) : many_block<DT_F32>(d);
   const int64_t whole = (n * G / a.block + batch) * kv_heads;
   // (one round of resident workgroups; 512 of 128 rows and 128 dims are 68 MB)
-  a.target = a.rows ? (d == 64 ? 480 : d == 128 ? 480 : 240) : d == 64 ? 1024 : d == 128 ? 768 : dt == DT_BF16 ? 512 : 256;
+  a.target = a.rows ? (d == 64 ? 512 : d == 128 ? 480 : 240) : d == 64 ? 1024 : d == 128 ? 768 : dt == DT_BF16 ? 512 : 256;
   if (whole >= a.target || tokens <= AT_MIN_TILES * C4_TILE) a.target = 0;
   a.units = whole + (a.target > 0 ? a.target + 64 : 0);
   return a;

@@ -1,7 +1,7 @@
 // Keys and values into the 4-bit cache as they come, and back (cache4.h has the
 // format and the places of the bytes).
 //
-// A block of 32 values of a head is four neighbouring lanes with 8 values each:
+// A block of 32 values of a head is four lanes of a wave with 8 values each:
 // its largest |value| over the four, the scale from its exponent, the codes by the
 // conversion of this chip, which rounds to the nearest value, of two as near to
 // the even code, and saturates.  Every step is exact but that rounding, so the
@@ -11,7 +11,11 @@
 
 namespace lookme {
 
-constexpr int CW_THREADS = 256;
+// A workgroup takes 32 rows of a head, of k or of v.  k goes a row at a time; for v,
+// where a lane of the attention reads 8 tokens, neighbouring threads take the 8 rows
+// that are such a lane's when the rows are a tile: their bytes are neighbours then
+// (any other slots are as right, only more scattered).
+constexpr int CW_THREADS = 256, CW_ROWS = 32;
 
 // 8 values from p (16-byte aligned)
 template <int DT>
@@ -45,119 +49,136 @@ __device__ __forceinline__ bool c4_slot(const CacheParams& p, int64_t s, int h, 
   return true;
 }
 
-// A thread: 8 values of one row's head, of k or of v.
-template <int DT, int D>
-__global__ __launch_bounds__(CW_THREADS) void cache_write_kernel(CacheParams p) {
-  constexpr int L = D / 8;                     // lanes of a head
-  const int64_t id = (int64_t)blockIdx.x * CW_THREADS + threadIdx.x;
-  const int lane = (int)(id % L);
-  const int64_t rest = id / L;
-  const int h = (int)(rest % p.heads);
-  const int64_t row = rest / p.heads;
-  const bool is_v = blockIdx.y != 0;
-  int64_t tile = 0;
-  int token = 0;
-  if (row >= p.n || !c4_slot(p, p.slots[row], h, &tile, &token)) return;   // whole teams of L
-  const char* src = is_v ? p.v + row * p.v_stride : p.k + row * p.k_stride;
-  float x[8];
-  cw_load<DT>(src + ((int64_t)h * D + lane * 8) * (DT == DT_BF16 ? 2 : 4), x);
-  uint32_t amax = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t a = as_u32(x[e]) & 0x7FFFFFFFu;
-    amax = a > amax ? a : amax;
-  }
-#pragma unroll
-  for (int d = 1; d < 4; d <<= 1) {
-    const uint32_t o = __shfl_xor(amax, d, 64);
-    amax = o > amax ? o : amax;
-  }
-  const int byte = c4_scale(amax);
-  uint32_t w = 0;
-  if (byte != C4_NAN) {
-    const float s = c4_power(byte);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], s, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
-  }
-  uint8_t* t = p.cache + tile;
-  const int dim = lane * 8;
-  if (!is_v) {
-    *reinterpret_cast<uint32_t*>(t + c4_k_code(D, token, dim)) = w;
-    if (lane % 4 == 0) t[c4_k_scale(D, token, dim)] = (uint8_t)byte;
+// Task i of the workgroup's 32 rows by d / 8 chunks of 8 values
+template <int D, bool V>
+__device__ __forceinline__ void cw_task(int i, int* row, int* dim) {
+  constexpr int L = D / 8;                     // chunks of a head
+  if constexpr (V) {
+    const int c = i / (8 * L), s = i % 8;
+    *row = 4 * c + s % 4 + 16 * (s / 4);
+    *dim = i / 8 % L * 8;
   } else {
-    if constexpr (D == 64) {   // two units of 4 values
+    *row = i / L;
+    *dim = i % L * 8;
+  }
+}
+
+template <int DT, int D, bool V>
+__device__ __forceinline__ void cw_write(const CacheParams& p) {
+  constexpr int STEP = V ? 8 : 1;
+  const int h = blockIdx.y;
+  const int64_t row0 = (int64_t)blockIdx.x * CW_ROWS;
+#pragma unroll
+  for (int i = 0; i < CW_ROWS * D / 8; i += CW_THREADS) {
+    int row, dim;
+    cw_task<D, V>(i + threadIdx.x, &row, &dim);
+    const int64_t r = row0 + row;
+    int64_t tile = 0;
+    int token = 0;
+    const bool live = r < p.n && c4_slot(p, p.slots[r < p.n ? r : 0], h, &tile, &token);
+    float x[8] = {};
+    if (live)
+      cw_load<DT>((V ? p.v + r * p.v_stride : p.k + r * p.k_stride) +
+                      ((int64_t)h * D + dim) * (DT == DT_BF16 ? 2 : 4), x);
+    uint32_t amax = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t a = as_u32(x[e]) & 0x7FFFFFFFu;
+      amax = a > amax ? a : amax;
+    }
+#pragma unroll
+    for (int d = STEP; d < 4 * STEP; d <<= 1) {
+      const uint32_t o = __shfl_xor(amax, d, 64);
+      amax = o > amax ? o : amax;
+    }
+    if (!live) continue;
+    const int byte = c4_scale(amax);
+    uint32_t w = 0;
+    if (byte != C4_NAN) {
+      const float s = c4_power(byte);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], s, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
+    }
+    uint8_t* t = p.cache + tile;
+    if constexpr (V && D == 64) {   // two units of 4 values
       *reinterpret_cast<uint16_t*>(t + c4_v_code(D, token, dim)) = (uint16_t)w;
       *reinterpret_cast<uint16_t*>(t + c4_v_code(D, token, dim + 4)) = (uint16_t)(w >> 16);
     } else {
-      *reinterpret_cast<uint32_t*>(t + c4_v_code(D, token, dim)) = w;
+      *reinterpret_cast<uint32_t*>(t + (V ? c4_v_code(D, token, dim) : c4_k_code(D, token, dim))) =
+          w;
     }
-    if (lane % 4 == 0) t[c4_v_scale(D, token, dim)] = (uint8_t)byte;
+    if (dim % 32 == 0)
+      t[V ? c4_v_scale(D, token, dim) : c4_k_scale(D, token, dim)] = (uint8_t)byte;
+  }
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(CW_THREADS) void cache_write_kernel(CacheParams p) {
+  if (blockIdx.z == 0) cw_write<DT, D, false>(p);
+  else cw_write<DT, D, true>(p);
+}
+
+template <int DT, int D, bool V>
+__device__ __forceinline__ void cw_read(const CacheParams& p) {
+  const int h = blockIdx.y;
+  const int64_t row0 = (int64_t)blockIdx.x * CW_ROWS;
+#pragma unroll
+  for (int i = 0; i < CW_ROWS * D / 8; i += CW_THREADS) {
+    int row, dim;
+    cw_task<D, V>(i + threadIdx.x, &row, &dim);
+    const int64_t r = row0 + row;
+    int64_t tile = 0;
+    int token = 0;
+    if (r >= p.n || !c4_slot(p, p.slots[r], h, &tile, &token)) continue;
+    const uint8_t* t = p.cache + tile;
+    uint32_t w;
+    if constexpr (V && D == 64) {
+      w = *reinterpret_cast<const uint16_t*>(t + c4_v_code(D, token, dim));
+      w |= (uint32_t)*reinterpret_cast<const uint16_t*>(t + c4_v_code(D, token, dim + 4)) << 16;
+    } else {
+      w = *reinterpret_cast<const uint32_t*>(
+          t + (V ? c4_v_code(D, token, dim) : c4_k_code(D, token, dim)));
+    }
+    const float s = c4_power(t[V ? c4_v_scale(D, token, dim) : c4_k_scale(D, token, dim)]);
+    u32x4_t v;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) v[b] = c4_pair(w, s, b);
+    char* dst = (V ? p.v_out + r * p.v_stride : p.k_out + r * p.k_stride) +
+                ((int64_t)h * D + dim) * (DT == DT_BF16 ? 2 : 4);
+    if constexpr (DT == DT_BF16) {
+      st16(dst, v);
+    } else {
+      u32x4_t a, b;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        a[2 * k] = as_u32(bf16lo(v[k]));
+        a[2 * k + 1] = as_u32(bf16hi(v[k]));
+        b[2 * k] = as_u32(bf16lo(v[2 + k]));
+        b[2 * k + 1] = as_u32(bf16hi(v[2 + k]));
+      }
+      st16(dst, a);
+      st16(dst + 16, b);
+    }
   }
 }
 
 template <int DT, int D>
 __global__ __launch_bounds__(CW_THREADS) void cache_read_kernel(CacheParams p) {
-  constexpr int L = D / 8;
-  const int64_t id = (int64_t)blockIdx.x * CW_THREADS + threadIdx.x;
-  const int lane = (int)(id % L);
-  const int64_t rest = id / L;
-  const int h = (int)(rest % p.heads);
-  const int64_t row = rest / p.heads;
-  const bool is_v = p.k_out == nullptr || blockIdx.y != 0;
-  int64_t tile = 0;
-  int token = 0;
-  if (row >= p.n || !c4_slot(p, p.slots[row], h, &tile, &token)) return;
-  const uint8_t* t = p.cache + tile;
-  const int dim = lane * 8;
-  uint32_t w;
-  int byte;
-  if (!is_v) {
-    w = *reinterpret_cast<const uint32_t*>(t + c4_k_code(D, token, dim));
-    byte = t[c4_k_scale(D, token, dim)];
-  } else {
-    if constexpr (D == 64) {
-      w = *reinterpret_cast<const uint16_t*>(t + c4_v_code(D, token, dim));
-      w |= (uint32_t)*reinterpret_cast<const uint16_t*>(t + c4_v_code(D, token, dim + 4)) << 16;
-    } else {
-      w = *reinterpret_cast<const uint32_t*>(t + c4_v_code(D, token, dim));
-    }
-    byte = t[c4_v_scale(D, token, dim)];
-  }
-  const float s = c4_power(byte);
-  u32x4_t v;
-#pragma unroll
-  for (int b = 0; b < 4; ++b) v[b] = c4_pair(w, s, b);
-  char* dst = is_v ? p.v_out + row * p.v_stride : p.k_out + row * p.k_stride;
-  dst += ((int64_t)h * D + dim) * (DT == DT_BF16 ? 2 : 4);
-  if constexpr (DT == DT_BF16) {
-    st16(dst, v);
-  } else {
-    u32x4_t a, b;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      a[2 * k] = as_u32(bf16lo(v[k]));
-      a[2 * k + 1] = as_u32(bf16hi(v[k]));
-      b[2 * k] = as_u32(bf16lo(v[2 + k]));
-      b[2 * k + 1] = as_u32(bf16hi(v[2 + k]));
-    }
-    st16(dst, a);
-    st16(dst + 16, b);
-  }
+  if (p.k_out != nullptr && blockIdx.z == 0) cw_read<DT, D, false>(p);
+  else cw_read<DT, D, true>(p);
 }
-
-constexpr int64_t CW_BLOCKS = 1 << 23;   // of a launch, which has under 2^32 threads
 
 template <int DT, int D>
 static hipError_t launch_cache_d(bool write, CacheParams p, hipStream_t st) {
-  const int64_t row_threads = (int64_t)p.heads * (D / 8);
-  const int64_t most = CW_BLOCKS * CW_THREADS / row_threads;   // rows of a launch
+  // (a launch has under 2^32 threads)
+  const int64_t most = ((int64_t)1 << 22) / p.heads * CW_ROWS;
   const unsigned sides = write || (p.k_out != nullptr && p.v_out != nullptr) ? 2 : 1;
   const int64_t n = p.n;
   for (int64_t row = 0; row < n; row += most) {
     p.n = n - row < most ? n - row : most;
-    const dim3 grid((unsigned)((p.n * row_threads + CW_THREADS - 1) / CW_THREADS), sides);
+    const dim3 grid((unsigned)((p.n + CW_ROWS - 1) / CW_ROWS), (unsigned)p.heads, sides);
     const hipError_t e =
         write ? launch_kernel(cache_write_kernel<DT, D>, grid, dim3(CW_THREADS), 0, st, p)
               : launch_kernel(cache_read_kernel<DT, D>, grid, dim3(CW_THREADS), 0, st, p);

@@ -65,7 +65,7 @@ __device__ __forceinline__ u32x4_t hr_pack(const float (&f)[hr_elems<DT>()]) {
 // a multiple of no chunk) the other element comes through LDS.
 enum : int { HR_PAIRED = 0, HR_NEIGHBOURS = 1, HR_ODD = 2 };
 
-template <int DT, int T, int MODE>
+template <int DT, int T, int MODE, bool STREAM>
 __global__ __launch_bounds__(HR_THREADS) void head_norm_rotary_kernel(RotaryParams p) {
   constexpr int E = hr_elems<DT>();
   constexpr int PAD = 16;                      // (read, not used, behind the last angle)
@@ -99,8 +99,8 @@ __global__ __launch_bounds__(HR_THREADS) void head_norm_rotary_kernel(RotaryPara
     const char* x = (w.is_k ? p.k.x + w.row * p.k.stride : p.q.x + w.row * p.q.stride) +
                     (int64_t)w.h * p.head_bytes;
     a = b = u32x4_t{0, 0, 0, 0};
-    if (live_a) a = ld16(x + ca * 16);
-    if (live_b) b = ld16(x + cb * 16);
+    if (live_a) a = STREAM ? ld16_nt(x + ca * 16) : ld16(x + ca * 16);
+    if (live_b) b = STREAM ? ld16_nt(x + cb * 16) : ld16(x + cb * 16);
   };
   u32x4_t na, nb;
   if (team < tasks) load(team, na, nb);        // (on its way during the angles)
@@ -229,15 +229,30 @@ static hipError_t launch_rotary_mode(RotaryParams p, hipStream_t st) {
   p.span = teams;
   if (p.n * ((heads + teams - 1) / teams) > 2048) {
     p.span = heads;
-    p.tokens = half4 > HR_ANGLES / 8 ? HR_ANGLES / half4 : 8;
+    const int64_t most = half4 > HR_ANGLES / 8 ? HR_ANGLES / half4 : 8, spread = p.n / 2048;
+    p.tokens = (int)(spread < 1 ? 1 : spread < most ? spread : most);
   }
   const dim3 grid((unsigned)((p.n + p.tokens - 1) / p.tokens),
                   (unsigned)((heads + p.span - 1) / p.span));
   const dim3 block(HR_THREADS);
-  if (T == 4) return launch_kernel(head_norm_rotary_kernel<DT, 4, MODE>, grid, block, 0, st, p);
-  if (T == 8) return launch_kernel(head_norm_rotary_kernel<DT, 8, MODE>, grid, block, 0, st, p);
-  if (T == 16) return launch_kernel(head_norm_rotary_kernel<DT, 16, MODE>, grid, block, 0, st, p);
-  return launch_kernel(head_norm_rotary_kernel<DT, 32, MODE>, grid, block, 0, st, p);
+  // rows that the caches cannot have kept are read past them (84 MB 40 -> 34 us; 31 MB, which
+  // they have, 10 -> 14)
+  if (p.n * heads * p.head_bytes >= (int64_t)1 << 26) {
+    if (T == 4)
+      return launch_kernel(head_norm_rotary_kernel<DT, 4, MODE, true>, grid, block, 0, st, p);
+    if (T == 8)
+      return launch_kernel(head_norm_rotary_kernel<DT, 8, MODE, true>, grid, block, 0, st, p);
+    if (T == 16)
+      return launch_kernel(head_norm_rotary_kernel<DT, 16, MODE, true>, grid, block, 0, st, p);
+    return launch_kernel(head_norm_rotary_kernel<DT, 32, MODE, true>, grid, block, 0, st, p);
+  }
+  if (T == 4)
+    return launch_kernel(head_norm_rotary_kernel<DT, 4, MODE, false>, grid, block, 0, st, p);
+  if (T == 8)
+    return launch_kernel(head_norm_rotary_kernel<DT, 8, MODE, false>, grid, block, 0, st, p);
+  if (T == 16)
+    return launch_kernel(head_norm_rotary_kernel<DT, 16, MODE, false>, grid, block, 0, st, p);
+  return launch_kernel(head_norm_rotary_kernel<DT, 32, MODE, false>, grid, block, 0, st, p);
 }
 
 template <int DT>

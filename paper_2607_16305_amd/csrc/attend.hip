@@ -915,10 +915,11 @@ void attend_many_kernel(AttendParams p) {
   at_store<DT, D, RT, BR>(p, k, row0, rows, refs);
 }
 
-// Joins the parts of a row's keys: W waves a row and query head.
+// Joins the parts of a row's keys: W waves a row and query head, 64 parts at a time
+// whose weights the lanes compute side by side.
 template <int DT, int D, int BR, int W>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
-  constexpr int E = D / 64, AHEAD = 4;     // values of a lane, parts on their way
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void attend_join_kernel(AttendParams p) {
+  constexpr int E = D / 64, AHEAD = 8;     // values of a lane, parts on their way
   typedef float fe_t __attribute__((ext_vector_type(E)));
   __shared__ fe_t accs[W][64];
   __shared__ float ms[W], ls[W];
@@ -957,22 +958,42 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p) {
   const fe_t* outs = reinterpret_cast<const fe_t*>(p.part) + lane;
   float m = -INFINITY, sum = 0.f;
   fe_t acc = {};
-  for (int x0 = wave % W; x0 < splits; x0 += W * AHEAD) {
+  const int mine = W == 1 ? splits : (splits - wave + W - 1) / W;   // parts wave, wave + W, ..
+  auto part_of = [&](int i) { return first + (int64_t)(W == 1 ? i : wave + i * W) * step; };
+  for (int i0 = 0; i0 < mine; i0 += 64) {
+    const int n = mine - i0 < 64 ? mine - i0 : 64;
+    f32x2_t ml = {-INFINITY, 0.f};
+    if (lane < n) ml = sums[part_of(i0 + lane)];
     fe_t v[AHEAD];
-    f32x2_t ml[AHEAD];
+    auto load = [&](int i) {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int x = x0 + i * W < splits ? x0 + i * W : x0;
-      ml[i] = sums[first + x * step];
-      v[i] = outs[(first + x * step) * 64];
+      for (int x = 0; x < AHEAD; ++x)
+        if (i + x < n) v[x] = outs[part_of(i0 + i + x) * 64];
+    };
+    load(0);
+    auto of_lane = [](float y, int l) { return as_f32(__builtin_amdgcn_readlane(as_u32(y), l)); };
+    float most = ml[0];
+    if (n <= AHEAD) {
+#pragma unroll
+      for (int x = 0; x < AHEAD; ++x) most = fmaxf(x == 0 ? m : most, of_lane(ml[0], x));
+    } else {
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+      most = fmaxf(most, m);
     }
+    const float f = at_weight(m, most), w = at_weight(ml[0], most);
+    m = most;
+    sum *= f;
+    acc *= f;
+    for (int i = 0; i < n; i += AHEAD) {
+      if (i > 0) load(i);
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      if (x0 + i * W >= splits) break;
-      const float most = fmaxf(m, ml[i][0]), a = at_weight(m, most), c = at_weight(ml[i][0], most);
-      m = most;
-      sum = sum * a + ml[i][1] * c;
-      acc = acc * a + v[i] * c;
+      for (int x = 0; x < AHEAD; ++x) {
+        if (i + x >= n) break;
+        const float g = of_lane(w, i + x);
+        sum = fmaf(of_lane(ml[1], i + x), g, sum);
+        acc += v[x] * g;
+      }
     }
   }
   if constexpr (W > 1) {
@@ -1048,12 +1069,19 @@ static hipError_t launch_attend_d(AttendParams p, hipStream_t st) {
       a.rows ? launch_kernel(attend_many_kernel<DT, D>, grid, dim3(64 * AM_WAVES), 0, st, p)
              : launch_kernel(attend_few_kernel<DT, D>, grid, dim3(64 * AF_WAVES), 0, st, p);
   if (e != hipSuccess || a.target == 0) return e;
-  // a wave a row where that fills the chip, else a workgroup
+  // a wave a row where that fills the chip, else as many as do
   const int64_t rows = (int64_t)p.n * p.q_heads;
   constexpr int BLOCK = 16 * AM_WAVES * am_row_tiles<DT, D>();
   const dim3 each((unsigned)rows), four((unsigned)((rows + 3) / 4));
   if (a.rows) return launch_kernel(attend_join_kernel<DT, D, BLOCK, 1>, four, dim3(256), 0, st, p);
-  if (rows >= 4096) return launch_kernel(attend_join_kernel<DT, D, 16, 1>, four, dim3(256), 0, st, p);
+  if (rows >= 4096)
+    return launch_kernel(attend_join_kernel<DT, D, 16, 1>, four, dim3(256), 0, st, p);
+  // (42 rows with up to 250 parts each took 25 us with four waves a row, 6 with
+  // sixteen; 16 rows of 16 parts 4.4 and 5.4)
+  const int64_t even = a.target / ((int64_t)p.batch * p.kv_heads),
+                held = ((int64_t)p.max_pages << p.page_log2) / (C4_TILE * AT_MIN_TILES);
+  if (rows < 512 && even > 32 && held > 32)
+    return launch_kernel(attend_join_kernel<DT, D, 16, 16>, each, dim3(1024), 0, st, p);
   return launch_kernel(attend_join_kernel<DT, D, 16, 4>, each, dim3(256), 0, st, p);
 }
 

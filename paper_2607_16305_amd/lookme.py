@@ -719,18 +719,21 @@ def quant_swiglu(x, w_gate, s_gate, w_up, s_up, out, z_gate=None, z_up=None, str
           p_out)
 
 
-def _heads(name, t, dtype, n, heads, d, device):
-    """(address, stride of a row) of t [n, heads, d], whose rows may lie apart"""
-    if t.dtype is not dtype or t.shape != (n, heads, d) or t.get_device() != device:
-        _wrong(name, t, dtype, (n, heads, d), device)
+def _heads(name, t, dtype, shape, device):
+    """(address, stride of a row) of t of the shape (n, heads, d), whose rows may lie
+    apart"""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        _wrong(name, t, dtype, shape, device)
+    n, heads, d = shape
+    if t.is_contiguous():
+        return t.data_ptr(), heads * d
     row, head, one = t.stride()
-    if n > 1:
-        if row < heads * d:
-            _refuse(f"the rows of {name} overlap (stride {row})")
-    else:
-        row = heads * d
-    if t.numel() and ((one != 1 and d > 1) or (head != d and heads > 1)):
+    if (one != 1 and d > 1) or (head != d and heads > 1):
         _refuse(f"the heads of {name} do not lie side by side (strides {t.stride()})")
+    if n < 2:
+        row = heads * d
+    elif row < heads * d:
+        _refuse(f"the rows of {name} overlap (stride {row})")
     return t.data_ptr(), row
 
 
@@ -745,20 +748,24 @@ def head_norm_rotary(q, q_out, k=None, k_out=None, norm=True, q_weight=None, k_w
     code = _dtype_code("q", dt)
     if q.dim() != 3:
         _refuse(f"q has {q.dim()} dimensions, not 3")
-    n, q_heads, d = q.shape
+    shape = q.shape
+    n, q_heads, d = shape
     if d >= INT32 or q_heads >= INT32:
         _int32(d, q_heads)
-    p_q, q_row = _heads("q", q, dt, n, q_heads, d, dev)
-    p_qo, qo_row = _heads("q_out", q_out, dt, n, q_heads, d, dev)
+    p_q, q_row = _heads("q", q, dt, shape, dev)
+    p_qo, qo_row = _heads("q_out", q_out, dt, shape, dev)
     k_heads, p_k, k_row, p_ko, ko_row = 0, None, 0, None, 0
     if (k is None) != (k_out is None):
         _refuse("k and k_out go together")
     if k is not None:
-        k_heads = k.shape[1] if k.dim() == 3 else 0
+        shape = k.shape
+        k_heads = shape[1] if len(shape) == 3 else 0
         if k_heads >= INT32:
             _int32(k_heads)
-        p_k, k_row = _heads("k", k, dt, n, k_heads, d, dev)
-        p_ko, ko_row = _heads("k_out", k_out, dt, n, k_heads, d, dev)
+        if len(shape) != 3 or shape[0] != n or shape[2] != d:
+            _wrong("k", k, dt, (n, k_heads, d), dev)
+        p_k, k_row = _heads("k", k, dt, shape, dev)
+        p_ko, ko_row = _heads("k_out", k_out, dt, shape, dev)
     elif k_weight is not None:
         _refuse("k_weight given without k")
     p_qw = None if q_weight is None else _tensor("q_weight", q_weight, dt, (d,), dev)
@@ -768,11 +775,18 @@ def head_norm_rotary(q, q_out, k=None, k_out=None, norm=True, q_weight=None, k_w
         rot = 2 * freq.numel()
         if pos is None:
             _refuse("freq given without pos")
-        axes = pos.shape[0] if pos.dim() == 2 else 1
+        two = pos.dim() == 2
+        axes = pos.shape[0] if two else 1
         if rot >= INT32 or axes >= INT32:
             _int32(rot, axes)
-        p_freq = _tensor("freq", freq, torch.float32, (rot // 2,), dev)
-        p_pos = _tensor("pos", pos, torch.int32, (axes, n) if pos.dim() == 2 else (n,), dev)
+        if (freq.dtype is not torch.float32 or freq.dim() != 1 or freq.get_device() != dev
+                or not freq.is_contiguous()):
+            _wrong("freq", freq, torch.float32, (rot // 2,), dev)
+        p_freq = freq.data_ptr()
+        if (pos.dtype is not torch.int32 or pos.shape != ((axes, n) if two else (n,))
+                or pos.get_device() != dev or not pos.is_contiguous()):
+            _wrong("pos", pos, torch.int32, (axes, n) if two else (n,), dev)
+        p_pos = pos.data_ptr()
         if axis is not None:
             p_axis = _tensor("axis", axis, torch.int32, (rot // 2,), dev)
         elif axes > 1:
@@ -810,9 +824,12 @@ def cache_write(k, v, slots, cache, stream=None):
     dev, dt = k.get_device(), k.dtype
     code = _dtype_code("k", dt)
     pages, heads, page, d, p_c = _cache(cache, dev)
-    n = k.shape[0] if k.dim() == 3 else 0
-    p_k, k_row = _heads("k", k, dt, n, heads, d, dev)
-    p_v, v_row = _heads("v", v, dt, n, heads, d, dev)
+    shape = k.shape
+    n = shape[0] if len(shape) == 3 else 0
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d:
+        _wrong("k", k, dt, (n, heads, d), dev)
+    p_k, k_row = _heads("k", k, dt, shape, dev)
+    p_v, v_row = _heads("v", v, dt, shape, dev)
     p_s = _tensor("slots", slots, torch.int32, (n,), dev)
     _call("lookme_cache_write", dev, stream, code, n, heads, d, p_k, k_row, p_v, v_row, p_s, pages,
           page, p_c)
@@ -829,8 +846,9 @@ def cache_read(slots, cache, k_out=None, v_out=None, stream=None):
     code = _dtype_code("the output", dt)
     pages, heads, page, d, p_c = _cache(cache, dev)
     p_s = _tensor("slots", slots, torch.int32, (n,), dev)
-    p_k, k_row = (None, 0) if k_out is None else _heads("k_out", k_out, dt, n, heads, d, dev)
-    p_v, v_row = (None, 0) if v_out is None else _heads("v_out", v_out, dt, n, heads, d, dev)
+    shape = (n, heads, d)
+    p_k, k_row = (None, 0) if k_out is None else _heads("k_out", k_out, dt, shape, dev)
+    p_v, v_row = (None, 0) if v_out is None else _heads("v_out", v_out, dt, shape, dev)
     _call("lookme_cache_read", dev, stream, code, n, heads, d, p_s, pages, page, p_c, p_k, k_row,
           p_v, v_row)
 
@@ -844,18 +862,24 @@ def cache_attention(q, cache, pages, lengths, out, workspace=None, q_offsets=Non
     what lookme_cache_attention_workspace gives for one)."""
     dev, dt, i32 = q.get_device(), q.dtype, torch.int32
     code = _dtype_code("q", dt)
-    if q.dim() != 3 or pages.dim() != 2:
+    shape, p_shape = q.shape, pages.shape
+    if len(shape) != 3 or len(p_shape) != 2:
         _refuse("q has 3 dimensions, pages has 2")
-    n, q_heads, _ = q.shape
+    n, q_heads, _ = shape
     num_pages, kv_heads, page, d, p_c = _cache(cache, dev)
-    batch, max_pages = pages.shape
+    batch, max_pages = p_shape
     if batch >= INT32 or max_pages >= INT32 or q_heads >= INT32:
         _int32(batch, max_pages, q_heads)
-    p_q, q_row = _heads("q", q, dt, n, q_heads, d, dev)
-    p_o, o_row = _heads("out", out, dt, n, q_heads, d, dev)
-    if (pages.dtype is not i32 or pages.get_device() != dev or not pages.is_contiguous()):
-        _wrong("pages", pages, i32, pages.shape, dev)
-    p_l = _tensor("lengths", lengths, i32, (batch,), dev)
+    if shape[2] != d:
+        _wrong("q", q, dt, (n, q_heads, d), dev)
+    p_q, q_row = _heads("q", q, dt, shape, dev)
+    p_o, o_row = _heads("out", out, dt, shape, dev)
+    if pages.dtype is not i32 or pages.get_device() != dev or not pages.is_contiguous():
+        _wrong("pages", pages, i32, p_shape, dev)
+    if (lengths.dtype is not i32 or lengths.shape != (batch,) or lengths.get_device() != dev
+            or not lengths.is_contiguous()):
+        _wrong("lengths", lengths, i32, (batch,), dev)
+    p_l = lengths.data_ptr()
     p_off = None if q_offsets is None else _tensor("q_offsets", q_offsets, i32, (batch + 1,), dev)
     p_w, w_bytes = None, 0
     if workspace is not None:

@@ -783,7 +783,7 @@ lookme_status_t lookme_cache_read(int32_t dtype, int64_t n, int32_t kv_heads, in
  *              where that is 0).  Nothing is kept in it between calls, but calls that
  *              may overlap on the GPU need one each.
  * float32 scores and sums; k and v are exact.  bf16: p is rounded to bf16 before
- * it multiplies v.  q_heads a multiple of kv_heads, n * q_heads at most 2^29,
+ * it multiplies v.  q_heads a multiple of kv_heads, n * q_heads at most 2^27,
  * batch * kv_heads at most 2^22, max_pages * page at most 2^30.  n = 0 does nothing.
  */
 lookme_status_t lookme_cache_attention(int32_t dtype, int64_t n, int32_t batch, int32_t q_heads,

@@ -84,12 +84,19 @@ __device__ __forceinline__ bool at_unit(const AttendParams& p, int64_t unit, Att
   if (lane < p.batch) s = at_seq(p, lane);
   int chunk = 0x7FFFFFFF;     // tiles of a part
   if (p.target > 0) {
-    float work = (float)blocks_of(s) * (float)((s.len + C4_TILE - 1) / C4_TILE);
-    for (int b = lane + 64; b < p.batch; b += 64) {
-      const AttendSeq o = at_seq(p, b);
-      work += (float)blocks_of(o) * (float)((o.len + C4_TILE - 1) / C4_TILE);
+    float work = 0.f, blocks = 0.f;
+    AttendSeq o = s;
+    for (int b = lane; b < p.batch; b += 64) {
+      if (b > lane) o = at_seq(p, b);
+      const float n = (float)blocks_of(o);
+      blocks += n;
+      work += n * (float)((o.len + C4_TILE - 1) / C4_TILE);
     }
-    const float c = ceilf(wave_sum(work) / (float)p.target);
+    // Parts are rounded up, half a part a block: of units of 32 to 64 rows, which are long
+    // in their beginning and end, none is to be left for a second round (15 x 40 rows over
+    // 6700 tokens 43 -> 35 us; units of 16 rows even out better without: 276 and 300)
+    const float room = BR > 16 && BR < 128 ? fminf(0.5f * wave_sum(blocks), 0.5f * p.target) : 0.f;
+    const float c = ceilf(wave_sum(work) / ((float)p.target - room));
     chunk = c < (float)AT_MIN_TILES ? AT_MIN_TILES : c > 1e9f ? 1000000000 : (int)c;
   } else {
     // without a cut the blocks of rows of one key head read the same keys: a
@@ -586,10 +593,14 @@ __device__ __forceinline__ u32x4_t at_k_operand(uint32_t k, float scale) {
 }
 
 // ---------------------------------------------------------------------------
-// few rows a key head (a decode step): 16 a unit, its waves along the tokens
+// few rows a key head (a decode step, some tokens more): RT tiles of 16 a unit, its waves
+// along the tokens
 // ---------------------------------------------------------------------------
 constexpr int AF_WAVES = 4;
-constexpr int af_occupancy(int dt, int d) {
+// Waves a SIMD, as the registers allow (rt: tiles of 16 rows a unit)
+constexpr int af_occupancy(int dt, int d, int rt) {
+  if (rt > 2) return d == 64 || rt == 3 ? 2 : 1;
+  if (rt == 2) return d == 64 && dt == DT_BF16 ? 3 : d == 256 || dt == DT_F32 ? 1 : 2;
   return d == 64 ? 4 : d == 128 ? 3 : dt == DT_BF16 ? 2 : 1;
 }
 // tiles of a wave's ring in LDS, one of them being multiplied
@@ -609,12 +620,12 @@ __device__ __forceinline__ void at_issue(const uint8_t* tile, char* dst) {
   if (lane < REST) load_lds16_nt(tile + FULL * 1024 + lane * 16, dst + FULL * 1024);
 }
 
-template <int DT, int D>
-__global__ __launch_bounds__(64 * AF_WAVES, af_occupancy(DT, D))
+template <int DT, int D, int RT>
+__global__ __launch_bounds__(64 * AF_WAVES, af_occupancy(DT, D, RT))
 void attend_few_kernel(AttendParams p) {
-  constexpr int U = D / 16, M = D / 32, BR = 16, TERMS = at_terms<DT>();
+  constexpr int U = D / 16, M = D / 32, BR = 16 * RT, TERMS = at_terms<DT>();
   constexpr int NB = af_ring(D), TILE = 34 * D;
-  constexpr int RING = AF_WAVES * NB * TILE, JOIN = AF_WAVES / 2 * AttendRows<D, 1>::LEFT;
+  constexpr int RING = AF_WAVES * NB * TILE, JOIN = AF_WAVES / 2 * AttendRows<D, RT>::LEFT;
   // the waves' rings of tiles, then what they join
   __shared__ __attribute__((aligned(1024))) char smem[RING > JOIN ? RING : JOIN];
   const int lane = threadIdx.x & 63, j = lane & 15;
@@ -622,9 +633,13 @@ void attend_few_kernel(AttendParams p) {
   AttendBlock k;
   if (!at_block<D, BR>(p, &k)) return;
   const int row0 = k.blk * BR;
-  AttendRows<D, 1> rows;
+  AttendRows<D, RT> rows;
   rows.clear();
-  rows.last[0] = row0 + j < k.R ? at_last(p, k, row0 + j) : -1;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = row0 + rt * 16 + j;
+    rows.last[rt] = r < k.R ? at_last(p, k, r) : -1;
+  }
   const int full = at_last(p, k, row0);      // every row sees the tokens up to here
   const float scl = p.scale_log2, slack = AT_SLACK / scl;
   const AttendPages<D> pages(p, k);
@@ -646,8 +661,8 @@ void attend_few_kernel(AttendParams p) {
     bad >>= 1;
     if (t + i * AF_WAVES < k.end) issue(t + i * AF_WAVES, i);
   }
-  u32x4_t q[1][M][TERMS];
-  at_queries<DT, D, 1>(p, k, row0, q);
+  u32x4_t q[RT][M][TERMS];
+  at_queries<DT, D, RT>(p, k, row0, q);
   for (; t < k.end; t += AF_WAVES) {
     bad >>= 1;
     if (t + (NB - 1) * AF_WAVES < k.end) {
@@ -661,16 +676,19 @@ void attend_few_kernel(AttendParams p) {
       AttendTile<D> cur;
       at_load(cur, tile);
       const int t0 = t * C4_TILE;
-      f32x4_t s[1][2];
+      f32x4_t s[RT][2];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        s[0][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) s[rt][half] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int m = 0; m < M; ++m) {
           const u32x4_t kv = at_k_operand(cur.k[half][m], at_scale(cur.ks[half][m / 4], m % 4));
 #pragma unroll
-          for (int x = TERMS - 1; x >= 0; --x)
-            s[0][half] = mfma_chunk<DT_BF16>(kv, q[0][m][x], s[0][half]);
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int x = TERMS - 1; x >= 0; --x)
+              s[rt][half] = mfma_chunk<DT_BF16>(kv, q[rt][m][x], s[rt][half]);
         }
       }
       const bool hole = __any(at_hole(cur.vs));
@@ -680,7 +698,7 @@ void attend_few_kernel(AttendParams p) {
         at_fill_holes<D>(cur.v, cur.vs, t0, k.u.seq.len);
       }
       rows.renew(s, scl, slack);
-      u32x4_t w[1][TERMS];
+      u32x4_t w[RT][TERMS];
       rows.template weights<DT>(s, scl, w);
       rows.add_ones(w);
 #pragma unroll
@@ -695,17 +713,19 @@ void attend_few_kernel(AttendParams p) {
     asm volatile("" ::: "memory");
   }
 
-  float refs[1] = {rows.ref(0)};
+  float refs[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) refs[rt] = rows.ref(rt);
   __syncthreads();   // the rings are free for the join
 #pragma unroll
   for (int step = AF_WAVES / 2; step > 0; step >>= 1) {
-    char* left = smem + (wave & (step - 1)) * AttendRows<D, 1>::LEFT;
+    char* left = smem + (wave & (step - 1)) * AttendRows<D, RT>::LEFT;
     if (wave >= step && wave < 2 * step) rows.leave(left, refs);
     __syncthreads();
     if (wave < step) rows.join(left, refs);
     if (step > 1) __syncthreads();
   }
-  if (wave == 0) at_store<DT, D, 1, BR>(p, k, row0, rows, refs);
+  if (wave == 0) at_store<DT, D, RT, BR>(p, k, row0, rows, refs);
 }
 
 // ---------------------------------------------------------------------------
@@ -714,24 +734,22 @@ void attend_few_kernel(AttendParams p) {
 // each wave, and read as matrix operands from LDS
 // ---------------------------------------------------------------------------
 constexpr int AM_WAVES = 4;
-template <int DT, int D>
-constexpr int am_row_tiles() {
-  return DT == DT_BF16 ? 2 : D == 256 ? 1 : D == 128 ? 2 : 3;
-}
-constexpr int am_occupancy(int d) { return d == 256 ? 1 : 2; }
+// As many row tiles as leave two waves a SIMD (bf16, 256 dims, 2 x 3954 rows over 9178
+// tokens x 4 heads: one 382 us, two and one wave 519; float32, 128 dims: one 185, two 201)
+constexpr int am_row_tiles(int dt, int d) { return dt == DT_BF16 && d == 128 ? 2 : 1; }
 
-// A wave's share of a tile: D / 64 of the D / 16 operands of k, and of the D / 32 pairs of
-// operands of v D / 128 (d = 64: k by the last two waves, v by the first two)
+// A wave's share of a tile of 128 or 256 dims: D / 64 of the D / 16 operands of k, D / 128
+// of the D / 32 pairs of operands of v
 template <int D>
 struct AttendShare {
   static constexpr int M = D / 32, U = D / 16;
-  static constexpr int KN = D == 64 ? 2 : D / 64, VN = D == 64 ? 1 : D / 128;
+  static constexpr int KN = D / 64, VN = D / 128;
   uint32_t k[KN], ks, v[U];
   uint32_t at_k, at_ks, at_v, at_vs;   // of the lane's bytes in a tile
   uint32_t ks_shift;                   // of its scales of k in their word
   __device__ __forceinline__ AttendShare(int wave) {
     const uint32_t lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
-    const uint32_t half = D == 64 ? wave & 1 : wave >> 1, m0 = D == 64 ? 0 : (wave & 1) * KN;
+    const uint32_t half = wave >> 1, m0 = (wave & 1) * KN;
     at_k = (16 * half + j) * (D / 2) + c * (D / 8) + 4 * m0;
     at_ks = 32 * D + (16 * half + j) * M + m0;
     ks_shift = at_ks % 4 * 8;
@@ -749,15 +767,12 @@ struct AttendShare {
   }
   // operands at lds + n 1024
   __device__ __forceinline__ void unpack_k(char* lds, int wave) const {
-    if (D == 64 && wave < 2) return;
-    const int n0 = D == 64 ? (wave & 1) * M : wave * KN;
     char* to = lds + (threadIdx.x & 63) * 16;
 #pragma unroll
     for (int n = 0; n < KN; ++n)
-      st16(to + (n0 + n) * 1024, at_k_operand(k[n], at_scale(ks >> ks_shift, n)));
+      st16(to + (wave * KN + n) * 1024, at_k_operand(k[n], at_scale(ks >> ks_shift, n)));
   }
   __device__ __forceinline__ void unpack_v(char* lds, int wave, const uint32_t (&vs)[2]) const {
-    if (D == 64 && wave >= 2) return;
     char* to = lds + (threadIdx.x & 63) * 16;
 #pragma unroll
     for (int n = 0; n < VN; ++n) {
@@ -766,8 +781,7 @@ struct AttendShare {
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
         uint32_t word;
-        if constexpr (U == 4) word = v[x / 2] >> (16 * (x % 2));
-        else if constexpr (U == 8) word = v[x];
+        if constexpr (U == 8) word = v[x];
         else word = b < 4 ? v[2 * x] : v[2 * x + 1];
         pair[x] = c4_pair(word >> (8 * (b & 3)), at_scale(vs[x / 4], x % 4), 0);
       }
@@ -784,9 +798,9 @@ struct AttendShare {
 };
 
 template <int DT, int D>
-__global__ __launch_bounds__(64 * AM_WAVES, am_occupancy(D))
+__global__ __launch_bounds__(64 * AM_WAVES, 2)
 void attend_many_kernel(AttendParams p) {
-  constexpr int U = D / 16, M = D / 32, TERMS = at_terms<DT>(), RT = am_row_tiles<DT, D>();
+  constexpr int U = D / 16, M = D / 32, TERMS = at_terms<DT>(), RT = am_row_tiles(DT, D);
   constexpr int BR = 16 * RT * AM_WAVES, STAGE = 4 * M * 1024;
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
   const int lane = threadIdx.x & 63, j = lane & 15;
@@ -1027,29 +1041,53 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void attend_join_kernel(Atte
 // launch
 // ---------------------------------------------------------------------------
 struct AttendPlan {
-  bool rows;        // many rows a sequence: the waves of a workgroup share the keys
+  int tiles;        // row tiles of a unit of few rows; 0: many, the waves share the keys
   int block;        // rows of a unit
   int target;       // units that the cut aims at; 0: no cut
   int64_t units;    // workgroups
 };
 
-template <int DT>
-static int many_block(int d) {
-  return 16 * AM_WAVES * (d == 64 ? am_row_tiles<DT, 64>()
-                                  : d == 128 ? am_row_tiles<DT, 128>() : am_row_tiles<DT, 256>());
+static int many_block(int dt, int d) {
+  return 16 * AM_WAVES * am_row_tiles(dt, d);
 }
 
+// Row tiles of a unit of attend_few_kernel for `rows` rows of a sequence and key head; 0:
+// attend_many_kernel.  A few-rows unit unpacks a tile of the cache once for its 16 to 64
+// rows, without a barrier; a many-rows unit once for 64 or 128, through LDS.  More row
+// tiles are better as long as the registers hold them (bf16 and 64 dims 4, 128 dims 3,
+// 256 dims 2; float32 2, 256 dims 1), and padded rows cost what rows cost.  Both sides
+// (us, 16 sequences x 8192 tokens x 4 heads of 128): 32 rows 33 and 55, 48 rows 36 and
+// 57, 80 rows 50 and 62, 128 rows 82 and 70; 16 x 8 heads of 256 over 4096 tokens: 36 rows
+// 68 and 83, 100 rows 126 and 107; float32, 128 dims: 36 rows 62 and 67, 2048 rows 404
+// and 337; 256 dims: 36 rows 123 and 129, 1024 rows 455 and 456.  64 dims have no
+// many-rows kernel: 2048 rows took it 127 us, this one 102 (float32 219 and 204).  Of 3 and
+// 4 tiles of 64 dims the rows of 4 cost 13 / 16 of the time.
+static int few_tiles(int dt, int d, int rows) {
+  if (rows <= 16 || (dt == DT_F32 && d == 256)) return 1;
+  if (rows <= 32 || (dt == DT_F32 && d == 64)) return 2;
+  if (d == 64) return (rows + 47) / 48 * 13 < (rows + 63) / 64 * 16 ? 3 : 4;
+  if (dt == DT_F32 || d == 256) return rows <= 64 ? 2 : 0;
+  return rows <= 96 ? 3 : 0;
+}
+
+// The keys are cut where that saves more than it costs.  It saves about a microsecond and
+// a half of a tile's turn, as far as the blocks of rows leave workgroups free; it costs a
+// launch, and each row's parts written and read again.  (500 rows of 500 tokens: 20 us
+// whole, 24 cut; 64 rows of 1024 tokens 12 and 17; a row of 2048 tokens 16 and 10; 11
+// sequences of up to 32000 tokens x 64 heads 340 and 282.)
 static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
                               int64_t tokens) {
-  const int G = q_heads / kv_heads;
+  const int64_t rows = n * (q_heads / kv_heads), each = (rows + batch - 1) / batch;
   AttendPlan a{};
-  a.rows = n * G > (int64_t)16 * batch;
-  a.block = !a.rows ? 16 : dt == DT_BF16 ? many_block<DT_BF16>(d) : many_block<DT_F32>(d);
-  const int64_t whole = (n * G / a.block + batch) * kv_heads;
+  a.tiles = few_tiles(dt, d, (int)(each < 65536 ? each : 65536));
+  a.block = a.tiles > 0 ? 16 * a.tiles : many_block(dt, d);
   // (one round of resident workgroups; 512 of 128 rows and 128 dims are 68 MB)
-  a.target = a.rows ? (d == 64 ? 512 : d == 128 ? 480 : 240) : d == 64 ? 1024 : d == 128 ? 768 : dt == DT_BF16 ? 512 : 256;
-  if (whole >= a.target || tokens <= AT_MIN_TILES * C4_TILE) a.target = 0;
-  a.units = whole + (a.target > 0 ? a.target + 64 : 0);
+  a.target = a.tiles > 0 ? 256 * af_occupancy(dt, d, a.tiles) : d == 128 ? 480 : 448;
+  const double turns = (double)((tokens + C4_TILE - 1) / C4_TILE) *
+                       (a.tiles > 0 ? 0.18 * (1 + a.tiles) / AF_WAVES : 0.5);
+  const double blocks = (double)((each + a.block - 1) / a.block) * batch * kv_heads;
+  if ((1.0 - blocks / a.target) * turns <= 4.0 + (double)n * q_heads * d * 16 / 2.5e6) a.target = 0;
+  a.units = (rows / a.block + batch) * kv_heads + (a.target > 0 ? a.target + 64 : 0);
   return a;
 }
 
@@ -1059,30 +1097,48 @@ size_t attend_workspace(int dt, int64_t n, int batch, int q_heads, int kv_heads,
   return a.target == 0 ? 0 : (size_t)2 * a.target * a.block * (d + 2) * 4 + (size_t)batch * 8;
 }
 
+template <int DT, int D, int RT>
+static hipError_t launch_few(const AttendPlan& a, const AttendParams& p, dim3 grid, hipStream_t st) {
+  const hipError_t e = launch_kernel(attend_few_kernel<DT, D, RT>, grid, dim3(64 * AF_WAVES), 0,
+                                     st, p);
+  if (e != hipSuccess || a.target == 0) return e;
+  // a wave a row where that fills the chip, else as many as do
+  const int64_t rows = (int64_t)p.n * p.q_heads;
+  const dim3 each((unsigned)rows), four((unsigned)((rows + 3) / 4));
+  if (rows >= 2048)
+    return launch_kernel(attend_join_kernel<DT, D, 16 * RT, 1>, four, dim3(256), 0, st, p);
+  // (42 rows with up to 250 parts each took 25 us with four waves a row, 6 with
+  // sixteen; 16 rows of 16 parts 4.4 and 5.4)
+  const int64_t even = a.target / ((int64_t)p.batch * p.kv_heads),
+                held = ((int64_t)p.max_pages << p.page_log2) / (C4_TILE * AT_MIN_TILES);
+  if (rows < 512 && even > 32 && held > 32)
+    return launch_kernel(attend_join_kernel<DT, D, 16 * RT, 16>, each, dim3(1024), 0, st, p);
+  return launch_kernel(attend_join_kernel<DT, D, 16 * RT, 4>, each, dim3(256), 0, st, p);
+}
+
 template <int DT, int D>
 static hipError_t launch_attend_d(AttendParams p, hipStream_t st) {
   const AttendPlan a = attend_plan(DT, p.n, p.batch, p.q_heads, p.kv_heads, D,
                                    (int64_t)p.max_pages << p.page_log2);
   p.target = a.target;
   const dim3 grid((unsigned)((a.units + 7) / 8 * 8));
-  const hipError_t e =
-      a.rows ? launch_kernel(attend_many_kernel<DT, D>, grid, dim3(64 * AM_WAVES), 0, st, p)
-             : launch_kernel(attend_few_kernel<DT, D>, grid, dim3(64 * AF_WAVES), 0, st, p);
-  if (e != hipSuccess || a.target == 0) return e;
-  // a wave a row where that fills the chip, else as many as do
-  const int64_t rows = (int64_t)p.n * p.q_heads;
-  constexpr int BLOCK = 16 * AM_WAVES * am_row_tiles<DT, D>();
-  const dim3 each((unsigned)rows), four((unsigned)((rows + 3) / 4));
-  if (a.rows) return launch_kernel(attend_join_kernel<DT, D, BLOCK, 1>, four, dim3(256), 0, st, p);
-  if (rows >= 4096)
-    return launch_kernel(attend_join_kernel<DT, D, 16, 1>, four, dim3(256), 0, st, p);
-  // (42 rows with up to 250 parts each took 25 us with four waves a row, 6 with
-  // sixteen; 16 rows of 16 parts 4.4 and 5.4)
-  const int64_t even = a.target / ((int64_t)p.batch * p.kv_heads),
-                held = ((int64_t)p.max_pages << p.page_log2) / (C4_TILE * AT_MIN_TILES);
-  if (rows < 512 && even > 32 && held > 32)
-    return launch_kernel(attend_join_kernel<DT, D, 16, 16>, each, dim3(1024), 0, st, p);
-  return launch_kernel(attend_join_kernel<DT, D, 16, 4>, each, dim3(256), 0, st, p);
+  // (what few_tiles chooses, and nothing else, is built)
+  if (a.tiles == 1) return launch_few<DT, D, 1>(a, p, grid, st);
+  if constexpr (DT == DT_BF16 || D < 256)
+    if (a.tiles == 2) return launch_few<DT, D, 2>(a, p, grid, st);
+  if constexpr (DT == DT_BF16 && D < 256)
+    if (a.tiles == 3) return launch_few<DT, D, 3>(a, p, grid, st);
+  if constexpr (DT == DT_BF16 && D == 64)
+    if (a.tiles == 4) return launch_few<DT, D, 4>(a, p, grid, st);
+  if constexpr (D == 128 || (DT == DT_BF16 && D == 256)) {
+    const hipError_t e =
+        launch_kernel(attend_many_kernel<DT, D>, grid, dim3(64 * AM_WAVES), 0, st, p);
+    if (e != hipSuccess || a.target == 0) return e;
+    constexpr int BLOCK = 16 * AM_WAVES * am_row_tiles(DT, D);
+    const dim3 four((unsigned)(((int64_t)p.n * p.q_heads + 3) / 4));
+    return launch_kernel(attend_join_kernel<DT, D, BLOCK, 1>, four, dim3(256), 0, st, p);
+  }
+  return hipErrorInvalidValue;   // (few_tiles gives no 0 there)
 }
 
 hipError_t launch_attend(int dt, int d, AttendParams p, hipStream_t st) {

@@ -408,7 +408,6 @@ struct AttendParams {
   bool causal;
   float scale_log2;
   int target;                // work units that the cut of the keys aims at; 0: no cut
-  int units_most;            // workgroups of the launch
 };
 // Bytes of workspace of a call (0: none needed).
 size_t attend_workspace(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,

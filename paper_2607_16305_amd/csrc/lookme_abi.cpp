@@ -416,8 +416,8 @@ lookme_status_t check_attention(int32_t dtype, int64_t n, int32_t batch, int32_t
   if ((int64_t)max_pages * page > (int64_t)1 << 30)
     return fail(LOOKME_ERR_UNSUPPORTED, "%d pages of %d tokens a sequence exceed 2^30", max_pages,
                 page);
-  if (n * q_heads > (int64_t)1 << 29 || (int64_t)batch * kv_heads > (int64_t)1 << 22)
-    return fail(LOOKME_ERR_UNSUPPORTED, "%lld rows of %d heads exceed 2^29, or %d sequences of %d "
+  if (n * q_heads > (int64_t)1 << 27 || (int64_t)batch * kv_heads > (int64_t)1 << 22)
+    return fail(LOOKME_ERR_UNSUPPORTED, "%lld rows of %d heads exceed 2^27, or %d sequences of %d "
                 "key heads 2^22", (long long)n, q_heads, batch, kv_heads);
   return LOOKME_OK;
 }

@@ -92,7 +92,7 @@ ATTENTION = dict(dtype=BF, n=6, batch=2, q_heads=4, kv_heads=2, head_dim=128, q=
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(dtype=2), INVALID), (dict(n=-1), INVALID), (dict(n=2 ** 28), UNSUPPORTED),
+    (dict(dtype=2), INVALID), (dict(n=-1), INVALID), (dict(n=2 ** 25 + 1), UNSUPPORTED),
     (dict(batch=-1), INVALID), (dict(batch=2 ** 22), UNSUPPORTED), (dict(q_heads=0), INVALID),
     (dict(kv_heads=0), INVALID), (dict(q_heads=5, q_stride=640, out_stride=640), INVALID),
     (dict(head_dim=80), UNSUPPORTED), (dict(q_stride=504), INVALID),
@@ -103,8 +103,9 @@ ATTENTION = dict(dtype=BF, n=6, batch=2, q_heads=4, kv_heads=2, head_dim=128, q=
     (dict(scale=INF), INVALID), (dict(scale=NAN), INVALID), (dict(causal=2), INVALID),
     (dict(q=None), INVALID), (dict(q_offsets=None), INVALID), (dict(q_offsets=P + 4), INVALID),
     (dict(lengths=None), INVALID), (dict(pages=None), INVALID), (dict(cache=None), INVALID),
-    (dict(out=None), INVALID), (dict(workspace=None), WORKSPACE),
-    (dict(workspace_bytes=1024), WORKSPACE), (dict(workspace=P + 16), INVALID),
+    (dict(out=None), INVALID), (dict(max_pages=300, workspace=None), WORKSPACE),
+    (dict(max_pages=300, workspace_bytes=1024), WORKSPACE),
+    (dict(max_pages=300, workspace=P + 16), INVALID),
     (dict(n=0, q=None, q_offsets=P, out=None, workspace=None), OK),
     (dict(n=0, batch=0, q_offsets=None, lengths=None, pages=None, workspace=None), OK)])
 def test_cache_attention_refuses(kw, status):

@@ -267,6 +267,26 @@ def test_cache_attention(case, dtype, d, causal):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("wide", [False, True], ids=["whole", "cut"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("m", [5, 12, 23, 31, 45, 70])
+def test_cache_attention_of_every_count_of_rows(m, dtype, d, wide):
+    """10 to 140 rows a key head, the keys whole and (a table that could hold more) cut"""
+    seqs = [(m, 500), (m + 1, 190), (m - 4, 31), (m, m)]
+    cache, table, _, vals = _sequences(seqs, 2, d, 32)
+    if wide:
+        table = torch.cat([table, torch.full((4, 2000), -7, dtype=I32)], 1)
+    n = sum(r for r, _ in seqs)
+    need = lk.lookme_cache_attention_workspace(int(dtype == "bf16"), n, 4, 4, 2, d,
+                                               table.shape[1], 32)
+    assert need > 0 or not wide
+    q = torch.randn((n, 4, d), generator=_gen(m)).to(DT[dtype])
+    for causal in (True, False):
+        out = _run(q.cuda(), cache, table, seqs, causal)
+        _check(out, q, vals, seqs, causal, d ** -0.5)
+
+
 def test_rows_apart_in_place_and_without_offsets():
     seqs = [(1, 77), (1, 1200), (1, 0)]
     cache, table, _, vals = _sequences(seqs, 2, 128, 64)
@@ -302,7 +322,7 @@ def _with(cache, slots, rows, what, heads=None):
 
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("what", ["k", "v"])
-@pytest.mark.parametrize("m", [3, 60])
+@pytest.mark.parametrize("m", [3, 11, 20, 30, 60])
 def test_blocks_that_are_not_finite_reach_only_the_rows_that_see_them(what, m, d):
     n = 200
     seqs = [(m, n)]

@@ -599,8 +599,8 @@ __device__ __forceinline__ u32x4_t at_k_operand(uint32_t k, float scale) {
 constexpr int AF_WAVES = 4;
 // Waves a SIMD, as the registers allow (rt: tiles of 16 rows a unit)
 constexpr int af_occupancy(int dt, int d, int rt) {
-  if (rt > 2) return d == 64 || rt == 3 ? 2 : 1;
-  if (rt == 2) return d == 64 && dt == DT_BF16 ? 3 : d == 256 || dt == DT_F32 ? 1 : 2;
+  if (rt > 2) return 2;
+  if (rt == 2) return dt == DT_F32 ? (d == 64 ? 2 : 1) : d == 64 ? 3 : d == 128 ? 2 : 1;
   return d == 64 ? 4 : d == 128 ? 3 : dt == DT_BF16 ? 2 : 1;
 }
 // tiles of a wave's ring in LDS, one of them being multiplied

@@ -773,12 +773,13 @@ lookme_status_t lookme_cache_read(int32_t dtype, int64_t n, int32_t kv_heads, in
  *   n          rows of q and out, [n, q_heads, head_dim] with strides as above;
  *              out may be q, with the same stride
  *   q_offsets  [batch + 1] int32, ascending, in [0, n] (clamped); NULL: row b is
- *              sequence b's (n = batch).  Rows of no sequence are left as they were
+ *              sequence b's (n = batch).  Rows of no sequence are left as they were;
+ *              what rows of several sequences get is not specified
  *   lengths    [batch] int32: the sequences' tokens, clamped to [0, max_pages * page]
  *   pages      [batch, max_pages] int32: token t of sequence b is token t % page of
  *              page pages[b, t / page].  Pages behind a length are not read; a page
  *              outside [0, num_pages) leaves its tokens out
- *   scale      positive and finite
+ *   scale      positive, at most 2^127
  *   workspace  lookme_cache_attention_workspace bytes, 256-byte aligned (may be NULL
  *              where that is 0).  Nothing is kept in it between calls, but calls that
  *              may overlap on the GPU need one each.

@@ -101,8 +101,9 @@ __device__ __forceinline__ bool at_unit(const AttendParams& p, int64_t unit, Att
   } else {
     // without a cut the blocks of rows of one key head read the same keys: a
     // neighbourhood of units for each XCD, so that they meet in its L2
-    int all = blocks_of(s);
-    for (int b = lane + 64; b < p.batch; b += 64) all += blocks_of(at_seq(p, b));
+    int64_t mine = blocks_of(s);
+    for (int b = lane + 64; b < p.batch; b += 64) mine += blocks_of(at_seq(p, b));
+    const int all = (int)(mine < AT_UNITS_OF_SEQ ? mine : AT_UNITS_OF_SEQ);
     unit = __builtin_amdgcn_readfirstlane(xcd_remap((int)unit, wave_sum(all)));
     if (unit < 0) return false;
   }
@@ -641,7 +642,7 @@ void attend_few_kernel(AttendParams p) {
     rows.last[rt] = r < k.R ? at_last(p, k, r) : -1;
   }
   const int full = at_last(p, k, row0);      // every row sees the tokens up to here
-  const float scl = p.scale_log2, slack = AT_SLACK / scl;
+  const float scl = p.scale_log2, slack = fminf(AT_SLACK / scl, 1e38f);
   const AttendPages<D> pages(p, k);
 
   // The wave's own ring: NB - 1 tiles on their way while one is multiplied, no barrier,
@@ -816,7 +817,7 @@ void attend_many_kernel(AttendParams p) {
     rows.last[rt] = r < k.R ? at_last(p, k, r) : -1;
   }
   const int full = row0 < k.R ? at_last(p, k, row0) : -1;   // every row sees the tokens up to here
-  const float scl = p.scale_log2, slack = AT_SLACK / scl;
+  const float scl = p.scale_log2, slack = fminf(AT_SLACK / scl, 1e38f);
   const AttendPages<D> pages(p, k);
 
   // In one turn, of tile t: the scores of tile t + 1 (matrix cores) beside the weights of t
@@ -962,12 +963,15 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void attend_join_kernel(Atte
   }
   const int* cut = at_cuts<D, BR>(p) + 2 * b;
   const int part = cut[0], splits = cut[1];
-  if (splits <= 1) return;
+  if (splits <= 1 || splits > 2 * p.target) return;
   const int blocks = (s.rows * G + BR - 1) / BR;
   const int h = head / G, r = (row - s.q0) * G + head - h * G, blk = r / BR;
   const int64_t first = ((int64_t)part + (int64_t)h * splits * blocks + (blocks - 1 - blk)) * BR +
                         (r - blk * BR);
   const int64_t step = (int64_t)blocks * BR;
+  // (sequences that share rows can be more units than the launch has: then one may not
+  // have written where its parts are)
+  if (part < 0 || first + (splits - 1) * step >= (int64_t)2 * p.target * BR) return;
   const f32x2_t* sums = reinterpret_cast<const f32x2_t*>(at_sums<D, BR>(p));
   const fe_t* outs = reinterpret_cast<const fe_t*>(p.part) + lane;
   float m = -INFINITY, sum = 0.f;

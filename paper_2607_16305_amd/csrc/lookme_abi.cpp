@@ -1618,8 +1618,9 @@ lookme_status_t lookme_cache_attention(int32_t dtype, int64_t n, int32_t batch, 
   if (q_offsets == nullptr && n != batch)
     return fail(LOOKME_ERR_INVALID, "%lld rows for %d sequences without q_offsets", (long long)n,
                 batch);
-  if (!(scale > 0.f) || !(scale - scale == 0.f))
-    return fail(LOOKME_ERR_INVALID, "scale must be positive and finite");
+  const float scale_log2 = scale * 1.44269504088896340736f;
+  if (!(scale > 0.f) || !(scale_log2 - scale_log2 == 0.f))
+    return fail(LOOKME_ERR_INVALID, "scale must be positive and at most 2^127");
   if (causal != 0 && causal != 1) return fail(LOOKME_ERR_INVALID, "causal must be 0 or 1");
   if (n == 0 || batch == 0) return LOOKME_OK;
   LOOKME_TRY(check_ptr(q, "q"));
@@ -1657,7 +1658,7 @@ lookme_status_t lookme_cache_attention(int32_t dtype, int64_t n, int32_t batch, 
   p.num_pages = (int)num_pages;
   p.page_log2 = log2_of(page);
   p.causal = causal != 0;
-  p.scale_log2 = scale * 1.44269504088896340736f;
+  p.scale_log2 = scale_log2;
   return hip_status(lookme::launch_attend(dtype, head_dim, p, static_cast<hipStream_t>(stream)),
                     "attention launch");
 }

@@ -100,7 +100,7 @@ ATTENTION = dict(dtype=BF, n=6, batch=2, q_heads=4, kv_heads=2, head_dim=128, q=
     (dict(max_pages=0), INVALID), (dict(max_pages=2 ** 25), UNSUPPORTED),
     (dict(num_pages=0), INVALID), (dict(num_pages=2 ** 26), UNSUPPORTED),
     (dict(page=48), UNSUPPORTED), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID),
-    (dict(scale=INF), INVALID), (dict(scale=NAN), INVALID), (dict(causal=2), INVALID),
+    (dict(scale=3e38), INVALID), (dict(scale=INF), INVALID), (dict(scale=NAN), INVALID), (dict(causal=2), INVALID),
     (dict(q=None), INVALID), (dict(q_offsets=None), INVALID), (dict(q_offsets=P + 4), INVALID),
     (dict(lengths=None), INVALID), (dict(pages=None), INVALID), (dict(cache=None), INVALID),
     (dict(out=None), INVALID), (dict(max_pages=300, workspace=None), WORKSPACE),

@@ -400,3 +400,34 @@ def test_exact_averages():
             out = _run(q.to(dt).cuda(), cache, table, [(1, n)])
             want = v.double().mean()
             assert (out.double().cpu() - want).abs().max() <= A.HALF[dt] * want
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("m", [3, 20, 200])
+def test_sequences_that_share_rows_stay_in_their_memory(m, d):
+    """offsets that are not ascending: what such rows get is not specified, the rest of
+    the outputs and of the workspace is left as it was"""
+    seqs = [(m, 700)] * 32
+    cache, table, _, _ = _sequences(seqs, 2, d, 64)
+    table = torch.cat([table, torch.full((32, 600), -7, dtype=I32)], 1)
+    q = torch.randn((m + 3, 8, d), generator=_gen(4)).bfloat16().cuda()
+    off = torch.tensor([0, m] * 16 + [m + 1], dtype=I32).cuda()   # (the last has a row of its own)
+    lens = torch.full((32,), 700, dtype=I32).cuda()
+    need = lk.lookme_cache_attention_workspace(1, m + 3, 32, 8, 2, d, table.shape[1], 64)
+    for fill in (0, 255, 1):              # (what an earlier call may have left in the workspace)
+        out = torch.full_like(q, 7.0)
+        ws = torch.full((need + 4096,), fill, dtype=torch.uint8, device="cuda")
+        lk.cache_attention(q, cache, table.cuda(), lens, out, ws[:need], q_offsets=off)
+        assert (out[m + 1:] == 7).all() and (ws[need:] == fill).all()
+
+
+def test_smallest_and_largest_scales():
+    """a score's range that float32 can hold: weights that are all alike, or one"""
+    seqs = [(2, 400)]
+    cache, table, slots, vals = _sequences(seqs, 1, 128, 32)
+    table[0, 0] = -1                      # (its tokens are left out: a first tile of nothing)
+    q = torch.randn((2, 1, 128), generator=_gen(6)).bfloat16()
+    k, v = vals[0]
+    for scale in (1e-44, 1e-38, 1e-30, 1e4):
+        out = _run(q.cuda(), cache, table, seqs, False, scale)
+        _check(out, q, [(k[32:], v[32:])], seqs, False, scale)

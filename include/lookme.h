@@ -704,8 +704,9 @@ lookme_status_t lookme_quant_swiglu(int32_t dtype, int64_t n, int32_t d_in, int3
  *            image beside the order of the text); any int32
  *   axis     [rot / 2] int32 in [0, axes) (clamped), or NULL (axis 0)
  *   freq     [rot / 2] float32, finite, |pos freq| below 2^40
- * head_dim * elem_size a multiple of 16 bytes, head_dim at most 256.  n = 0 does
- * nothing.  Needs no handle and no workspace.
+ * head_dim * elem_size a multiple of 16 bytes, head_dim at most 256.  A head whose
+ * sum of squares passes float32's range gives y = 0.  n = 0 does nothing.  Needs no
+ * handle and no workspace.
  */
 lookme_status_t lookme_head_norm_rotary(int32_t dtype, int64_t n, int32_t head_dim,
                                         int32_t q_heads, const void* q, int64_t q_stride,
@@ -771,7 +772,7 @@ lookme_status_t lookme_cache_read(int32_t dtype, int64_t n, int32_t kv_heads, in
  * whose scores are all minus infinity) gives 0.  Tokens that a row does not see do
  * not touch it, whatever their bytes; a visible block that is not finite gives NaN.
  *   n          rows of q and out, [n, q_heads, head_dim] with strides as above;
- *              out may be q, with the same stride
+ *              out may be q, with the same stride, else they do not overlap
  *   q_offsets  [batch + 1] int32, ascending, in [0, n] (clamped); NULL: row b is
  *              sequence b's (n = batch).  Rows of no sequence are left as they were;
  *              what rows of several sequences get is not specified

@@ -621,6 +621,17 @@ __device__ __forceinline__ void at_issue(const uint8_t* tile, char* dst) {
   if (lane < REST) load_lds16_nt(tile + FULL * 1024 + lane * 16, dst + FULL * 1024);
 }
 
+// Bound by memory for a row or two a key head, by vector instructions from there on (two
+// values an unpacking instruction, an exponential a score).  A row of 64 heads over 131072
+// tokens of 8 key heads of 128, 4 sequences (570 MB), takes 97 us, 5.9 TB/s; the same
+// stream with the arithmetic left out takes 93.  What carried it there (us of that case): tiles in
+// registers, waited for one by one 160 and in turns 134; each wave's own ring in LDS,
+// filled past the registers and without barriers, 120; nontemporal loads and the rows'
+// sums in the matrix cores 104; rare cases (masks, blocks that are not finite) out of
+// everybody's way 97.  Rings of 3 tiles and 8 waves were no faster.  64 sequences of up to
+// 8192 tokens, 290 MB, take 54.  300 rows of 16 heads of 64 over up to 2880 tokens, 8
+// sequences, take 41 to 45: matrix cores 0.22, the rest unpacking, exponentials and the
+// uneven end.
 template <int DT, int D, int RT>
 __global__ __launch_bounds__(64 * AF_WAVES, af_occupancy(DT, D, RT))
 void attend_few_kernel(AttendParams p) {
@@ -798,6 +809,13 @@ struct AttendShare {
   }
 };
 
+// Bound by the issue of instructions: the matrix cores are busy 0.44 of the time and vector
+// instructions take 0.54 (2 x 4096 rows of 16 heads of 128, 4 key heads, at the end of 8192
+// tokens: 414 to 507 us from card to card, 995 to 813 TFLOP/s).  Steps (us of that case):
+// unpacking in every wave 1226, turns in registers 822, shared through LDS with the blocks of
+// a key head on one XCD 587, the next tile's scores beside this one's weights and no
+// copies of registers 560, rare cases out of the way 502.  Codes through a ring in LDS 605;
+// three row tiles 617, one and more waves 613.
 template <int DT, int D>
 __global__ __launch_bounds__(64 * AM_WAVES, 2)
 void attend_many_kernel(AttendParams p) {
@@ -931,7 +949,8 @@ void attend_many_kernel(AttendParams p) {
 }
 
 // Joins the parts of a row's keys: W waves a row and query head, 64 parts at a time
-// whose weights the lanes compute side by side.
+// whose weights the lanes compute side by side (250 parts one after the other took 25 us,
+// so 6).  Bound by latency, 4 to 5 us of which 2.7 are a launch.
 template <int DT, int D, int BR, int W>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void attend_join_kernel(AttendParams p) {
   constexpr int E = D / 64, AHEAD = 8;     // values of a lane, parts on their way

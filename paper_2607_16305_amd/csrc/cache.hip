@@ -6,6 +6,10 @@
 // conversion of this chip, which rounds to the nearest value, of two as near to
 // the even code, and saturates.  Every step is exact but that rounding, so the
 // bytes are a function of the 32 values alone.
+//
+// Both are bound by memory: 32768 rows of 8 heads of 128 in bf16 are written in 39 us (134
+// MB read, 36 written: 4.4 TB/s) and read in 34 (36 read, 134 written: 5.0 TB/s); a large
+// copy reaches 4.9.  64 rows take 3 us each, a launch.
 #include "cache4.h"
 #include "kernels.h"
 
@@ -14,7 +18,8 @@ namespace lookme {
 // A workgroup takes 32 rows of a head, of k or of v.  k goes a row at a time; for v,
 // where a lane of the attention reads 8 tokens, neighbouring threads take the 8 rows
 // that are such a lane's when the rows are a tile: their bytes are neighbours then
-// (any other slots are as right, only more scattered).
+// (any other slots are as right, only more scattered; v a row at a time took 52 us of
+// the 39, each byte of a tile's line from another workgroup).
 constexpr int CW_THREADS = 256, CW_ROWS = 32;
 
 // 8 values from p (16-byte aligned)

@@ -12,6 +12,13 @@
 // whole number, good to 2^-53 of the turns, so a position of 10^6 has the angle
 // that a float32 product would miss by 0.03.  What is left is float32 (2^-26 of
 // a turn).  A token's angles are computed once for all of its heads.
+//
+// Bound by memory: 8192 rows of 40 heads of 128 in bf16, 168 MB read and written, take 33
+// us (5.0 TB/s; a large copy reaches 4.9).  Each lane holds its two chunks of 16 bytes
+// through norm and rotation, so a head is read and written once and nothing but the
+// angles goes through LDS; the next head's loads are on their way meanwhile.  (Heads in
+// LDS took 56 us, register pairs without loads past the caches 40.)  One token of 18
+// heads: 3.2 us, a launch.
 #include "common.h"
 #include "kernels.h"
 
@@ -225,6 +232,8 @@ template <int DT, int MODE>
 static hipError_t launch_rotary_mode(RotaryParams p, hipStream_t st) {
   const int T = p.chunks <= 8 ? 4 : p.chunks <= 16 ? 8 : p.chunks <= 32 ? 16 : 32;
   const int teams = HR_THREADS / T, heads = p.q_heads + p.k_heads, half4 = (p.rot / 2 + 3) & ~3;
+  // few rows: a team a head, so that the launch is as wide as it can be (3001 rows of 16
+  // heads of 80 in float32 15 -> 10 us); many: whole tokens, up to 8 for one set of angles
   p.tokens = 1;
   p.span = teams;
   if (p.n * ((heads + teams - 1) / teams) > 2048) {

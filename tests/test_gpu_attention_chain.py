@@ -265,7 +265,7 @@ def test_a_cache_and_rows_past_4_gib():
     kk, vv = torch.randn((n, 1, d), generator=g), torch.randn((n, 1, d), generator=g)
     slots = (pages - 3) * 32 + torch.arange(n)
     lk.cache_write(kk.cuda(), vv.cuda(), slots.to(I32).cuda(), cache)
-    q = wide[3072:].as_strided((5, 1, d), (step, d, 1))
+    q = wide[2560:].as_strided((5, 1, d), (step, d, 1))
     qc = torch.randn((5, 1, d), generator=g).to(BF)
     q.copy_(qc)
     ws = torch.empty(lk.LOOKME_ATTENTION_WORKSPACE, dtype=torch.uint8, device="cuda")

@@ -71,9 +71,10 @@ __device__ __forceinline__ T wave_sum(T v) {
   return v;
 }
 
-// Unit `unit` of the batch, the same for every lane of the wave.  The keys of all
-// sequences are cut into parts of about the same size, so that there are about
-// p.target units in all, whatever the lengths.
+// Unit `unit` of the batch, the same for every lane of the wave.  Where the longest
+// sequence would keep its workgroups more than it costs to join parts, the keys of all
+// sequences are cut into parts of about the same size, so that there are about p.target
+// units in all, whatever the lengths.
 template <int BR>
 __device__ __forceinline__ bool at_unit(const AttendParams& p, int64_t unit, AttendUnit* u) {
   const int lane = threadIdx.x & 63, G = p.q_heads / p.kv_heads;
@@ -82,29 +83,40 @@ __device__ __forceinline__ bool at_unit(const AttendParams& p, int64_t unit, Att
   };
   AttendSeq s{0, 0, 0};       // of sequence lane, or of the 64 that are looked at
   if (lane < p.batch) s = at_seq(p, lane);
+  int64_t mine = 0;           // blocks of the lane's sequences
+  float work = 0.f, longest = 0.f;
+  AttendSeq o = s;
+  for (int b = lane; b < p.batch; b += 64) {
+    if (b > lane) o = at_seq(p, b);
+    const int n = blocks_of(o);
+    const float tiles = (float)((o.len + C4_TILE - 1) / C4_TILE);
+    mine += n;
+    work += (float)n * tiles;
+    longest = fmaxf(longest, n > 0 ? tiles : 0.f);
+  }
+  mine = mine < AT_UNITS_OF_SEQ ? mine : AT_UNITS_OF_SEQ;
+  const int blocks = wave_sum((int)mine);
   int chunk = 0x7FFFFFFF;     // tiles of a part
-  if (p.target > 0) {
-    float work = 0.f, blocks = 0.f;
-    AttendSeq o = s;
-    for (int b = lane; b < p.batch; b += 64) {
-      if (b > lane) o = at_seq(p, b);
-      const float n = (float)blocks_of(o);
-      blocks += n;
-      work += n * (float)((o.len + C4_TILE - 1) / C4_TILE);
-    }
+  bool cut = p.target > 0;
+  if (cut) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) longest = fmaxf(longest, __shfl_xor(longest, d, 64));
+    work = wave_sum(work);
+    // (alike in every lane, and known to be: what follows from it stays in scalar registers)
+    cut = __builtin_amdgcn_readfirstlane((longest - work / (float)p.target) * p.tile_us >
+                                         p.join_us);
+  }
+  if (cut) {
     // Parts are rounded up, half a part a block: of units of 32 to 64 rows, which are long
     // in their beginning and end, none is to be left for a second round (15 x 40 rows over
     // 6700 tokens 43 -> 35 us; units of 16 rows even out better without: 276 and 300)
-    const float room = BR > 16 && BR < 128 ? fminf(0.5f * wave_sum(blocks), 0.5f * p.target) : 0.f;
-    const float c = ceilf(wave_sum(work) / ((float)p.target - room));
+    const float room = BR > 16 && BR < 128 ? 0.5f * fminf((float)blocks, (float)p.target) : 0.f;
+    const float c = ceilf(work / ((float)p.target - room));
     chunk = c < (float)AT_MIN_TILES ? AT_MIN_TILES : c > 1e9f ? 1000000000 : (int)c;
   } else {
     // without a cut the blocks of rows of one key head read the same keys: a
     // neighbourhood of units for each XCD, so that they meet in its L2
-    int64_t mine = blocks_of(s);
-    for (int b = lane + 64; b < p.batch; b += 64) mine += blocks_of(at_seq(p, b));
-    const int all = (int)(mine < AT_UNITS_OF_SEQ ? mine : AT_UNITS_OF_SEQ);
-    unit = __builtin_amdgcn_readfirstlane(xcd_remap((int)unit, wave_sum(all)));
+    unit = __builtin_amdgcn_readfirstlane(xcd_remap((int)unit, blocks));
     if (unit < 0) return false;
   }
   int64_t before = 0, parts = 0;
@@ -1068,6 +1080,7 @@ struct AttendPlan {
   int block;        // rows of a unit
   int target;       // units that the cut aims at; 0: no cut
   int64_t units;    // workgroups
+  float tile_us, join_us;   // what a tile and a join take, for at_unit
 };
 
 static int many_block(int dt, int d) {
@@ -1093,11 +1106,16 @@ static int few_tiles(int dt, int d, int rows) {
   return rows <= 96 ? 3 : 0;
 }
 
-// The keys are cut where that saves more than it costs.  It saves about a microsecond and
-// a half of a tile's turn, as far as the blocks of rows leave workgroups free; it costs a
+// The keys are cut where that saves more than it costs.  It saves a unit's turns (tile_us a
+// tile, in microseconds) as far as the blocks of rows leave workgroups free; it costs a
 // launch, and each row's parts written and read again.  (500 rows of 500 tokens: 20 us
 // whole, 24 cut; 64 rows of 1024 tokens 12 and 17; a row of 2048 tokens 16 and 10; 11
-// sequences of up to 32000 tokens x 64 heads 340 and 282.)
+// sequences of up to 32000 tokens x 64 heads 340 and 282.)  Here the lengths are not known,
+// only what the page table could hold: the call gets a join where the keys would be cut
+// were they all that long, or where one long sequence among short ones could keep a few
+// workgroups busy by itself (one of 131072 tokens among 127 of 1000, 8 key heads: 631 us
+// whole, 64 cut); the kernel then decides by the lengths (at_unit), and a join with nothing
+// to do takes 4 to 5 us (256 rows of 500 tokens 37 -> 42).
 static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
                               int64_t tokens) {
   const int64_t rows = n * (q_heads / kv_heads), each = (rows + batch - 1) / batch;
@@ -1106,10 +1124,13 @@ static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_
   a.block = a.tiles > 0 ? 16 * a.tiles : many_block(dt, d);
   // (one round of resident workgroups; 512 of 128 rows and 128 dims are 68 MB)
   a.target = a.tiles > 0 ? 256 * af_occupancy(dt, d, a.tiles) : d == 128 ? 480 : 448;
-  const double turns = (double)((tokens + C4_TILE - 1) / C4_TILE) *
-                       (a.tiles > 0 ? 0.18 * (1 + a.tiles) / AF_WAVES : 0.5);
-  const double blocks = (double)((each + a.block - 1) / a.block) * batch * kv_heads;
-  if ((1.0 - blocks / a.target) * turns <= 4.0 + (double)n * q_heads * d * 16 / 2.5e6) a.target = 0;
+  a.tile_us = a.tiles > 0 ? 0.18f * (1 + a.tiles) / AF_WAVES : 0.5f;
+  a.join_us = (float)((double)n * q_heads * d * 16 / 2.5e6);
+  const double turns = (double)((tokens + C4_TILE - 1) / C4_TILE) * a.tile_us;
+  const double blocks = (double)((each + a.block - 1) / a.block) * kv_heads;   // of a sequence
+  if ((1.0 - blocks * batch / a.target) * turns <= 4.0 + a.join_us &&
+      (a.tiles == 0 || (1.0 - blocks / a.target) * turns <= 40.0 + a.join_us))
+    a.target = 0;
   a.units = (rows / a.block + batch) * kv_heads + (a.target > 0 ? a.target + 64 : 0);
   return a;
 }
@@ -1144,6 +1165,8 @@ static hipError_t launch_attend_d(AttendParams p, hipStream_t st) {
   const AttendPlan a = attend_plan(DT, p.n, p.batch, p.q_heads, p.kv_heads, D,
                                    (int64_t)p.max_pages << p.page_log2);
   p.target = a.target;
+  p.tile_us = a.tile_us;
+  p.join_us = a.join_us;
   const dim3 grid((unsigned)((a.units + 7) / 8 * 8));
   // (what few_tiles chooses, and nothing else, is built)
   if (a.tiles == 1) return launch_few<DT, D, 1>(a, p, grid, st);

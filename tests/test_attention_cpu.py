@@ -119,12 +119,17 @@ def test_cache_attention_refuses(kw, status):
 def test_workspace_has_one_bound(dtype, d):
     """the constant serves every call; small and large ones need none"""
     most = 0
-    for n, batch in ((1, 1), (64, 64), (2048, 2048), (7, 1), (35, 7), (600, 2), (10 ** 5, 4)):
+    for n, batch in ((1, 1), (64, 64), (2048, 2048), (7, 1), (35, 7), (600, 2), (10 ** 5, 4),
+                     (2 ** 16, 2 ** 16), (2 ** 21, 2 ** 16)):
         for hq, hkv in ((1, 1), (8, 1), (32, 8), (64, 64)):
             for pages in (1, 4, 2 ** 14):
                 b = lk.lookme_cache_attention_workspace(dtype, n, batch, hq, hkv, d, pages, 32)
                 assert 0 <= b <= lk.LOOKME_ATTENTION_WORKSPACE
                 most = max(most, b)
+    for n in (2 ** 22, 2 ** 25, 2 ** 27):
+        for page in (32, 1024):
+            b = lk.lookme_cache_attention_workspace(dtype, n, 2 ** 22, 1, 1, d, 2 ** 20, page)
+            assert 0 <= b <= lk.LOOKME_ATTENTION_WORKSPACE
     assert most > 0
     assert lk.lookme_cache_attention_workspace(dtype, 0, 0, 8, 1, d, 4, 32) == 0
 

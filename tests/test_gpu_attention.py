@@ -287,6 +287,22 @@ def test_cache_attention_of_every_count_of_rows(m, dtype, d, wide):
         _check(out, q, vals, seqs, causal, d ** -0.5)
 
 
+@pytest.mark.parametrize("seqs,hq,hkv", [
+    ([(1, 5000)] + [(1, 37)] * 130, 8, 8),    # one long sequence among short ones: cut
+    ([(300, 320), (290, 290)], 16, 1),        # rows enough and few tokens: whole
+])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_lengths_choose_whether_keys_are_cut(seqs, hq, hkv, d):
+    cache, table, _, vals = _sequences(seqs, hkv, d, 32)
+    table = torch.cat([table, torch.full((len(seqs), 8000), -7, dtype=I32)], 1)
+    n = sum(r for r, _ in seqs)
+    assert lk.lookme_cache_attention_workspace(1, n, len(seqs), hq, hkv, d, table.shape[1], 32) > 0
+    q = torch.randn((n, hq, d), generator=_gen(n)).bfloat16()
+    out = _run(q.cuda(), cache, table, seqs)
+    _check(out, q, vals, seqs, True, d ** -0.5)
+    assert torch.equal(out, _run(q.cuda(), cache, table, seqs))
+
+
 def test_rows_apart_in_place_and_without_offsets():
     seqs = [(1, 77), (1, 1200), (1, 0)]
     cache, table, _, vals = _sequences(seqs, 2, 128, 64)

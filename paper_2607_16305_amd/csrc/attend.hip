@@ -17,6 +17,7 @@
 // weights p to bf16 for the second product (half a step, 2^-8 relative, of independent
 // signs; the output has the same step), float32 rows take q and p as three bf16
 // values each, which hold all 24 bits.
+#include <numeric>
 #include <type_traits>
 
 #include "cache4.h"
@@ -34,6 +35,7 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 constexpr int AT_MIN_TILES = 4;
 constexpr float AT_SLACK = 8.f;
 constexpr int AT_UNITS_OF_SEQ = 1 << 24;
+constexpr int AT_INLINE = 64;    // sequences that a unit looks at by itself
 
 // ---------------------------------------------------------------------------
 // work units: (sequence, key head, block of rows, part of the keys)
@@ -71,95 +73,250 @@ __device__ __forceinline__ T wave_sum(T v) {
   return v;
 }
 
-// Unit `unit` of the batch, the same for every lane of the wave.  Where the longest
-// sequence would keep its workgroups more than it costs to join parts, the keys of all
-// sequences are cut into parts of about the same size, so that there are about p.target
-// units in all, whatever the lengths.
-template <int BR>
-__device__ __forceinline__ bool at_unit(const AttendParams& p, int64_t unit, AttendUnit* u) {
-  const int lane = threadIdx.x & 63, G = p.q_heads / p.kv_heads;
-  auto blocks_of = [&](const AttendSeq& s) {
-    return (int)(((int64_t)s.rows * G + BR - 1) / BR) * p.kv_heads;
-  };
-  AttendSeq s{0, 0, 0};       // of sequence lane, or of the 64 that are looked at
-  if (lane < p.batch) s = at_seq(p, lane);
-  int64_t mine = 0;           // blocks of the lane's sequences
-  float work = 0.f, longest = 0.f;
-  AttendSeq o = s;
-  for (int b = lane; b < p.batch; b += 64) {
-    if (b > lane) o = at_seq(p, b);
-    const int n = blocks_of(o);
-    const float tiles = (float)((o.len + C4_TILE - 1) / C4_TILE);
-    mine += n;
-    work += (float)n * tiles;
-    longest = fmaxf(longest, n > 0 ? tiles : 0.f);
-  }
-  mine = mine < AT_UNITS_OF_SEQ ? mine : AT_UNITS_OF_SEQ;
-  const int blocks = wave_sum((int)mine);
-  int chunk = 0x7FFFFFFF;     // tiles of a part
-  bool cut = p.target > 0;
-  if (cut) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) longest = fmaxf(longest, __shfl_xor(longest, d, 64));
-    work = wave_sum(work);
-    // (alike in every lane, and known to be: what follows from it stays in scalar registers)
-    cut = __builtin_amdgcn_readfirstlane((longest - work / (float)p.target) * p.tile_us >
-                                         p.join_us);
-  }
-  if (cut) {
-    // Parts are rounded up, half a part a block: of units of 32 to 64 rows, which are long
-    // in their beginning and end, none is to be left for a second round (15 x 40 rows over
-    // 6700 tokens 43 -> 35 us; units of 16 rows even out better without: 276 and 300)
-    const float room = BR > 16 && BR < 128 ? 0.5f * fminf((float)blocks, (float)p.target) : 0.f;
-    const float c = ceilf(work / ((float)p.target - room));
-    chunk = c < (float)AT_MIN_TILES ? AT_MIN_TILES : c > 1e9f ? 1000000000 : (int)c;
-  } else {
-    // without a cut the blocks of rows of one key head read the same keys: a
-    // neighbourhood of units for each XCD, so that they meet in its L2
-    unit = __builtin_amdgcn_readfirstlane(xcd_remap((int)unit, blocks));
-    if (unit < 0) return false;
-  }
-  int64_t before = 0, parts = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    if (b0 > 0) {
-      s = AttendSeq{0, 0, 0};
-      if (b0 + lane < p.batch) s = at_seq(p, b0 + lane);
-    }
-    const int tiles = (s.len + C4_TILE - 1) / C4_TILE;
-    const int splits = tiles > chunk ? (tiles + chunk - 1) / chunk : 1;
-    const int64_t all = (int64_t)blocks_of(s) * splits;
-    const int units = all > AT_UNITS_OF_SEQ ? AT_UNITS_OF_SEQ : (int)all;
-    const int cut = splits > 1 ? units : 0;
-    const int incl = wave_scan_incl(units), cut_incl = wave_scan_incl(cut);
-    const uint64_t found = __ballot(unit < before + incl);
-    if (found != 0) {
-      const int l = __ffsll((unsigned long long)found) - 1;
-      u->b = b0 + l;
-      u->seq.q0 = __builtin_amdgcn_readlane(s.q0, l);
-      u->seq.rows = __builtin_amdgcn_readlane(s.rows, l);
-      u->seq.len = __builtin_amdgcn_readlane(s.len, l);
-      u->splits = __builtin_amdgcn_readlane(splits, l);
-      u->local = (int)(unit - before - (__builtin_amdgcn_readlane(incl, l) -
-                                        __builtin_amdgcn_readlane(units, l)));
-      u->part = (int)(parts + __builtin_amdgcn_readlane(cut_incl, l) -
-                      __builtin_amdgcn_readlane(cut, l));
-      return true;
-    }
-    before += __builtin_amdgcn_readlane(incl, 63);
-    parts += __builtin_amdgcn_readlane(cut_incl, 63);
-  }
-  return false;
-}
-
-// The workspace: p.target 2 units' outputs [BR, D], their rows' (maximum, sum), then for
-// every sequence (its first unit there, parts of its keys), for the join
+// The workspace: p.target 2 units' outputs [BR, D], their rows' (maximum, sum), then the plan:
+// whether keys are cut and the count of units, and of every sequence where its units and
+// its parts begin and the parts of its keys
 template <int D, int BR>
 __device__ __forceinline__ float* at_sums(const AttendParams& p) {
   return p.part + (int64_t)2 * p.target * BR * D;
 }
+struct AttendCut {
+  uint32_t unit;     // its first unit (where attend_plan_kernel has written it)
+  int part;          // index among the units whose keys are cut, of its first one
+  int splits, pad;   // parts of its keys
+};
+struct AttendHead {
+  int cut;
+  uint32_t units;
+  int pad[2];
+};
 template <int D, int BR>
-__device__ __forceinline__ int* at_cuts(const AttendParams& p) {
-  return reinterpret_cast<int*>(at_sums<D, BR>(p) + (int64_t)2 * p.target * BR * 2);
+__device__ __forceinline__ AttendHead* at_head(const AttendParams& p) {
+  return reinterpret_cast<AttendHead*>(at_sums<D, BR>(p) + (int64_t)2 * p.target * BR * 2);
+}
+template <int D, int BR>
+__device__ __forceinline__ AttendCut* at_cuts(const AttendParams& p) {
+  return reinterpret_cast<AttendCut*>(at_head<D, BR>(p) + 1);
+}
+
+// Inclusive sum over the 1024 threads of a workgroup, and the sum of all (wrapping: what
+// offsets that are not ascending give is checked where it is used)
+__device__ __forceinline__ uint32_t at_block_scan(uint32_t v, int* sums, uint32_t* all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_up(v, d, 64);
+    if (lane >= d) v += o;
+  }
+  if (lane == 63) sums[wave] = (int)v;
+  __syncthreads();
+  uint32_t off = 0, sum = 0;
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) off += (uint32_t)sums[w];
+    sum += (uint32_t)sums[w];
+  }
+  __syncthreads();
+  *all = sum;
+  return v + off;
+}
+
+// Blocks of BR rows of a sequence, of all its key heads
+template <int BR>
+__device__ __forceinline__ int at_blocks(const AttendParams& p, const AttendSeq& s) {
+  return (int)(((int64_t)s.rows * (p.q_heads / p.kv_heads) + BR - 1) / BR) * p.kv_heads;
+}
+__device__ __forceinline__ int at_tiles(const AttendSeq& s) {
+  return (s.len + C4_TILE - 1) / C4_TILE;
+}
+
+// Tiles of a part of the keys, of sequences with `blocks` blocks of rows, `work` tiles of
+// them in all and `longest` of one: parts of about the same size, so that there are about
+// p.target units whatever the lengths, or everything, where the longest sequence keeps its
+// workgroups less than it costs to join parts.
+template <int BR>
+__device__ __forceinline__ int at_chunk(const AttendParams& p, int blocks, float work,
+                                        float longest) {
+  if ((longest - work / (float)p.target) * p.tile_us <= p.join_us) return 0x7FFFFFFF;
+  // Parts are rounded up, half a part a block: of units of 32 to 64 rows, which are long
+  // in their beginning and end, none is to be left for a second round (15 x 40 rows over
+  // 6700 tokens 43 -> 35 us; units of 16 rows even out better without: 276 and 300)
+  const float room = BR > 16 && BR < 128 ? 0.5f * fminf((float)blocks, (float)p.target) : 0.f;
+  const float c = ceilf(work / ((float)p.target - room));
+  return c < (float)AT_MIN_TILES ? AT_MIN_TILES : c > 1e9f ? 1000000000 : (int)c;
+}
+
+// The last of `count` entries whose key (ascending) is at most x, 64 at a time; 0 where
+// none is
+template <class F>
+__device__ __forceinline__ int at_search(int count, F at_most) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = count;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64, b = lo + lane * step;
+    const uint64_t found = __ballot(b < hi && at_most(b)) | 1u;
+    lo += (63 - __clzll((long long)found)) * step;
+    hi = lo + step < hi ? lo + step : hi;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Unit `unit` of the batch, the same for every lane of the wave.  64 sequences are looked
+// at by the lanes of every wave.  More would cost each of the many units that they are as
+// much as its work (1024 rows of 500 tokens 215 us, 4096 1983): with whole keys a unit
+// finds its sequence by q_offsets alone, from a count of blocks that never is too small,
+// and where they may be cut attend_plan_kernel has written where each one begins (107 to
+// 117 us and 435 to 502).
+template <int D, int BR>
+__device__ __forceinline__ bool at_unit(const AttendParams& p, int unit, AttendUnit* u) {
+  const int lane = threadIdx.x & 63;
+  if (p.batch <= AT_INLINE) {
+    AttendSeq s{0, 0, 0};
+    if (lane < p.batch) s = at_seq(p, lane);
+    const int mine = at_blocks<BR>(p, s), tiles = at_tiles(s);
+    const int blocks = wave_sum(mine < AT_UNITS_OF_SEQ ? mine : AT_UNITS_OF_SEQ);
+    int chunk = 0x7FFFFFFF;
+    if (p.target > 0) {
+      float longest = mine > 0 ? (float)tiles : 0.f;
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) longest = fmaxf(longest, __shfl_xor(longest, d, 64));
+      // (alike in every lane, and known to be: what follows stays in scalar registers)
+      chunk = __builtin_amdgcn_readfirstlane(
+          at_chunk<BR>(p, blocks, wave_sum((float)mine * (float)tiles), longest));
+      if (unit == 0 && threadIdx.x == 0) at_head<D, BR>(p)->cut = chunk != 0x7FFFFFFF;
+    }
+    if (chunk == 0x7FFFFFFF) {
+      // without a cut the blocks of rows of one key head read the same keys: a
+      // neighbourhood of units for each XCD, so that they meet in its L2
+      unit = __builtin_amdgcn_readfirstlane(xcd_remap(unit, blocks));
+      if (unit < 0) return false;
+    }
+    const int splits = tiles > chunk ? (tiles + chunk - 1) / chunk : 1;
+    const int64_t all = (int64_t)mine * splits;
+    const int units = all > AT_UNITS_OF_SEQ ? AT_UNITS_OF_SEQ : (int)all;
+    const int cut = splits > 1 ? units : 0;
+    const int incl = wave_scan_incl(units), cut_incl = wave_scan_incl(cut);
+    const uint64_t found = __ballot(unit < incl);
+    if (found == 0) return false;
+    const int l = __ffsll((unsigned long long)found) - 1;
+    u->b = l;
+    u->seq.q0 = __builtin_amdgcn_readlane(s.q0, l);
+    u->seq.rows = __builtin_amdgcn_readlane(s.rows, l);
+    u->seq.len = __builtin_amdgcn_readlane(s.len, l);
+    u->splits = __builtin_amdgcn_readlane(splits, l);
+    u->local = unit - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(units, l));
+    u->part = __builtin_amdgcn_readlane(cut_incl, l) - __builtin_amdgcn_readlane(cut, l);
+    if (p.target > 0 && u->local == 0 && threadIdx.x == 0) {
+      AttendCut* c = at_cuts<D, BR>(p) + l;
+      c->part = u->part;
+      c->splits = u->splits;
+    }
+    return true;
+  }
+  const AttendCut* cuts = at_cuts<D, BR>(p);
+  uint32_t first;
+  int count = 0;
+  if (p.target > 0) {
+    const AttendHead* head = at_head<D, BR>(p);
+    const uint32_t units = head->units;
+    if (head->cut == 0) unit = __builtin_amdgcn_readfirstlane(xcd_remap(unit, (int)units));
+    if (unit < 0 || (uint32_t)unit >= units) return false;
+    u->b = at_search(p.batch, [&](int b) { return cuts[b].unit <= (uint32_t)unit; });
+    first = cuts[u->b].unit;
+    u->part = cuts[u->b].part;
+    u->splits = cuts[u->b].splits;
+  } else {
+    // Sequence b's blocks, of one key head, begin at or behind (q0 G + b pad) / BR: with pad =
+    // BR - gcd(G, BR), that leaves it room for its last, partial block
+    const int G = p.q_heads / p.kv_heads;
+    auto begin = [&](int b) {
+      int64_t q0 = b;
+      if (p.q_offsets != nullptr) {
+        const int a = p.q_offsets[b];
+        q0 = a < 0 ? 0 : a > p.n ? p.n : a;
+      }
+      return (int)((q0 * G + (int64_t)b * p.pad) / BR);
+    };
+    unit = __builtin_amdgcn_readfirstlane(xcd_remap(unit, begin(p.batch) * p.kv_heads));
+    if (unit < 0) return false;
+    const int slot = unit / p.kv_heads;
+    u->b = at_search(p.batch, [&](int b) { return begin(b) <= slot; });
+    first = (uint32_t)(begin(u->b) * p.kv_heads);
+    count = begin(u->b + 1) * p.kv_heads - (int)first;
+    u->part = 0;
+    u->splits = 1;
+  }
+  u->seq = at_seq(p, u->b);
+  const int blocks = at_blocks<BR>(p, u->seq);
+  u->local = (int)((uint32_t)unit - first);
+  if (p.target == 0) {
+    // (by key head: its blocks, then what was left over)
+    const int slots = count / p.kv_heads, each = blocks / p.kv_heads;
+    if (u->local < 0 || u->local >= count) return false;
+    const int h = u->local / slots, x = u->local - h * slots;
+    u->local = h * each + x;
+    if (x >= each) return false;
+  }
+  u->seq.q0 = __builtin_amdgcn_readfirstlane(u->seq.q0);
+  u->seq.rows = __builtin_amdgcn_readfirstlane(u->seq.rows);
+  u->seq.len = __builtin_amdgcn_readfirstlane(u->seq.len);
+  u->splits = __builtin_amdgcn_readfirstlane(u->splits);
+  u->part = __builtin_amdgcn_readfirstlane(u->part);
+  u->local = __builtin_amdgcn_readfirstlane(u->local);
+  return u->local >= 0 && u->local < (int64_t)blocks * u->splits;
+}
+
+// The plan of a call of more than AT_INLINE sequences whose keys may be cut, by one workgroup
+template <int D, int BR>
+__global__ __launch_bounds__(1024) void attend_plan_kernel(AttendParams p) {
+  __shared__ float works[16], longs[16];
+  __shared__ int sums[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float work = 0.f, longest = 0.f;
+  int64_t mine = 0;
+  for (int b = threadIdx.x; b < p.batch; b += 1024) {
+    const AttendSeq s = at_seq(p, b);
+    const int n = at_blocks<BR>(p, s);
+    mine += n;
+    work += (float)n * (float)at_tiles(s);
+    longest = fmaxf(longest, n > 0 ? (float)at_tiles(s) : 0.f);
+  }
+  // (what is not more than the launch's units; offsets that are not ascending may give more)
+  const int some = wave_sum((int)(mine < 1 << 20 ? mine : 1 << 20));
+  work = wave_sum(work);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) longest = fmaxf(longest, __shfl_xor(longest, d, 64));
+  if (lane == 0) {
+    works[wave] = work;
+    longs[wave] = longest;
+    sums[wave] = some;
+  }
+  __syncthreads();
+  int blocks = 0;
+  work = longest = 0.f;
+  for (int w = 0; w < 16; ++w) {
+    work += works[w];
+    longest = fmaxf(longest, longs[w]);
+    blocks += sums[w];
+  }
+  __syncthreads();
+  const int chunk = at_chunk<BR>(p, blocks, work, longest);
+  AttendCut* cuts = at_cuts<D, BR>(p);
+  uint32_t before = 0, parts = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 1024) {
+    const int b = b0 + threadIdx.x;
+    AttendSeq s{0, 0, 0};
+    if (b < p.batch) s = at_seq(p, b);
+    const int tiles = at_tiles(s), splits = tiles > chunk ? (tiles + chunk - 1) / chunk : 1;
+    const uint32_t units = (uint32_t)at_blocks<BR>(p, s) * (uint32_t)splits;
+    const uint32_t cut = splits > 1 ? units : 0;
+    uint32_t all, all_cut;
+    const uint32_t at = before + at_block_scan(units, sums, &all) - units;
+    const uint32_t part = parts + at_block_scan(cut, sums, &all_cut) - cut;
+    if (b < p.batch) cuts[b] = AttendCut{at, (int)part, splits, 0};
+    before += all;
+    parts += all_cut;
+  }
+  if (threadIdx.x == 0) *at_head<D, BR>(p) = AttendHead{parts > 0, before, {0, 0}};
 }
 
 // ---------------------------------------------------------------------------
@@ -414,18 +571,13 @@ struct AttendBlock {
 
 template <int D, int BR>
 __device__ __forceinline__ bool at_block(const AttendParams& p, AttendBlock* k) {
-  if (!at_unit<BR>(p, blockIdx.x, &k->u)) return false;
+  if (!at_unit<D, BR>(p, blockIdx.x, &k->u)) return false;
   k->G = p.q_heads / p.kv_heads;
   k->R = k->u.seq.rows * k->G;
   const int blocks = (k->R + BR - 1) / BR, hs = k->u.local / blocks;
   k->blk = blocks - 1 - k->u.local % blocks;     // the longest first
   k->h = hs / k->u.splits;
   k->split = hs % k->u.splits;
-  if (p.target > 0 && k->u.local == 0 && threadIdx.x == 0) {
-    int* cut = at_cuts<D, BR>(p) + 2 * k->u.b;
-    cut[0] = k->u.part;
-    cut[1] = k->u.splits;
-  }
   const int end_row = k->blk * BR + BR < k->R ? k->blk * BR + BR : k->R;
   const int seen = p.causal ? k->u.seq.len - k->u.seq.rows + (end_row - 1) / k->G + 1 : k->u.seq.len;
   const int tiles = seen > 0 ? (seen + C4_TILE - 1) / C4_TILE : 0;   // (early rows may see none)
@@ -974,26 +1126,13 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void attend_join_kernel(Atte
   const int at = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;   // of all rows' query heads
   if (at >= p.n * p.q_heads) return;
   const int row = at / p.q_heads, head = at - row * p.q_heads, G = p.q_heads / p.kv_heads;
+  if (at_head<D, BR>(p)->cut == 0) return;
   // the row's sequence
-  int b = row;
-  AttendSeq s{row, 1, 0};
-  if (p.q_offsets != nullptr) {
-    b = -1;
-    for (int b0 = 0; b0 < p.batch && b < 0; b0 += 64) {
-      AttendSeq o{0, 0, 0};
-      if (b0 + lane < p.batch) o = at_seq(p, b0 + lane);
-      const uint64_t found = __ballot(row >= o.q0 && row < o.q0 + o.rows);
-      if (found != 0) {
-        const int l = __ffsll((unsigned long long)found) - 1;
-        b = b0 + l;
-        s.q0 = __builtin_amdgcn_readlane(o.q0, l);
-        s.rows = __builtin_amdgcn_readlane(o.rows, l);
-      }
-    }
-    if (b < 0) return;
-  }
-  const int* cut = at_cuts<D, BR>(p) + 2 * b;
-  const int part = cut[0], splits = cut[1];
+  const int b = p.q_offsets == nullptr
+                    ? row : at_search(p.batch, [&](int i) { return p.q_offsets[i] <= row; });
+  const AttendSeq s = at_seq(p, b);
+  if (row < s.q0 || row >= s.q0 + s.rows) return;
+  const int part = at_cuts<D, BR>(p)[b].part, splits = at_cuts<D, BR>(p)[b].splits;
   if (splits <= 1 || splits > 2 * p.target) return;
   const int blocks = (s.rows * G + BR - 1) / BR;
   const int h = head / G, r = (row - s.q0) * G + head - h * G, blk = r / BR;
@@ -1115,7 +1254,7 @@ static int few_tiles(int dt, int d, int rows) {
 // were they all that long, or where one long sequence among short ones could keep a few
 // workgroups busy by itself (one of 131072 tokens among 127 of 1000, 8 key heads: 631 us
 // whole, 64 cut); the kernel then decides by the lengths (at_unit), and a join with nothing
-// to do takes 4 to 5 us (256 rows of 500 tokens 37 -> 42).
+// to do takes 4 to 5 us with the plan (64 rows of 1000 tokens 12 -> 18).
 static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
                               int64_t tokens) {
   const int64_t rows = n * (q_heads / kv_heads), each = (rows + batch - 1) / batch;
@@ -1129,7 +1268,8 @@ static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_
   const double turns = (double)((tokens + C4_TILE - 1) / C4_TILE) * a.tile_us;
   const double blocks = (double)((each + a.block - 1) / a.block) * kv_heads;   // of a sequence
   if ((1.0 - blocks * batch / a.target) * turns <= 4.0 + a.join_us &&
-      (a.tiles == 0 || (1.0 - blocks / a.target) * turns <= 40.0 + a.join_us))
+      (a.tiles == 0 || batch > 1 << 17 ||
+       (1.0 - blocks / a.target) * turns <= 40.0 + a.join_us))
     a.target = 0;
   a.units = (rows / a.block + batch) * kv_heads + (a.target > 0 ? a.target + 64 : 0);
   return a;
@@ -1138,13 +1278,21 @@ static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_
 size_t attend_workspace(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
                         int64_t tokens) {
   const AttendPlan a = attend_plan(dt, n, batch, q_heads, kv_heads, d, tokens);
-  return a.target == 0 ? 0 : (size_t)2 * a.target * a.block * (d + 2) * 4 + (size_t)batch * 8;
+  return a.target == 0 ? 0 : (size_t)2 * a.target * a.block * (d + 2) * 4 +
+                               sizeof(AttendHead) + sizeof(AttendCut) * batch;
+}
+
+template <int D, int BR>
+static hipError_t launch_plan(const AttendParams& p, hipStream_t st) {
+  if (p.target == 0 || p.batch <= AT_INLINE) return hipSuccess;
+  return launch_kernel(attend_plan_kernel<D, BR>, dim3(1), dim3(1024), 0, st, p);
 }
 
 template <int DT, int D, int RT>
 static hipError_t launch_few(const AttendPlan& a, const AttendParams& p, dim3 grid, hipStream_t st) {
-  const hipError_t e = launch_kernel(attend_few_kernel<DT, D, RT>, grid, dim3(64 * AF_WAVES), 0,
-                                     st, p);
+  hipError_t e = launch_plan<D, 16 * RT>(p, st);
+  if (e == hipSuccess)
+    e = launch_kernel(attend_few_kernel<DT, D, RT>, grid, dim3(64 * AF_WAVES), 0, st, p);
   if (e != hipSuccess || a.target == 0) return e;
   // a wave a row where that fills the chip, else as many as do
   const int64_t rows = (int64_t)p.n * p.q_heads;
@@ -1167,6 +1315,7 @@ static hipError_t launch_attend_d(AttendParams p, hipStream_t st) {
   p.target = a.target;
   p.tile_us = a.tile_us;
   p.join_us = a.join_us;
+  p.pad = a.block - std::gcd(p.q_heads / p.kv_heads, a.block);
   const dim3 grid((unsigned)((a.units + 7) / 8 * 8));
   // (what few_tiles chooses, and nothing else, is built)
   if (a.tiles == 1) return launch_few<DT, D, 1>(a, p, grid, st);
@@ -1177,10 +1326,11 @@ static hipError_t launch_attend_d(AttendParams p, hipStream_t st) {
   if constexpr (DT == DT_BF16 && D == 64)
     if (a.tiles == 4) return launch_few<DT, D, 4>(a, p, grid, st);
   if constexpr (D == 128 || (DT == DT_BF16 && D == 256)) {
-    const hipError_t e =
-        launch_kernel(attend_many_kernel<DT, D>, grid, dim3(64 * AM_WAVES), 0, st, p);
-    if (e != hipSuccess || a.target == 0) return e;
     constexpr int BLOCK = 16 * AM_WAVES * am_row_tiles(DT, D);
+    hipError_t e = launch_plan<D, BLOCK>(p, st);
+    if (e == hipSuccess)
+      e = launch_kernel(attend_many_kernel<DT, D>, grid, dim3(64 * AM_WAVES), 0, st, p);
+    if (e != hipSuccess || a.target == 0) return e;
     const dim3 four((unsigned)(((int64_t)p.n * p.q_heads + 3) / 4));
     return launch_kernel(attend_join_kernel<DT, D, BLOCK, 1>, four, dim3(256), 0, st, p);
   }

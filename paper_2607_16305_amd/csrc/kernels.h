@@ -409,6 +409,7 @@ struct AttendParams {
   float scale_log2;
   int target;                // work units that the cut of the keys aims at; 0: no cut
   float tile_us, join_us;    // estimates of the time of a unit's tile and of the join
+  int pad;                   // rows that a unit may hold beside whole rows' query heads
 };
 // Bytes of workspace of a call (0: none needed).
 size_t attend_workspace(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,

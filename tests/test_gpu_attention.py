@@ -303,6 +303,26 @@ def test_the_lengths_choose_whether_keys_are_cut(seqs, hq, hkv, d):
     assert torch.equal(out, _run(q.cuda(), cache, table, seqs))
 
 
+@pytest.mark.parametrize("wide", [False, True], ids=["narrow", "wide"])
+@pytest.mark.parametrize("hq,hkv", [(14, 2), (4, 4), (12, 1)])
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "bf16"), (256, "f32")])
+def test_many_sequences(d, dtype, hq, hkv, wide):
+    """more sequences than a wave has lanes: without rows, without tokens, and a long one"""
+    g = _gen(hq)
+    rows = torch.tensor([0, 1, 1, 2, 5, 11])[torch.randint(0, 6, (90,), generator=g)].tolist()
+    lens = torch.randint(0, 150, (90,), generator=g).tolist()
+    rows[-3:], lens[70] = [0, 3, 0], 1800
+    seqs = list(zip(rows, lens))
+    cache, table, _, vals = _sequences(seqs, hkv, d, 32)
+    if wide:
+        table = torch.cat([table, torch.full((90, 9000), -7, dtype=I32)], 1)
+    n = sum(rows)
+    q = torch.randn((n + 40, hq, d), generator=g).to(DT[dtype])
+    out = _run(q.cuda(), cache, table, seqs)
+    assert (out[n:] == 7).all()
+    _check(out[:n], q, vals, seqs, True, d ** -0.5)
+
+
 def test_rows_apart_in_place_and_without_offsets():
     seqs = [(1, 77), (1, 1200), (1, 0)]
     cache, table, _, vals = _sequences(seqs, 2, 128, 64)
@@ -418,22 +438,24 @@ def test_exact_averages():
             assert (out.double().cpu() - want).abs().max() <= A.HALF[dt] * want
 
 
+@pytest.mark.parametrize("wide", [0, 600])
+@pytest.mark.parametrize("batch", [32, 80])
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("m", [3, 20, 200])
-def test_sequences_that_share_rows_stay_in_their_memory(m, d):
+def test_sequences_that_share_rows_stay_in_their_memory(m, d, batch, wide):
     """offsets that are not ascending: what such rows get is not specified, the rest of
     the outputs and of the workspace is left as it was"""
-    seqs = [(m, 700)] * 32
-    cache, table, _, _ = _sequences(seqs, 2, d, 64)
-    table = torch.cat([table, torch.full((32, 600), -7, dtype=I32)], 1)
+    cache = torch.full(lk.cache_shape(40, 2, 64, d), 120, dtype=torch.uint8, device="cuda")
+    table = torch.randint(0, 40, (batch, 11 + wide), generator=_gen(m), dtype=I32)
     q = torch.randn((m + 3, 8, d), generator=_gen(4)).bfloat16().cuda()
-    off = torch.tensor([0, m] * 16 + [m + 1], dtype=I32).cuda()   # (the last has a row of its own)
-    lens = torch.full((32,), 700, dtype=I32).cuda()
-    need = lk.lookme_cache_attention_workspace(1, m + 3, 32, 8, 2, d, table.shape[1], 64)
+    off = torch.tensor([0, m] * (batch // 2) + [m + 1], dtype=I32).cuda()   # (the last: its own)
+    lens = torch.full((batch,), 700, dtype=I32).cuda()
+    need = lk.lookme_cache_attention_workspace(1, m + 3, batch, 8, 2, d, table.shape[1], 64)
     for fill in (0, 255, 1):              # (what an earlier call may have left in the workspace)
         out = torch.full_like(q, 7.0)
         ws = torch.full((need + 4096,), fill, dtype=torch.uint8, device="cuda")
-        lk.cache_attention(q, cache, table.cuda(), lens, out, ws[:need], q_offsets=off)
+        lk.cache_attention(q, cache, table.cuda(), lens, out, ws[:need] if need else ws,
+                           q_offsets=off)
         assert (out[m + 1:] == 7).all() and (ws[need:] == fill).all()
 
 

@@ -794,7 +794,7 @@ __device__ __forceinline__ void at_issue(const uint8_t* tile, char* dst) {
 // sums in the matrix cores 104; rare cases (masks, blocks that are not finite) out of
 // everybody's way 97.  Rings of 3 tiles and 8 waves were no faster.  64 sequences of up to
 // 8192 tokens, 290 MB, take 54.  300 rows of 16 heads of 64 over up to 2880 tokens, 8
-// sequences, take 41 to 45: matrix cores 0.22, the rest unpacking, exponentials and the
+// sequences, take 36 to 40: matrix cores 0.21, the rest unpacking, exponentials and the
 // uneven end.
 template <int DT, int D, int RT>
 __global__ __launch_bounds__(64 * AF_WAVES, af_occupancy(DT, D, RT))
@@ -1227,22 +1227,22 @@ static int many_block(int dt, int d) {
 }
 
 // Row tiles of a unit of attend_few_kernel for `rows` rows of a sequence and key head; 0:
-// attend_many_kernel.  A few-rows unit unpacks a tile of the cache once for its 16 to 64
-// rows, without a barrier; a many-rows unit once for 64 or 128, through LDS.  More row
-// tiles are better as long as the registers hold them (bf16 and 64 dims 4, 128 dims 3,
-// 256 dims 2; float32 2, 256 dims 1), and padded rows cost what rows cost.  Both sides
-// (us, 16 sequences x 8192 tokens x 4 heads of 128): 32 rows 33 and 55, 48 rows 36 and
-// 57, 80 rows 50 and 62, 128 rows 82 and 70; 16 x 8 heads of 256 over 4096 tokens: 36 rows
-// 68 and 83, 100 rows 126 and 107; float32, 128 dims: 36 rows 62 and 67, 2048 rows 404
-// and 337; 256 dims: 36 rows 123 and 129, 1024 rows 455 and 456.  64 dims have no
-// many-rows kernel: 2048 rows took it 127 us, this one 102 (float32 219 and 204).  Of 3 and
-// 4 tiles of 64 dims the rows of 4 cost 13 / 16 of the time.
-static int few_tiles(int dt, int d, int rows) {
+// attend_many_kernel.  A few-rows unit unpacks a tile of the cache once for its 16 to 48
+// rows, without a barrier; a many-rows unit once for 64 or 128, through LDS.  Two tiles keep
+// two or three waves a SIMD, three save a block where two would hold padding.  Both sides
+// (us, 16 sequences x 8192 tokens x 4 heads of 128): 32 rows, two tiles and many 33 and 55;
+// 48 rows, three, two and many 36, 41, 57; 64 rows 50, 41, 60; 80 rows 50, 67, 62; 128 rows 83,
+// 68, 70; 200 rows of 32 x 16 heads over 1500 tokens 145, 161, 138; 16 x 8 heads of 256
+// over 4096 tokens: 36 rows, two and many 68 and 83, 100 rows 126 and 107; float32, 128
+// dims: 36 rows 62 and 67, 2048 rows 404 and 337; 256 dims, one and many: 36 rows 123 and
+// 129, 1024 rows 455 and 456.  64 dims have no many-rows kernel: 2048 rows took it 127 us,
+// two tiles take 107 and four 101, but 300 rows of 8 x 16 heads over 2880 tokens 40 and
+// 45, 64 rows of 20 x 16 heads over 4000 34 and 50 (float32 219 with it, two tiles 182).
+static int few_tiles(int dt, int d, int64_t rows) {
   if (rows <= 16 || (dt == DT_F32 && d == 256)) return 1;
-  if (rows <= 32 || (dt == DT_F32 && d == 64)) return 2;
-  if (d == 64) return (rows + 47) / 48 * 13 < (rows + 63) / 64 * 16 ? 3 : 4;
+  if (rows <= 32 || d == 64) return 2;
   if (dt == DT_F32 || d == 256) return rows <= 64 ? 2 : 0;
-  return rows <= 96 ? 3 : 0;
+  return rows <= 48 ? 3 : rows <= 64 ? 2 : rows <= 96 ? 3 : 0;
 }
 
 // The keys are cut where that saves more than it costs.  It saves a unit's turns (tile_us a
@@ -1259,7 +1259,11 @@ static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_
                               int64_t tokens) {
   const int64_t rows = n * (q_heads / kv_heads), each = (rows + batch - 1) / batch;
   AttendPlan a{};
-  a.tiles = few_tiles(dt, d, (int)(each < 65536 ? each : 65536));
+  a.tiles = few_tiles(dt, d, each);
+  // many rows, but too few for most of the chip, over few tokens: more and shorter units
+  // (500 rows of 8 heads over 500 tokens 12 us, as many rows 20)
+  const int64_t large = ((each + many_block(dt, d) - 1) / many_block(dt, d)) * batch * kv_heads;
+  if (a.tiles == 0 && large <= 120 && tokens <= 64 * C4_TILE) a.tiles = 2;
   a.block = a.tiles > 0 ? 16 * a.tiles : many_block(dt, d);
   // (one round of resident workgroups; 512 of 128 rows and 128 dims are 68 MB)
   a.target = a.tiles > 0 ? 256 * af_occupancy(dt, d, a.tiles) : d == 128 ? 480 : 448;
@@ -1321,10 +1325,8 @@ static hipError_t launch_attend_d(AttendParams p, hipStream_t st) {
   if (a.tiles == 1) return launch_few<DT, D, 1>(a, p, grid, st);
   if constexpr (DT == DT_BF16 || D < 256)
     if (a.tiles == 2) return launch_few<DT, D, 2>(a, p, grid, st);
-  if constexpr (DT == DT_BF16 && D < 256)
+  if constexpr (DT == DT_BF16 && D == 128)
     if (a.tiles == 3) return launch_few<DT, D, 3>(a, p, grid, st);
-  if constexpr (DT == DT_BF16 && D == 64)
-    if (a.tiles == 4) return launch_few<DT, D, 4>(a, p, grid, st);
   if constexpr (D == 128 || (DT == DT_BF16 && D == 256)) {
     constexpr int BLOCK = 16 * AM_WAVES * am_row_tiles(DT, D);
     hipError_t e = launch_plan<D, BLOCK>(p, st);

@@ -1004,7 +1004,9 @@ void attend_many_kernel(AttendParams p) {
 
   // In one turn, of tile t: the scores of tile t + 1 (matrix cores) beside the weights of t
   // (vector instructions), then the outputs of t beside the unpacking of k of t + 2 and
-  // v of t + 1 into the halves of LDS that the last turn has read; one barrier.
+  // v of t + 1 into the halves of LDS that were read before the last barrier: a half is
+  // never written before one that follows its last reading.  One barrier a turn, and one
+  // between the scores of the first tile and turn 0.
   char* const lds_k = smem;
   char* const lds_v = smem + STAGE;
   constexpr int HALF = STAGE / 2;
@@ -1064,6 +1066,7 @@ void attend_many_kernel(AttendParams p) {
     share.load_scales(tile, vs_odd);
     __syncthreads();
     scores(s_even, lds_k);
+    __syncthreads();   // (turn 0 writes k of tile 2 where these were read)
     seen(s_even, 0, id);
     hole1 = __any(at_hole(vs_even));
     // (even and odd turns: what is loaded or computed for a later one keeps its registers)
@@ -1214,14 +1217,6 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void attend_join_kernel(Atte
 // ---------------------------------------------------------------------------
 // launch
 // ---------------------------------------------------------------------------
-struct AttendPlan {
-  int tiles;        // row tiles of a unit of few rows; 0: many, the waves share the keys
-  int block;        // rows of a unit
-  int target;       // units that the cut aims at; 0: no cut
-  int64_t units;    // workgroups
-  float tile_us, join_us;   // what a tile and a join take, for at_unit
-};
-
 static int many_block(int dt, int d) {
   return 16 * AM_WAVES * am_row_tiles(dt, d);
 }
@@ -1255,8 +1250,8 @@ static int few_tiles(int dt, int d, int64_t rows) {
 // workgroups busy by itself (one of 131072 tokens among 127 of 1000, 8 key heads: 631 us
 // whole, 64 cut); the kernel then decides by the lengths (at_unit), and a join with nothing
 // to do takes 4 to 5 us with the plan (64 rows of 1000 tokens 12 -> 18).
-static AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
-                              int64_t tokens) {
+AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
+                       int64_t tokens) {
   const int64_t rows = n * (q_heads / kv_heads), each = (rows + batch - 1) / batch;
   AttendPlan a{};
   a.tiles = few_tiles(dt, d, each);

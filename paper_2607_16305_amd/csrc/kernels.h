@@ -411,6 +411,16 @@ struct AttendParams {
   float tile_us, join_us;    // estimates of the time of a unit's tile and of the join
   int pad;                   // rows that a unit may hold beside whole rows' query heads
 };
+// How a call's rows and keys are shared out.
+struct AttendPlan {
+  int tiles;        // row tiles of a unit of few rows; 0: many, the waves share the keys
+  int block;        // rows of a unit
+  int target;       // units that the cut aims at; 0: no cut
+  int64_t units;    // workgroups
+  float tile_us, join_us;   // what a tile and a join take, for at_unit
+};
+AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
+                       int64_t tokens);
 // Bytes of workspace of a call (0: none needed).
 size_t attend_workspace(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
                         int64_t tokens);

@@ -1,5 +1,6 @@
 """Attention's kernel of many rows on the GPU against a plain float64 form: whole keys
-and cut ones, few sequences and more than a wave has lanes.  Every call asks the rule whether that kernel runs."""
+and cut ones, few sequences and more than a wave has lanes, blocks that are not finite,
+pages out of range, captured graphs.  Every call asks the rule whether that kernel runs."""
 
 import pytest
 import torch
@@ -12,6 +13,7 @@ pytestmark = pytest.mark.gpu
 
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 I32 = torch.int32
+NAN = float("nan")
 
 
 def _gen(seed=0):
@@ -118,3 +120,85 @@ def test_the_first_tiles_decide(name, dtype, d):
     c.check(out, False)
     for _ in range(50):
         assert torch.equal(out, c.run(False, q))
+
+
+@pytest.mark.parametrize("dtype,d", M.MANY)
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("name", list(M.CALLS))
+def test_blocks_that_are_not_finite_reach_only_the_rows_that_see_them(name, what, dtype, d):
+    """one that the last two rows of every sequence see, in a tile that others see too, and
+    one in an early tile of some sequences that all rows but the first ones see"""
+    c = Call(name, dtype, d)
+    good = c.run(True)
+    want = [M.attention(c.q[c.rows(b)], A.value(*A.quantize(c.k[b])), A.value(*A.quantize(c.v[b])),
+                        c.scale, True) for b in range(len(c.seqs))]
+    hit = torch.zeros(c.n, dtype=torch.bool)
+    for b, (m, n) in enumerate(c.seqs):
+        for bad in [n - 2] + ([n - m + 3] if b % 3 == 0 else []):
+            if m >= 8 and 0 <= bad < n:
+                (c.k if what == "k" else c.v)[b][bad, 0, 33] = NAN
+                hit[c.offsets[b] + max(0, bad - (n - m)):c.offsets[b + 1]] = True
+    c.write()
+    out = c.run(True).cpu()
+    good, G = good.cpu(), c.hq // c.hkv
+    assert hit.any() and not hit.all()
+    assert torch.equal(out[:c.n, G:], good[:c.n, G:])                # the other key heads
+    if what == "v":
+        assert torch.equal(out[:c.n][~hit], good[:c.n][~hit])
+    else:                  # (rows of a wave renew their maxima together)
+        for b in range(len(c.seqs)):
+            at = c.rows(b)
+            far = (out[at].double() - want[b][0]).abs() - want[b][1]
+            assert not far[~hit[at]].isnan().any() and (far[~hit[at]] <= 0).all()
+    out, good = out[:c.n][hit][:, :G], good[:c.n][hit][:, :G]
+    if what == "k":
+        assert out.isnan().all()
+    else:                              # value 33 is in the second block of 32
+        assert out[..., 32:64].isnan().all()
+        rest = [i for i in range(d) if not 32 <= i < 64]
+        assert torch.equal(out[..., rest], good[..., rest])
+
+
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "cross"])
+@pytest.mark.parametrize("garbage", [255, 120])
+@pytest.mark.parametrize("dtype,d", M.MANY)
+@pytest.mark.parametrize("name", list(M.CALLS))
+def test_pages_out_of_range(name, dtype, d, garbage, causal):
+    """the first, a middle and the last page of some sequences, and all of one's, are none"""
+    c = Call(name, dtype, d, garbage=garbage)
+    keep = [torch.ones(n, dtype=torch.bool) for _, n in c.seqs]
+    none = [-1, c.num_pages, 2 ** 31 - 1]
+    for b, (m, n) in enumerate(c.seqs):
+        pages = -(-n // M.PAGE)
+        lost = [[0], [pages // 2], [pages - 1], [0, 1, pages - 1], range(pages)][b % 5]
+        for p in lost:
+            if 0 <= p < pages:
+                c.table[b, p] = none[p % 3]
+                keep[b][p * M.PAGE:(p + 1) * M.PAGE] = False
+    c.check(c.run(causal), causal, keep)
+
+
+@pytest.mark.parametrize("dtype,d", M.MANY)
+@pytest.mark.parametrize("name", ["whole, many sequences", "cut", "cut, many sequences"])
+def test_captured(name, dtype, d):
+    """replays with other queries, eager calls and synchronizations between them, in place"""
+    c = Call(name, dtype, d)
+    x = c.q.cuda()
+    table = c.table.cuda()
+
+    def call():
+        lk.cache_attention(x, c.cache, table, c.args[0], x, c.ws, q_offsets=c.args[1],
+                           scale=c.scale)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        q = torch.randn(c.q.shape, generator=_gen(i)).to(c.dt).cuda()
+        want = c.run(True, q)
+        x.copy_(q)
+        graph.replay()
+        assert torch.equal(x[:c.n], want[:c.n]) and torch.equal(x[c.n:], q[c.n:])
+        torch.cuda.synchronize()

@@ -726,7 +726,9 @@ lookme_status_t lookme_head_norm_rotary(int32_t dtype, int64_t n, int32_t head_d
  * 3, 4, 6.  The byte is the smallest E + 127 with max|x| <= 7 2^E, in [27, 252]
  * (below, values become zeros; above, they saturate at 6 2^125), or 255 where one
  * of the 32 is not finite: the block then reads as NaN.  The code is the nearest
- * value's, of two as near the even code.
+ * value's, of two as near the even code.  Other bytes are not written; in memory
+ * that was never written they may stand, and only a row of lookme_cache_attention
+ * that sees a block with one gets values that are not specified.
  *   A tile of 32 tokens of a head, d = head_dim, u = d / 16; dim, dim + 1 of an
  * even dim share a byte, dim in its low half:
  *   k of token t:  byte t d/2 + (dim % 32 / 8) d/8 + (dim / 32) 4 + dim % 8 / 2

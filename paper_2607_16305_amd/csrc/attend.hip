@@ -436,8 +436,8 @@ struct AttendRows {
           if (t0 + 16 * half + 4 * c + i > last[rt]) s[rt][half][i] = -INFINITY;
   }
 
-  // NaN into the dims of the blocks of v that are not finite (byte 255 among the tile's
-  // scales) of rows that see them.  The products take such blocks as zeros, which
+  // NaN into the dims of the blocks of v that are not finite (a byte above C4_HIGHEST among
+  // the tile's scales) of rows that see them.  The products take such blocks as zeros, which
   // would meet weights of 0 otherwise.
   __device__ __forceinline__ void holes(const uint8_t* scales, int t0) {
     const int c = (threadIdx.x & 63) >> 4;
@@ -448,7 +448,7 @@ struct AttendRows {
       uint32_t vs[2];
       at_load_words(vs, scales + g * 32 + c * 8);
       for (int x = 0; x < 8; ++x) {
-        const bool hole = ((vs[x / 4] >> (8 * (x % 4))) & 0xFFu) == (uint32_t)C4_NAN;
+        const bool hole = ((vs[x / 4] >> (8 * (x % 4))) & 0xFFu) > (uint32_t)C4_HIGHEST;
         const int token = t0 + 4 * c + x % 4 + 16 * (x / 4);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
@@ -706,10 +706,12 @@ __device__ __forceinline__ void at_store(const AttendParams& p, const AttendBloc
   }
 }
 
-// Whether one of 8 scale bytes is 255 (its complement is 0)
+// Whether one of 8 scale bytes is above C4_HIGHEST (its complement below 3): 255, or what no
+// write leaves, 253 and 254, whose larger values bf16 cannot hold
 __device__ __forceinline__ bool at_hole(const uint32_t (&vs)[2]) {
   const uint32_t a = ~vs[0], b = ~vs[1];
-  return ((((a - 0x01010101u) & ~a) | ((b - 0x01010101u) & ~b)) & 0x80808080u) != 0;
+  constexpr uint32_t BELOW = (255 - C4_HIGHEST) * 0x01010101u;
+  return ((((a - BELOW) & ~a) | ((b - BELOW) & ~b)) & 0x80808080u) != 0;
 }
 
 // Zeros in the place of the lane's tokens whose block of v is not finite, or which lie
@@ -723,7 +725,7 @@ __device__ __forceinline__ void at_fill_holes(uint32_t (&v)[D / 16], uint32_t (&
   for (int x = 0; x < 8; ++x) {
     const int token = t0 + 4 * c + x % 4 + 16 * (x / 4), bit = 8 * (x % 4);
     asm volatile("");   // (rare: not to be turned into selects on everybody's way)
-    if (token >= len || ((vs[x / 4] >> bit) & 0xFFu) == (uint32_t)C4_NAN) {
+    if (token >= len || ((vs[x / 4] >> bit) & 0xFFu) > (uint32_t)C4_HIGHEST) {
       vs[x / 4] = (vs[x / 4] & ~(0xFFu << bit)) | (127u << bit);
       if constexpr (U == 4) {
         v[x / 2] &= x % 2 == 0 ? 0xFFFF0000u : 0x0000FFFFu;

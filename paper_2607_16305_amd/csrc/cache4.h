@@ -22,6 +22,7 @@ namespace lookme {
 
 constexpr int C4_TILE = 32;            // tokens
 constexpr int C4_NAN = 255;            // scale byte of a block that is not finite
+                                       // (so reads any above C4_HIGHEST)
 constexpr int C4_LOWEST = 127 - 100;   // smallest scale byte: smaller values become zeros
 constexpr int C4_HIGHEST = 127 + 125;  // largest: 6 2^125 is finite, larger values saturate
 
@@ -49,7 +50,7 @@ __device__ __forceinline__ int c4_scale(uint32_t amax_bits) {
   return e < C4_LOWEST ? C4_LOWEST : e > C4_HIGHEST ? C4_HIGHEST : e;
 }
 __device__ __forceinline__ float c4_power(int byte) {
-  return byte == C4_NAN ? as_f32(0x7FC00000u) : as_f32((uint32_t)byte << 23);
+  return byte > C4_HIGHEST ? as_f32(0x7FC00000u) : as_f32((uint32_t)byte << 23);
 }
 
 // two values from byte SEL of w: bf16, exact

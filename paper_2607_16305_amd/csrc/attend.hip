@@ -34,6 +34,10 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 // 2^AT_SLACK.
 constexpr int AT_MIN_TILES = 4;
 constexpr float AT_SLACK = 8.f;
+// Scaled scores beyond this leave a weight's exponent to the rounding of the maximum.  Float32
+// scores that differ are 2^6 apart there, so that any scale that keeps the maximum exact gives
+// their weights: the next power of two.
+constexpr float AT_WIDE = 1073741824.f;
 constexpr int AT_UNITS_OF_SEQ = 1 << 24;
 constexpr int AT_INLINE = 64;    // sequences that a unit looks at by itself
 
@@ -412,13 +416,15 @@ struct AttendRows {
   static constexpr int U = D / 16;
   f32x4_t acc[RT][U + 1];
   float top[RT], next[RT], base[RT];   // maximum, where it is renewed, in powers of two
+  float scl[RT];                       // that a score has for a power of two
   int last[RT];                        // the last token that the row sees
 
-  __device__ __forceinline__ void clear() {
+  __device__ __forceinline__ void clear(float scale) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       top[rt] = next[rt] = -INFINITY;
       base[rt] = 0.f;
+      scl[rt] = scale;
 #pragma unroll
       for (int m = 0; m <= U; ++m) acc[rt][m] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
@@ -470,7 +476,8 @@ struct AttendRows {
   // The maximum is renewed, and what there is rescaled, only when a score has passed
   // it by 2^AT_SLACK: the weights stay far from float32's ends, and most tiles need
   // neither.
-  __device__ __forceinline__ void renew(const f32x4_t (&s)[RT][2], float scl, float slack) {
+  __device__ __forceinline__ void renew(const f32x4_t (&s)[RT][2], const AttendParams& p,
+                                        float slack) {
     float mx[RT];
     bool grown = false;
 #pragma unroll
@@ -484,7 +491,12 @@ struct AttendRows {
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         const float now = fmaxf(top[rt], at_row_max(mx[rt]));
-        const float b = now == -INFINITY ? 0.f : now * scl;
+        // (finite, so that scaled scores past float32 are what their infinities would be:
+        // minus weighs 0, plus gives NaN)
+        const bool wide = now != -INFINITY && fabsf(now * p.scale_log2) > AT_WIDE;
+        scl[rt] = wide ? p.scale_wide : p.scale_log2;
+        const float b = now == -INFINITY ? 0.f
+                                         : fminf(fmaxf(now * scl[rt], -__FLT_MAX__), __FLT_MAX__);
         const float f = top[rt] == -INFINITY ? 0.f : exp2f(base[rt] - b);
         top[rt] = now;
         next[rt] = now + slack;
@@ -497,14 +509,14 @@ struct AttendRows {
 
   // Scores into weights 2^(s scl - base)
   template <int DT>
-  __device__ __forceinline__ void weights(const f32x4_t (&s)[RT][2], float scl,
+  __device__ __forceinline__ void weights(const f32x4_t (&s)[RT][2],
                                           u32x4_t (&w)[RT][at_terms<DT>()]) const {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       float e[8];
 #pragma unroll
       for (int x = 0; x < 8; ++x)
-        e[x] = __builtin_amdgcn_exp2f(fmaf(s[rt][x / 4][x % 4], scl, -base[rt]));
+        e[x] = __builtin_amdgcn_exp2f(fmaf(s[rt][x / 4][x % 4], scl[rt], -base[rt]));
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         uint32_t o[at_terms<DT>()];
@@ -812,14 +824,14 @@ void attend_few_kernel(AttendParams p) {
   if (!at_block<D, BR>(p, &k)) return;
   const int row0 = k.blk * BR;
   AttendRows<D, RT> rows;
-  rows.clear();
+  rows.clear(p.scale_log2);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = row0 + rt * 16 + j;
     rows.last[rt] = r < k.R ? at_last(p, k, r) : -1;
   }
   const int full = at_last(p, k, row0);      // every row sees the tokens up to here
-  const float scl = p.scale_log2, slack = fminf(AT_SLACK / scl, 1e38f);
+  const float slack = fminf(AT_SLACK / p.scale_log2, 1e38f);
   const AttendPages<D> pages(p, k);
 
   // The wave's own ring: NB - 1 tiles on their way while one is multiplied, no barrier,
@@ -875,9 +887,9 @@ void attend_few_kernel(AttendParams p) {
         if (hole) rows.holes(tile + 33 * D, t0);
         at_fill_holes<D>(cur.v, cur.vs, t0, k.u.seq.len);
       }
-      rows.renew(s, scl, slack);
+      rows.renew(s, p, slack);
       u32x4_t w[RT][TERMS];
-      rows.template weights<DT>(s, scl, w);
+      rows.template weights<DT>(s, w);
       rows.add_ones(w);
 #pragma unroll
       for (int b = 0; b < U / 2; ++b) {
@@ -994,14 +1006,14 @@ void attend_many_kernel(AttendParams p) {
   if (!at_block<D, BR>(p, &k)) return;
   const int row0 = k.blk * BR + wave * RT * 16;
   AttendRows<D, RT> rows;
-  rows.clear();
+  rows.clear(p.scale_log2);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = row0 + rt * 16 + j;
     rows.last[rt] = r < k.R ? at_last(p, k, r) : -1;
   }
   const int full = row0 < k.R ? at_last(p, k, row0) : -1;   // every row sees the tokens up to here
-  const float scl = p.scale_log2, slack = fminf(AT_SLACK / scl, 1e38f);
+  const float slack = fminf(AT_SLACK / p.scale_log2, 1e38f);
   const AttendPages<D> pages(p, k);
 
   // In one turn, of tile t: the scores of tile t + 1 (matrix cores) beside the weights of t
@@ -1038,7 +1050,7 @@ void attend_many_kernel(AttendParams p) {
       const int t0 = (k.first + i) * C4_TILE;
       if (__builtin_expect(t0 + C4_TILE - 1 > full || !pages.held(id), 0))
         rows.mask(s, pages.held(id) ? t0 : 0x7FFFFF00);
-      rows.renew(s, scl, slack);
+      rows.renew(s, p, slack);
     };
     bool hole, hole1;   // in v of tiles i and i + 1
     auto mend = [&](int i, bool hole, uint32_t (&vs)[2]) {
@@ -1079,7 +1091,7 @@ void attend_many_kernel(AttendParams p) {
       const int id3 = pages.id(at(i + 3));
       scores(ahead, lds_k + THERE);
       u32x4_t w[RT][TERMS];
-      rows.template weights<DT>(s, scl, w);
+      rows.template weights<DT>(s, w);
       const char* ops = lds_v + HERE + lane * 16;
       rows.add_ones(w);
 #pragma unroll

@@ -407,6 +407,7 @@ struct AttendParams {
   int n, batch, q_heads, kv_heads, max_pages, num_pages, page_log2;
   bool causal;
   float scale_log2;
+  float scale_wide;          // the next power of two of it, for huge scores
   int target;                // work units that the cut of the keys aims at; 0: no cut
   float tile_us, join_us;    // estimates of the time of a unit's tile and of the join
   int pad;                   // rows that a unit may hold beside whole rows' query heads

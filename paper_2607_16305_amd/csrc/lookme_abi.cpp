@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -1619,8 +1620,8 @@ lookme_status_t lookme_cache_attention(int32_t dtype, int64_t n, int32_t batch, 
     return fail(LOOKME_ERR_INVALID, "%lld rows for %d sequences without q_offsets", (long long)n,
                 batch);
   const float scale_log2 = scale * 1.44269504088896340736f;
-  if (!(scale > 0.f) || !(scale_log2 - scale_log2 == 0.f))
-    return fail(LOOKME_ERR_INVALID, "scale must be positive and at most 2^127");
+  if (!(scale > 0.f) || !(scale <= 0x1p126f))
+    return fail(LOOKME_ERR_INVALID, "scale must be positive and at most 2^126");
   if (causal != 0 && causal != 1) return fail(LOOKME_ERR_INVALID, "causal must be 0 or 1");
   if (n == 0 || batch == 0) return LOOKME_OK;
   LOOKME_TRY(check_ptr(q, "q"));
@@ -1659,6 +1660,8 @@ lookme_status_t lookme_cache_attention(int32_t dtype, int64_t n, int32_t batch, 
   p.page_log2 = log2_of(page);
   p.causal = causal != 0;
   p.scale_log2 = scale_log2;
+  int exponent;
+  p.scale_wide = std::frexp(scale_log2, &exponent) == 0.5f ? scale_log2 : std::ldexp(1.f, exponent);
   return hip_status(lookme::launch_attend(dtype, head_dim, p, static_cast<hipStream_t>(stream)),
                     "attention launch");
 }

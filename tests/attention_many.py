@@ -57,7 +57,12 @@ def of(name, dtype, d):
 
 def attention(q, k, v, scale, causal, keep=None):
     """attention.attention of all rows at once, with its bound; keep [n]: tokens that are on
-    some page"""
+    some page.
+
+    The bound holds what float32 loses at its lower end too: weights are relative to a
+    maximum, up to 2^8, and add up to at least 1; what is below 2^-126 of them may be
+    flushed as a weight (three parts of a float32 one), where waves are joined, and where
+    parts of the keys are: (2 2^8 + 3) 2^-126, below 2^-116, of the sum of |v|."""
     m, hq, d = q.shape
     n, hkv = k.shape[:2]
     G = hq // hkv
@@ -81,6 +86,7 @@ def attention(q, k, v, scale, causal, keep=None):
     part = 2 * x + (seen.sum(-1)[:, None] + 64) * A.U32
     if q.dtype == torch.bfloat16:
         part = part + A.HALF[q.dtype] * (1 + 2.0 ** -7)
-    bound = part * size + A.HALF[q.dtype] * out.abs() * (1 + 2.0 ** -7) + 2.0 ** -126
+    size_all = vh.abs().sum(1, keepdim=True)
+    bound = part * size + 2.0 ** -116 * size_all + A.HALF[q.dtype] * out.abs() * (1 + 2.0 ** -7) + 2.0 ** -126
     back = lambda t: t.view(hkv, m, G, d).permute(1, 0, 2, 3).reshape(m, hq, d)  # noqa: E731
     return back(out), back(bound)

@@ -9,6 +9,7 @@ import pytest
 import torch
 
 from paper_2607_16305_amd import build
+from paper_2607_16305_amd import lookme as lk
 from tests import attention as A
 from tests import attention_many as M
 
@@ -66,3 +67,16 @@ def test_the_form_of_all_rows_is_the_form_of_each(dtype, causal):
             got = M.attention(q, k, v, 0.2, False, keep)
             want = A.attention(q, k[keep], v[keep], 0.2, False)
             assert (got[0] - want[0]).abs().max() <= 1e-12
+
+
+def test_the_largest_scale():
+    args = [1, 0, 0, 4, 2, 128, 0, 512, 0, 0, 0, 3, 8, 64, 0, None, 1, 0, 512, 0, 0]
+    for scale, status in ((2.0 ** 126, None), (2.0 ** 127, lk.LOOKME_ERR_INVALID),
+                          (1.0001 * 2.0 ** 126, lk.LOOKME_ERR_INVALID), (1e-45, None)):
+        args[15] = scale
+        if status is None:
+            lk.lookme_cache_attention(*args, stream=0)
+        else:
+            with pytest.raises(lk.LookmeError) as e:
+                lk.lookme_cache_attention(*args, stream=0)
+            assert e.value.status == status

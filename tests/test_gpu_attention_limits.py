@@ -1,5 +1,5 @@
 """Attention over the 4-bit cache at the ends of what its inputs may hold: bytes that no
-write leaves."""
+write leaves, scores at and past float32's ends."""
 
 import pytest
 import torch
@@ -97,3 +97,78 @@ def test_bytes_that_no_write_leaves_in_what_a_row_does_not_see(shape, dtype, d, 
     slot = table[0, last // 32] * 32 + last % 32
     lk.cache_read(slot[None].to(I32).cuda(), cache, v_out=got)
     assert got.isnan().all()
+
+
+@pytest.mark.parametrize("dtype,d", KINDS)
+@pytest.mark.parametrize("shape", list(SHAPES))
+def test_scores_at_the_largest_scales(shape, dtype, d):
+    """queries so small that the scaled scores are ordinary ones again: whole powers of two,
+    so that no product with a key is a float32 denormal"""
+    q, k, v, cache, table = _inputs(shape, dtype, d)
+    _fill(cache, table, k, v)
+    for scale, to in ((2.0 ** 126, -122), (2.0 ** 120, -122), (1e30, -100)):
+        small = torch.where(q < 0, -1.0, 1.0).to(q.dtype) * 2.0 ** to
+        out = _run(small, cache, table, k.shape[0], True, scale)
+        _close(out, M.attention(small, _values(k), _values(v), scale, True))
+
+
+def _check_range(out, q, k, v, scale):
+    """out of queries and keys with one element that is not zero, every row seeing every
+    token, where scaled scores may pass float32: a row with one above is NaN, those below
+    weigh nothing.  The scores that stay are one product each, exact but for a rounding that
+    tokens of the same key share, and apart by more than a weight can bridge or alike: no
+    error of theirs counts.  (The largest power of two up to which a scaled score stays, 2^126
+    or more, is the library's to choose.)"""
+    hkv, G = k.shape[1], q.shape[1] // k.shape[1]
+    kd, vd = _values(k)[..., 0], _values(v)
+    out, most = out.cpu().double(), torch.finfo(torch.float32).max
+    for h in range(q.shape[1]):
+        s = scale * q[:, h, :1].double() * kd[:, h // G]                # [rows, n]
+        log2 = s * 1.4426950408889634
+        unsure = ((s.abs() > 2.0 ** 126) & (log2.abs() <= most)).any(-1)
+        over = (log2 > most).any(-1)
+        p = torch.softmax(s.masked_fill(log2 < -most, -torch.inf), -1).nan_to_num(0)
+        want, size = p @ vd[:, h // G], p @ vd[:, h // G].abs()
+        half = A.HALF[q.dtype] * (1 + 2.0 ** -7)
+        e = (half + (len(k) + 64) * A.U32) * size + half * want.abs() + 2.0 ** -126
+        assert out[over, h].isnan().all()
+        rest = ~over & ~unsure
+        assert not ((out[:, h] - want).abs() - e)[rest].isnan().any()
+        assert (((out[:, h] - want).abs() - e)[rest] <= 0).all()
+
+
+@pytest.mark.parametrize("dtype,d", KINDS)
+@pytest.mark.parametrize("shape", list(SHAPES))
+def test_scaled_scores_past_float32(shape, dtype, d):
+    """minus infinity weighs nothing, alone it gives 0; plus infinity gives NaN"""
+    q, k, v, cache, table = _inputs(shape, dtype, d)
+    n = k.shape[0]
+    q[..., 0] = q[..., 0].abs() + 1
+    q[..., 1:] = 0
+    k[:, :, 0] = -k[:, :, 0].abs() - 1                    # every score is below zero
+    _fill(cache, table, k, v)
+    assert not _run(q * 1e20, cache, table, n, False, 1e30).any()
+    huge = [(sign * top, scale) for sign in (1, -1)
+            for top, scale in ((1.0, 2.0 ** 126), (1.0, 1e30), (1e20, 1e30))]
+    for top, scale in huge:
+        _check_range(_run(q * top, cache, table, n, False, scale), q * top, k, v, scale)
+    # some tokens with scores of zero: they share the row
+    k[torch.rand(n, generator=_gen(3)) < 0.4, :, 0] = 0
+    _fill(cache, table, k, v)
+    for top, scale in huge:
+        _check_range(_run(q * top, cache, table, n, False, scale), q * top, k, v, scale)
+
+
+@pytest.mark.parametrize("dtype,d", KINDS)
+@pytest.mark.parametrize("shape", list(SHAPES))
+def test_scores_whose_spacing_is_more_than_a_weight_can_bridge(shape, dtype, d):
+    """scaled scores from 2^12 to 2^100, positive and negative: the tokens with the largest
+    share the row, however its maximum is rounded"""
+    q, k, v, cache, table = _inputs(shape, dtype, d)
+    q[..., 0] = q[..., 0].abs() + 1
+    q[..., 1:] = 0
+    _fill(cache, table, k, v)
+    for log2 in (12, 24, 28, 29, 30, 31, 32, 36, 45, 63, 100):
+        for sign in (1.3, -1.1):
+            x, scale = q * sign, 1.7 * 2.0 ** log2
+            _check_range(_run(x, cache, table, k.shape[0], False, scale), x, k, v, scale)

@@ -394,6 +394,20 @@ __device__ __forceinline__ void at_split(float a, float b, uint32_t (&w)[at_term
   }
 }
 
+// x as three bf16 values that add up to it, also where it is infinite, or finite and the
+// nearest bf16 is not: then the first one is x cut off
+__device__ __forceinline__ void at_split_any(float a, float b, uint32_t (&w)[3]) {
+  auto first = [](float x, uint32_t near) {
+    return (near & 0x7FFFu) == 0x7F80u ? as_u32(x) >> 16 : near;
+  };
+  const uint32_t near = at_pack(a, b);
+  w[0] = first(a, near & 0xFFFFu) | first(b, near >> 16) << 16;
+  a = fabsf(a) == INFINITY ? 0.f : a - bf16lo(w[0]);
+  b = fabsf(b) == INFINITY ? 0.f : b - bf16hi(w[0]);
+  w[1] = at_pack(a, b);
+  w[2] = at_pack(a - bf16lo(w[1]), b - bf16hi(w[1]));
+}
+
 // The largest of the four lanes that hold a row
 __device__ __forceinline__ float at_row_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16, 64));
@@ -651,8 +665,8 @@ __device__ __forceinline__ void at_queries(const AttendParams& p, const AttendBl
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           uint32_t w[TERMS], x[TERMS];
-          at_split<DT>(af[2 * e], af[2 * e + 1], w);
-          at_split<DT>(bf[2 * e], bf[2 * e + 1], x);
+          at_split_any(af[2 * e], af[2 * e + 1], w);
+          at_split_any(bf[2 * e], bf[2 * e + 1], x);
 #pragma unroll
           for (int n = 0; n < TERMS; ++n) {
             q[rt][m][n][e] = w[n];

@@ -172,3 +172,33 @@ def test_scores_whose_spacing_is_more_than_a_weight_can_bridge(shape, dtype, d):
         for sign in (1.3, -1.1):
             x, scale = q * sign, 1.7 * 2.0 ** log2
             _check_range(_run(x, cache, table, k.shape[0], False, scale), x, k, v, scale)
+
+
+@pytest.mark.parametrize("dtype,d", KINDS)
+@pytest.mark.parametrize("shape", list(SHAPES))
+def test_queries_at_and_past_the_end_of_their_type(shape, dtype, d):
+    """infinite ones: a row whose scores are all minus infinity gives 0, one with plus infinity
+    NaN, the others what they were; and the largest finite ones, over keys so small that the
+    scores are ordinary"""
+    q, k, v, cache, table = _inputs(shape, dtype, d)
+    m, n, scale = q.shape[0], k.shape[0], d ** -0.5
+    k[..., 3] = k[..., 3].abs() + 1
+    _fill(cache, table, k, v)
+    good = _run(q, cache, table, n, False, scale).cpu()
+    q[0, 0, 3], q[m // 2, 1, 3], q[m - 1, -1, 3] = -torch.inf, torch.inf, -torch.inf
+    out = _run(q, cache, table, n, False, scale).cpu()
+    assert not out[0, 0].any() and not out[m - 1, -1].any() and out[m // 2, 1].isnan().all()
+    want = M.attention(q.nan_to_num(0, 0, 0), _values(k), _values(v), scale, False)
+    rest = torch.ones(q.shape[:2], dtype=torch.bool)
+    rest[0, 0] = rest[m // 2, 1] = rest[m - 1, -1] = False
+    assert ((out.double() - want[0]).abs() <= want[1])[rest].all()
+    assert good.isfinite().all()
+    # (a block of keys of 2^-98 and less, queries of nearly 2^128)
+    k[..., :32] *= 2.0 ** -98
+    most = torch.finfo(q.dtype).max
+    q = torch.randn(q.shape, generator=_gen(8)).to(q.dtype) * 2.0 ** 10
+    q[..., :32] = torch.where(torch.rand(q[..., :32].shape, generator=_gen(9)) < 0.5, most, -most)
+    q[..., :4] *= 0.9990234375
+    _fill(cache, table, k, v)
+    scale = 2.0 ** -33
+    _close(_run(q, cache, table, n, True, scale), M.attention(q, _values(k), _values(v), scale, True))

@@ -788,8 +788,9 @@ lookme_status_t lookme_cache_read(int32_t dtype, int64_t n, int32_t kv_heads, in
  *              may overlap on the GPU need one each.
  * float32 scores and sums; k and v are exact.  A scaled score past 2^126 may count
  * as infinite: minus infinity weighs nothing, plus infinity gives NaN.
- * bf16: p is rounded to bf16 before it multiplies v.  q_heads a multiple of kv_heads, n * q_heads at most 2^27,
- * batch * kv_heads at most 2^22, max_pages * page at most 2^30.  n = 0 does nothing.
+ * bf16: p is rounded to bf16 before it multiplies v.  q_heads a multiple of kv_heads,
+ * n * q_heads at most 2^27, batch * kv_heads at most 2^22, max_pages * page at most
+ * 2^30.  n = 0 does nothing.
  */
 lookme_status_t lookme_cache_attention(int32_t dtype, int64_t n, int32_t batch, int32_t q_heads,
                                        int32_t kv_heads, int32_t head_dim, const void* q,

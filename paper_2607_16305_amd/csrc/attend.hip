@@ -394,8 +394,8 @@ __device__ __forceinline__ void at_split(float a, float b, uint32_t (&w)[at_term
   }
 }
 
-// x as three bf16 values that add up to it, also where it is infinite, or finite and the
-// nearest bf16 is not: then the first one is x cut off
+// at_split of float32 of any size: also where it is infinite, or finite and the nearest bf16
+// is not, its first value is then what it begins with
 __device__ __forceinline__ void at_split_any(float a, float b, uint32_t (&w)[3]) {
   auto first = [](float x, uint32_t near) {
     return (near & 0x7FFFu) == 0x7F80u ? as_u32(x) >> 16 : near;
@@ -646,11 +646,12 @@ __device__ __forceinline__ void at_queries(const AttendParams& p, const AttendBl
                                            u32x4_t (&q)[RT][D / 32][at_terms<DT>()]) {
   constexpr int TERMS = at_terms<DT>(), ES = DT == DT_BF16 ? 2 : 4;
   const int lane = threadIdx.x & 63, j = lane & 15, c = lane >> 4;
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
+  // `any`: by at_split_any
+  auto load = [&](auto any, int rt) {
     const int r = row0 + rt * 16 + j, i = r < k.R ? r / k.G : 0;
     const char* src = p.q + (k.u.seq.q0 + i) * p.q_stride +
                       ((int64_t)k.h * k.G + (r < k.R ? r - i * k.G : 0)) * D * ES;
+    float most = 0.f;
 #pragma unroll
     for (int m = 0; m < D / 32; ++m) {
       if constexpr (DT == DT_BF16) {
@@ -663,10 +664,17 @@ __device__ __forceinline__ void at_queries(const AttendParams& p, const AttendBl
         }
         const f32x4_t af = __builtin_bit_cast(f32x4_t, a), bf = __builtin_bit_cast(f32x4_t, b);
 #pragma unroll
+        for (int e = 0; e < 4; ++e) most = fmaxf(fmaxf(most, fabsf(af[e])), fabsf(bf[e]));
+#pragma unroll
         for (int e = 0; e < 2; ++e) {
           uint32_t w[TERMS], x[TERMS];
-          at_split_any(af[2 * e], af[2 * e + 1], w);
-          at_split_any(bf[2 * e], bf[2 * e + 1], x);
+          if constexpr (decltype(any)::value) {
+            at_split_any(af[2 * e], af[2 * e + 1], w);
+            at_split_any(bf[2 * e], bf[2 * e + 1], x);
+          } else {
+            at_split<DT>(af[2 * e], af[2 * e + 1], w);
+            at_split<DT>(bf[2 * e], bf[2 * e + 1], x);
+          }
 #pragma unroll
           for (int n = 0; n < TERMS; ++n) {
             q[rt][m][n][e] = w[n];
@@ -675,6 +683,14 @@ __device__ __forceinline__ void at_queries(const AttendParams& p, const AttendBl
         }
       }
     }
+    return most;
+  };
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const float most = load(std::false_type(), rt);
+    constexpr float BF16_MOST = 0x1.fep127f;
+    if constexpr (DT == DT_F32)
+      if (__builtin_expect(__any(most > BF16_MOST), 0)) load(std::true_type(), rt);
   }
   // (waited for here, once: the compiler would wait for every load in the loop)
 #pragma unroll

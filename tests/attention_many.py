@@ -87,6 +87,7 @@ def attention(q, k, v, scale, causal, keep=None):
     if q.dtype == torch.bfloat16:
         part = part + A.HALF[q.dtype] * (1 + 2.0 ** -7)
     size_all = vh.abs().sum(1, keepdim=True)
-    bound = part * size + 2.0 ** -116 * size_all + A.HALF[q.dtype] * out.abs() * (1 + 2.0 ** -7) + 2.0 ** -126
+    bound = (part * size + 2.0 ** -116 * size_all +
+             A.HALF[q.dtype] * out.abs() * (1 + 2.0 ** -7) + 2.0 ** -126)
     back = lambda t: t.view(hkv, m, G, d).permute(1, 0, 2, 3).reshape(m, hq, d)  # noqa: E731
     return back(out), back(bound)

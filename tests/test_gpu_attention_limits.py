@@ -201,4 +201,5 @@ def test_queries_at_and_past_the_end_of_their_type(shape, dtype, d):
     q[..., :4] *= 0.9990234375
     _fill(cache, table, k, v)
     scale = 2.0 ** -33
-    _close(_run(q, cache, table, n, True, scale), M.attention(q, _values(k), _values(v), scale, True))
+    _close(_run(q, cache, table, n, True, scale),
+           M.attention(q, _values(k), _values(v), scale, True))

@@ -1161,16 +1161,18 @@ void attend_many_kernel(AttendParams p) {
 
 // Joins the parts of a row's keys: W waves a row and query head, 64 parts at a time
 // whose weights the lanes compute side by side (250 parts one after the other took 25 us,
-// so 6).  Bound by latency, 4 to 5 us of which 2.7 are a launch.
+// so 6).  Bound by latency, 4 to 5 us of which 2.7 are a launch.  Rows from `from` on, of all
+// rows' query heads.
 template <int DT, int D, int BR, int W>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void attend_join_kernel(AttendParams p) {
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void attend_join_kernel(AttendParams p,
+                                                                            int from) {
   constexpr int E = D / 64, AHEAD = 8;     // values of a lane, parts on their way
   typedef float fe_t __attribute__((ext_vector_type(E)));
   __shared__ fe_t accs[W][64];
   __shared__ float ms[W], ls[W];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int at = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;   // of all rows' query heads
+  const int at = from + (W == 1 ? blockIdx.x * 4 + wave : blockIdx.x);
   if (at >= p.n * p.q_heads) return;
   const int row = at / p.q_heads, head = at - row * p.q_heads, G = p.q_heads / p.kv_heads;
   if (at_head<D, BR>(p)->cut == 0) return;
@@ -1331,6 +1333,21 @@ static hipError_t launch_plan(const AttendParams& p, hipStream_t st) {
   return launch_kernel(attend_plan_kernel<D, BR>, dim3(1), dim3(1024), 0, st, p);
 }
 
+// A wave a row: 64 threads each, and a launch has under 2^32
+template <int DT, int D, int BR>
+static hipError_t launch_join(const AttendParams& p, hipStream_t st) {
+  constexpr int64_t MOST = 1 << 25;
+  const int64_t rows = (int64_t)p.n * p.q_heads;
+  for (int64_t from = 0; from < rows; from += MOST) {
+    const int64_t n = rows - from < MOST ? rows - from : MOST;
+    const dim3 grid((unsigned)((n + 3) / 4));
+    const hipError_t e =
+        launch_kernel(attend_join_kernel<DT, D, BR, 1>, grid, dim3(256), 0, st, p, (int)from);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <int DT, int D, int RT>
 static hipError_t launch_few(const AttendPlan& a, const AttendParams& p, dim3 grid, hipStream_t st) {
   hipError_t e = launch_plan<D, 16 * RT>(p, st);
@@ -1339,16 +1356,15 @@ static hipError_t launch_few(const AttendPlan& a, const AttendParams& p, dim3 gr
   if (e != hipSuccess || a.target == 0) return e;
   // a wave a row where that fills the chip, else as many as do
   const int64_t rows = (int64_t)p.n * p.q_heads;
-  const dim3 each((unsigned)rows), four((unsigned)((rows + 3) / 4));
-  if (rows >= 2048)
-    return launch_kernel(attend_join_kernel<DT, D, 16 * RT, 1>, four, dim3(256), 0, st, p);
+  if (rows >= 2048) return launch_join<DT, D, 16 * RT>(p, st);
+  const dim3 each((unsigned)rows);
   // (42 rows with up to 250 parts each took 25 us with four waves a row, 6 with
   // sixteen; 16 rows of 16 parts 4.4 and 5.4)
   const int64_t even = a.target / ((int64_t)p.batch * p.kv_heads),
                 held = ((int64_t)p.max_pages << p.page_log2) / (C4_TILE * AT_MIN_TILES);
   if (rows < 512 && even > 32 && held > 32)
-    return launch_kernel(attend_join_kernel<DT, D, 16 * RT, 16>, each, dim3(1024), 0, st, p);
-  return launch_kernel(attend_join_kernel<DT, D, 16 * RT, 4>, each, dim3(256), 0, st, p);
+    return launch_kernel(attend_join_kernel<DT, D, 16 * RT, 16>, each, dim3(1024), 0, st, p, 0);
+  return launch_kernel(attend_join_kernel<DT, D, 16 * RT, 4>, each, dim3(256), 0, st, p, 0);
 }
 
 template <int DT, int D>
@@ -1372,8 +1388,7 @@ static hipError_t launch_attend_d(AttendParams p, hipStream_t st) {
     if (e == hipSuccess)
       e = launch_kernel(attend_many_kernel<DT, D>, grid, dim3(64 * AM_WAVES), 0, st, p);
     if (e != hipSuccess || a.target == 0) return e;
-    const dim3 four((unsigned)(((int64_t)p.n * p.q_heads + 3) / 4));
-    return launch_kernel(attend_join_kernel<DT, D, BLOCK, 1>, four, dim3(256), 0, st, p);
+    return launch_join<DT, D, BLOCK>(p, st);
   }
   return hipErrorInvalidValue;   // (few_tiles gives no 0 there)
 }

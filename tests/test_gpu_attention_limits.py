@@ -1,5 +1,5 @@
 """Attention over the 4-bit cache at the ends of what its inputs may hold: bytes that no
-write leaves, scores at and past float32's ends."""
+write leaves, scores at and past float32's ends, more rows than a launch of waves has."""
 
 import pytest
 import torch
@@ -203,3 +203,34 @@ def test_queries_at_and_past_the_end_of_their_type(shape, dtype, d):
     scale = 2.0 ** -33
     _close(_run(q, cache, table, n, True, scale),
            M.attention(q, _values(k), _values(v), scale, True))
+
+
+def test_the_parts_of_more_rows_than_a_launch_are_joined():
+    """2^26 rows of query heads, a wave each, of which the first and the last sequence's have
+    cut keys: alike, so that the outputs are averages of small whole numbers"""
+    B, heads, d, page = 1 << 17, 512, 64, 1 << 20
+    plan = M.plan("bf16", B, B, heads, 1, d, 8 * page)
+    assert plan.target > 0 and B * heads * 64 >= 2 ** 32
+    cache = torch.zeros(lk.cache_shape(2, 1, page, d), dtype=torch.uint8, device="cuda")
+    k = torch.ones((page, 1, d), dtype=torch.bfloat16, device="cuda")
+    t = torch.arange(page, dtype=I32, device="cuda")
+    for p in (0, 1):
+        v = (t % 4 + 2 * p).to(k.dtype)[:, None, None].expand(page, 1, d).contiguous()
+        lk.cache_write(k, v, t + p * page, cache)
+    table = torch.zeros((B, 8), dtype=I32)
+    table[-1] = 1
+    lengths = torch.arange(B, dtype=I32) % 5
+    want = torch.tensor([0, 0, 0.5, 1.0, 1.5])[lengths.long()]
+    lengths[0] = lengths[-1] = 8 * page
+    held = _values((torch.arange(8) % 4 + torch.arange(8) // 4 * 2).float()[:, None].expand(8, 32))
+    assert held[:, 0].tolist() == [0, 1, 2, 3, 2, 3, 4, 4]      # (5 is as near to 4 as to 6)
+    want[0], want[-1] = held[:4].mean(), held[4:].mean()
+    x = torch.full((B, heads, d), 0.25, dtype=k.dtype, device="cuda")
+    ws = torch.empty(lk.LOOKME_ATTENTION_WORKSPACE, dtype=torch.uint8, device="cuda")
+    lk.cache_attention(x, cache, table.cuda(), lengths.cuda(), x, ws)
+    for part, w in zip(x.view(B, -1).split(4096), want.split(4096)):
+        assert torch.equal(part.amin(1).float().cpu(), w)
+        assert torch.equal(part.amax(1).float().cpu(), w)
+    # (the kernel did cut them: what it leaves for the join)
+    blocks = 2 * plan.target * plan.block * (d + 2) * 4
+    assert ws[blocks:blocks + 4].view(I32).item() == 1

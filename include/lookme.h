@@ -705,8 +705,9 @@ lookme_status_t lookme_quant_swiglu(int32_t dtype, int64_t n, int32_t d_in, int3
  *   axis     [rot / 2] int32 in [0, axes) (clamped), or NULL (axis 0)
  *   freq     [rot / 2] float32, finite, |pos freq| below 2^40
  * head_dim * elem_size a multiple of 16 bytes, head_dim at most 256.  A head whose
- * sum of squares passes float32's range gives y = 0.  n = 0 does nothing.  Needs no
- * handle and no workspace.
+ * sum of squares passes float32's range gives y = 0; with eps = 0, one whose mean
+ * square is below it gives infinities and NaN.  n = 0 does nothing.  Needs no handle
+ * and no workspace.
  */
 lookme_status_t lookme_head_norm_rotary(int32_t dtype, int64_t n, int32_t head_dim,
                                         int32_t q_heads, const void* q, int64_t q_stride,
@@ -787,7 +788,9 @@ lookme_status_t lookme_cache_read(int32_t dtype, int64_t n, int32_t kv_heads, in
  *              where that is 0).  Nothing is kept in it between calls, but calls that
  *              may overlap on the GPU need one each.
  * float32 scores and sums; k and v are exact.  A scaled score past 2^126 may count
- * as infinite: minus infinity weighs nothing, plus infinity gives NaN.
+ * as infinite: minus infinity weighs nothing, plus infinity gives NaN.  The sums are
+ * of weights up to 2^8 and divided at the end: they stay finite while the tokens that
+ * a row sees times the largest |v| are below 2^119.
  * bf16: p is rounded to bf16 before it multiplies v.  q_heads a multiple of kv_heads,
  * n * q_heads at most 2^27, batch * kv_heads at most 2^22, max_pages * page at most
  * 2^30.  n = 0 does nothing.

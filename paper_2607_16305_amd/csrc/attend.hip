@@ -1294,8 +1294,11 @@ static int few_tiles(int dt, int d, int64_t rows) {
 // only what the page table could hold: the call gets a join where the keys would be cut
 // were they all that long, or where one long sequence among short ones could keep a few
 // workgroups busy by itself (one of 131072 tokens among 127 of 1000, 8 key heads: 631 us
-// whole, 64 cut); the kernel then decides by the lengths (at_unit), and a join with nothing
-// to do takes 4 to 5 us with the plan (64 rows of 1000 tokens 12 -> 18).
+// whole, 64 cut; units of many rows only in the first case); the kernel then decides by
+// the lengths (at_unit), and a join with nothing to do takes 4 to 5 us with the plan (64
+// rows of 1000 tokens 12 -> 18).  Units are of one size for all sequences, from the mean of
+// their rows: single rows beside a long block of rows take units of many rows too, whole
+// where that block fills the chip.
 AttendPlan attend_plan(int dt, int64_t n, int batch, int q_heads, int kv_heads, int d,
                        int64_t tokens) {
   const int64_t rows = n * (q_heads / kv_heads), each = (rows + batch - 1) / batch;

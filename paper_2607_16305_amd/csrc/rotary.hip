@@ -9,16 +9,18 @@
 // head keeps y.  Float32 sums and products, one rounding into the output.
 //
 // The angle is reduced in float64, in turns: pos freq / (2 pi) less the nearest
-// whole number, good to 2^-53 of the turns, so a position of 10^6 has the angle
-// that a float32 product would miss by 0.03.  What is left is float32 (2^-26 of
-// a turn).  A token's angles are computed once for all of its heads.
+// whole number, good to 2^-51 of the turns (two products and the constant round to
+// 2^-53 each), so a position of 10^6 has the angle that a float32 product would miss by
+// 0.03.  What is left is float32 (2^-26 of a turn).  A token's angles are computed once
+// for all of its heads.
 //
 // Bound by memory: 8192 rows of 40 heads of 128 in bf16, 168 MB read and written, take 33
 // us (5.0 TB/s; a large copy reaches 4.9).  Each lane holds its two chunks of 16 bytes
 // through norm and rotation, so a head is read and written once and nothing but the
 // angles goes through LDS; the next head's loads are on their way meanwhile.  (Heads in
 // LDS took 56 us, register pairs without loads past the caches 40.)  One token of 18
-// heads: 3.2 us, a launch.
+// heads: 3.2 us, a launch.  Halves whose boundary is no chunk's take their pairs through LDS:
+// the same rows with 100 of 128 elements turned 57 us, with 96 40.
 #include "common.h"
 #include "kernels.h"
 

@@ -205,6 +205,20 @@ def test_queries_at_and_past_the_end_of_their_type(shape, dtype, d):
            M.attention(q, _values(k), _values(v), scale, True))
 
 
+@pytest.mark.parametrize("dtype,d", KINDS)
+@pytest.mark.parametrize("shape", list(SHAPES))
+def test_the_largest_sums(shape, dtype, d):
+    """values of which as many as there are tokens, times 2^8, stay below float32's end"""
+    q, k, v, cache, table = _inputs(shape, dtype, d)
+    n, scale = k.shape[0], d ** -0.5
+    v *= 2.0 ** (119 - n.bit_length()) / 8                # (v is below 8, as is what is kept of it)
+    _fill(cache, table, k, v)
+    assert v.abs().max() * n < 2.0 ** 119 and _values(v).abs().max() * n < 2.0 ** 119
+    for causal in (True, False):
+        _close(_run(q, cache, table, n, causal, scale),
+               M.attention(q, _values(k), _values(v), scale, causal))
+
+
 def test_the_parts_of_more_rows_than_a_launch_are_joined():
     """2^26 rows of query heads, a wave each, of which the first and the last sequence's have
     cut keys: alike, so that the outputs are averages of small whole numbers"""

@@ -44,6 +44,8 @@ def _spread(batch, rows, length):
 CALLS = {
     "whole": (_spread(25, 40, 250), 30, 6, 8, True),
     "whole, many sequences": (_spread(80, 15, 90), 20, 2, 3, True),
+    "whole, decode rows beside a prompt": ([(1, 20 * i + 1) for i in range(6)] + [(600, 600)] +
+                                           [(1, 40 * i + 300) for i in range(6)], 32, 4, 20, True),
     "whole, as the kernel finds": ([(300, 320), (290, 290)], 16, 2, 2000, False),
     "cut": ([(50, 700), (37, 222), (60, 64), (45, 20), (0, 90)], 12, 3, 80, False),
     "cut, many sequences": (_spread(70, 14, 60)[:-1] + [(20, 2300)], 8, 1, 75, False),
